@@ -75,10 +75,11 @@ typedef enum {
     NA_ERR_HEAD_DIM = 7,              /* head_dim not in {32, 64, 128} */
     NA_ERR_DTYPE = 8,                 /* dtype not an na_dtype value */
     NA_ERR_ALIGNMENT = 9,             /* a device pointer is not 16-byte aligned */
-    /* 10 is not used */
+    /* 10 and 14 are not used */
     NA_ERR_HIP = 11,                  /* a HIP launch or query failed */
     NA_ERR_SCALE = 12,                /* scale is not finite */
-    NA_ERR_TILING = 13                /* an explicit tiling is not valid for the problem */
+    NA_ERR_TILING = 13,               /* an explicit tiling is not valid for the problem */
+    NA_ERR_WORKSPACE = 15             /* a workspace is smaller than the problem needs (na_seq.h) */
 } na_status;
 
 /*

@@ -510,3 +510,10 @@ def unfused_backward(q, k, v, probs, dout, kernel_size, dilation=1, scale=None, 
     dk = unfused_in(da, q, kernel_size, dilation, scale, causal)
     dv = unfused_in(probs, dout, kernel_size, dilation, 1.0, causal)
     return dq, dk, dv
+
+
+# ---------------------------------------------------------------- sequence operators
+from .sequence import (cache_attention, cache_step, cache_tables, cache_write,  # noqa: E402
+                       sink_forward)
+
+__all__ += ["sink_forward", "cache_tables", "cache_write", "cache_attention", "cache_step"]

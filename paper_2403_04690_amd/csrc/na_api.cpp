@@ -19,7 +19,7 @@
 
 namespace {
 
-constexpr int kVersion = 400;  // 0.4.0
+constexpr int kVersion = 500;  // 0.5.0
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -793,6 +793,7 @@ const char* na_status_string(na_status status) {
         case NA_ERR_HIP: return "HIP launch failed";
         case NA_ERR_SCALE: return "scale must be finite";
         case NA_ERR_TILING: return "the tiling is not valid for this problem";
+        case NA_ERR_WORKSPACE: return "the workspace is smaller than this problem needs";
     }
     return "unknown status";
 }

@@ -1,0 +1,332 @@
+// na_seq_api.cpp -- the C ABI of the sequence operators (na_seq.h): validation, the split of
+// the work and dispatch.  Host code; nothing allocates, synchronises or keeps state.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+
+#include "na_launch.h"
+#include "na_seq.h"
+#include "na_seq_kernels.h"
+
+namespace {
+
+constexpr int64_t kMaxRows = int64_t(1) << 30;   // rows of a (sequence, key/value head), positions
+constexpr int64_t kMaxGrid = int64_t(1) << 24;   // workgroups of 256 threads in 2^32 threads
+constexpr int64_t kMaxToken = int64_t(1) << 26;  // bytes of a token stride
+
+bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+int elem_bytes(int dtype) { return dtype == NA_FP32 ? 4 : 2; }
+
+na_status check_types(int64_t head_dim, int32_t dtype, float scale) {
+    if (head_dim != 32 && head_dim != 64 && head_dim != 128) return NA_ERR_HEAD_DIM;
+    if (dtype != NA_FP32 && dtype != NA_FP16 && dtype != NA_BF16) return NA_ERR_DTYPE;
+    return std::isfinite(scale) ? NA_OK : NA_ERR_SCALE;
+}
+
+// Heads in whole groups, a window and first tokens that are counts.
+na_status check_heads(int64_t heads, int64_t kv_heads, int64_t kernel_size, int64_t sinks) {
+    if (heads < 0 || kv_heads < 0 || heads >= kMaxRows) return NA_ERR_SHAPE;
+    if (heads > 0 && (kv_heads == 0 || heads % kv_heads != 0)) return NA_ERR_SHAPE;
+    if (kernel_size < 1) return NA_ERR_KERNEL_SIZE;
+    return sinks < 0 ? NA_ERR_SHAPE : NA_OK;
+}
+
+// Strides of a [batch, heads, tokens, head_dim] tensor (see na_seq.h).  Outputs: the axes of
+// more than one entry, ordered by stride, do not overlap.
+bool good_strides(const na_strides& s, int es, int64_t batch, int64_t heads, int64_t tokens,
+                  int64_t head_dim, bool output) {
+    const int64_t st[3] = {s.batch, s.head, s.token}, n[3] = {batch, heads, tokens};
+    for (int i = 0; i < 3; ++i) {
+        if (st[i] < 0 || st[i] >= (int64_t(1) << 40) || (st[i] * es) % 16 != 0) return false;
+    }
+    if (s.token * es >= kMaxToken) return false;
+    if (!output) return true;
+    __int128 reach = head_dim;  // entries that the axes so far cover
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int a, int b) { return st[a] < st[b]; });
+    for (int i : order) {
+        if (n[i] <= 1) continue;
+        if (st[i] < reach) return false;
+        reach += (__int128)st[i] * (n[i] - 1);
+    }
+    return true;
+}
+
+int clamp_count(int64_t x) { return (int)std::min<int64_t>(x, INT32_MAX); }
+
+// The fields that both forms of the attention share.
+void fill_common(na::SeqGeo& g, int64_t heads, int64_t kv_heads, int64_t kernel_size,
+                 int64_t sinks, float scale) {
+    std::memset(&g, 0, sizeof g);
+    g.G = (int)(heads / kv_heads);
+    g.Hkv = (int)kv_heads;
+    g.W = clamp_count(kernel_size);
+    g.S = (int)std::min<int64_t>(sinks, kMaxRows);
+    g.c = scale * na::kLog2e;
+    g.nsplit = 1;
+    g.chunk = INT32_MAX;
+    g.fd_G.init(g.G);
+    g.fd_kv.init(g.Hkv);
+    g.fd_split.init(1);
+}
+
+// ---- contiguous sequences ----
+na_status check_sink(const na_sink_problem& p, bool backward) {
+    na_status st = check_types(p.head_dim, p.dtype, p.scale);
+    if (st != NA_OK) return st;
+    if ((st = check_heads(p.heads, p.kv_heads, p.kernel_size, p.sinks)) != NA_OK) return st;
+    if (p.batch < 0 || p.tokens < 0 || p.batch >= kMaxRows || p.tokens >= kMaxRows)
+        return NA_ERR_SHAPE;
+    if (p.batch == 0 || p.heads == 0 || p.tokens == 0) return NA_OK;
+    const int64_t rows = p.tokens * (p.heads / p.kv_heads);
+    if (rows >= kMaxRows) return NA_ERR_SHAPE;
+    // row tiles of every slice fit a launch (checked without overflow)
+    if (p.batch * p.kv_heads >= kMaxGrid ||
+        p.batch * p.kv_heads * ((rows + 127) / 128) >= kMaxGrid)
+        return NA_ERR_SHAPE;
+    const int es = elem_bytes(p.dtype);
+    auto q_like = [&](const na_strides& s, bool o) {
+        return good_strides(s, es, p.batch, p.heads, p.tokens, p.head_dim, o);
+    };
+    auto k_like = [&](const na_strides& s, bool o) {
+        return good_strides(s, es, p.batch, p.kv_heads, p.tokens, p.head_dim, o);
+    };
+    if (!q_like(p.q, false) || !k_like(p.k, false) || !k_like(p.v, false)) return NA_ERR_SHAPE;
+    if (!backward) return q_like(p.out, true) ? NA_OK : NA_ERR_SHAPE;
+    if (!q_like(p.out, false) || !q_like(p.dout, false) || !q_like(p.dq, true) ||
+        !k_like(p.dk, true) || !k_like(p.dv, true))
+        return NA_ERR_SHAPE;
+    return NA_OK;
+}
+
+bool empty_sink(const na_sink_problem& p) { return p.batch == 0 || p.heads == 0 || p.tokens == 0; }
+
+void fill_sink(const na_sink_problem& p, const int32_t* lengths, na::SeqGeo& g) {
+    fill_common(g, p.heads, p.kv_heads, p.kernel_size, p.sinks, p.scale);
+    const int64_t es = elem_bytes(p.dtype);
+    g.n = (int)p.tokens;
+    g.B = (int)p.batch;
+    g.ntiles = (int)((p.tokens * g.G + 127) / 128);
+    g.fd_tiles.init(g.ntiles);
+    auto put = [&](const na_strides& s, int64_t& b, int64_t& h, int64_t& t) {
+        b = s.batch * es;
+        h = s.head * es;
+        t = s.token * es;
+    };
+    put(p.q, g.qb, g.qh, g.qt);
+    put(p.k, g.kb, g.kh, g.kt);
+    put(p.v, g.vb, g.vh, g.vt);
+    put(p.out, g.ob, g.oh, g.ot);
+    g.lb = p.heads * p.tokens;
+    g.lh = p.tokens;
+    g.lt = 1;
+    g.lengths = lengths;
+}
+
+// ---- paged cache ----
+na_status check_cache(const na_cache_problem& p) {
+    if (p.requests < 0 || p.tokens < 0 || p.requests >= kMaxGrid || p.tokens >= kMaxRows)
+        return NA_ERR_SHAPE;
+    if (p.pages < 0 || p.pages >= kMaxRows) return NA_ERR_SHAPE;
+    if (p.page_size < 16 || p.page_size > (1 << 20) || (p.page_size & (p.page_size - 1)))
+        return NA_ERR_SHAPE;
+    return NA_OK;
+}
+
+na_status check_attention(const na_cache_problem& p) {
+    na_status st = check_types(p.head_dim, p.dtype, p.scale);
+    if (st != NA_OK) return st;
+    if ((st = check_heads(p.heads, p.kv_heads, p.kernel_size, p.sinks)) != NA_OK) return st;
+    if ((st = check_cache(p)) != NA_OK) return st;
+    if (p.max_pages < 0 || p.max_pages >= kMaxRows || p.max_pages * p.page_size > kMaxRows ||
+        p.requests * p.max_pages >= (int64_t(1) << 31) || p.max_new < 0 || p.max_context < 0)
+        return NA_ERR_SHAPE;
+    if (p.heads == 0 || p.tokens == 0 || p.requests == 0) return NA_OK;
+    const int64_t G = p.heads / p.kv_heads;
+    if (p.tokens * G >= kMaxRows || (p.tokens * G / 32 + p.requests) >= kMaxGrid ||
+        (p.tokens * G / 32 + p.requests) * p.kv_heads >= kMaxGrid)
+        return NA_ERR_SHAPE;
+    const int es = elem_bytes(p.dtype);
+    if (!good_strides(p.q, es, 1, p.heads, p.tokens, p.head_dim, false) ||
+        !good_strides(p.out, es, 1, p.heads, p.tokens, p.head_dim, true))
+        return NA_ERR_SHAPE;
+    return NA_OK;
+}
+
+// Few new tokens per request (their rows fill one block of 32): the narrow form.
+bool cache_narrow(const na_cache_problem& p) {
+    const int64_t most = p.max_new > 0 ? std::min(p.max_new, p.tokens) : p.tokens;
+    return most * (p.heads / p.kv_heads) <= 32;
+}
+
+// Splits the keys of a row tile when the row tiles alone would leave most of the 256 CUs idle.
+// A split has at least 16 key tiles (512 keys), so that joining costs less than it gains.
+void fill_split(const na_cache_problem& p, bool narrow, na::SeqGeo& g) {
+    const int64_t M = narrow ? 32 : 128;
+    const int64_t rows = p.tokens * g.G;
+    g.ntiles = (int)(rows / M + p.requests);
+    const int64_t room = p.max_pages * p.page_size;
+    int64_t keys = p.max_context > 0 ? std::min(p.max_context, room) : room;
+    keys = std::min(keys, (int64_t)g.W + g.S + M + 64);
+    const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32 + 1);
+    const int64_t busy = std::max<int64_t>((rows + M - 1) / M, std::min(p.requests, p.tokens)) * g.Hkv;
+    int64_t split = std::min<int64_t>(na::kSeqMaxSplit, std::max<int64_t>(1, 1024 / busy));
+    split = std::min(split, std::max<int64_t>(1, (kMaxGrid - 1) / ((int64_t)g.ntiles * g.Hkv)));
+    int64_t chunk = std::max<int64_t>(16, (tiles + split - 1) / split);
+    chunk = (chunk + 3) / 4 * 4;
+    g.chunk = (int)chunk;
+    g.nsplit = (int)((tiles + chunk - 1) / chunk);
+    g.fd_split.init(g.nsplit);
+}
+
+size_t split_bytes(const na_cache_problem& p, bool narrow, const na::SeqGeo& g) {
+    if (g.nsplit == 1) return 0;
+    return (size_t)g.ntiles * g.Hkv * g.nsplit * (narrow ? 32 : 128) * (p.head_dim + 1) * 4;
+}
+
+}  // namespace
+
+extern "C" {
+
+na_status na_sink_forward(const na_sink_problem* problem, const void* q, const void* k,
+                          const void* v, const int32_t* lengths, void* out, float* logsumexp,
+                          na_stream_t stream) {
+    if (!problem) return NA_ERR_NULL;
+    const na_sink_problem& p = *problem;
+    const na_status st = check_sink(p, false);
+    if (st != NA_OK) return st;
+    if (empty_sink(p)) return NA_OK;
+    if (!q || !k || !v || !out || !logsumexp) return NA_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) ||
+        !aligned(logsumexp, 16) || !aligned(lengths, 4))
+        return NA_ERR_ALIGNMENT;
+    na::SeqGeo g;
+    fill_sink(p, lengths, g);
+    return na::launch_seq_forward(g, (int)p.head_dim, p.dtype, false, false, q, k, v, out,
+                                  logsumexp, nullptr, reinterpret_cast<hipStream_t>(stream)) ==
+                   hipSuccess
+               ? NA_OK
+               : NA_ERR_HIP;
+}
+
+na_status na_cache_tables(int64_t requests, int64_t tokens, int64_t page_size, int64_t max_pages,
+                          int64_t num_free, const int32_t* context_lens, const int32_t* new_lens,
+                          const int32_t* free_pages, const int32_t* head, int32_t* page_table,
+                          int32_t* cu_new, int64_t* slots, int32_t* positions, int32_t* new_head,
+                          na_stream_t stream) {
+    if (requests < 0 || requests >= kMaxRows || tokens < 0 || tokens >= kMaxRows || num_free < 0 ||
+        num_free >= kMaxRows || page_size < 16 || page_size > (1 << 20) ||
+        (page_size & (page_size - 1)) || max_pages < 0 || max_pages >= kMaxRows ||
+        max_pages * page_size > kMaxRows || requests * max_pages >= (int64_t(1) << 31))
+        return NA_ERR_SHAPE;
+    if (!cu_new || !new_head || (requests && (!context_lens || !new_lens)) ||
+        (requests && max_pages && !page_table) || (num_free && !free_pages) ||
+        (tokens && (!slots || !positions)))
+        return NA_ERR_NULL;
+    if (!aligned(context_lens, 4) || !aligned(new_lens, 4) || !aligned(free_pages, 4) ||
+        !aligned(head, 4) || !aligned(page_table, 4) || !aligned(cu_new, 4) ||
+        !aligned(slots, 8) || !aligned(positions, 4) || !aligned(new_head, 4))
+        return NA_ERR_ALIGNMENT;
+    if (head == new_head) return NA_ERR_SHAPE;
+    return na::launch_cache_tables((int)requests, (int)tokens, __builtin_ctzll(page_size),
+                                   (int)max_pages, (int)num_free, context_lens, new_lens,
+                                   free_pages, head, page_table, cu_new, slots, positions,
+                                   new_head, reinterpret_cast<hipStream_t>(stream)) == hipSuccess
+               ? NA_OK
+               : NA_ERR_HIP;
+}
+
+na_status na_cache_write(const na_cache_problem* problem, const void* k, const void* v,
+                         const int64_t* slots, void* k_pages, void* v_pages, na_stream_t stream) {
+    if (!problem) return NA_ERR_NULL;
+    const na_cache_problem& p = *problem;
+    na_status st = check_types(p.head_dim, p.dtype, 1.f);
+    if (st != NA_OK) return st;
+    if ((st = check_cache(p)) != NA_OK) return st;
+    if (p.kv_heads < 0 || p.kv_heads >= kMaxGrid) return NA_ERR_SHAPE;
+    if (p.tokens == 0 || p.kv_heads == 0 || p.pages == 0) return NA_OK;
+    const int es = elem_bytes(p.dtype);
+    const int64_t row = p.head_dim * es;
+    if (p.tokens * p.kv_heads >= kMaxRows || p.tokens * p.kv_heads * (row / 16) >= 2 * kMaxRows)
+        return NA_ERR_SHAPE;
+    if (!good_strides(p.k, es, 1, p.kv_heads, p.tokens, p.head_dim, false) ||
+        !good_strides(p.v, es, 1, p.kv_heads, p.tokens, p.head_dim, false))
+        return NA_ERR_SHAPE;
+    if (!k || !v || !slots || !k_pages || !v_pages) return NA_ERR_NULL;
+    if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) ||
+        !aligned(slots, 8))
+        return NA_ERR_ALIGNMENT;
+    return na::launch_cache_write((int)p.tokens, (int)p.kv_heads, (int)row,
+                                  __builtin_ctzll(p.page_size), p.pages * p.page_size,
+                                  p.k.token * es, p.k.head * es, p.v.token * es, p.v.head * es, k,
+                                  v, slots, k_pages, v_pages,
+                                  reinterpret_cast<hipStream_t>(stream)) == hipSuccess
+               ? NA_OK
+               : NA_ERR_HIP;
+}
+
+size_t na_cache_attention_workspace(const na_cache_problem* problem) {
+    if (!problem || check_attention(*problem) != NA_OK) return 0;
+    const na_cache_problem& p = *problem;
+    if (p.heads == 0 || p.tokens == 0 || p.requests == 0) return 0;
+    na::SeqGeo g;
+    fill_common(g, p.heads, p.kv_heads, p.kernel_size, p.sinks, p.scale);
+    fill_split(p, cache_narrow(p), g);
+    return split_bytes(p, cache_narrow(p), g);
+}
+
+na_status na_cache_attention(const na_cache_problem* problem, const void* q, const void* k_pages,
+                             const void* v_pages, const int32_t* page_table,
+                             const int32_t* context_lens, const int32_t* cu_new, void* out,
+                             float* logsumexp, void* workspace, size_t workspace_bytes,
+                             na_stream_t stream) {
+    if (!problem) return NA_ERR_NULL;
+    const na_cache_problem& p = *problem;
+    const na_status st = check_attention(p);
+    if (st != NA_OK) return st;
+    if (p.heads == 0 || p.tokens == 0 || p.requests == 0) return NA_OK;
+    const bool cached = p.pages > 0 && p.max_pages > 0;  // (else every page reads as zeros)
+    if (!q || !context_lens || !cu_new || !out || !logsumexp ||
+        (cached && (!k_pages || !v_pages || !page_table)))
+        return NA_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16) ||
+        !aligned(logsumexp, 16) || !aligned(workspace, 16) || !aligned(page_table, 4) ||
+        !aligned(context_lens, 4) || !aligned(cu_new, 4))
+        return NA_ERR_ALIGNMENT;
+    const bool narrow = cache_narrow(p);
+    na::SeqGeo g;
+    fill_common(g, p.heads, p.kv_heads, p.kernel_size, p.sinks, p.scale);
+    fill_split(p, narrow, g);
+    const size_t need = split_bytes(p, narrow, g);
+    if (workspace_bytes < need) return NA_ERR_WORKSPACE;
+    if (need && !workspace) return NA_ERR_NULL;
+    const int64_t es = elem_bytes(p.dtype);
+    g.n = (int)p.tokens;
+    g.B = (int)p.requests;
+    g.pages = cached ? (int)p.pages : 0;
+    g.max_pages = cached ? (int)p.max_pages : 0;
+    g.lgps = __builtin_ctzll(p.page_size);
+    g.qh = p.q.head * es;
+    g.qt = p.q.token * es;
+    g.oh = p.out.head * es;
+    g.ot = p.out.token * es;
+    g.kt = g.vt = p.head_dim * es;
+    g.kh = g.vh = g.kt << g.lgps;
+    g.kb = g.vb = g.kh * p.kv_heads;
+    g.lh = 1;
+    g.lt = p.heads;
+    g.context = context_lens;
+    g.cu = cu_new;
+    g.table = page_table;
+    return na::launch_seq_forward(g, (int)p.head_dim, p.dtype, true, narrow, q, k_pages, v_pages,
+                                  out, logsumexp, static_cast<float*>(workspace),
+                                  reinterpret_cast<hipStream_t>(stream)) == hipSuccess
+               ? NA_OK
+               : NA_ERR_HIP;
+}
+
+}  // extern "C"

@@ -1,0 +1,556 @@
+// na_seq_fwd.hip -- forward of attention over a sliding window and the first tokens, for
+// contiguous sequences and for new tokens against a paged cache (gfx950).
+//
+//   out_i = sum_j exp(s_ij - lse_i) v_j,  s_ij = scale q_i . k_j,  lse_i = log sum_j exp s_ij
+//   over the j <= i with i - j < W or j < S.
+//
+// One pass over the keys with the running maximum and sum of an online softmax, in base 2.
+//   S^T = K Q^T (32 keys x 32 rows a step) leaves a row's scores in one lane column (two
+//   lanes), so the maximum needs one lane swap and P^T feeds O^T = V^T P^T from registers.
+// Sums, maxima and accumulators are fp32.  P is rounded once to the type of V for its matrix
+// product (16-bit types); the sum that divides it and the logsumexp take P unrounded.
+//
+// Two forms:
+//   wide    four waves of 32 rows each share the staged key tiles: many rows
+//   narrow  one block of 32 rows (new tokens x heads of a group); the four waves take
+//           every fourth key tile each, from LDS buffers of their own without barriers, and
+//           join their sums at the end: single tokens, where reading the cache is the work
+#include <cmath>
+
+#include "na_launch.h"
+#include "na_seq_kernels.h"
+
+namespace na {
+
+constexpr float kSeqLazy = 8.f;  // base-2 headroom before the running maximum is raised
+
+// Running state of 32 rows: lane l holds row l % 32, and of the keys those of its half.
+template <typename T, int D>
+struct SeqState {
+    using F = SeqFrags<T, D>;
+    using x8 = typename Tr<T>::x8;
+    x8 qf[F::kKS];
+    f32x16 o[F::kDB];
+    float mref, thr, l;
+
+    __device__ __forceinline__ void init() {
+        mref = -INFINITY;
+        thr = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int db = 0; db < F::kDB; ++db) o[db] = f32x16{} * 0.f;
+    }
+
+    // One tile of 32 keys from position j0.  MASK: some pair is not seen; pos: this lane's row.
+    template <bool MASK>
+    __device__ __forceinline__ void tile(const F& f, const unsigned char* kt,
+                                         const unsigned char* vt, int lane, float c, int j0,
+                                         int pos, int W, int S) {
+        f32x16 s = f32x16{} * 0.f;
+#pragma unroll
+        for (int st = 0; st < F::kKS; ++st) s = mma32<T>(f.row(kt, st), qf[st], s);
+        const float negm = mref == -INFINITY ? 0.f : -mref;
+        float y[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[i] = fmaf(s[i], c, negm);
+        if constexpr (MASK) {
+            // entry i is key position j0 + 4 h + entry_row(i)
+            const int base = j0 + 4 * (lane >> 5);
+            const int dist = pos - base;
+            const int few = min(S - base, dist + 1);  // first tokens not after the row
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int e = entry_row(i);
+                y[i] = (unsigned)(dist - e) < (unsigned)W || e < few ? y[i] : -INFINITY;
+            }
+        }
+        float top = y[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, y[i]);
+        // raise the reference on a row's first key, or when it grows by more than kSeqLazy
+        if (__builtin_amdgcn_ballot_w64(top > thr)) {
+            const float ymax = col_max<32>(top);
+            const bool raise = ymax > thr;
+            const float up = raise ? ymax : 0.f;
+            const float alpha = thr == -INFINITY ? 0.f : fast_exp2(-up);
+            mref = raise ? up - negm : mref;
+            thr = mref != -INFINITY ? kSeqLazy : -INFINITY;
+            l *= alpha;
+#pragma unroll
+            for (int db = 0; db < F::kDB; ++db) o[db] *= alpha;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) y[i] -= up;
+        }
+        x8 pf[2];
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float p = fast_exp2(y[i]);
+            sum[i & 1] += p;
+            pf[i >> 3][i & 7] = Tr<T>::cvt(p);
+        }
+        l += sum[0] + sum[1];
+#pragma unroll
+        for (int db = 0; db < F::kDB; ++db)
+#pragma unroll
+            for (int bi = 0; bi < 2; ++bi)
+                o[db] = mma32<T>(f.col(vt, db, bi, lane), pf[bi], o[db]);
+    }
+};
+
+// Stages key tile `e` of the workgroup's tile (instructions first, first + step, ... of the
+// 2 kInstr of K and V).
+template <typename T, int D, bool PAGED, int STEP>
+struct SeqStage {
+    using R = SeqRows<T, D>;
+    static constexpr int kCount = 2 * R::kInstr / STEP;
+    static_assert(2 * R::kInstr % STEP == 0, "equal shares");
+    const unsigned char *kb, *vb;  // head's rows (paged: of page 0)
+    R rows;
+    uint32_t klane, vlane;  // rowl * token stride
+
+    __device__ __forceinline__ void init(const SeqGeo& g, const SeqTile& t, int kvh, int lane,
+                                         const void* k, const void* v) {
+        rows.init(lane);
+        kb = static_cast<const unsigned char*>(k) + kvh * g.kh;
+        vb = static_cast<const unsigned char*>(v) + kvh * g.vh;
+        if (!PAGED) {
+            kb += t.b * g.kb;
+            vb += t.b * g.vb;
+        }
+        klane = rows.rowl * (uint32_t)g.kt;
+        vlane = rows.rowl * (uint32_t)g.vt;
+    }
+
+    __device__ __forceinline__ void issue(const SeqGeo& g, const SeqTile& t, int e, int first,
+                                          unsigned char* dst) const {
+        const int j0 = t.tile(e);
+        bool fast = j0 + 31 <= t.pmax && (j0 >= t.lo || j0 + 31 < g.S);
+        // of the tile's two 16-row blocks: byte offset from kb, vb, and whether it exists
+        int64_t ko[2], vo[2];
+        bool ok[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int j = j0 + 16 * i;
+            if constexpr (PAGED) {
+                const int col = j >> g.lgps;
+                int id = -1;
+                if (col < g.max_pages && j <= t.pmax)
+                    id = g.table[(int64_t)t.b * g.max_pages + col];
+                ok[i] = (unsigned)id < (unsigned)g.pages;
+                id = ok[i] ? id : 0;
+                const int in = j & ((1 << g.lgps) - 1);
+                ko[i] = id * g.kb + in * g.kt;
+                vo[i] = id * g.vb + in * g.vt;
+            } else {
+                ok[i] = true;
+                ko[i] = j * g.kt;
+                vo[i] = j * g.vt;
+            }
+            fast = fast && ok[i];
+        }
+#pragma unroll
+        for (int u = 0; u < kCount; ++u) {
+            const int x = first + u * STEP;
+            const bool isv = x >= R::kInstr;
+            const int n = isv ? x - R::kInstr : x;
+            const int r0 = n * R::kRpi;
+            const int blk = r0 >> 4;
+            const int64_t in = (int64_t)(r0 & 15) * (isv ? g.vt : g.kt);
+            const unsigned char* base = (isv ? vb : kb) + (isv ? (blk ? vo[1] : vo[0])
+                                                               : (blk ? ko[1] : ko[0])) + in;
+            const uint32_t off = rows.off(n, isv ? vlane : klane);
+            if (fast) {
+                seq_load(base, off, dst + x * 1024);
+            } else {
+                const int j = j0 + r0 + rows.rowl;
+                const bool see = (blk ? ok[1] : ok[0]) && t.sees(g, j);
+                seq_load(see ? base + off : reinterpret_cast<const unsigned char*>(&kZeroRow),
+                         dst + x * 1024);
+            }
+        }
+    }
+};
+
+// Row m of the tile: token (of the request) and head of the group.
+__device__ __forceinline__ void seq_row(const SeqGeo& g, const SeqTile& t, int m, int& tok,
+                                        int& head) {
+    const int r = t.row0 + min(m, t.rows - 1);
+    tok = g.fd_G.div(r);
+    head = r - tok * g.G;
+}
+
+// Stage of the wide form: key tiles per stage.
+template <typename T, int D>
+constexpr int seq_stage_tiles() {
+    return sizeof(T) == 4 && D == 128 ? 1 : 2;
+}
+
+template <typename T, int D, bool PAGED>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 3) : 1)) void seq_wide_kernel(
+    SeqGeo g, const T* __restrict__ qg, const T* __restrict__ kg, const T* __restrict__ vg,
+    T* __restrict__ og, float* __restrict__ lseg, float* __restrict__ part) {
+    using F = SeqFrags<T, D>;
+    constexpr int SK = seq_stage_tiles<T, D>();
+    constexpr int kBuf = SK * 2 * F::kTile;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 63;
+    const int wave = uniform((threadIdx.x >> 6) & 3);
+
+    // ---- workgroup -> (split, row tile, key/value head, sequence) ----
+    SeqTile t;
+    int split = 0, kvh, tile;
+    if constexpr (PAGED) {
+        const int id = g.fd_split.div(blockIdx.x);
+        split = blockIdx.x - id * g.nsplit;
+        tile = g.fd_kv.div(id);
+        kvh = id - tile * g.Hkv;
+        tile = g.ntiles - 1 - tile;
+        if (!seq_locate(g, tile, 7, lane, t)) return;
+    } else {
+        const int id = xcd_remap(blockIdx.x, gridDim.x);
+        const int slice = g.fd_tiles.div(id);
+        tile = g.ntiles - 1 - (id - slice * g.ntiles);
+        t.b = g.fd_kv.div(slice);
+        kvh = slice - t.b * g.Hkv;
+        t.row0 = tile * 128;
+        t.rows = min(g.n * g.G - t.row0, 128);
+        t.qtok = t.pos0 = 0;
+        t.valid = g.lengths ? min(max(g.lengths[t.b], 0), g.n) : g.n;
+        t.pmin = g.fd_G.div(t.row0);
+        t.pmax = min(g.fd_G.div(t.row0 + t.rows - 1), t.valid - 1);
+        t.nT = 0;
+        if (t.pmin < t.valid) t.span(g);
+    }
+    int e0 = 0, e1 = t.nT, splits = 1;
+    if constexpr (PAGED) {
+        splits = seq_splits(g, t.nT);
+        if (split >= splits) return;
+        e0 = split * g.chunk;
+        e1 = split == splits - 1 ? t.nT : e0 + g.chunk;
+    }
+
+    SeqStage<T, D, PAGED, 4> ld;
+    ld.init(g, t, kvh, lane, kg, vg);
+    auto issue_stage = [&](int e, int buf) {
+#pragma unroll
+        for (int i = 0; i < SK; ++i)
+            if (e + i < e1) ld.issue(g, t, e + i, wave, smem + buf * kBuf + i * 2 * F::kTile);
+    };
+    if (e0 < e1) issue_stage(e0, 0);
+
+    // ---- this lane's row, and the positions of the wave's rows ----
+    const int m = wave * 32 + (lane & 31);
+    int tok, head;
+    seq_row(g, t, m, tok, head);
+    const int pos = t.pos0 + tok;
+    const bool live = wave * 32 < t.rows;
+    int tf, tl, hh;
+    seq_row(g, t, wave * 32, tf, hh);
+    seq_row(g, t, wave * 32 + 31, tl, hh);
+    const int wmin = t.pos0 + tf;
+    const int wmax = min(t.pos0 + tl, PAGED ? t.pmax : t.valid - 1);
+    const int64_t hq = (int64_t)kvh * g.G + head;
+    SeqState<T, D> st;
+    st.init();
+    {
+        const unsigned char* qp = reinterpret_cast<const unsigned char*>(qg) +
+                                  (PAGED ? 0 : t.b * g.qb) + hq * g.qh +
+                                  // (rows behind the length hold anything: not theirs)
+                                  (int64_t)(t.qtok + max(min(tok, t.valid - 1), 0)) * g.qt;
+#pragma unroll
+        for (int s = 0; s < F::kKS; ++s)
+            st.qf[s] = ld_x8<T>(reinterpret_cast<const T*>(qp) + s * 16 + 8 * (lane >> 5));
+    }
+    F f;
+    f.init(lane);
+
+    stage_barrier();
+    for (int e = e0, buf = 0; e < e1; e += SK, buf ^= 1) {
+        if (e + SK < e1) issue_stage(e + SK, buf ^ 1);
+#pragma unroll
+        for (int i = 0; i < SK; ++i) {
+            const int j0 = t.tile(e + i);
+            // outside every window of the wave's rows, and no first tokens
+            const bool out = j0 > wmax || (wmin - (j0 + 31) >= g.W && j0 >= g.S);
+            if (e + i < e1 && live && !out) {
+                const unsigned char* kt = smem + buf * kBuf + i * 2 * F::kTile;
+                const bool full = j0 + 31 <= wmin && (wmax - j0 < g.W || j0 + 31 < g.S);
+                if (full)
+                    st.template tile<false>(f, kt, kt + F::kTile, lane, g.c, j0, pos, g.W, g.S);
+                else
+                    st.template tile<true>(f, kt, kt + F::kTile, lane, g.c, j0, pos, g.W, g.S);
+            }
+        }
+        if (e + SK < e1) stage_barrier();
+    }
+
+    // ---- epilogue ----
+    const float l = col_sum<32>(st.l);
+    if (m >= t.rows) return;
+    const bool some = l > 0.f && (PAGED || tok < t.valid);
+    const float inv = some ? 1.f / l : 0.f;
+    const float lse2 = some ? st.mref + __log2f(l) : -INFINITY;
+    const int h = lane >> 5;
+    if (PAGED && splits > 1) {
+        const int64_t row = ((int64_t)(tile * g.Hkv + kvh) * g.nsplit + split) * 128 + m;
+        float* po = part + row * D;
+#pragma unroll
+        for (int db = 0; db < F::kDB; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                st16<f32x4>(po + db * 32 + i * 8 + h * 4,
+                            f32x4{st.o[db][4 * i], st.o[db][4 * i + 1], st.o[db][4 * i + 2],
+                                  st.o[db][4 * i + 3]} * inv);
+        if (h == 0) part[(int64_t)g.ntiles * g.Hkv * g.nsplit * 128 * D + row] = lse2;
+        return;
+    }
+    T* op = reinterpret_cast<T*>(reinterpret_cast<unsigned char*>(og) + (PAGED ? 0 : t.b * g.ob) +
+                                 hq * g.oh + (int64_t)(t.qtok + tok) * g.ot);
+#pragma unroll
+    for (int db = 0; db < F::kDB; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            st_x4<T>(op + db * 32 + i * 8 + h * 4,
+                     f32x4{st.o[db][4 * i], st.o[db][4 * i + 1], st.o[db][4 * i + 2],
+                           st.o[db][4 * i + 3]} * inv);
+    if (h == 0)
+        lseg[(PAGED ? 0 : t.b * g.lb) + hq * g.lh + (int64_t)(t.qtok + tok) * g.lt] =
+            some ? lse2 * kLn2 : -INFINITY;
+}
+
+// Waves of the narrow form: the buffers of each (two key tiles) fit four to a CU's LDS, fp32
+// at D = 128 two.
+template <typename T, int D>
+constexpr int seq_narrow_waves() {
+    return sizeof(T) == 4 && D == 128 ? 2 : 4;
+}
+
+template <typename T, int D>
+struct SeqNarrow {
+    static constexpr int W = seq_narrow_waves<T, D>();
+    static constexpr int kTile = SeqFrags<T, D>::kTile;
+    static constexpr int kStages = W * 4 * kTile;
+    static constexpr int kRow = (D + 4) * 4;           // a joined row (padded: LDS banks)
+    static constexpr int kJoin = W * 32 * kRow;
+    static constexpr int kStat = kStages > kJoin ? kStages : kJoin;  // offset of the statistics
+    static constexpr int kLds = kStat + W * 32 * 8;
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__((seq_narrow_waves<T, D>() * 64), 1) void seq_narrow_kernel(
+    SeqGeo g, const T* __restrict__ qg, const T* __restrict__ kg, const T* __restrict__ vg,
+    T* __restrict__ og, float* __restrict__ lseg, float* __restrict__ part) {
+    using F = SeqFrags<T, D>;
+    using N = SeqNarrow<T, D>;
+    constexpr int W = N::W;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & 63;
+    const int wave = uniform((threadIdx.x >> 6) & (W - 1));
+
+    SeqTile t;
+    const int id = g.fd_split.div(blockIdx.x);
+    const int split = blockIdx.x - id * g.nsplit;
+    const int tile = g.fd_kv.div(id);
+    const int kvh = id - tile * g.Hkv;
+    if (!seq_locate(g, tile, 5, lane, t)) return;
+    const int splits = seq_splits(g, t.nT);
+    if (split >= splits) return;
+    const int e0 = split * g.chunk;
+    const int e1 = split == splits - 1 ? t.nT : e0 + g.chunk;
+
+    SeqStage<T, D, true, 1> ld;
+    ld.init(g, t, kvh, lane, kg, vg);
+    unsigned char* buf0 = smem + wave * 4 * F::kTile;
+    int e = e0 + wave;
+    if (e < e1) ld.issue(g, t, e, 0, buf0);
+
+    int tok, head;
+    seq_row(g, t, lane & 31, tok, head);
+    const int pos = t.pos0 + tok;
+    const int64_t hq = (int64_t)kvh * g.G + head;
+    SeqState<T, D> st;
+    st.init();
+    {
+        const unsigned char* qp = reinterpret_cast<const unsigned char*>(qg) + hq * g.qh +
+                                  (int64_t)(t.qtok + tok) * g.qt;
+#pragma unroll
+        for (int s = 0; s < F::kKS; ++s)
+            st.qf[s] = ld_x8<T>(reinterpret_cast<const T*>(qp) + s * 16 + 8 * (lane >> 5));
+    }
+    F f;
+    f.init(lane);
+    wait_vmem();  // (the first tile too: from here on only stage loads are outstanding)
+    for (int buf = 0; e < e1; e += W, buf ^= 1) {
+        if (e + W < e1) {
+            ld.issue(g, t, e + W, 0, buf0 + (buf ^ 1) * 2 * F::kTile);
+            wait_vmem_but<2 * SeqRows<T, D>::kInstr>();
+        } else {
+            wait_vmem();
+        }
+        const unsigned char* kt = buf0 + buf * 2 * F::kTile;
+        const int j0 = t.tile(e);
+        const bool full = j0 + 31 <= t.pmin && (t.pmax - j0 < g.W || j0 + 31 < g.S);
+        if (full)
+            st.template tile<false>(f, kt, kt + F::kTile, lane, g.c, j0, pos, g.W, g.S);
+        else
+            st.template tile<true>(f, kt, kt + F::kTile, lane, g.c, j0, pos, g.W, g.S);
+        wait_lds();  // before the next loads into this buffer
+    }
+
+    // ---- join the waves: every sum relative to the largest reference ----
+    const float l = col_sum<32>(st.l);
+    float* stat = reinterpret_cast<float*>(smem + N::kStat);  // [wave][32] of (reference, sum)
+    if (lane < 32) {
+        stat[(wave * 32 + lane) * 2] = st.mref;
+        stat[(wave * 32 + lane) * 2 + 1] = l;
+    }
+    __syncthreads();
+    const int col = lane & 31, h = lane >> 5;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < W; ++w) top = fmaxf(top, stat[(w * 32 + col) * 2]);
+    const float scale = st.mref == -INFINITY ? 0.f : fast_exp2(st.mref - top);
+    {
+        float* mine = reinterpret_cast<float*>(smem + (wave * 32 + col) * N::kRow);
+#pragma unroll
+        for (int db = 0; db < F::kDB; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                st16<f32x4>(mine + db * 32 + i * 8 + h * 4,
+                            f32x4{st.o[db][4 * i], st.o[db][4 * i + 1], st.o[db][4 * i + 2],
+                                  st.o[db][4 * i + 3]} * scale);
+    }
+    __syncthreads();
+    // each thread: four columns of a row
+    for (int x = threadIdx.x; x < t.rows * (D / 4); x += W * 64) {
+        const int row = x / (D / 4), d = x % (D / 4) * 4;
+        float mx = -INFINITY, sum = 0.f;
+        f32x4 acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < W; ++w) mx = fmaxf(mx, stat[(w * 32 + row) * 2]);
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float m = stat[(w * 32 + row) * 2];
+            sum += m == -INFINITY ? 0.f : fast_exp2(m - mx) * stat[(w * 32 + row) * 2 + 1];
+            acc += *reinterpret_cast<const f32x4*>(smem + (w * 32 + row) * N::kRow + d * 4);
+        }
+        const bool some = sum > 0.f;
+        acc *= some ? 1.f / sum : 0.f;
+        const float lse2 = some ? mx + __log2f(sum) : -INFINITY;
+        if (splits > 1) {
+            const int64_t pr = ((int64_t)(tile * g.Hkv + kvh) * g.nsplit + split) * 32 + row;
+            st16<f32x4>(part + pr * D + d, acc);
+            if (d == 0) part[(int64_t)g.ntiles * g.Hkv * g.nsplit * 32 * D + pr] = lse2;
+        } else {
+            int tk, hd;
+            seq_row(g, t, row, tk, hd);
+            const int64_t hr = (int64_t)kvh * g.G + hd;
+            T* op = reinterpret_cast<T*>(reinterpret_cast<unsigned char*>(og) + hr * g.oh +
+                                         (int64_t)(t.qtok + tk) * g.ot);
+            st_x4<T>(op + d, acc);
+            if (d == 0)
+                lseg[hr * g.lh + (int64_t)(t.qtok + tk) * g.lt] = some ? lse2 * kLn2 : -INFINITY;
+        }
+    }
+}
+
+// Joins the splits of each row: out = sum_s 2^(lse_s - lse) out_s, in a fixed order.  One
+// workgroup per (row tile, key/value head); D / 4 threads a row.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void seq_join_kernel(SeqGeo g, int lgM, T* __restrict__ og,
+                                                       float* __restrict__ lseg,
+                                                       const float* __restrict__ part) {
+    const int tile = g.fd_kv.div(blockIdx.x);
+    const int kvh = blockIdx.x - tile * g.Hkv;
+    SeqTile t;
+    if (!seq_locate(g, tile, lgM, threadIdx.x & 63, t)) return;
+    const int splits = seq_splits(g, t.nT);
+    if (splits == 1) return;  // written by the only split
+    const int64_t row0 = (int64_t)(tile * g.Hkv + kvh) * g.nsplit << lgM;
+    const float* pl = part + ((int64_t)g.ntiles * g.Hkv * g.nsplit << lgM) * D + row0;
+    for (int x = threadIdx.x; x < t.rows * (D / 4); x += 256) {
+        const int row = x / (D / 4), d = x % (D / 4) * 4;
+        float mx = -INFINITY;
+        for (int s = 0; s < splits; ++s) mx = fmaxf(mx, pl[(s << lgM) + row]);
+        float sum = 0.f;
+        f32x4 acc{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < splits; ++s) {
+            const float e = pl[(s << lgM) + row];
+            const float w = e == -INFINITY ? 0.f : fast_exp2(e - mx);
+            sum += w;
+            acc += ld16<f32x4>(part + (row0 + (s << lgM) + row) * D + d) * w;
+        }
+        const bool some = sum > 0.f;
+        int tk, hd;
+        seq_row(g, t, row, tk, hd);
+        const int64_t hr = (int64_t)kvh * g.G + hd;
+        T* op = reinterpret_cast<T*>(reinterpret_cast<unsigned char*>(og) + hr * g.oh +
+                                     (int64_t)(t.qtok + tk) * g.ot);
+        st_x4<T>(op + d, acc * (some ? 1.f / sum : 0.f));
+        if (d == 0)
+            lseg[hr * g.lh + (int64_t)(t.qtok + tk) * g.lt] =
+                some ? (mx + __log2f(sum)) * kLn2 : -INFINITY;
+    }
+}
+
+// ---- host ----
+template <typename K>
+static hipError_t allow_lds(K kern, size_t lds) {
+    return lds <= 65536 ? hipSuccess
+                        : hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
+                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+}
+
+template <typename T, int D>
+static hipError_t launch_fwd(const SeqGeo& g, bool paged, bool narrow, const T* q, const T* k,
+                             const T* v, T* out, float* lse, float* part, hipStream_t s) {
+    const unsigned tiles = (unsigned)g.ntiles * g.Hkv * (paged ? 1 : g.B);
+    hipError_t e;
+    if (narrow) {
+        using N = SeqNarrow<T, D>;
+        auto kern = seq_narrow_kernel<T, D>;
+        if ((e = allow_lds(kern, N::kLds)) != hipSuccess) return e;
+        hipLaunchKernelGGL(kern, dim3(tiles * g.nsplit), dim3(N::W * 64), N::kLds, s, g, q, k, v,
+                           out, lse, part);
+    } else {
+        constexpr size_t lds = 2 * seq_stage_tiles<T, D>() * 2 * SeqFrags<T, D>::kTile;
+        auto kern = paged ? seq_wide_kernel<T, D, true> : seq_wide_kernel<T, D, false>;
+        if ((e = allow_lds(kern, lds)) != hipSuccess) return e;
+        hipLaunchKernelGGL(kern, dim3(tiles * g.nsplit), dim3(256), lds, s, g, q, k, v, out, lse,
+                           part);
+    }
+    if ((e = hipGetLastError()) != hipSuccess || g.nsplit == 1) return e;
+    hipLaunchKernelGGL((seq_join_kernel<T, D>), dim3(tiles), dim3(256), 0, s, g, narrow ? 5 : 7,
+                       out, lse, part);
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t launch_fwd_d(const SeqGeo& g, int D, bool paged, bool narrow, const void* q,
+                               const void* k, const void* v, void* out, float* lse, float* part,
+                               hipStream_t s) {
+    auto q_ = static_cast<const T*>(q);
+    auto k_ = static_cast<const T*>(k);
+    auto v_ = static_cast<const T*>(v);
+    auto o_ = static_cast<T*>(out);
+    switch (D) {
+        case 32: return launch_fwd<T, 32>(g, paged, narrow, q_, k_, v_, o_, lse, part, s);
+        case 64: return launch_fwd<T, 64>(g, paged, narrow, q_, k_, v_, o_, lse, part, s);
+        case 128: return launch_fwd<T, 128>(g, paged, narrow, q_, k_, v_, o_, lse, part, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_seq_forward(const SeqGeo& g, int D, int dtype, bool paged, bool narrow,
+                              const void* q, const void* k, const void* v, void* out, float* lse,
+                              float* part, hipStream_t s) {
+    switch (dtype) {
+        case 0: return launch_fwd_d<float>(g, D, paged, narrow, q, k, v, out, lse, part, s);
+        case 1: return launch_fwd_d<_Float16>(g, D, paged, narrow, q, k, v, out, lse, part, s);
+        case 2: return launch_fwd_d<__bf16>(g, D, paged, narrow, q, k, v, out, lse, part, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace na

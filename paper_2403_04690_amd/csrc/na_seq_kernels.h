@@ -1,0 +1,263 @@
+// na_seq_kernels.h -- what the sequence kernels share: attention of a causal 1-D sequence whose
+// queries see the `W` nearest tokens up to themselves and the first `S` tokens, over
+// contiguous (strided) rows or over the pages of a cache.
+//
+// Rows.  The G query heads that share a key/value head are rows of one problem: row m of a
+// (sequence, key/value head) is token m / G, head m % G of the group.  A workgroup tile is M
+// consecutive rows, so any G packs without waste, a staged key serves every head of its
+// group, and a tile of a window problem spans M / G tokens, which keeps its halo small.
+//
+// Keys are visited in 32-row tiles, aligned to 32 positions: the tiles of the first S tokens
+// that lie before the window, then the window's.
+#pragma once
+
+#include "na_stage.h"
+
+namespace na {
+
+// Largest split of the pages of a request over workgroups (joined by a second launch).
+constexpr int kSeqMaxSplit = 64;
+
+struct SeqGeo {
+    int n;          // tokens per sequence (contiguous form); all new tokens (paged form)
+    int G, Hkv, B;  // query heads per key/value head, key/value heads, sequences or requests
+    int W, S;       // window (itself included), first tokens that stay visible
+    int ntiles;     // row tiles per (sequence, key/value head); paged: over all requests
+    int nsplit;     // key splits of a row tile (paged form; 1: none)
+    int chunk;      // key tiles of a split
+    int lgps, pages, max_pages;  // paged form: log2 page size, pages of the pool, table columns
+    FastDiv fd_G, fd_tiles, fd_kv, fd_split;
+    // byte strides of batch, head, token (paged form: head, token of q and out)
+    int64_t qb, qh, qt, kb, kh, kt, vb, vh, vt, ob, oh, ot;
+    int64_t lb, lh, lt;  // logsumexp, in elements
+    float c;             // scale * log2(e)
+    const int32_t* lengths;  // contiguous form: valid tokens per sequence, or null
+    const int32_t *context, *cu, *table;  // paged form
+};
+
+// 16 zero bytes: what is staged for a row that nothing may see (behind the sequence, before
+// the window, on a page that does not exist), so that such memory is not read at all.
+__device__ const i32x4 kZeroRow = {0, 0, 0, 0};
+
+// c + a b on 32x32x16 steps (fp32: eight 32x32x2 steps; step j contracts slots j of both
+// halves of the wave).  A: lane l holds row l % 32, slots 8 (l / 32) .. +7; B the same of
+// column l % 32; C entry i: row 8 (i / 4) + 4 (l / 32) + i % 4, column l % 32.
+template <typename T>
+__device__ __forceinline__ f32x16 mma32(typename Tr<T>::x8 a, typename Tr<T>::x8 b, f32x16 c) {
+    if constexpr (sizeof(T) == 2) {
+        return Tr<T>::mma(a, b, c);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+        return c;
+    }
+}
+
+// row (of 0..7) of entry i of a 32x32 result, without the lane's 4 (l / 32)
+__device__ __forceinline__ constexpr int entry_row(int i) { return 8 * (i >> 2) + (i & 3); }
+
+// Operands read from a staged tile of 32 rows (layout Rows<T, D>).
+template <typename T, int D>
+struct SeqFrags {
+    using L = Rows<T, D>;
+    using x8 = typename Tr<T>::x8;
+    static constexpr int kKS = D / 16;  // contraction steps along D
+    static constexpr int kDB = D / 32;  // blocks of 32 columns
+    static constexpr int kRowB = L::kRowBytes;
+    static constexpr int kTile = 32 * kRowB;
+    static constexpr int kStepB = 16 * (int)sizeof(T);  // bytes of a row per contraction step
+    int ro, co;
+
+    __device__ __forceinline__ void init(int lane) {
+        const int r = lane & 31, h = lane >> 5;
+        ro = L::off(r, sizeof(T) == 2 ? h : 2 * h);
+        if constexpr (sizeof(T) == 2) {
+            // 16-lane group (2 h + e) of the transposed read: rows 4 h + s, columns
+            // e * 16 + 4 q .. +3
+            const int e = (lane >> 4) & 1, i = lane & 15;
+            co = L::off(4 * h + (i >> 2), e * 2 + ((i & 3) >> 1)) + (i & 1) * 8;
+        } else {
+            co = h;
+        }
+    }
+
+    // lane l: row l % 32, elements 16 st + 8 (l / 32) .. +7
+    __device__ __forceinline__ x8 row(const unsigned char* tile, int st) const {
+        const unsigned char* p = tile + (ro ^ (st * kStepB));
+        if constexpr (sizeof(T) == 2) {
+            return __builtin_bit_cast(x8, lds16(p));
+        } else {
+            const f32x4 a = __builtin_bit_cast(f32x4, lds16(p));
+            const f32x4 b = __builtin_bit_cast(f32x4, lds16(tile + (ro ^ (st * kStepB) ^ 16)));
+            return x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        }
+    }
+
+    // Transposed: lane l holds column 32 db + l % 32; slots 0..3 rows 16 bi + 4 (l / 32) + j,
+    // slots 4..7 the rows 8 further on: the rows of entries 8 bi .. 8 bi + 7 of a 32x32
+    // result, so such a result feeds the next product without a shuffle.
+    __device__ __forceinline__ x8 col(const unsigned char* tile, int db, int bi, int lane) const {
+        if constexpr (sizeof(T) == 2) {
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            // (rows 8 further on have another swizzle)
+            constexpr int kSwz8 = L::swz(8) << 4;
+            const unsigned char* p = tile + bi * 16 * kRowB;
+            const i32x2 a = __builtin_bit_cast(
+                i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + (co ^ (db << 6)))));
+            const i32x2 b = __builtin_bit_cast(
+                i32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                           (lds_s16x4*)(p + 8 * kRowB + (co ^ (db << 6) ^ kSwz8))));
+            return __builtin_bit_cast(x8, i32x4{a[0], a[1], b[0], b[1]});
+        } else {
+            const int d = db * 32 + (lane & 31);
+            x8 v;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int r = bi * 16 + (j < 4 ? 0 : 8) + 4 * co + (j & 3);
+                v[j] = *reinterpret_cast<const float*>(tile + L::off(r, d >> 2) + (d & 3) * 4);
+            }
+            return v;
+        }
+    }
+};
+
+
+// ---- staging: 32 rows straight to LDS, 1024 bytes per wave instruction ----
+// Instruction t covers rows t * kRpi .. of the tile, all inside one 16-row block, so its
+// source is a uniform base plus a lane offset that differs between instructions only by the
+// swizzle of the first row.
+template <typename T, int D>
+struct SeqRows {
+    using L = Rows<T, D>;
+    static constexpr int kRowB = L::kRowBytes;
+    static constexpr int kTile = 32 * kRowB;
+    static constexpr int kInstr = kTile / 1024;
+    static constexpr int kRpi = 64 / L::kSegs;
+    int rowl;      // this lane's row of an instruction
+    uint32_t seg;  // byte of its segment, swizzled by that row
+    __device__ __forceinline__ void init(int lane) {
+        rowl = lane / L::kSegs;
+        seg = (uint32_t)((lane % L::kSegs) ^ L::swz(rowl)) << 4;
+    }
+    // lane offset of instruction t from its first row; lane_rows: rowl * row stride
+    __device__ __forceinline__ uint32_t off(int t, uint32_t lane_rows) const {
+        return (seg ^ ((uint32_t)L::swz((t * kRpi) & 15) << 4)) + lane_rows;
+    }
+};
+
+// 16 bytes per lane to consecutive LDS positions from dst, from a uniform base + lane offset
+// or from lane addresses, in inline assembly: the compiler tracks none of them (it would wait
+// for every one before each transposed LDS read), so every wait is written out.  No output
+// registers.  The move and four idle states keep the distances that the hardware needs
+// between a scalar register's write and its use by a vector memory instruction.
+__device__ __forceinline__ void seq_load(const unsigned char* base, uint32_t off,
+                                         unsigned char* dst) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const unsigned m0 = (unsigned)(size_t)(lds_void*)dst;
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1"
+                 :
+                 : "v"(off), "s"(base), "s"(m0)
+                 : "memory");
+#endif
+}
+__device__ __forceinline__ void seq_load(const unsigned char* addr, unsigned char* dst) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const unsigned m0 = (unsigned)(size_t)(lds_void*)dst;
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, off"
+                 :
+                 : "v"(addr), "s"(m0)
+                 : "memory");
+#endif
+}
+
+// Waits until at most N of this wave's vector memory operations are outstanding.
+template <int N>
+__device__ __forceinline__ void wait_vmem_but() {
+    static_assert(N < 64, "6-bit counter");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+// This wave's LDS reads are done (what they read may be overwritten).
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// This wave's stage loads have landed and its LDS reads are done, and so for all waves.
+__device__ __forceinline__ void stage_barrier() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// The rows of one workgroup tile: which request or sequence, which tokens, what they see.
+struct SeqTile {
+    int b;        // sequence or request
+    int row0;     // first row (of n * G)
+    int rows;     // rows of the tile that exist
+    int qtok;     // first token of the request in q (paged; contiguous: 0)
+    int pos0;     // position of the request's token 0
+    int valid;    // tokens [0, valid) attend and are attended (contiguous: the length)
+    int pmin, pmax;  // first and last position of the tile's attending rows
+    int lo;       // first position that a row's window reaches
+    int nS, w0, nT;  // tiles of the first tokens, first window tile, tiles in all (0: none)
+    __device__ __forceinline__ void span(const SeqGeo& g) {
+        lo = max(pmin - g.W + 1, 0);
+        w0 = lo >> 5;
+        nS = min((g.S + 31) >> 5, w0);
+        nT = nS + (pmax >> 5) - w0 + 1;
+    }
+    // first position of key tile e
+    __device__ __forceinline__ int tile(int e) const { return (e < nS ? e : w0 + e - nS) << 5; }
+    // whether some row may see position j
+    __device__ __forceinline__ bool sees(const SeqGeo& g, int j) const {
+        return (j >= lo || j < g.S) && j <= pmax;
+    }
+};
+
+// Paged form: row tile `tile` of M = 2^lgM rows -> its request.  Request r's tiles start at
+// floor(cu[r] G / M) + r, which leaves each at least as many as it has and needs no table;
+// the lanes of a wave search 64 requests at a time.  False: no such tile.
+__device__ __forceinline__ bool seq_locate(const SeqGeo& g, int tile, int lgM, int lane,
+                                           SeqTile& t) {
+    auto first = [&](int r) { return (int)(((uint32_t)g.cu[r] * (uint32_t)g.G) >> lgM) + r; };
+    int lo = 0, span = g.B;  // the request is in [lo, lo + span)
+    while (span > 1) {
+        const int step = (span + 63) >> 6;
+        const int r = lo + lane * step;
+        const bool in = lane * step < span && first(min(r, g.B - 1)) <= tile;
+        const int below = __builtin_popcountll(__builtin_amdgcn_ballot_w64(in));
+        lo += (below > 0 ? below - 1 : 0) * step;
+        span = min(step, g.B - lo);
+    }
+    const int r = uniform(lo);
+    const int start = g.cu[r], n = g.cu[r + 1] - start;
+    if (start < 0 || n <= 0 || start > g.n - n) return false;
+    t.b = r;
+    t.row0 = (tile - first(r)) << lgM;
+    if (t.row0 < 0 || t.row0 >= n * g.G) return false;
+    t.rows = min(n * g.G - t.row0, 1 << lgM);
+    t.qtok = start;
+    t.pos0 = min(max(g.context[r], 0), g.max_pages << g.lgps);
+    t.valid = n;
+    t.pmin = t.pos0 + g.fd_G.div(t.row0);
+    t.pmax = t.pos0 + g.fd_G.div(t.row0 + t.rows - 1);
+    t.span(g);
+    return true;
+}
+
+// Key splits of a row tile of nT key tiles: split s < seq_splits has tiles [s chunk, ..), the
+// last one whatever is left (the host sizes chunk by a bound that it is told).
+__device__ __forceinline__ int seq_splits(const SeqGeo& g, int nT) {
+    return max(1, min(g.nsplit, (nT + g.chunk - 1) / g.chunk));
+}
+
+// Launchers (host).  part: split results, see the workspace of na_cache_attention.
+hipError_t launch_seq_forward(const SeqGeo& g, int D, int dtype, bool paged, bool narrow,
+                              const void* q, const void* k, const void* v, void* out, float* lse,
+                              float* part, hipStream_t s);
+hipError_t launch_cache_tables(int R, int tokens, int lgps, int max_pages, int num_free,
+                               const int32_t* context, const int32_t* fresh,
+                               const int32_t* free_pages, const int32_t* head, int32_t* table,
+                               int32_t* cu, int64_t* slots, int32_t* positions, int32_t* new_head,
+                               hipStream_t s);
+hipError_t launch_cache_write(int tokens, int Hkv, int row_bytes, int lgps, int64_t slots_end,
+                              int64_t kt, int64_t kh, int64_t vt, int64_t vh, const void* k,
+                              const void* v, const int64_t* slots, void* k_pages, void* v_pages,
+                              hipStream_t s);
+
+}  // namespace na

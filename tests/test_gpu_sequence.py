@@ -1,0 +1,483 @@
+"""The sequence operators on the GPU against plain 64-bit forms (tests/sequence_plain.py, which
+derives the tolerances)."""
+import math
+import random
+
+import pytest
+import torch
+
+from tests import sequence_plain as plain
+
+pytestmark = pytest.mark.gpu
+
+DT = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def na():
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible")
+    import paper_2403_04690_amd as lib
+
+    lib.load_library()
+    return lib
+
+
+def _randn(shape, dtype, seed):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(DT[dtype]).cuda()
+
+
+def _sink_check(na, q, k, v, W, S, scale=None, lengths=None, **kw):
+    lens = None if lengths is None else torch.tensor(lengths, dtype=torch.int32).cuda()
+    out, lse = na.sink_forward(q, k, v, W, S, scale, lens, **kw)
+    torch.cuda.synchronize()
+    scale = 1 / math.sqrt(q.shape[-1]) if scale is None else scale
+    ro, rl, to, tl = plain.sink(q, k, v, W, S, scale, lengths)
+    plain.close(out, ro, to, "out")
+    plain.close(lse, rl, tl, "lse")
+    return out, lse
+
+
+# ---------------------------------------------------------------- contiguous sequences
+
+SINK_CASES = [
+    # batch, heads, kv_heads, tokens, head_dim, kernel_size, sinks, dtype, lengths
+    (1, 1, 1, 1, 32, 1, 0, "fp32", None),
+    (1, 1, 1, 1, 64, 5, 4, "fp16", None),
+    (2, 2, 2, 31, 32, 7, 0, "bf16", None),
+    (1, 2, 1, 33, 64, 8, 1, "fp32", None),
+    (1, 4, 4, 127, 128, 16, 4, "bf16", None),
+    (1, 3, 1, 129, 64, 1, 0, "fp16", None),
+    (1, 3, 1, 129, 64, 1, 2, "fp16", None),
+    (2, 6, 2, 300, 64, 33, 5, "bf16", None),
+    (1, 8, 1, 200, 32, 64, 33, "fp16", None),
+    (1, 40, 1, 70, 64, 20, 3, "bf16", None),
+    (1, 130, 1, 10, 32, 4, 2, "fp32", None),
+    (1, 5, 5, 257, 128, 300, 0, "fp16", None),      # full causal
+    (1, 2, 2, 257, 128, 31, 400, "fp32", None),     # first tokens beyond the length
+    (2, 2, 1, 500, 128, 100, 64, "fp32", None),
+    (1, 2, 2, 1000, 64, 96, 40, "fp16", None),
+    (1, 2, 2, 700, 32, 2 ** 40, 0, "bf16", None),
+    (3, 4, 2, 130, 64, 32, 4, "fp16", (130, 0, 77)),
+    (4, 2, 2, 65, 128, 9, 2, "bf16", (1, 64, 200, -3)),
+    (2, 2, 1, 300, 32, 500, 0, "fp32", (300, 33)),
+]
+
+
+@pytest.mark.parametrize("B,H,Hkv,N,D,W,S,dtype,lengths", SINK_CASES)
+def test_sink_forward(na, B, H, Hkv, N, D, W, S, dtype, lengths):
+    q, k, v = (_randn((B, h, N, D), dtype, 10 + i) for i, h in enumerate((H, Hkv, Hkv)))
+    _sink_check(na, q, k, v, W, S, lengths=lengths)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+def test_sink_forward_of_strided_tensors(na, dtype):
+    B, H, Hkv, N, D = 2, 6, 3, 150, 64
+    # one projection's output, cut into q, k and v
+    fused = _randn((B, N, H + 2 * Hkv, D), dtype, 3).transpose(1, 2)
+    q, k, v = fused[:, :H], fused[:, H:H + Hkv], fused[:, H + Hkv:]
+    out, _ = _sink_check(na, q, k, v, 40, 4)
+    # the caller's output in the same order, beside memory that stays as it was
+    room = torch.full((B, N, H + 1, D), 7.0, dtype=DT[dtype], device="cuda")
+    own = room.transpose(1, 2)[:, :H]
+    _sink_check(na, q, k, v, 40, 4, out=own)
+    assert torch.equal(own, out) and bool((room[:, :, H] == 7).all())
+    # heads and sequences that share one key row
+    k1 = _randn((1, 1, N, D), dtype, 4).expand(B, Hkv, N, D)
+    _sink_check(na, q, k1, k1, 40, 4)
+    # the same key for every token
+    k2 = _randn((B, Hkv, 1, D), dtype, 5).expand(B, Hkv, N, D)
+    _sink_check(na, q, k2, v, 40, 4)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 4.0])
+def test_sink_forward_scales(na, scale):
+    q, k, v = (_randn((1, 2, 200, 64), "bf16", 20 + i) for i in range(3))
+    _sink_check(na, q, k, v, 50, 4, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("poison", [math.nan, math.inf, "lowest"])
+def test_sink_forward_reads_nothing_behind_a_length(na, dtype, poison):
+    value = torch.finfo(DT[dtype]).min if poison == "lowest" else poison
+    q, k, v = (_randn((2, 4, 130, 64), dtype, 30 + i) for i in range(3))
+    lengths = (70, 0)
+    want = _sink_check(na, q, k, v, 40, 4, lengths=lengths)
+    for t in (q, k, v):
+        t[0, :, 70:] = value
+        t[1] = value
+    lens = torch.tensor(lengths, dtype=torch.int32).cuda()
+    for a, b in zip(want, na.sink_forward(q, k, v, 40, 4, lengths=lens)):
+        assert torch.equal(a, b)
+
+
+def test_sink_forward_without_first_tokens_is_the_causal_window(na):
+    q, k, v = (_randn((1, 4, 600, 64), "fp32", 40 + i) for i in range(3))
+    out, lse = na.sink_forward(q, k, v, 77)
+    ref, rlse = na.forward(q, k, v, (77,), causal=(True,))
+    # two fp32 kernels, each within its bound of about 1e-5 here
+    assert float((out - ref).abs().max()) < 2e-5 and float((lse - rlse).abs().max()) < 2e-5
+
+
+def test_sink_forward_repeats_bit_for_bit(na):
+    q, k, v = (_randn((1, 4, 3000, 128), "bf16", 50 + i) for i in range(3))
+    a, b = (na.sink_forward(q, k, v, 512, 4) for _ in range(2))
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_empty_sequences(na):
+    for shape in ((0, 2, 5, 32), (1, 0, 5, 32), (1, 2, 0, 32)):
+        q = torch.empty(shape, device="cuda")
+        out, lse = na.sink_forward(q, q, q, 3, 1)
+        assert out.shape == q.shape and lse.shape == q.shape[:-1]
+
+
+# ---------------------------------------------------------------- tables
+
+def _table(rows, most):
+    return torch.tensor([list(r) + [-1] * (most - len(r)) for r in rows],
+                        dtype=torch.int32).reshape(len(rows), most)
+
+
+def _server(context, new, page, seed=0, spare=3, most=None):
+    """Page table, free list and pool of requests in a random order of pages."""
+    order = list(range(sum(-(-(c + n) // page) for c, n in zip(context, new)) + spare))
+    random.Random(seed).shuffle(order)
+    rows = []
+    for c in context:
+        need = -(-c // page)
+        rows.append(order[:need])
+        order = order[need:]
+    if most is None:
+        most = max([1] + [-(-(c + n) // page) for c, n in zip(context, new)])
+    return _table(rows, most), torch.tensor(order, dtype=torch.int32)
+
+
+def _tables_check(na, context, new, page, room=None, head=None, free=None, most=None, seed=0):
+    table, pool = _server(context, new, page, seed, most=most)
+    pool = pool if free is None else pool[:free]
+    tokens = sum(max(n, 0) for n in new) if room is None else room
+    dev = [torch.tensor(x, dtype=torch.int32).cuda() for x in (context, new)]
+    gtable = table.cuda()
+    at = None if head is None else torch.tensor([head], dtype=torch.int32).cuda()
+    got = na.cache_tables(*dev, gtable, pool.cuda(), page, tokens, head=at)
+    want_table = table.tolist()
+    want = plain.tables(context, new, want_table, pool.tolist(), page, tokens, head or 0)
+    assert got[0].tolist() == want[0]
+    assert got[1].tolist() == want[1]
+    assert got[2].tolist() == want[2]
+    assert got[3].tolist() == [want[3]]
+    assert gtable.tolist() == want_table
+
+
+@pytest.mark.parametrize("context,new,page", [
+    ([0], [0], 16), ([0], [1], 16), ([15], [1], 16), ([16], [1], 16), ([17], [100], 16),
+    ([0, 5, 16, 31], [1, 0, 17, 1], 16), ([100, 0, 0, 63], [0, 0, 129, 1], 64),
+    ([7] * 64, [1] * 64, 32),
+])
+def test_tables(na, context, new, page):
+    _tables_check(na, context, new, page)
+
+
+def test_tables_of_many_requests_and_long_prompts(na):
+    rng = random.Random(5)
+    context = [rng.choice((0, 1, 16, 40, 333)) for _ in range(2500)]
+    new = [rng.choice((0, 0, 1, 1, 3, 40)) for _ in range(2500)]
+    new[7], new[1300], new[2499] = 5000, 1, 2049
+    _tables_check(na, context, new, 16)
+    _tables_check(na, [3] * 1024, [1] * 1024, 128)
+    _tables_check(na, [0] * 1025, [0] * 1024 + [3], 16)
+
+
+def test_tables_with_a_head_room_and_a_dry_pool(na):
+    _tables_check(na, [3, 20], [30, 5], 16, room=50)             # room behind the last token
+    _tables_check(na, [3, 20], [30, 5], 16, room=20)             # and too little of it
+    _tables_check(na, [3, 20, 0], [30, 50, 9], 16, head=1)       # pages already handed out
+    _tables_check(na, [3, 20, 0], [30, 50, 9], 16, free=2)       # a pool that runs dry
+    _tables_check(na, [3, 20, 0], [30, 50, 9], 16, free=0)
+    _tables_check(na, [3, 20, 0], [30, 50, 9], 16, most=2)       # a table too narrow
+    _tables_check(na, [-4, 20], [-3, 2], 16)                     # counts below zero are none
+    _tables_check(na, [0, 0], [0, 0], 16, room=0)
+
+
+def test_tables_of_no_requests(na):
+    e = torch.empty(0, dtype=torch.int32, device="cuda")
+    cu, slots, pos, head = na.cache_tables(e, e, torch.empty(0, 4, dtype=torch.int32,
+                                                            device="cuda"), e, 16, 3)
+    assert cu.tolist() == [0] and slots.tolist() == [-1] * 3 and head.tolist() == [0]
+
+
+# ---------------------------------------------------------------- writes
+
+@pytest.mark.parametrize("dtype", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("tokens,Hkv,D,page", [(1, 1, 32, 16), (77, 3, 64, 16), (300, 2, 128, 64)])
+def test_write(na, dtype, tokens, Hkv, D, page):
+    P = -(-tokens // page) + 4
+    fused = _randn((tokens, 3 * Hkv, D), dtype, 1)
+    k, v = fused[:, Hkv:2 * Hkv], fused[:, 2 * Hkv:]
+    pages = [_randn((P, Hkv, page, D), dtype, 2 + i) for i in range(2)]
+    want = [p.clone() for p in pages]
+    slots = torch.randperm(P * page, generator=torch.Generator().manual_seed(4))[:tokens]
+    slots[tokens // 2] = -1
+    if tokens > 3:
+        slots[0], slots[1] = P * page, 2 ** 40  # beyond the pages: skipped, like -1
+    na.cache_write(k, v, slots.cuda(), *pages)
+    for t, s in enumerate(slots.tolist()):
+        if 0 <= s < P * page:
+            want[0][s // page, :, s % page] = k[t]
+            want[1][s // page, :, s % page] = v[t]
+    assert torch.equal(pages[0], want[0]) and torch.equal(pages[1], want[1])
+
+
+def test_write_of_nothing(na):
+    pages = torch.zeros(2, 2, 16, 32, device="cuda")
+    k = torch.ones(0, 2, 32, device="cuda")
+    na.cache_write(k, k, torch.empty(0, dtype=torch.int64, device="cuda"), pages, pages.clone())
+    assert not bool(pages.any())
+
+
+# ---------------------------------------------------------------- attention over the cache
+
+def _cache_check(na, context, new, H, Hkv, D, page, dtype, W=None, S=0, seed=0, poison=True,
+                 scale=None, **hints):
+    table, pool = _server(context, new, page, seed)
+    for r, (c, n) in enumerate(zip(context, new)):  # the pages of the new tokens too
+        have, need = -(-c // page), -(-(c + n) // page)
+        table[r, have:need] = pool[:need - have]
+        pool = pool[need - have:]
+    P = sum(-(-(c + n) // page) for c, n in zip(context, new)) + 3
+    kp, vp = (_randn((P, Hkv, page, D), dtype, seed + 1 + i) for i in range(2))
+    q = _randn((sum(new), H, D), dtype, seed + 3)
+    w = 2 ** 31 - 1 if W is None else W
+    s = 1 / math.sqrt(D) if scale is None else scale
+    want = plain.cache(q, kp, vp, table.tolist(), context, new, w, S, s)
+    if poison:  # whatever no token sees: unused pages and rows
+        mine = set()
+        for r, (c, n) in enumerate(zip(context, new)):
+            seen = plain.visible(torch.arange(c, c + n), torch.arange(c + n), w, S).any(0)
+            mine |= {(int(table[r, j // page]), j % page) for j in range(c + n) if seen[j]}
+        keep = torch.zeros(P, page, dtype=torch.bool)
+        for a, b in mine:
+            keep[a, b] = True
+        for t in (kp, vp):
+            t.masked_fill_(~keep.cuda()[:, None, :, None], math.nan)
+    cu = torch.tensor([0] + new).cumsum(0).int().cuda()
+    out, lse = na.cache_attention(q, kp, vp, table.cuda(), torch.tensor(context).int().cuda(), cu,
+                                  W, S, scale, **hints)
+    torch.cuda.synchronize()
+    plain.close(out, want[0], want[2], "out")
+    plain.close(lse, want[1], want[3], "lse")
+    return out, lse
+
+
+CACHE_CASES = [
+    # context, new, heads, kv_heads, head_dim, page, dtype, kernel_size, sinks
+    ([0], [1], 1, 1, 32, 16, "fp32", None, 0),
+    ([40], [1], 4, 1, 64, 16, "fp16", None, 0),
+    ([5, 700, 31, 32, 64], [1] * 5, 8, 2, 128, 16, "bf16", None, 0),
+    ([5, 700, 31, 32, 64], [1] * 5, 16, 4, 64, 32, "fp16", 100, 4),
+    ([1000, 900], [1, 1], 8, 8, 128, 64, "fp32", 33, 40),
+    ([0, 0, 50], [1, 0, 2], 4, 4, 32, 16, "bf16", 1, 0),
+    ([300], [1], 64, 1, 64, 16, "bf16", None, 0),       # a group of two blocks of rows
+    ([0], [200], 4, 2, 64, 16, "bf16", None, 0),        # a prompt
+    ([77, 0, 500], [130, 1, 63], 6, 2, 64, 16, "fp16", None, 0),
+    ([77, 0, 500], [130, 1, 63], 6, 2, 128, 64, "bf16", 50, 20),
+    ([77, 0, 500, 9], [130, 0, 63, 0], 5, 1, 32, 128, "fp32", 50, 3),
+    ([600], [300], 3, 3, 128, 16, "fp32", None, 0),
+    ([2000], [40], 2, 2, 32, 16, "fp16", 300, 16),
+]
+
+
+@pytest.mark.parametrize("context,new,H,Hkv,D,page,dtype,W,S", CACHE_CASES)
+def test_cache_attention(na, context, new, H, Hkv, D, page, dtype, W, S):
+    # without hints; with exact ones; and with hints that are wrong
+    most, longest = max(new), max(c + n for c, n in zip(context, new))
+    for hints in ({}, {"max_new": most, "max_context": longest},
+                  {"max_new": 1, "max_context": 1}, {"max_new": 5000, "max_context": 2 ** 30}):
+        _cache_check(na, context, new, H, Hkv, D, page, dtype, W, S, **hints)
+
+
+@pytest.mark.parametrize("dtype,D", [("fp16", 128), ("bf16", 64), ("fp32", 128), ("fp32", 32)])
+@pytest.mark.parametrize("new", [[1, 1], [90, 1]])
+def test_cache_attention_of_long_contexts_is_split_and_joined(na, dtype, D, new):
+    _cache_check(na, [5000, 1290], new, 4, 2, D, 16, dtype, max_new=max(new), max_context=5100)
+    _cache_check(na, [5000, 1290], new, 4, 2, D, 64, dtype, 4000, 4, max_new=max(new))
+
+
+def test_cache_attention_of_many_requests(na):
+    rng = random.Random(9)
+    context = [rng.randrange(0, 60) for _ in range(200)]
+    new = [rng.choice((0, 1, 1, 2, 9)) for _ in range(200)]
+    _cache_check(na, context, new, 4, 2, 32, 16, "fp16", poison=False)
+    _cache_check(na, context, [1] * 200, 4, 2, 32, 16, "fp16", max_new=1, poison=False)
+    # more requests than one search step covers twice over
+    _cache_check(na, [3] * 4200, [1, 0] * 2100, 1, 1, 32, 16, "fp32", poison=False)
+
+
+def test_cache_attention_leaves_rows_behind_the_last_token(na):
+    kp, vp = (_randn((4, 2, 16, 64), "bf16", i) for i in range(2))
+    table = torch.tensor([[0, 1], [2, 3]], dtype=torch.int32).cuda()
+    ctx = torch.tensor([20, 3], dtype=torch.int32).cuda()
+    cu = torch.tensor([0, 3, 4], dtype=torch.int32).cuda()
+    q = _randn((10, 4, 64), "bf16", 5)
+    out = torch.full_like(q, 7.0)
+    lse = torch.full((10, 4), 7.0, device="cuda")
+    for most in (None, 1):
+        na.cache_attention(q, kp, vp, table, ctx, cu, out=out, lse=lse, max_new=most)
+        assert bool((out[4:] == 7).all()) and bool((lse[4:] == 7).all())
+        want = plain.cache(q[:4], kp, vp, table.tolist(), [20, 3], [3, 1], 2 ** 31 - 1, 0, 0.125)
+        plain.close(out[:4], want[0], want[2], "out")
+
+
+@pytest.mark.parametrize("new", [[1, 2], [70, 2]])
+def test_cache_attention_reads_pages_that_do_not_exist_as_zeros(na, new):
+    page, ctx = 16, [100, 50]
+    table = [[0, -1, 2, 9999, 4, 5, 6, -2 ** 31, 8, 9, 10], [11, 2 ** 31 - 1, 13, 14, -7, 0, 1, 2,
+                                                            3, 4, 5]]
+    kp, vp = (_randn((15, 2, page, 64), "fp16", i) for i in range(2))
+    q = _randn((sum(new), 4, 64), "fp16", 3)
+    cu = torch.tensor([0] + new).cumsum(0).int().cuda()
+    args = (torch.tensor(table, dtype=torch.int32).cuda(), torch.tensor(ctx).int().cuda(), cu)
+    want = plain.cache(q, kp, vp, table, ctx, new, 2 ** 31 - 1, 0, 0.125)
+    out, lse = na.cache_attention(q, kp, vp, *args)
+    plain.close(out, want[0], want[2], "out")
+    plain.close(lse, want[1], want[3], "lse")
+    # new tokens beyond the table's columns read zeros too; a context counts up to them
+    want = plain.cache(q, kp, vp, [t[:3] for t in table], [48, 48], new, 2 ** 31 - 1, 0, 0.125)
+    out, _ = na.cache_attention(q, kp, vp, args[0][:, :3].contiguous(), *args[1:])
+    plain.close(out, want[0], want[2], "out")
+
+
+def test_cache_attention_of_offsets_that_make_no_sense_stays_inside(na):
+    """Offsets that do not increase, or lie outside q: such requests have no rows."""
+    kp, vp = (_randn((4, 2, 16, 64), "bf16", i) for i in range(2))
+    table = torch.zeros(3, 2, dtype=torch.int32, device="cuda")
+    q = _randn((6, 4, 64), "bf16", 5)
+    out = torch.full_like(q, 7.0)
+    for cu in ([0, 2, 1, 6], [-5, 0, 2, 2], [0, 100, 200, 300], [2 ** 31 - 1, -2 ** 31, 0, 6]):
+        for ctx in ([0, 5, 31], [-9, 2 ** 31 - 1, -2 ** 31]):
+            na.cache_attention(q, kp, vp, table, torch.tensor(ctx).int().cuda(),
+                               torch.tensor(cu, dtype=torch.int64).int().cuda(), out=out)
+    torch.cuda.synchronize()
+
+
+def test_cache_beyond_32_bit_offsets(na):
+    """Pages whose byte offsets pass 2^32 (and element offsets 2^31)."""
+    page, Hkv, D = 64, 8, 128
+    P = (1 << 32) // (page * Hkv * D * 2) + 2048  # 4 GiB of keys and 256 MiB more
+    kp, vp = (torch.zeros(P, Hkv, page, D, dtype=torch.float16, device="cuda") for _ in range(2))
+    ids = [P - 1, 3, P - 2048]
+    table = torch.tensor([ids], dtype=torch.int32).cuda()
+    k, v = (_randn((150, Hkv, D), "fp16", i) for i in range(2))
+    slots = torch.tensor([ids[t // page] * page + t % page for t in range(150)])
+    na.cache_write(k, v, slots.cuda(), kp, vp)
+    assert torch.equal(kp[P - 1, :, 5], k[5]) and torch.equal(vp[P - 2048, :, 7], v[135])
+    for n in (1, 40):
+        q = _randn((n, Hkv, D), "fp16", 7)
+        out, lse = na.cache_attention(q, kp, vp, table, torch.tensor([150 - n]).int().cuda(),
+                                      torch.tensor([0, n]).int().cuda())
+        pos = torch.arange(150 - n, 150)
+        seen = plain.visible(pos, torch.arange(150), 2 ** 31, 0)
+        for h in range(Hkv):
+            r = plain.attend(*(x[:, h].cpu().double() for x in (q, k, v)), seen, D ** -0.5,
+                             torch.float16)
+            plain.close(out[:, h], r[0], r[2], "out")
+            plain.close(lse[:, h], r[1], r[3], "lse")
+
+
+# ---------------------------------------------------------------- together
+
+def _serve(na, dtype, W, S, steps, H=4, Hkv=2, D=64, page=16, stream=None):
+    """Serves two requests step by step, and checks each step against the whole sequences."""
+    total = [sum(s[r] for s in steps) for r in range(2)]
+    seqs = [[_randn((n, h, D), dtype, 60 + 3 * r + i) for i, h in enumerate((H, Hkv, Hkv))]
+            for r, n in enumerate(total)]
+    most = max(-(-n // page) for n in total)
+    table = torch.full((2, most), -1, dtype=torch.int32, device="cuda")
+    pool = torch.randperm(2 * most + 2, generator=torch.Generator().manual_seed(1)).int().cuda()
+    kp, vp = (torch.full((2 * most + 2, Hkv, page, D), math.nan, dtype=DT[dtype], device="cuda")
+              for _ in range(2))
+    ctx = torch.zeros(2, dtype=torch.int32, device="cuda")
+    head = torch.zeros(1, dtype=torch.int32, device="cuda")
+    done, got = [0, 0], [[], []]
+    for new in steps:
+        q, k, v = (torch.cat([seqs[r][i][done[r]:done[r] + new[r]] for r in range(2)])
+                   for i in range(3))
+        lens = torch.tensor(new, dtype=torch.int32).cuda()
+        out, _, head = na.cache_step(q, k, v, kp, vp, table, ctx, lens, pool, W, S, head=head)
+        got[0].append(out[:new[0]])
+        got[1].append(out[new[0]:])
+        ctx = ctx + lens
+        done = [d + n for d, n in zip(done, new)]
+    for r in range(2):
+        q, k, v = (t.transpose(0, 1)[None] for t in seqs[r])
+        want = plain.sink(q, k, v, 2 ** 31 if W is None else W, S, D ** -0.5)
+        plain.close(torch.cat(got[r]).transpose(0, 1)[None], want[0], want[2], f"request {r}")
+        once, _ = na.sink_forward(q, k, v, 2 ** 31 if W is None else W, S)
+        plain.close(once, want[0], want[2], f"sequence {r}")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("W,S", [(None, 0), (30, 4)])
+def test_serving_steps_agree_with_the_whole_sequence(na, dtype, W, S):
+    _serve(na, dtype, W, S, [(50, 0), (1, 70), (1, 1), (1, 1), (20, 1), (0, 33), (1, 1)])
+
+
+def test_serving_on_another_stream(na):
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        _serve(na, "bf16", 30, 4, [(50, 3), (1, 1), (1, 40)])
+    s.synchronize()
+
+
+def test_layers_share_a_steps_tables(na):
+    ctx = torch.tensor([20, 0], dtype=torch.int32).cuda()
+    new = torch.tensor([1, 5], dtype=torch.int32).cuda()
+    table = torch.tensor([[3, 1], [-1, -1]], dtype=torch.int32).cuda()
+    pool = torch.tensor([0, 2], dtype=torch.int32).cuda()
+    t = na.cache_tables(ctx, new, table, pool, 16, 6)
+    for layer in range(2):
+        kp, vp = (_randn((4, 2, 16, 32), "fp32", 5 * layer + i) for i in range(2))
+        q, k, v = (_randn((6, h, 32), "fp32", 9 * layer + i) for i, h in enumerate((4, 2, 2)))
+        out, lse, head = na.cache_step(q, k, v, kp, vp, table, ctx, new, pool, tables=t)
+        assert head is t[3] and head.tolist() == [1]
+        want = plain.cache(q, kp, vp, [[3, 1], [0]], [20, 0], [1, 5], 2 ** 31, 0, 32 ** -0.5)
+        plain.close(out, want[0], want[2], "out")
+
+
+def test_a_captured_step_replays_with_new_lengths(na):
+    """Decoding from a graph: lengths, table and tokens change in place between replays."""
+    R, H, Hkv, D, page, most = 3, 4, 2, 64, 16, 80
+    kp, vp = (_randn((R * most, Hkv, page, D), "bf16", i) for i in range(2))
+    table = torch.arange(R * most, dtype=torch.int32).reshape(R, most).cuda()
+    pool = torch.empty(0, dtype=torch.int32, device="cuda")
+    new = torch.ones(R, dtype=torch.int32, device="cuda")
+    ctx = torch.tensor([5, 640, 1200], dtype=torch.int32).cuda()
+    q, k, v = (_randn((R, h, D), "bf16", 7 + i) for i, h in enumerate((H, Hkv, Hkv)))
+
+    def step():
+        return na.cache_step(q, k, v, kp, vp, table, ctx, new, pool, None, 0, max_new=1)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    outs = []
+    for g in graphs:  # two graphs, each with a workspace of its own
+        with torch.cuda.graph(g):
+            outs.append(step()[:2])
+    for turn in range(6):
+        # (contexts whose last page exists, so that the empty pool is never asked)
+        ctx.copy_(torch.tensor([5 + turn, 641 + turn, 1201 + turn]).int())
+        for i, t in enumerate((q, k, v)):
+            t.copy_(_randn(t.shape, "bf16", 100 + 3 * turn + i))
+        graphs[turn % 2].replay()
+        out, lse = (t.clone() for t in outs[turn % 2])
+        eager = step()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[0]) and torch.equal(lse, eager[1])
+        want = plain.cache(q, kp, vp, table.tolist(), ctx.tolist(), [1] * R, 2 ** 31, 0, 0.125)
+        plain.close(out, want[0], want[2], "out")
