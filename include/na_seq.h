@@ -57,6 +57,20 @@ na_status na_sink_forward(const na_sink_problem* problem, const void* q, const v
                           const void* v, const int32_t* lengths, void* out, float* logsumexp,
                           na_stream_t stream);
 
+/*
+ * Gradients of out with respect to q, k and v given dout, from the saved out and logsumexp of
+ * na_sink_forward on the same inputs.  A shared key/value head sums the rows of its whole
+ * group.  dq, dk, dv are fully overwritten (0 behind a length) and must not alias the inputs or
+ * each other.  Deterministic: the same inputs give bit-identical gradients.
+ * workspace: na_sink_backward_workspace(problem) bytes; NA_ERR_WORKSPACE if workspace_bytes is
+ * less.  (0 for a problem that is empty or not valid.)
+ */
+size_t na_sink_backward_workspace(const na_sink_problem* problem);
+na_status na_sink_backward(const na_sink_problem* problem, const void* q, const void* k,
+                           const void* v, const int32_t* lengths, const void* out,
+                           const float* logsumexp, const void* dout, void* dq, void* dk, void* dv,
+                           void* workspace, size_t workspace_bytes, na_stream_t stream);
+
 /* The paged cache.  A page holds page_size tokens (a power of two, 16 or more) of every
  * key/value head: k_pages, v_pages are contiguous [pages, kv_heads, page_size, head_dim]
  * arrays.  Row r of the page table (int32 [requests, max_pages]) lists the pages of request

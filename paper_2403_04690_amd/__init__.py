@@ -514,6 +514,7 @@ def unfused_backward(q, k, v, probs, dout, kernel_size, dilation=1, scale=None, 
 
 # ---------------------------------------------------------------- sequence operators
 from .sequence import (cache_attention, cache_step, cache_tables, cache_write,  # noqa: E402
-                       sink_forward)
+                       sink_attention, sink_backward, sink_forward)
 
-__all__ += ["sink_forward", "cache_tables", "cache_write", "cache_attention", "cache_step"]
+__all__ += ["sink_forward", "sink_backward", "sink_attention", "cache_tables", "cache_write",
+            "cache_attention", "cache_step"]

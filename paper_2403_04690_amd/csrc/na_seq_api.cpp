@@ -127,6 +127,58 @@ void fill_sink(const na_sink_problem& p, const int32_t* lengths, na::SeqGeo& g) 
     g.lengths = lengths;
 }
 
+// The cut of dk, dv over workgroups, and the workspace: logsumexp and delta per row, then the
+// fp32 parts.  Fewer than 256 key tiles (a CU each) share the heads of a group among
+// workgroups.  The rows behind the windows of first tokens are cut into chunks of about a
+// window workgroup's length, no more of them than fill the GPU four times over.
+// False: too large to launch.
+bool fill_backward(const na_sink_problem& p, const int32_t* lengths, na::SeqBwd& b, size_t& bytes) {
+    std::memset(&b, 0, sizeof b);
+    fill_sink(p, lengths, b.g);
+    const na::SeqGeo& g = b.g;
+    const int64_t n = p.tokens, slices = p.batch * p.kv_heads;
+    b.scale = p.scale;
+    const int64_t ktiles = (n + 127) / 128, base = slices * ktiles;
+    const int64_t hsplit = base >= 256 ? 1 : std::min<int64_t>(g.G, (511 + base) / base);
+    int64_t blocks = 0, chunks = 1;
+    if (g.S > 0 && n > g.W) {
+        blocks = (std::min<int64_t>(g.S, n - g.W) + 31) / 32;
+        const int64_t window = (g.G + hsplit - 1) / hsplit * (std::min<int64_t>(n, g.W + 128L) / 32 + 1);
+        const int64_t tiles = g.G * ((n - g.W) / 32 + 1);
+        const int64_t share = na::kFirstParts * std::max<int64_t>(16, window);
+        chunks = std::min((tiles + share - 1) / share,
+                          std::max<int64_t>(1, 1024 / (slices * blocks)));
+    }
+    const int64_t first_jobs = slices * blocks * chunks;
+    if (first_jobs + base * hsplit >= kMaxGrid) return false;
+    b.ktiles = (int)ktiles;
+    b.hsplit = (int)hsplit;
+    b.blocks = (int)blocks;
+    b.chunks = (int)chunks;
+    b.first_jobs = (int)first_jobs;
+    b.fd_ktiles.init(b.ktiles);
+    b.fd_hsplit.init(b.hsplit);
+    b.fd_blocks.init(std::max(1, b.blocks));
+    b.fd_chunks.init(b.chunks);
+    const size_t rows = ((size_t)(p.batch * p.heads * n) + 3) / 4 * 4;
+    const size_t key = 2 * (size_t)p.head_dim;
+    const size_t part = (size_t)slices * key *
+                        (hsplit > 1 ? (size_t)(hsplit * n) : (size_t)blocks * 32);
+    const size_t first = (size_t)(chunks * na::kFirstParts) * slices * blocks * 32 * key;
+    bytes = (2 * rows + part + first) * 4;
+    return true;
+}
+
+void place_workspace(const na_sink_problem& p, float* w, na::SeqBwd& b) {
+    const size_t rows = ((size_t)(p.batch * p.heads * p.tokens) + 3) / 4 * 4;
+    const size_t key = 2 * (size_t)p.head_dim;
+    b.lse2 = w;
+    b.delta = w + rows;
+    b.part = w + 2 * rows;
+    b.first_part = b.part + (size_t)(p.batch * p.kv_heads) * key *
+                                (b.hsplit > 1 ? (size_t)b.hsplit * p.tokens : (size_t)b.blocks * 32);
+}
+
 // ---- paged cache ----
 na_status check_cache(const na_cache_problem& p) {
     if (p.requests < 0 || p.tokens < 0 || p.requests >= kMaxGrid || p.tokens >= kMaxRows)
@@ -209,6 +261,52 @@ na_status na_sink_forward(const na_sink_problem* problem, const void* q, const v
     return na::launch_seq_forward(g, (int)p.head_dim, p.dtype, false, false, q, k, v, out,
                                   logsumexp, nullptr, reinterpret_cast<hipStream_t>(stream)) ==
                    hipSuccess
+               ? NA_OK
+               : NA_ERR_HIP;
+}
+
+size_t na_sink_backward_workspace(const na_sink_problem* problem) {
+    na::SeqBwd b;
+    size_t bytes = 0;
+    if (!problem || check_sink(*problem, true) != NA_OK || empty_sink(*problem) ||
+        !fill_backward(*problem, nullptr, b, bytes))
+        return 0;
+    return bytes;
+}
+
+na_status na_sink_backward(const na_sink_problem* problem, const void* q, const void* k,
+                           const void* v, const int32_t* lengths, const void* out,
+                           const float* logsumexp, const void* dout, void* dq, void* dk, void* dv,
+                           void* workspace, size_t workspace_bytes, na_stream_t stream) {
+    if (!problem) return NA_ERR_NULL;
+    const na_sink_problem& p = *problem;
+    const na_status st = check_sink(p, true);
+    if (st != NA_OK) return st;
+    if (empty_sink(p)) return NA_OK;
+    const void* ptrs[] = {q, k, v, out, logsumexp, dout, dq, dk, dv};
+    for (const void* x : ptrs)
+        if (!x) return NA_ERR_NULL;
+    for (const void* x : ptrs)
+        if (!aligned(x, 16)) return NA_ERR_ALIGNMENT;
+    if (!aligned(workspace, 16) || !aligned(lengths, 4)) return NA_ERR_ALIGNMENT;
+    na::SeqBwd b;
+    size_t need = 0;
+    if (!fill_backward(p, lengths, b, need)) return NA_ERR_SHAPE;
+    if (workspace_bytes < need) return NA_ERR_WORKSPACE;
+    if (!workspace) return NA_ERR_NULL;
+    place_workspace(p, static_cast<float*>(workspace), b);
+    const int64_t es = elem_bytes(p.dtype);
+    auto put = [&](const na_strides& s, int64_t& x, int64_t& h, int64_t& t) {
+        x = s.batch * es;
+        h = s.head * es;
+        t = s.token * es;
+    };
+    put(p.dout, b.gb, b.gh, b.gt);
+    put(p.dq, b.qb, b.qh, b.qt);
+    put(p.dk, b.kb, b.kh, b.kt);
+    put(p.dv, b.vb, b.vh, b.vt);
+    return na::launch_seq_backward(b, (int)p.head_dim, p.dtype, q, k, v, out, logsumexp, dout, dq,
+                                   dk, dv, reinterpret_cast<hipStream_t>(stream)) == hipSuccess
                ? NA_OK
                : NA_ERR_HIP;
 }

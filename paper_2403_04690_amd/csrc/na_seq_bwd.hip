@@ -1,0 +1,552 @@
+// na_seq_bwd.hip -- gradient of the attention of na_seq_fwd.hip over contiguous sequences
+// (gfx950).
+//
+//   P_ij = exp(s_ij - lse_i), delta_i = dout_i . out_i, dA_ij = P_ij (dout_i . v_j - delta_i)
+//   dq_i = scale sum_j dA_ij k_j
+//   dk_j = scale sum_i dA_ij q_i,  dv_j = sum_i P_ij dout_i   over the rows of every head that
+//                                                             shares the key head
+//
+// P is recomputed from the logsumexp; no weight reaches global memory; no atomics, every sum
+// in a fixed order.  Three launches (two without first tokens and without split heads):
+//   dq      row-major like the forward: 128 rows a workgroup, over the keys they see; it forms
+//           delta, and leaves delta and the logsumexp in base 2 per row for the next launch
+//   dk, dv  key-major: 128 keys a workgroup over the rows whose window holds them.  Rows run
+//           head by head, so that staged rows are consecutive tokens.  Few key tiles (short
+//           sequences, many heads a group) split the heads over workgroups.  The first tokens
+//           are attended by every later row: those pairs (outside the window) are cut over
+//           rows into workgroups of their own, in the same launch, ahead of the others
+//   join    sums the fp32 parts that split heads and first tokens leave
+// P and dA are rounded once to the tensors' type for their matrix products (16-bit types);
+// everything else is fp32.
+#include "na_launch.h"
+#include "na_seq_kernels.h"
+
+namespace na {
+
+// ---- dq: 32 rows a wave ----
+template <typename T, int D>
+struct DqState {
+    using F = SeqFrags<T, D>;
+    using x8 = typename Tr<T>::x8;
+    x8 qf[F::kKS], gf[F::kKS];
+    f32x16 dq[F::kDB];
+    float lse2, delta;
+
+    template <bool MASK>
+    __device__ __forceinline__ void tile(const F& f, const unsigned char* kt,
+                                         const unsigned char* vt, int lane, float c, int j0,
+                                         int pos, int W, int S) {
+        f32x16 s = f32x16{} * 0.f, dp = f32x16{} * 0.f;
+#pragma unroll
+        for (int st = 0; st < F::kKS; ++st) s = mma32<T>(f.row(kt, st), qf[st], s);
+#pragma unroll
+        for (int st = 0; st < F::kKS; ++st) dp = mma32<T>(f.row(vt, st), gf[st], dp);
+        const int base = j0 + 4 * (lane >> 5);
+        const int dist = pos - base;
+        const int few = min(S - base, dist + 1);
+        x8 pf[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float y = fmaf(s[i], c, -lse2);
+            if constexpr (MASK) {
+                const int e = entry_row(i);
+                y = (unsigned)(dist - e) < (unsigned)W || e < few ? y : -INFINITY;
+            }
+            pf[i >> 3][i & 7] = Tr<T>::cvt(fast_exp2(y) * (dp[i] - delta));
+        }
+#pragma unroll
+        for (int db = 0; db < F::kDB; ++db)
+#pragma unroll
+            for (int bi = 0; bi < 2; ++bi)
+                dq[db] = mma32<T>(f.col(kt, db, bi, lane), pf[bi], dq[db]);
+    }
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dq_kernel(
+    SeqBwd b, const T* __restrict__ qg, const T* __restrict__ kg, const T* __restrict__ vg,
+    const T* __restrict__ og, const float* __restrict__ lseg, const T* __restrict__ dog,
+    T* __restrict__ dqg) {
+    using F = SeqFrags<T, D>;
+    constexpr int SK = seq_stage_tiles<T, D>();
+    constexpr int kBuf = SK * 2 * F::kTile;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const SeqGeo& g = b.g;
+    const int lane = threadIdx.x & 63;
+    const int wave = uniform((threadIdx.x >> 6) & 3);
+
+    SeqTile t;
+    const int id = xcd_remap(blockIdx.x, gridDim.x);
+    const int slice = g.fd_tiles.div(id);
+    seq_contiguous(g, g.ntiles - 1 - (id - slice * g.ntiles), slice, t);
+    const int kvh = slice - t.b * g.Hkv;
+
+    SeqStage<T, D, false, 4> ld;
+    ld.init(g, t, kvh, lane, kg, vg);
+    auto issue_stage = [&](int e, int buf) {
+#pragma unroll
+        for (int i = 0; i < SK; ++i)
+            if (e + i < t.nT) ld.issue(g, t, e + i, wave, smem + buf * kBuf + i * 2 * F::kTile);
+    };
+    if (t.nT > 0) issue_stage(0, 0);
+
+    const int m = wave * 32 + (lane & 31), h = lane >> 5;
+    int tok, head;
+    seq_row(g, t, m, tok, head);
+    const bool live = wave * 32 < t.rows;
+    int tf, tl, hh;
+    seq_row(g, t, wave * 32, tf, hh);
+    seq_row(g, t, wave * 32 + 31, tl, hh);
+    const int wmin = tf, wmax = min(tl, t.valid - 1);
+    const int64_t hq = (int64_t)kvh * g.G + head;
+    const int64_t from = max(min(tok, t.valid - 1), 0);  // (rows behind the length: not theirs)
+    DqState<T, D> st;
+    {
+        const T* qp = reinterpret_cast<const T*>(reinterpret_cast<const unsigned char*>(qg) +
+                                                 t.b * g.qb + hq * g.qh + from * g.qt) + 8 * h;
+        const T* op = reinterpret_cast<const T*>(reinterpret_cast<const unsigned char*>(og) +
+                                                 t.b * g.ob + hq * g.oh + from * g.ot) + 8 * h;
+        const T* gp = reinterpret_cast<const T*>(reinterpret_cast<const unsigned char*>(dog) +
+                                                 t.b * b.gb + hq * b.gh + from * b.gt) + 8 * h;
+        float d = 0.f;
+#pragma unroll
+        for (int s = 0; s < F::kKS; ++s) {
+            st.qf[s] = ld_x8<T>(qp + s * 16);
+            st.gf[s] = ld_x8<T>(gp + s * 16);
+            d = dot8<T>(st.gf[s], ld_x8<T>(op + s * 16), d);
+        }
+        st.delta = col_sum<32>(d);
+        st.lse2 = lseg[t.b * g.lb + hq * g.lh + from] * kLog2e;
+    }
+#pragma unroll
+    for (int db = 0; db < F::kDB; ++db) st.dq[db] = f32x16{} * 0.f;
+    if (m < t.rows && h == 0) {
+        const int64_t at = t.b * g.lb + hq * g.lh + tok;
+        b.lse2[at] = st.lse2;
+        b.delta[at] = st.delta;
+    }
+    F f;
+    f.init(lane);
+
+    stage_barrier();
+    for (int e = 0, buf = 0; e < t.nT; e += SK, buf ^= 1) {
+        if (e + SK < t.nT) issue_stage(e + SK, buf ^ 1);
+#pragma unroll
+        for (int i = 0; i < SK; ++i) {
+            const int j0 = t.tile(e + i);
+            const bool out = j0 > wmax || (wmin - (j0 + 31) >= g.W && j0 >= g.S);
+            if (e + i < t.nT && live && !out) {
+                const unsigned char* kt = smem + buf * kBuf + i * 2 * F::kTile;
+                const bool full = j0 + 31 <= wmin && (wmax - j0 < g.W || j0 + 31 < g.S);
+                if (full)
+                    st.template tile<false>(f, kt, kt + F::kTile, lane, g.c, j0, tok, g.W, g.S);
+                else
+                    st.template tile<true>(f, kt, kt + F::kTile, lane, g.c, j0, tok, g.W, g.S);
+            }
+        }
+        if (e + SK < t.nT) stage_barrier();
+    }
+
+    if (m >= t.rows) return;
+    const bool some = tok < t.valid;
+    T* dp = reinterpret_cast<T*>(reinterpret_cast<unsigned char*>(dqg) + t.b * b.qb + hq * b.qh +
+                                 (int64_t)tok * b.qt);
+#pragma unroll
+    for (int db = 0; db < F::kDB; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f32x4 x;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = some ? st.dq[db][4 * i + r] * b.scale : 0.f;
+            st_x4<T>(dp + db * 32 + i * 8 + h * 4, x);
+        }
+}
+
+// ---- dk, dv: 32 keys a wave ----
+// A staged tile: 32 rows of q, the same of dout, then their lse2 and delta (256 bytes).
+template <typename T, int D>
+struct KvTile {
+    static constexpr int kRows = SeqFrags<T, D>::kTile;
+    static constexpr int kBytes = 2 * kRows + 256;
+    static constexpr int kStage = sizeof(T) == 4 && D == 128 ? 1 : 2;  // tiles per stage
+    static constexpr int kLds = 2 * kStage * kBytes;
+    // waves of a workgroup of first tokens: one buffer each
+    static constexpr int kFirstWaves = kLds / kBytes;
+    static_assert(kFirstWaves <= kFirstParts, "parts of a chunk");
+};
+
+// OUT: kDk | kDv.  fp32 at D = 128 holds only one gradient's accumulators beside its
+// fragments, and forms dv and dk in two launches.
+enum { kDk = 1, kDv = 2 };
+template <typename T, int D, int OUT>
+struct KvState {
+    using F = SeqFrags<T, D>;
+    using x8 = typename Tr<T>::x8;
+    x8 kf[F::kKS], vf[OUT & kDk ? F::kKS : 1];
+    f32x16 dk[OUT & kDk ? F::kDB : 1], dv[OUT & kDv ? F::kDB : 1];
+
+    // Keys of this wave: lane l has key l % 32.
+    __device__ __forceinline__ void init(const unsigned char* kp, const unsigned char* vp, int h) {
+#pragma unroll
+        for (int s = 0; s < F::kKS; ++s) {
+            kf[s] = ld_x8<T>(reinterpret_cast<const T*>(kp) + s * 16 + 8 * h);
+            if constexpr (OUT & kDk)
+                vf[s] = ld_x8<T>(reinterpret_cast<const T*>(vp) + s * 16 + 8 * h);
+        }
+#pragma unroll
+        for (int db = 0; db < F::kDB; ++db) {
+            if constexpr (OUT & kDk) dk[db] = f32x16{} * 0.f;
+            if constexpr (OUT & kDv) dv[db] = f32x16{} * 0.f;
+        }
+    }
+
+    // Rows i0 .. i0 + 31.  Unless `full` (uniform), row i0 + 4 h + e sees this lane's key when
+    // (unsigned)(dist + e) < len.  (One body with a branch around the mask alone: two bodies
+    // meeting again in the accumulators spill them at D = 128.)
+    __device__ __forceinline__ void tile(const F& f, const unsigned char* qt, int lane, float c,
+                                         bool full, int dist, unsigned len) {
+        const unsigned char* gt = qt + F::kTile;
+        const float* stat = reinterpret_cast<const float*>(gt + F::kTile) + 4 * (lane >> 5);
+        const int ro = opaque(f.ro), co = opaque(f.co);
+        f32x16 s = f32x16{} * 0.f, dp = f32x16{} * 0.f;
+#pragma unroll
+        for (int st = 0; st < F::kKS; ++st) s = mma32<T>(F::row_at(qt, ro, st), kf[st], s);
+        x8 pf[2];
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+            const f32x4 lse2 = *reinterpret_cast<const f32x4*>(stat + 8 * i4);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 4 * i4 + r;
+                s[i] = fast_exp2(fmaf(s[i], c, -lse2[r]));
+            }
+        }
+        if (!full)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = (unsigned)(dist + entry_row(i)) < len ? s[i] : 0.f;
+        if constexpr (OUT & kDv) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) pf[i >> 3][i & 7] = Tr<T>::cvt(s[i]);
+#pragma unroll
+            for (int db = 0; db < F::kDB; ++db)
+#pragma unroll
+                for (int bi = 0; bi < 2; ++bi)
+                    dv[db] = mma32<T>(F::col_at(gt, co, db, bi, lane), pf[bi], dv[db]);
+        }
+        if constexpr (!(OUT & kDk)) return;
+#pragma unroll
+        for (int st = 0; st < F::kKS; ++st)
+            if constexpr (OUT & kDk) dp = mma32<T>(F::row_at(gt, ro, st), vf[st], dp);
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+            const f32x4 delta = *reinterpret_cast<const f32x4*>(stat + 32 + 8 * i4);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 4 * i4 + r;
+                pf[i >> 3][i & 7] = Tr<T>::cvt(s[i] * (dp[i] - delta[r]));
+            }
+        }
+#pragma unroll
+        for (int db = 0; db < F::kDB; ++db)
+#pragma unroll
+            for (int bi = 0; bi < 2; ++bi)
+                if constexpr (OUT & kDk)
+                    dk[db] = mma32<T>(F::col_at(qt, co, db, bi, lane), pf[bi], dk[db]);
+    }
+};
+
+// Stages rows [i0, i0 + 32) of one head: q, dout, statistics; rows from `valid` on as zeros
+// (their statistics are those of the last row; such pairs are masked).  Instructions first,
+// first + STEP, .. of the tile.
+template <typename T, int D, int STEP>
+struct KvStage {
+    using R = SeqRows<T, D>;
+    static constexpr int kCount = 2 * R::kInstr / STEP;
+    R rows;
+    uint32_t qlane, glane;
+    __device__ __forceinline__ void init(const SeqBwd& b, int lane) {
+        rows.init(lane);
+        qlane = rows.rowl * (uint32_t)b.g.qt;
+        glane = rows.rowl * (uint32_t)b.gt;
+    }
+    __device__ __forceinline__ void issue(const SeqBwd& b, const unsigned char* q,
+                                          const unsigned char* dout, const float* lse2,
+                                          const float* delta, int i0, int valid, int first,
+                                          int lane, unsigned char* dst) const {
+        const bool fast = i0 + 32 <= valid;
+#pragma unroll
+        for (int u = 0; u < kCount; ++u) {
+            const int x = first + u * STEP;
+            const bool isg = x >= R::kInstr;
+            const int n = isg ? x - R::kInstr : x;
+            const int r0 = n * R::kRpi;
+            const unsigned char* base = (isg ? dout : q) + (int64_t)(i0 + r0) * (isg ? b.gt : b.g.qt);
+            const uint32_t off = rows.off(n, isg ? glane : qlane);
+            if (fast)
+                seq_load(base, off, dst + x * 1024);
+            else
+                seq_load(i0 + r0 + rows.rowl < valid
+                             ? base + off
+                             : reinterpret_cast<const unsigned char*>(&kZeroRow),
+                         dst + x * 1024);
+        }
+        if (first == 0) {
+            const int row = min(i0 + (lane & 31), valid - 1);
+            seq_load4(reinterpret_cast<const unsigned char*>((lane < 32 ? lse2 : delta) + row),
+                      dst + 2 * R::kTile);
+        }
+    }
+};
+
+// Four values at a time of the 32 keys' gradients of a wave: put(column, values) for each.
+template <int D, typename Put>
+__device__ __forceinline__ void each_four(const f32x16* acc, int h, float scale, Put put) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f32x4 x;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = acc[db][4 * i + r] * scale;
+            put(db * 32 + i * 8 + h * 4, x);
+        }
+}
+// into fp32 parts ([key][dk, dv][D])
+template <typename T, int D, int OUT>
+__device__ __forceinline__ void store_part(const KvState<T, D, OUT>& st, float* p, int h,
+                                           float scale) {
+    auto put = [&](int d, f32x4 x) { st16<f32x4>(p + d, x); };
+    if constexpr (OUT & kDk) each_four<D>(st.dk, h, scale, put);
+    p += D;
+    if constexpr (OUT & kDv) each_four<D>(st.dv, h, 1.f, put);
+}
+
+template <typename T, int D, int OUT>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dkv_kernel(
+    SeqBwd b, const T* __restrict__ qg, const T* __restrict__ kg, const T* __restrict__ vg,
+    const T* __restrict__ dog, T* __restrict__ dkg, T* __restrict__ dvg) {
+    using F = SeqFrags<T, D>;
+    using KT = KvTile<T, D>;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const SeqGeo& g = b.g;
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const int wave = uniform((threadIdx.x >> 6) & 3);
+    F f;
+    f.init(lane);
+    KvState<T, D, OUT> st;
+
+    const bool first_role = (int)blockIdx.x < b.first_jobs;
+    int slice, k0, part;  // part: chunk of rows (first tokens), or of heads
+    if (first_role) {
+        const int id = b.fd_chunks.div(blockIdx.x);
+        part = blockIdx.x - id * b.chunks;
+        slice = b.fd_blocks.div(id);
+        k0 = (id - slice * b.blocks) * 32;
+    } else {
+        const int job = xcd_remap(blockIdx.x - b.first_jobs, gridDim.x - b.first_jobs);
+        const int id = b.fd_hsplit.div(job);
+        part = job - id * b.hsplit;
+        slice = b.fd_ktiles.div(id);
+        k0 = (id - slice * b.ktiles) * 128;
+    }
+    const int sb = g.fd_kv.div(slice), kvh = slice - sb * g.Hkv;
+    const int valid = g.lengths ? min(max(g.lengths[sb], 0), g.n) : g.n;
+    const unsigned char* qs = reinterpret_cast<const unsigned char*>(qg) + sb * g.qb +
+                              (int64_t)kvh * g.G * g.qh;
+    const unsigned char* gs = reinterpret_cast<const unsigned char*>(dog) + sb * b.gb +
+                              (int64_t)kvh * g.G * b.gh;
+    const int64_t stat = sb * g.lb + (int64_t)kvh * g.G * g.lh;
+
+    const int w0 = first_role ? k0 : k0 + wave * 32;  // this wave's first key
+    const int key = w0 + (lane & 31);
+    const int from = max(min(key, valid - 1), 0);
+    st.init(reinterpret_cast<const unsigned char*>(kg) + sb * g.kb + kvh * g.kh + from * g.kt,
+            reinterpret_cast<const unsigned char*>(vg) + sb * g.vb + kvh * g.vh + from * g.vt, h);
+
+    if (first_role) {
+        // rows W or more behind the key: tiles of every head in turn, this chunk's share of
+        // them, one wave a tile
+        const int t0 = (int)min(((int64_t)k0 + g.W) >> 5, (int64_t)1 << 26);
+        const int nt = max(0, ((valid - 1) >> 5) - t0 + 1);
+        const int all = nt * g.G, per = (all + b.chunks - 1) / b.chunks;
+        const int end = min(all, (part + 1) * per);
+        if (wave >= KT::kFirstWaves) return;
+        KvStage<T, D, 1> ld;
+        ld.init(b, lane);
+        unsigned char* buf = smem + wave * KT::kBytes;
+        const unsigned len = key < g.S && valid - key > g.W ? valid - key - g.W : 0;
+        for (int e = part * per + wave; e < end; e += KT::kFirstWaves) {
+            const int hd = e / nt, i0 = (t0 + e - hd * nt) * 32;
+            ld.issue(b, qs + hd * g.qh, gs + hd * b.gh, b.lse2 + stat + hd * g.lh,
+                     b.delta + stat + hd * g.lh, i0, valid, 0, lane, buf);
+            wait_vmem();
+            const bool full = i0 - (k0 + 31) >= g.W && i0 + 32 <= valid && k0 + 31 < g.S;
+            st.tile(f, buf, lane, g.c, full, i0 + 4 * h - key - g.W, len);
+            wait_lds();
+        }
+        const int64_t row = ((int64_t)(part * KT::kFirstWaves + wave) * g.B * g.Hkv + slice) *
+                                (b.blocks * 32) + key;
+        store_part<T, D, OUT>(st, b.first_part + row * 2 * D, h, b.scale);
+        return;
+    }
+
+    // ---- rows whose window holds the tile's keys, head by head ----
+    const int h0 = (int)((int64_t)g.G * part / b.hsplit);
+    const int h1 = (int)((int64_t)g.G * (part + 1) / b.hsplit);
+    const int klast = min(k0 + 127, valid - 1);
+    const int64_t reach = (int64_t)klast + g.W - 1;
+    const int last = (int)min((int64_t)valid - 1, reach);
+    const int nt = k0 < valid ? (last >> 5) - (k0 >> 5) + 1 : 0;
+    const int all = nt * (h1 - h0);
+    KvStage<T, D, 4> ld;
+    ld.init(b, lane);
+    struct Iter {
+        int hd, i;
+    } in{h0, 0}, at{h0, 0};
+    auto next = [&](Iter& x) {
+        if (++x.i == nt) {
+            x.i = 0;
+            ++x.hd;
+        }
+    };
+    auto issue_stage = [&](int e, int buf) {
+#pragma unroll
+        for (int i = 0; i < KT::kStage; ++i)
+            if (e + i < all) {
+                ld.issue(b, qs + in.hd * g.qh, gs + in.hd * b.gh, b.lse2 + stat + in.hd * g.lh,
+                         b.delta + stat + in.hd * g.lh, k0 + in.i * 32, valid, wave, lane,
+                         smem + (buf * KT::kStage + i) * KT::kBytes);
+                next(in);
+            }
+    };
+    if (all > 0) issue_stage(0, 0);
+    const unsigned len = valid > key ? (unsigned)min(g.W, valid - key) : 0u;
+    stage_barrier();
+    for (int e = 0, buf = 0; e < all; e += KT::kStage, buf ^= 1) {
+        if (e + KT::kStage < all) issue_stage(e + KT::kStage, buf ^ 1);
+#pragma unroll
+        for (int i = 0; i < KT::kStage; ++i) {
+            if (e + i < all) {
+                const int i0 = k0 + at.i * 32;
+                next(at);
+                // some row sees some key of the wave; all see all
+                const bool some = i0 + 31 >= w0 && i0 - (w0 + 31) < g.W && w0 < valid;
+                const bool full = i0 >= w0 + 31 && i0 + 31 - w0 < g.W && i0 + 32 <= valid;
+                const unsigned char* qt = smem + (buf * KT::kStage + i) * KT::kBytes;
+                if (some) st.tile(f, qt, lane, g.c, full, i0 + 4 * h - key, len);
+            }
+        }
+        if (e + KT::kStage < all) stage_barrier();
+    }
+
+    if (key >= g.n) return;
+    if (b.hsplit > 1 || w0 < b.blocks * 32) {
+        // (with one part only the first tokens' blocks have parts)
+        const int keys = b.hsplit > 1 ? g.n : b.blocks * 32;
+        const int64_t row = ((int64_t)part * g.B * g.Hkv + slice) * keys + key;
+        store_part<T, D, OUT>(st, b.part + row * 2 * D, h, b.scale);
+        return;
+    }
+    T* dk = reinterpret_cast<T*>(reinterpret_cast<unsigned char*>(dkg) + sb * b.kb + kvh * b.kh +
+                                 (int64_t)key * b.kt);
+    T* dv = reinterpret_cast<T*>(reinterpret_cast<unsigned char*>(dvg) + sb * b.vb + kvh * b.vh +
+                                 (int64_t)key * b.vt);
+    if constexpr (OUT & kDk)
+        each_four<D>(st.dk, h, b.scale, [&](int d, f32x4 x) { st_x4<T>(dk + d, x); });
+    if constexpr (OUT & kDv)
+        each_four<D>(st.dv, h, 1.f, [&](int d, f32x4 x) { st_x4<T>(dv + d, x); });
+}
+
+// Sums the parts of each key (heads, then first tokens' chunks) and rounds once: a thread per
+// four columns of dk or dv.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void seq_dkv_join_kernel(SeqBwd b, int first_parts,
+                                                           T* __restrict__ dkg,
+                                                           T* __restrict__ dvg) {
+    const SeqGeo& g = b.g;
+    const int keys = b.hsplit > 1 ? g.n : min(g.n, b.blocks * 32);
+    const int stride = b.hsplit > 1 ? g.n : b.blocks * 32;  // keys of a slice's parts
+    constexpr int kPer = 2 * D / 4;
+    const int64_t total = (int64_t)g.B * g.Hkv * keys * kPer;
+    for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < total;
+         x += (int64_t)gridDim.x * 256) {
+        const int64_t row = x / kPer;
+        const int d = (int)(x % kPer) * 4;
+        const int slice = (int)(row / keys), key = (int)(row % keys);
+        const int64_t slices = (int64_t)g.B * g.Hkv;
+        f32x4 sum{0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < b.hsplit; ++p)
+            sum += ld16<f32x4>(b.part + ((p * slices + slice) * stride + key) * 2 * D + d);
+        if (key < b.blocks * 32)
+            for (int p = 0; p < first_parts; ++p)
+                sum += ld16<f32x4>(b.first_part +
+                                   ((p * slices + slice) * (b.blocks * 32) + key) * 2 * D + d);
+        const int sb = g.fd_kv.div(slice), kvh = slice - sb * g.Hkv;
+        unsigned char* to =
+            d < D ? reinterpret_cast<unsigned char*>(dkg) + sb * b.kb + kvh * b.kh + key * b.kt
+                  : reinterpret_cast<unsigned char*>(dvg) + sb * b.vb + kvh * b.vh + key * b.vt;
+        st_x4<T>(reinterpret_cast<T*>(to) + (d < D ? d : d - D), sum);
+    }
+}
+
+// ---- host ----
+template <typename T, int D>
+static hipError_t launch_bwd(const SeqBwd& b, const T* q, const T* k, const T* v, const T* out,
+                             const float* lse, const T* dout, T* dq, T* dk, T* dv, hipStream_t s) {
+    const SeqGeo& g = b.g;
+    const unsigned slices = (unsigned)g.B * g.Hkv;
+    hipError_t e;
+    constexpr size_t qlds = 2 * seq_stage_tiles<T, D>() * 2 * SeqFrags<T, D>::kTile;
+    auto kq = seq_dq_kernel<T, D>;
+    if ((e = seq_allow_lds(kq, qlds)) != hipSuccess) return e;
+    hipLaunchKernelGGL(kq, dim3(slices * g.ntiles), dim3(256), qlds, s, b, q, k, v, out, lse, dout,
+                       dq);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    using KT = KvTile<T, D>;
+    auto launch_dkv = [&](auto kern) {
+        hipError_t r = seq_allow_lds(kern, KT::kLds);
+        if (r != hipSuccess) return r;
+        hipLaunchKernelGGL(kern, dim3(b.first_jobs + slices * b.ktiles * b.hsplit), dim3(256),
+                           KT::kLds, s, b, q, k, v, dout, dk, dv);
+        return hipGetLastError();
+    };
+    if constexpr (sizeof(T) == 4 && D == 128) {
+        e = launch_dkv(seq_dkv_kernel<T, D, kDk>);
+        if (e == hipSuccess) e = launch_dkv(seq_dkv_kernel<T, D, kDv>);
+    } else {
+        e = launch_dkv(seq_dkv_kernel<T, D, kDk | kDv>);
+    }
+    if (e != hipSuccess || (b.hsplit == 1 && b.blocks == 0)) return e;
+    const int64_t units = (int64_t)slices * (b.hsplit > 1 ? g.n : b.blocks * 32) * (D / 2);
+    const unsigned grid = (unsigned)std::min<int64_t>((units + 255) / 256, 1 << 16);
+    hipLaunchKernelGGL((seq_dkv_join_kernel<T, D>), dim3(grid), dim3(256), 0, s, b,
+                       b.chunks * KT::kFirstWaves, dk, dv);
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t launch_bwd_d(const SeqBwd& b, int D, const void* q, const void* k, const void* v,
+                               const void* out, const float* lse, const void* dout, void* dq,
+                               void* dk, void* dv, hipStream_t s) {
+    auto c = [](const void* p) { return static_cast<const T*>(p); };
+    auto m = [](void* p) { return static_cast<T*>(p); };
+    switch (D) {
+        case 32: return launch_bwd<T, 32>(b, c(q), c(k), c(v), c(out), lse, c(dout), m(dq), m(dk), m(dv), s);
+        case 64: return launch_bwd<T, 64>(b, c(q), c(k), c(v), c(out), lse, c(dout), m(dq), m(dk), m(dv), s);
+        case 128: return launch_bwd<T, 128>(b, c(q), c(k), c(v), c(out), lse, c(dout), m(dq), m(dk), m(dv), s);
+    }
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_seq_backward(const SeqBwd& b, int D, int dtype, const void* q, const void* k,
+                               const void* v, const void* out, const float* lse, const void* dout,
+                               void* dq, void* dk, void* dv, hipStream_t s) {
+    switch (dtype) {
+        case 0: return launch_bwd_d<float>(b, D, q, k, v, out, lse, dout, dq, dk, dv, s);
+        case 1: return launch_bwd_d<_Float16>(b, D, q, k, v, out, lse, dout, dq, dk, dv, s);
+        case 2: return launch_bwd_d<__bf16>(b, D, q, k, v, out, lse, dout, dq, dk, dv, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace na

@@ -98,94 +98,6 @@ struct SeqState {
     }
 };
 
-// Stages key tile `e` of the workgroup's tile (instructions first, first + step, ... of the
-// 2 kInstr of K and V).
-template <typename T, int D, bool PAGED, int STEP>
-struct SeqStage {
-    using R = SeqRows<T, D>;
-    static constexpr int kCount = 2 * R::kInstr / STEP;
-    static_assert(2 * R::kInstr % STEP == 0, "equal shares");
-    const unsigned char *kb, *vb;  // head's rows (paged: of page 0)
-    R rows;
-    uint32_t klane, vlane;  // rowl * token stride
-
-    __device__ __forceinline__ void init(const SeqGeo& g, const SeqTile& t, int kvh, int lane,
-                                         const void* k, const void* v) {
-        rows.init(lane);
-        kb = static_cast<const unsigned char*>(k) + kvh * g.kh;
-        vb = static_cast<const unsigned char*>(v) + kvh * g.vh;
-        if (!PAGED) {
-            kb += t.b * g.kb;
-            vb += t.b * g.vb;
-        }
-        klane = rows.rowl * (uint32_t)g.kt;
-        vlane = rows.rowl * (uint32_t)g.vt;
-    }
-
-    __device__ __forceinline__ void issue(const SeqGeo& g, const SeqTile& t, int e, int first,
-                                          unsigned char* dst) const {
-        const int j0 = t.tile(e);
-        bool fast = j0 + 31 <= t.pmax && (j0 >= t.lo || j0 + 31 < g.S);
-        // of the tile's two 16-row blocks: byte offset from kb, vb, and whether it exists
-        int64_t ko[2], vo[2];
-        bool ok[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int j = j0 + 16 * i;
-            if constexpr (PAGED) {
-                const int col = j >> g.lgps;
-                int id = -1;
-                if (col < g.max_pages && j <= t.pmax)
-                    id = g.table[(int64_t)t.b * g.max_pages + col];
-                ok[i] = (unsigned)id < (unsigned)g.pages;
-                id = ok[i] ? id : 0;
-                const int in = j & ((1 << g.lgps) - 1);
-                ko[i] = id * g.kb + in * g.kt;
-                vo[i] = id * g.vb + in * g.vt;
-            } else {
-                ok[i] = true;
-                ko[i] = j * g.kt;
-                vo[i] = j * g.vt;
-            }
-            fast = fast && ok[i];
-        }
-#pragma unroll
-        for (int u = 0; u < kCount; ++u) {
-            const int x = first + u * STEP;
-            const bool isv = x >= R::kInstr;
-            const int n = isv ? x - R::kInstr : x;
-            const int r0 = n * R::kRpi;
-            const int blk = r0 >> 4;
-            const int64_t in = (int64_t)(r0 & 15) * (isv ? g.vt : g.kt);
-            const unsigned char* base = (isv ? vb : kb) + (isv ? (blk ? vo[1] : vo[0])
-                                                               : (blk ? ko[1] : ko[0])) + in;
-            const uint32_t off = rows.off(n, isv ? vlane : klane);
-            if (fast) {
-                seq_load(base, off, dst + x * 1024);
-            } else {
-                const int j = j0 + r0 + rows.rowl;
-                const bool see = (blk ? ok[1] : ok[0]) && t.sees(g, j);
-                seq_load(see ? base + off : reinterpret_cast<const unsigned char*>(&kZeroRow),
-                         dst + x * 1024);
-            }
-        }
-    }
-};
-
-// Row m of the tile: token (of the request) and head of the group.
-__device__ __forceinline__ void seq_row(const SeqGeo& g, const SeqTile& t, int m, int& tok,
-                                        int& head) {
-    const int r = t.row0 + min(m, t.rows - 1);
-    tok = g.fd_G.div(r);
-    head = r - tok * g.G;
-}
-
-// Stage of the wide form: key tiles per stage.
-template <typename T, int D>
-constexpr int seq_stage_tiles() {
-    return sizeof(T) == 4 && D == 128 ? 1 : 2;
-}
-
 template <typename T, int D, bool PAGED>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 3) : 1)) void seq_wide_kernel(
     SeqGeo g, const T* __restrict__ qg, const T* __restrict__ kg, const T* __restrict__ vg,
@@ -211,16 +123,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 3) : 1)) voi
         const int id = xcd_remap(blockIdx.x, gridDim.x);
         const int slice = g.fd_tiles.div(id);
         tile = g.ntiles - 1 - (id - slice * g.ntiles);
-        t.b = g.fd_kv.div(slice);
+        seq_contiguous(g, tile, slice, t);
         kvh = slice - t.b * g.Hkv;
-        t.row0 = tile * 128;
-        t.rows = min(g.n * g.G - t.row0, 128);
-        t.qtok = t.pos0 = 0;
-        t.valid = g.lengths ? min(max(g.lengths[t.b], 0), g.n) : g.n;
-        t.pmin = g.fd_G.div(t.row0);
-        t.pmax = min(g.fd_G.div(t.row0 + t.rows - 1), t.valid - 1);
-        t.nT = 0;
-        if (t.pmin < t.valid) t.span(g);
     }
     int e0 = 0, e1 = t.nT, splits = 1;
     if constexpr (PAGED) {
@@ -495,13 +399,6 @@ __global__ __launch_bounds__(256) void seq_join_kernel(SeqGeo g, int lgM, T* __r
 }
 
 // ---- host ----
-template <typename K>
-static hipError_t allow_lds(K kern, size_t lds) {
-    return lds <= 65536 ? hipSuccess
-                        : hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
-                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-}
-
 template <typename T, int D>
 static hipError_t launch_fwd(const SeqGeo& g, bool paged, bool narrow, const T* q, const T* k,
                              const T* v, T* out, float* lse, float* part, hipStream_t s) {
@@ -510,13 +407,13 @@ static hipError_t launch_fwd(const SeqGeo& g, bool paged, bool narrow, const T* 
     if (narrow) {
         using N = SeqNarrow<T, D>;
         auto kern = seq_narrow_kernel<T, D>;
-        if ((e = allow_lds(kern, N::kLds)) != hipSuccess) return e;
+        if ((e = seq_allow_lds(kern, N::kLds)) != hipSuccess) return e;
         hipLaunchKernelGGL(kern, dim3(tiles * g.nsplit), dim3(N::W * 64), N::kLds, s, g, q, k, v,
                            out, lse, part);
     } else {
         constexpr size_t lds = 2 * seq_stage_tiles<T, D>() * 2 * SeqFrags<T, D>::kTile;
         auto kern = paged ? seq_wide_kernel<T, D, true> : seq_wide_kernel<T, D, false>;
-        if ((e = allow_lds(kern, lds)) != hipSuccess) return e;
+        if ((e = seq_allow_lds(kern, lds)) != hipSuccess) return e;
         hipLaunchKernelGGL(kern, dim3(tiles * g.nsplit), dim3(256), lds, s, g, q, k, v, out, lse,
                            part);
     }

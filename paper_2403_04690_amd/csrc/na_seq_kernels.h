@@ -83,12 +83,17 @@ struct SeqFrags {
 
     // lane l: row l % 32, elements 16 st + 8 (l / 32) .. +7
     __device__ __forceinline__ x8 row(const unsigned char* tile, int st) const {
-        const unsigned char* p = tile + (ro ^ (st * kStepB));
+        return row_at(tile, ro, st);
+    }
+    // (o: ro, or a copy of it that the compiler cannot see through, so that the offsets of the
+    // steps are formed where they are used instead of kept in registers over the tile loop)
+    __device__ __forceinline__ static x8 row_at(const unsigned char* tile, int o, int st) {
+        const unsigned char* p = tile + (o ^ (st * kStepB));
         if constexpr (sizeof(T) == 2) {
             return __builtin_bit_cast(x8, lds16(p));
         } else {
             const f32x4 a = __builtin_bit_cast(f32x4, lds16(p));
-            const f32x4 b = __builtin_bit_cast(f32x4, lds16(tile + (ro ^ (st * kStepB) ^ 16)));
+            const f32x4 b = __builtin_bit_cast(f32x4, lds16(tile + (o ^ (st * kStepB) ^ 16)));
             return x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
         }
     }
@@ -97,6 +102,10 @@ struct SeqFrags {
     // slots 4..7 the rows 8 further on: the rows of entries 8 bi .. 8 bi + 7 of a 32x32
     // result, so such a result feeds the next product without a shuffle.
     __device__ __forceinline__ x8 col(const unsigned char* tile, int db, int bi, int lane) const {
+        return col_at(tile, co, db, bi, lane);
+    }
+    __device__ __forceinline__ static x8 col_at(const unsigned char* tile, int co, int db, int bi,
+                                                int lane) {
         if constexpr (sizeof(T) == 2) {
             typedef short s16x4 __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -246,10 +255,150 @@ __device__ __forceinline__ int seq_splits(const SeqGeo& g, int nT) {
     return max(1, min(g.nsplit, (nT + g.chunk - 1) / g.chunk));
 }
 
+// Contiguous form: row tile `tile` of (sequence, key/value head) `slice`.
+__device__ __forceinline__ void seq_contiguous(const SeqGeo& g, int tile, int slice, SeqTile& t) {
+    t.b = g.fd_kv.div(slice);
+    t.row0 = tile * 128;
+    t.rows = min(g.n * g.G - t.row0, 128);
+    t.qtok = t.pos0 = 0;
+    t.valid = g.lengths ? min(max(g.lengths[t.b], 0), g.n) : g.n;
+    t.pmin = g.fd_G.div(t.row0);
+    t.pmax = min(g.fd_G.div(t.row0 + t.rows - 1), t.valid - 1);
+    t.nT = 0;
+    if (t.pmin < t.valid) t.span(g);
+}
+
+// Stages key tile `e` of the workgroup's tile (instructions first, first + step, ... of the
+// 2 kInstr of K and V).
+template <typename T, int D, bool PAGED, int STEP>
+struct SeqStage {
+    using R = SeqRows<T, D>;
+    static constexpr int kCount = 2 * R::kInstr / STEP;
+    static_assert(2 * R::kInstr % STEP == 0, "equal shares");
+    const unsigned char *kb, *vb;  // head's rows (paged: of page 0)
+    R rows;
+    uint32_t klane, vlane;  // rowl * token stride
+
+    __device__ __forceinline__ void init(const SeqGeo& g, const SeqTile& t, int kvh, int lane,
+                                         const void* k, const void* v) {
+        rows.init(lane);
+        kb = static_cast<const unsigned char*>(k) + kvh * g.kh;
+        vb = static_cast<const unsigned char*>(v) + kvh * g.vh;
+        if (!PAGED) {
+            kb += t.b * g.kb;
+            vb += t.b * g.vb;
+        }
+        klane = rows.rowl * (uint32_t)g.kt;
+        vlane = rows.rowl * (uint32_t)g.vt;
+    }
+
+    __device__ __forceinline__ void issue(const SeqGeo& g, const SeqTile& t, int e, int first,
+                                          unsigned char* dst) const {
+        const int j0 = t.tile(e);
+        bool fast = j0 + 31 <= t.pmax && (j0 >= t.lo || j0 + 31 < g.S);
+        // of the tile's two 16-row blocks: byte offset from kb, vb, and whether it exists
+        int64_t ko[2], vo[2];
+        bool ok[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int j = j0 + 16 * i;
+            if constexpr (PAGED) {
+                const int col = j >> g.lgps;
+                int id = -1;
+                if (col < g.max_pages && j <= t.pmax)
+                    id = g.table[(int64_t)t.b * g.max_pages + col];
+                ok[i] = (unsigned)id < (unsigned)g.pages;
+                id = ok[i] ? id : 0;
+                const int in = j & ((1 << g.lgps) - 1);
+                ko[i] = id * g.kb + in * g.kt;
+                vo[i] = id * g.vb + in * g.vt;
+            } else {
+                ok[i] = true;
+                ko[i] = j * g.kt;
+                vo[i] = j * g.vt;
+            }
+            fast = fast && ok[i];
+        }
+#pragma unroll
+        for (int u = 0; u < kCount; ++u) {
+            const int x = first + u * STEP;
+            const bool isv = x >= R::kInstr;
+            const int n = isv ? x - R::kInstr : x;
+            const int r0 = n * R::kRpi;
+            const int blk = r0 >> 4;
+            const int64_t in = (int64_t)(r0 & 15) * (isv ? g.vt : g.kt);
+            const unsigned char* base = (isv ? vb : kb) + (isv ? (blk ? vo[1] : vo[0])
+                                                               : (blk ? ko[1] : ko[0])) + in;
+            const uint32_t off = rows.off(n, isv ? vlane : klane);
+            if (fast) {
+                seq_load(base, off, dst + x * 1024);
+            } else {
+                const int j = j0 + r0 + rows.rowl;
+                const bool see = (blk ? ok[1] : ok[0]) && t.sees(g, j);
+                seq_load(see ? base + off : reinterpret_cast<const unsigned char*>(&kZeroRow),
+                         dst + x * 1024);
+            }
+        }
+    }
+};
+
+// Row m of the tile: token (of the request) and head of the group.
+__device__ __forceinline__ void seq_row(const SeqGeo& g, const SeqTile& t, int m, int& tok,
+                                        int& head) {
+    const int r = t.row0 + min(m, t.rows - 1);
+    tok = g.fd_G.div(r);
+    head = r - tok * g.G;
+}
+
+// Stage of the wide form: key tiles per stage.
+template <typename T, int D>
+constexpr int seq_stage_tiles() {
+    return sizeof(T) == 4 && D == 128 ? 1 : 2;
+}
+
+// The backward's geometry: the forward's, the gradients' byte strides, and the cut of dk, dv.
+constexpr int kFirstParts = 4;  // parts that a chunk of the first tokens' rows leaves, at most
+struct SeqBwd {
+    SeqGeo g;
+    int64_t gb, gh, gt;  // dout
+    int64_t qb, qh, qt, kb, kh, kt, vb, vh, vt;  // dq, dk, dv
+    float scale;
+    int ktiles;   // tiles of 128 keys
+    int hsplit;   // workgroups that share the heads of a group
+    int blocks;   // blocks of 32 keys with first tokens that rows outside the window see
+    int chunks;   // row chunks of such a block, a workgroup each
+    int first_jobs;
+    FastDiv fd_ktiles, fd_hsplit, fd_blocks, fd_chunks;
+    float *lse2, *delta;       // [B, H, n] each
+    float *part, *first_part;  // [part][slice][key][dk, dv][D]
+};
+
+// 4 bytes per lane from lane addresses to consecutive LDS positions from dst (as seq_load).
+__device__ __forceinline__ void seq_load4(const unsigned char* addr, unsigned char* dst) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const unsigned m0 = (unsigned)(size_t)(lds_void*)dst;
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dword %0, off"
+                 :
+                 : "v"(addr), "s"(m0)
+                 : "memory");
+#endif
+}
+
+// More LDS than a launch may ask for by default.
+template <typename K>
+inline hipError_t seq_allow_lds(K kern, size_t lds) {
+    return lds <= 65536 ? hipSuccess
+                        : hipFuncSetAttribute(reinterpret_cast<const void*>(kern),
+                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+}
+
 // Launchers (host).  part: split results, see the workspace of na_cache_attention.
 hipError_t launch_seq_forward(const SeqGeo& g, int D, int dtype, bool paged, bool narrow,
                               const void* q, const void* k, const void* v, void* out, float* lse,
                               float* part, hipStream_t s);
+hipError_t launch_seq_backward(const SeqBwd& b, int D, int dtype, const void* q, const void* k,
+                               const void* v, const void* out, const float* lse, const void* dout,
+                               void* dq, void* dk, void* dv, hipStream_t s);
 hipError_t launch_cache_tables(int R, int tokens, int lgps, int max_pages, int num_free,
                                const int32_t* context, const int32_t* fresh,
                                const int32_t* free_pages, const int32_t* head, int32_t* table,

@@ -9,6 +9,8 @@ Training and prompts, on ``[batch, heads, tokens, head_dim]`` tensors of any bat
 token strides (the last axis contiguous):
 
     out, lse = sink_forward(q, k, v, kernel_size, sinks)
+    dq, dk, dv = sink_backward(q, k, v, out, lse, dout, kernel_size, sinks)
+    out = sink_attention(q, k, v, kernel_size, sinks)          # under torch.autograd
 
 Serving, one step of a batch of requests over a paged cache:
 
@@ -28,7 +30,8 @@ import torch
 
 from . import DTYPES, _check, _stream, load_library
 
-__all__ = ["sink_forward", "cache_tables", "cache_write", "cache_attention", "cache_step"]
+__all__ = ["sink_forward", "sink_backward", "sink_attention", "cache_tables", "cache_write",
+           "cache_attention", "cache_step"]
 
 _vp = ctypes.c_void_p
 _i64 = ctypes.c_int64
@@ -64,6 +67,9 @@ def _library():
     if _bound is not lib:
         sink, cache = ctypes.POINTER(_SinkProblem), ctypes.POINTER(_CacheProblem)
         lib.na_sink_forward.argtypes = [sink] + [_vp] * 7
+        lib.na_sink_backward.argtypes = [sink] + [_vp] * 11 + [ctypes.c_size_t, _vp]
+        lib.na_sink_backward_workspace.argtypes = [sink]
+        lib.na_sink_backward_workspace.restype = ctypes.c_size_t
         lib.na_cache_tables.argtypes = [_i64] * 5 + [_vp] * 10
         lib.na_cache_write.argtypes = [cache] + [_vp] * 6
         lib.na_cache_attention.argtypes = ([cache] + [_vp] * 9 + [ctypes.c_size_t, _vp])
@@ -132,12 +138,13 @@ def _like(t):
 
 @functools.lru_cache(maxsize=256)
 def _sink_problem(shape, kv_heads, kernel_size, sinks, dtype, scale, strides):
-    """strides: of q, k, v, out[, dout, dq, dk, dv], each (batch, head, token, 1)."""
+    """strides: of q, k, v, out[, dout, dq, dk, dv], each (batch, head, token, 1).  With the
+    backward's workspace size, where its strides are there."""
     p = _SinkProblem(shape[0], shape[1], kv_heads, shape[2], shape[3], kernel_size, sinks)
     for name, s in zip(("q", "k", "v", "out", "dout", "dq", "dk", "dv"), strides):
         setattr(p, name, _Strides(*s[:3]))
     p.dtype, p.scale = DTYPES[dtype], scale
-    return p
+    return p, _library().na_sink_backward_workspace(p) if len(strides) > 4 else 0
 
 
 def _sink_args(q, k, v, kernel_size, sinks, scale, lengths):
@@ -177,11 +184,64 @@ def sink_forward(q, k, v, kernel_size, sinks=0, scale=None, lengths=None, out=No
         raise ValueError("out must have the shape of q")
     _rows(q, out)
     _check_lse(lse, q)
-    p = _sink_problem(q.shape, k.shape[1], kernel_size, sinks, q.dtype, scale,
-                      (q.stride(), k.stride(), v.stride(), out.stride()))
+    p, _ = _sink_problem(q.shape, k.shape[1], kernel_size, sinks, q.dtype, scale,
+                         (q.stride(), k.stride(), v.stride(), out.stride()))
     _call(lib.na_sink_forward, q.device, p, q.data_ptr(), k.data_ptr(), v.data_ptr(),
           0 if lengths is None else lengths.data_ptr(), out.data_ptr(), lse.data_ptr())
     return out, lse
+
+
+def sink_backward(q, k, v, out, lse, dout, kernel_size, sinks=0, scale=None, lengths=None,
+                  dq=None, dk=None, dv=None):
+    """Gradients of sink_forward's out with respect to q, k and v, from the out and lse that it
+    returned.  Returns (dq, dk, dv), 0 behind a length; the same inputs give the same bits."""
+    lib = _library()
+    kernel_size, sinks, scale = _sink_args(q, k, v, kernel_size, sinks, scale, lengths)
+    dq = _like(q) if dq is None else dq
+    dk = _like(k) if dk is None else dk
+    dv = _like(v) if dv is None else dv
+    for t, ref in ((out, q), (dout, q), (dq, q), (dk, k), (dv, k)):
+        if t.shape != ref.shape:
+            raise ValueError("out, dout and the gradients must have the shapes of q, k and v")
+    _rows(q, out, dout, dq, dk, dv)
+    _check_lse(lse, q)
+    p, need = _sink_problem(q.shape, k.shape[1], kernel_size, sinks, q.dtype, scale,
+                            tuple(t.stride() for t in (q, k, v, out, dout, dq, dk, dv)))
+    # (the allocator hands it out stream by stream, and to a captured graph from its own pool)
+    work = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _call(lib.na_sink_backward, q.device, p, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+          0 if lengths is None else lengths.data_ptr(), out.data_ptr(), lse.data_ptr(),
+          dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), work.data_ptr(), need)
+    return dq, dk, dv
+
+
+def _readable(t):
+    """t, or a contiguous copy where its strides are none that the kernels read."""
+    if t.stride(-1) == 1 and t.data_ptr() % 16 == 0 and all(
+            s * t.element_size() % 16 == 0 for s in t.stride()[:-1]):
+        return t
+    return t.contiguous()
+
+
+class _SinkFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, kernel_size, sinks, scale, lengths):
+        out, lse = sink_forward(q, k, v, kernel_size, sinks, scale, lengths)
+        ctx.save_for_backward(q, k, v, out, lse, lengths)
+        ctx.cfg = (kernel_size, sinks, scale)
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        q, k, v, out, lse, lengths = ctx.saved_tensors
+        grads = sink_backward(q, k, v, out, lse, _readable(dout), *ctx.cfg, lengths)
+        return grads + (None,) * 4
+
+
+def sink_attention(q, k, v, kernel_size, sinks=0, scale=None, lengths=None):
+    """Autograd-aware window attention with visible first tokens (see sink_forward)."""
+    return _SinkFunction.apply(q, k, v, kernel_size, sinks, scale, lengths)
 
 
 # ---------------------------------------------------------------- the paged cache

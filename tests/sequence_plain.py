@@ -12,6 +12,14 @@ Bounds.  A kernel works from the same (already rounded) inputs.  u is half a ste
     (against the row's largest P, which is at least 1);
   * out is a P-weighted mean, so each relative error of P moves it by at most that times
     (P |V|), once from the numerator and once from the sum, and it is rounded once more.
+
+Gradients start from the out and logsumexp that the forward stored, like the kernels:
+P = exp(s - lse), delta = dout . out.
+  * dout . v and delta are sums of D products in fp32: off by (D + 2) U of their absolute sums;
+  * dA = P (dout . v - delta) is off by the relative errors of P (its score's, exp2's) and by P
+    times those sums' errors, then rounded to the type (u, and 2^-25 absolute in fp16);
+  * dq, dk and dv sum n such terms in fp32, at most n U of their absolute sum more, and are
+    rounded once.
 """
 import math
 
@@ -67,6 +75,42 @@ def sink(q, k, v, kernel_size, sinks, scale, lengths=None):
             r = attend(q[b, h, :n], k[b, c, :n], v[b, c, :n], seen, scale, dtype)
             out[b, h, :n], lse[b, h, :n], tol[b, h, :n], tol_lse[b, h, :n] = r
     return out, lse, tol, tol_lse
+
+
+def sink_grad(q, k, v, out, lse, dout, kernel_size, sinks, scale, lengths=None):
+    """dq, dk, dv and their tolerances (float64 on the CPU) from the stored out and lse."""
+    dtype = q.dtype
+    q, k, v, out, lse, dout = (t.detach().cpu().double() for t in (q, k, v, out, lse, dout))
+    B, H, N, D = q.shape
+    G = H // k.shape[1]
+    grads = [torch.zeros_like(t) for t in (q, k, v)]
+    tols = [torch.zeros_like(t) for t in (q, k, v)]
+    u = HALF[dtype]
+    u_p = u if dtype != torch.float32 else 0.0
+    tiny = 2.0 ** -25 if dtype == torch.float16 else 0.0
+    for b in range(B):
+        n = N if lengths is None else max(0, min(N, int(lengths[b])))
+        pos = torch.arange(n)
+        seen = visible(pos, pos, kernel_size, sinks)
+        for h in range(H):
+            c = h // G
+            qq, kk, vv = q[b, h, :n], k[b, c, :n], v[b, c, :n]
+            g, o = dout[b, h, :n], out[b, h, :n]
+            s = (qq @ kk.T) * scale
+            p = torch.where(seen, torch.exp(s - lse[b, h, :n, None]), torch.zeros_like(s))
+            e = (D + 4) * U * abs(scale) * (qq.abs() @ kk.abs().T) \
+                + 2 * U * (s.abs() + lse[b, h, :n, None].abs()) + 2.0 ** -21
+            da = p * (g @ vv.T - (g * o).sum(-1, keepdim=True))
+            e_da = (e + u_p) * da.abs() + tiny * seen + (1 + e) * p * (D + 2) * U * (
+                g.abs() @ vv.abs().T + (g * o).abs().sum(-1, keepdim=True))
+            e_p = p * (e + u_p) + tiny * seen
+            grads[0][b, h, :n] = scale * da @ kk
+            tols[0][b, h, :n] = abs(scale) * (e_da + n * U * da.abs()) @ kk.abs()
+            grads[1][b, c, :n] += scale * da.T @ qq
+            tols[1][b, c, :n] += abs(scale) * (e_da + G * n * U * da.abs()).T @ qq.abs()
+            grads[2][b, c, :n] += p.T @ g
+            tols[2][b, c, :n] += (e_p + G * n * U * p).T @ g.abs()
+    return grads, [t + u * g.abs() + tiny for t, g in zip(tols, grads)]
 
 
 def tables(context, new, page_table, free, page_size, tokens, head=0):

@@ -130,6 +130,171 @@ def test_empty_sequences(na):
         q = torch.empty(shape, device="cuda")
         out, lse = na.sink_forward(q, q, q, 3, 1)
         assert out.shape == q.shape and lse.shape == q.shape[:-1]
+        for g in na.sink_backward(q, q, q, out, lse, q, 3, 1):
+            assert g.shape == q.shape
+
+
+# ---------------------------------------------------------------- gradients
+
+def _grad_check(na, q, k, v, dout, W, S, scale=None, lengths=None, **own):
+    lens = None if lengths is None else torch.tensor(lengths, dtype=torch.int32).cuda()
+    out, lse = na.sink_forward(q, k, v, W, S, scale, lens)
+    grads = na.sink_backward(q, k, v, out, lse, dout, W, S, scale, lens, **own)
+    torch.cuda.synchronize()
+    s = 1 / math.sqrt(q.shape[-1]) if scale is None else scale
+    want, tols = plain.sink_grad(q, k, v, out, lse, dout, W, S, s, lengths)
+    for name, g, w, t in zip(("dq", "dk", "dv"), grads, want, tols):
+        plain.close(g, w, t, name)
+    return grads
+
+
+GRAD_CASES = SINK_CASES + [
+    (1, 2, 2, 1500, 64, 40, 4, "fp16", None),       # first tokens' rows in several chunks
+    (1, 8, 2, 900, 128, 64, 40, "bf16", None),      # two blocks of first tokens, split heads
+    (2, 4, 1, 700, 32, 20, 70, "fp32", (700, 333)),
+    (1, 2, 1, 600, 128, 30, 4, "fp32", None),
+    (1, 12, 1, 260, 64, 260, 0, "bf16", None),
+    (1, 2, 2, 300, 64, 1, 1, "fp32", None),
+    (40, 8, 8, 100, 32, 17, 3, "fp16", None),       # more key tiles than CUs: heads not split
+    (1, 4, 4, 97, 64, 96, 3, "bf16", None),         # one row beyond the window
+]
+
+
+@pytest.mark.parametrize("B,H,Hkv,N,D,W,S,dtype,lengths", GRAD_CASES)
+def test_sink_backward(na, B, H, Hkv, N, D, W, S, dtype, lengths):
+    q, k, v, g = (_randn((B, h, N, D), dtype, 70 + i) for i, h in enumerate((H, Hkv, Hkv, H)))
+    _grad_check(na, q, k, v, g, W, S, lengths=lengths)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+def test_sink_backward_of_strided_tensors(na, dtype):
+    B, H, Hkv, N, D = 2, 6, 3, 150, 64
+    fused = _randn((B, N, H + 2 * Hkv, D), dtype, 3).transpose(1, 2)
+    q, k, v = fused[:, :H], fused[:, H:H + Hkv], fused[:, H + Hkv:]
+    g = _randn((B, N, H, D), dtype, 4).transpose(1, 2)
+    grads = _grad_check(na, q, k, v, g, 40, 4)
+    # into one buffer of the projection's layout
+    room = torch.full((B, N, H + 2 * Hkv + 1, D), 7.0, dtype=DT[dtype], device="cuda")
+    own = room.transpose(1, 2)
+    into = {"dq": own[:, :H], "dk": own[:, H:H + Hkv], "dv": own[:, H + Hkv:H + 2 * Hkv]}
+    for a, b in zip(_grad_check(na, q, k, v, g, 40, 4, **into), grads):
+        assert torch.equal(a, b)
+    assert bool((own[:, -1] == 7).all())
+    # broadcast inputs and output gradient
+    k1 = _randn((1, 1, N, D), dtype, 5).expand(B, Hkv, N, D)
+    _grad_check(na, q, k1, k1, g[:, :1].expand(B, H, N, D), 40, 4)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1.0])
+def test_sink_backward_scales(na, scale):
+    q, k, v, g = (_randn((1, 2, 200, 64), "bf16", 20 + i) for i in range(4))
+    _grad_check(na, q, k, v, g, 50, 4, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("poison", [math.nan, math.inf, "lowest"])
+def test_sink_backward_reads_nothing_behind_a_length(na, dtype, poison):
+    value = torch.finfo(DT[dtype]).min if poison == "lowest" else poison
+    q, k, v, g = (_randn((2, 4, 130, 64), dtype, 30 + i) for i in range(4))
+    lengths = (70, 0)
+    want = _grad_check(na, q, k, v, g, 40, 4, lengths=lengths)
+    lens = torch.tensor(lengths, dtype=torch.int32).cuda()
+    out, lse = na.sink_forward(q, k, v, 40, 4, lengths=lens)
+    for t in (q, k, v, g, out):
+        t[0, :, 70:] = value
+        t[1] = value
+    for a, b in zip(want, na.sink_backward(q, k, v, out, lse, g, 40, 4, lengths=lens)):
+        assert torch.equal(a, b)
+        assert not bool(a[0, :, 70:].any()) and not bool(a[1].any())
+
+
+def test_sink_backward_repeats_bit_for_bit(na):
+    q, k, v, g = (_randn((1, h, 3000, 128), "bf16", 50 + i) for i, h in enumerate((4, 2, 2, 4)))
+    out, lse = na.sink_forward(q, k, v, 200, 4)
+    a, b = (na.sink_backward(q, k, v, out, lse, g, 200, 4) for _ in range(2))
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_sink_attention_under_autograd(na):
+    """Against differences of the plain form, with an output gradient of no strides at all."""
+    q, k, v = (_randn((1, h, 120, 32), "fp32", 80 + i) for i, h in enumerate((4, 2, 2)))
+    leaves = [t.requires_grad_(True) for t in (q, k[:, :1].clone(), v)]
+    wide = leaves[1].expand(1, 2, 120, 32)  # one key head behind both
+    na.sink_attention(leaves[0], wide, leaves[2], 30, 3).sum().backward()
+
+    def loss(q, k, v):
+        return float(plain.sink(q.float(), k.expand(1, 2, 120, 32).float(), v.float(), 30, 3,
+                                32 ** -0.5)[0].sum())
+
+    host = [t.detach().cpu() for t in leaves]
+    gen = torch.Generator().manual_seed(3)
+    for i, leaf in enumerate(leaves):
+        d = torch.randn(host[i].shape, generator=gen)
+        step = 2.0 ** -7  # (inputs are fp32; the loss is 64-bit: the third derivative shows)
+        up, down = list(host), list(host)
+        up[i], down[i] = host[i] + step * d, host[i] - step * d
+        moved = (up[i].double() - down[i].double()) / (2 * step)
+        slope = (loss(*up) - loss(*down)) / (2 * step)
+        got = float((leaf.grad.cpu().double() * moved).sum())
+        # differences: step^2 / 6 times third derivatives of order |d|^3 over 3840 values
+        assert abs(got - slope) < 2e-3 * (1 + abs(slope)) + 0.05, (i, got, slope)
+
+
+def test_sink_attention_refuses_a_second_derivative(na):
+    q = _randn((1, 1, 20, 32), "fp32", 1).requires_grad_(True)
+    (g,) = torch.autograd.grad(na.sink_attention(q, q, q, 4).sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+
+
+def test_a_captured_training_step_replays(na):
+    q, k, v, g = (_randn((2, h, 300, 64), "fp16", 90 + i) for i, h in enumerate((4, 2, 2, 4)))
+    lens = torch.tensor([300, 100], dtype=torch.int32).cuda()
+
+    def step():
+        out, lse = na.sink_forward(q, k, v, 40, 4, lengths=lens)
+        return (out, lse) + na.sink_backward(q, k, v, out, lse, g, 40, 4, lengths=lens)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graphs, outs = [torch.cuda.CUDAGraph() for _ in range(2)], []
+    for graph in graphs:
+        with torch.cuda.graph(graph):
+            outs.append(step())
+    for turn in range(6):
+        lens.copy_(torch.tensor([300 - 17 * turn, 100 + 30 * turn]).int())
+        for i, t in enumerate((q, k, v, g)):
+            t.copy_(_randn(t.shape, "fp16", 200 + 4 * turn + i))
+        graphs[turn % 2].replay()
+        got = [t.clone() for t in outs[turn % 2]]
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_two_steps_at_once_on_two_streams(na):
+    data = [[_randn((1, h, 500, 64), "bf16", 300 + 10 * s + i) for i, h in enumerate((8, 2, 2, 8))]
+            for s in range(2)]
+
+    def step(q, k, v, g):
+        out, lse = na.sink_forward(q, k, v, 60, 4)
+        return (out, lse) + na.sink_backward(q, k, v, out, lse, g, 60, 4)
+
+    want = [step(*d) for d in data]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for turn in range(5):
+        for s in range(2):
+            with torch.cuda.stream(streams[s]):
+                got[s].append(step(*data[s]))
+    torch.cuda.synchronize()
+    for s in range(2):
+        for r in got[s]:
+            assert all(torch.equal(a, b) for a, b in zip(r, want[s]))
 
 
 # ---------------------------------------------------------------- tables

@@ -29,7 +29,7 @@ def lib():
 def test_library_exports_every_declared_symbol(lib):
     text = open(os.path.join(ROOT, "include", "na_seq.h")).read()
     names = set(re.findall(r"\b(na_[a-z_]+)\s*\(", re.sub(r"/\*.*?\*/", "", text, flags=re.S)))
-    assert {"na_sink_forward", "na_cache_tables", "na_cache_write", "na_cache_attention",
+    assert {"na_sink_forward", "na_sink_backward", "na_sink_backward_workspace", "na_cache_tables", "na_cache_write", "na_cache_attention",
             "na_cache_attention_workspace"} <= names
     for name in names:
         assert hasattr(lib, name), name
@@ -97,6 +97,35 @@ def test_sink_forward_pointers(lib):
         assert _forward(lib, _sink(**change), q=None, out=FAKE + 2) == OK
 
 
+def _backward(lib, p, work=FAKE, size=1 << 40, lengths=None, **ptr):
+    names = ("q", "k", "v", "out", "lse", "dout", "dq", "dk", "dv")
+    ps = [ptr.get(n, FAKE) for n in names]
+    return lib.na_sink_backward(p, *ps[:3], lengths, *ps[3:], work, size, None)
+
+
+@pytest.mark.parametrize("change,status", BAD_SINK + [
+    ({"dout": (2560, 640, 60)}, SHAPE), ({"dq": (2560, 640, 0)}, SHAPE),
+    ({"dk": (0, 640, 64)}, SHAPE), ({"dv": (1280, 640, 32)}, SHAPE)])
+def test_sink_backward_rejects_before_launch(lib, change, status):
+    assert _backward(lib, _sink(**change)) == status
+    assert lib.na_sink_backward_workspace(_sink(**change)) == 0
+
+
+def test_sink_backward_pointers_and_workspace(lib):
+    assert lib.na_sink_backward(None, *[FAKE] * 11, 0, None) == NULL
+    for name in ("q", "k", "v", "out", "lse", "dout", "dq", "dk", "dv"):
+        assert _backward(lib, _sink(), **{name: None}) == NULL
+        assert _backward(lib, _sink(), **{name: FAKE + 4}) == ALIGN
+    assert _backward(lib, _sink(), lengths=FAKE + 2) == ALIGN
+    need = lib.na_sink_backward_workspace(_sink())
+    assert need >= 2 * 2 * 4 * 10 * 4  # two fp32 a row at least
+    assert _backward(lib, _sink(), size=need - 1) == WORKSPACE
+    assert _backward(lib, _sink(), work=None) == NULL
+    assert _backward(lib, _sink(), work=FAKE + 8) == ALIGN
+    for change in ({"batch": 0}, {"tokens": 0}, {"heads": 0, "kv_heads": 0}):
+        assert _backward(lib, _sink(**change), q=None, work=None, size=0) == OK
+
+
 def _cache(requests=3, tokens=5, heads=4, kv_heads=2, head_dim=64, pages=8, page_size=16,
            max_pages=4, kernel_size=100, sinks=0, max_new=0, max_context=0, dtype=1, scale=0.1,
            q=None, k=None, v=None, out=None):
@@ -155,6 +184,8 @@ def test_extreme_counts_do_not_overflow(lib):
               _cache(max_new=big, max_context=big)):
         assert _attend(lib, p, q=None) == NULL  # (valid: the pointer is what is refused)
     assert _forward(lib, _sink(kernel_size=big, sinks=big), q=None) == NULL
+    assert _backward(lib, _sink(kernel_size=big, sinks=big), q=None) == NULL
+    assert _backward(lib, _sink(sinks=big), q=None) == NULL
     for name in ("requests", "tokens", "heads", "kv_heads", "pages", "page_size", "max_pages"):
         assert _attend(lib, _cache(**{name: big})) == SHAPE
     for name in ("batch", "heads", "kv_heads", "tokens"):
@@ -279,6 +310,46 @@ def test_plain_sink_is_the_softmax_of_the_visible_scores():
             ref = sum(a * v[0, h // 2, j].double() for a, j in zip(w, js))
             assert float((out[0, h, i] - ref).abs().max()) < 1e-12
             assert abs(float(lse[0, h, i] - torch.exp(s).sum().log())) < 1e-12
+
+
+@pytest.mark.parametrize("W,S,lengths", [(3, 2, None), (1, 0, None), (100, 0, [7]), (2, 5, [9])])
+def test_plain_gradient_is_that_of_the_plain_forward(W, S, lengths):
+    gen = torch.Generator().manual_seed(2)
+    q, k, v = (torch.randn(1, h, 9, 32, generator=gen).double() for h in (4, 2, 2))
+    dout = torch.randn(1, 4, 9, 32, generator=gen).double()
+    scale = 0.3
+
+    # (plain.sink takes its bounds from a type: fp32 stands in, the values stay 64-bit)
+    def loss(q, k, v):
+        n = 9 if lengths is None else lengths[0]
+        pos = torch.arange(n)
+        seen = plain.visible(pos, pos, W, S)
+        total = 0.0
+        for h in range(4):
+            r = plain.attend(q[0, h, :n], k[0, h // 2, :n], v[0, h // 2, :n], seen, scale,
+                             torch.float32)
+            total += float((r[0] * dout[0, h, :n]).sum())
+        return total
+
+    out, lse = torch.zeros_like(q), torch.full((1, 4, 9), -math.inf).double()
+    n = 9 if lengths is None else lengths[0]
+    pos = torch.arange(n)
+    for h in range(4):
+        r = plain.attend(q[0, h, :n], k[0, h // 2, :n], v[0, h // 2, :n],
+                         plain.visible(pos, pos, W, S), scale, torch.float32)
+        out[0, h, :n], lse[0, h, :n] = r[:2]
+    plain.HALF[torch.float64] = 0.0
+    grads, _ = plain.sink_grad(q, k, v, out, lse, dout, W, S, scale, lengths)
+    del plain.HALF[torch.float64]
+    step = 1e-5
+    for i, g in enumerate(grads):  # central differences along random directions
+        for _ in range(3):
+            d = torch.randn(g.shape, generator=gen).double()
+            x = [q, k, v]
+            up, down = list(x), list(x)
+            up[i], down[i] = x[i] + step * d, x[i] - step * d
+            slope = (loss(*up) - loss(*down)) / (2 * step)
+            assert abs(slope - float((g * d).sum())) < 1e-7 * (1 + abs(slope))
 
 
 def test_plain_tables_by_hand():
