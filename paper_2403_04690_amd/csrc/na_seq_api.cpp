@@ -56,7 +56,9 @@ bool good_strides(const na_strides& s, int es, int64_t batch, int64_t heads, int
     return true;
 }
 
-int clamp_count(int64_t x) { return (int)std::min<int64_t>(x, INT32_MAX); }
+// A window in 32 bits.  Positions stay below kMaxRows + kMaxRows - 256, so the clamp keeps every
+// distance inside it, and the kernels may add the entries of a tile to it.
+int clamp_window(int64_t x) { return (int)std::min<int64_t>(x, INT32_MAX - 64); }
 
 // The fields that both forms of the attention share.
 void fill_common(na::SeqGeo& g, int64_t heads, int64_t kv_heads, int64_t kernel_size,
@@ -64,7 +66,7 @@ void fill_common(na::SeqGeo& g, int64_t heads, int64_t kv_heads, int64_t kernel_
     std::memset(&g, 0, sizeof g);
     g.G = (int)(heads / kv_heads);
     g.Hkv = (int)kv_heads;
-    g.W = clamp_count(kernel_size);
+    g.W = clamp_window(kernel_size);
     g.S = (int)std::min<int64_t>(sinks, kMaxRows);
     g.c = scale * na::kLog2e;
     g.nsplit = 1;
@@ -199,7 +201,7 @@ na_status check_attention(const na_cache_problem& p) {
         return NA_ERR_SHAPE;
     if (p.heads == 0 || p.tokens == 0 || p.requests == 0) return NA_OK;
     const int64_t G = p.heads / p.kv_heads;
-    if (p.tokens * G >= kMaxRows || (p.tokens * G / 32 + p.requests) >= kMaxGrid ||
+    if (p.tokens * G >= kMaxRows - 256 || (p.tokens * G / 32 + p.requests) >= kMaxGrid ||
         (p.tokens * G / 32 + p.requests) * p.kv_heads >= kMaxGrid)
         return NA_ERR_SHAPE;
     const int es = elem_bytes(p.dtype);

@@ -32,28 +32,25 @@ struct DqState {
     f32x16 dq[F::kDB];
     float lse2, delta;
 
-    template <bool MASK>
     __device__ __forceinline__ void tile(const F& f, const unsigned char* kt,
-                                         const unsigned char* vt, int lane, float c, int j0,
-                                         int pos, int W, int S) {
+                                         const unsigned char* vt, int lane, float c, bool full,
+                                         int j0, int pos, int W, int S) {
         f32x16 s = f32x16{} * 0.f, dp = f32x16{} * 0.f;
 #pragma unroll
         for (int st = 0; st < F::kKS; ++st) s = mma32<T>(f.row(kt, st), qf[st], s);
 #pragma unroll
         for (int st = 0; st < F::kKS; ++st) dp = mma32<T>(f.row(vt, st), gf[st], dp);
-        const int base = j0 + 4 * (lane >> 5);
-        const int dist = pos - base;
-        const int few = min(S - base, dist + 1);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = fast_exp2(fmaf(s[i], c, -lse2));
+        if (!full) {
+            const int base = j0 + 4 * (lane >> 5);
+            const unsigned m = seen_keys(pos - base, W, S - base);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = keep(m, i, s[i], 0.f);
+        }
         x8 pf[2];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float y = fmaf(s[i], c, -lse2);
-            if constexpr (MASK) {
-                const int e = entry_row(i);
-                y = (unsigned)(dist - e) < (unsigned)W || e < few ? y : -INFINITY;
-            }
-            pf[i >> 3][i & 7] = Tr<T>::cvt(fast_exp2(y) * (dp[i] - delta));
-        }
+        for (int i = 0; i < 16; ++i) pf[i >> 3][i & 7] = Tr<T>::cvt(s[i] * (dp[i] - delta));
 #pragma unroll
         for (int db = 0; db < F::kDB; ++db)
 #pragma unroll
@@ -127,6 +124,13 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dq_kernel(
     }
     F f;
     f.init(lane);
+#pragma unroll
+    for (int s = 0; s < F::kKS; ++s) {
+        settle(st.qf[s]);
+        settle(st.gf[s]);
+    }
+    settle(st.lse2);
+    settle(st.delta);
 
     stage_barrier();
     for (int e = 0, buf = 0; e < t.nT; e += SK, buf ^= 1) {
@@ -138,10 +142,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dq_kernel(
             if (e + i < t.nT && live && !out) {
                 const unsigned char* kt = smem + buf * kBuf + i * 2 * F::kTile;
                 const bool full = j0 + 31 <= wmin && (wmax - j0 < g.W || j0 + 31 < g.S);
-                if (full)
-                    st.template tile<false>(f, kt, kt + F::kTile, lane, g.c, j0, tok, g.W, g.S);
-                else
-                    st.template tile<true>(f, kt, kt + F::kTile, lane, g.c, j0, tok, g.W, g.S);
+                st.tile(f, kt, kt + F::kTile, lane, g.c, full, j0, tok, g.W, g.S);
             }
         }
         if (e + SK < t.nT) stage_barrier();
@@ -199,6 +200,13 @@ struct KvState {
             if constexpr (OUT & kDv) dv[db] = f32x16{} * 0.f;
         }
     }
+    __device__ __forceinline__ void settle_keys() {
+#pragma unroll
+        for (int s = 0; s < F::kKS; ++s) {
+            settle(kf[s]);
+            if constexpr (OUT & kDk) settle(vf[s]);
+        }
+    }
 
     // Rows i0 .. i0 + 31.  Unless `full` (uniform), row i0 + 4 h + e sees this lane's key when
     // (unsigned)(dist + e) < len.  (One body with a branch around the mask alone: two bodies
@@ -221,9 +229,11 @@ struct KvState {
                 s[i] = fast_exp2(fmaf(s[i], c, -lse2[r]));
             }
         }
-        if (!full)
+        if (!full) {
+            const unsigned m = below((int)len - dist) & ~below(-dist);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = (unsigned)(dist + entry_row(i)) < len ? s[i] : 0.f;
+            for (int i = 0; i < 16; ++i) s[i] = keep(m, i, s[i], 0.f);
+        }
         if constexpr (OUT & kDv) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) pf[i >> 3][i & 7] = Tr<T>::cvt(s[i]);
@@ -375,6 +385,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dkv_kernel(
         ld.init(b, lane);
         unsigned char* buf = smem + wave * KT::kBytes;
         const unsigned len = key < g.S && valid - key > g.W ? valid - key - g.W : 0;
+        st.settle_keys();
         for (int e = part * per + wave; e < end; e += KT::kFirstWaves) {
             const int hd = e / nt, i0 = (t0 + e - hd * nt) * 32;
             ld.issue(b, qs + hd * g.qh, gs + hd * b.gh, b.lse2 + stat + hd * g.lh,
@@ -421,6 +432,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dkv_kernel(
     };
     if (all > 0) issue_stage(0, 0);
     const unsigned len = valid > key ? (unsigned)min(g.W, valid - key) : 0u;
+    st.settle_keys();
     stage_barrier();
     for (int e = 0, buf = 0; e < all; e += KT::kStage, buf ^= 1) {
         if (e + KT::kStage < all) issue_stage(e + KT::kStage, buf ^ 1);

@@ -41,11 +41,12 @@ struct SeqState {
         for (int db = 0; db < F::kDB; ++db) o[db] = f32x16{} * 0.f;
     }
 
-    // One tile of 32 keys from position j0.  MASK: some pair is not seen; pos: this lane's row.
-    template <bool MASK>
+    // One tile of 32 keys from position j0.  Unless `full` (uniform), some pair is not seen;
+    // pos: this lane's row.  (One body with a branch around the mask alone: two bodies that
+    // meet again in the accumulators cost registers.)
     __device__ __forceinline__ void tile(const F& f, const unsigned char* kt,
-                                         const unsigned char* vt, int lane, float c, int j0,
-                                         int pos, int W, int S) {
+                                         const unsigned char* vt, int lane, float c, bool full,
+                                         int j0, int pos, int W, int S) {
         f32x16 s = f32x16{} * 0.f;
 #pragma unroll
         for (int st = 0; st < F::kKS; ++st) s = mma32<T>(f.row(kt, st), qf[st], s);
@@ -53,16 +54,11 @@ struct SeqState {
         float y[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) y[i] = fmaf(s[i], c, negm);
-        if constexpr (MASK) {
-            // entry i is key position j0 + 4 h + entry_row(i)
-            const int base = j0 + 4 * (lane >> 5);
-            const int dist = pos - base;
-            const int few = min(S - base, dist + 1);  // first tokens not after the row
+        if (!full) {
+            const int base = j0 + 4 * (lane >> 5);  // entry i is key base + entry_row(i)
+            const unsigned m = seen_keys(pos - base, W, S - base);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int e = entry_row(i);
-                y[i] = (unsigned)(dist - e) < (unsigned)W || e < few ? y[i] : -INFINITY;
-            }
+            for (int i = 0; i < 16; ++i) y[i] = keep(m, i, y[i], -INFINITY);
         }
         float top = y[0];
 #pragma unroll
@@ -168,6 +164,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 3) : 1)) voi
     }
     F f;
     f.init(lane);
+#pragma unroll
+    for (int s = 0; s < F::kKS; ++s) settle(st.qf[s]);
 
     stage_barrier();
     for (int e = e0, buf = 0; e < e1; e += SK, buf ^= 1) {
@@ -180,10 +178,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 3) : 1)) voi
             if (e + i < e1 && live && !out) {
                 const unsigned char* kt = smem + buf * kBuf + i * 2 * F::kTile;
                 const bool full = j0 + 31 <= wmin && (wmax - j0 < g.W || j0 + 31 < g.S);
-                if (full)
-                    st.template tile<false>(f, kt, kt + F::kTile, lane, g.c, j0, pos, g.W, g.S);
-                else
-                    st.template tile<true>(f, kt, kt + F::kTile, lane, g.c, j0, pos, g.W, g.S);
+                st.tile(f, kt, kt + F::kTile, lane, g.c, full, j0, pos, g.W, g.S);
             }
         }
         if (e + SK < e1) stage_barrier();
@@ -284,6 +279,8 @@ __global__ __launch_bounds__((seq_narrow_waves<T, D>() * 64), 1) void seq_narrow
     }
     F f;
     f.init(lane);
+#pragma unroll
+    for (int s = 0; s < F::kKS; ++s) settle(st.qf[s]);
     wait_vmem();  // (the first tile too: from here on only stage loads are outstanding)
     for (int buf = 0; e < e1; e += W, buf ^= 1) {
         if (e + W < e1) {
@@ -295,10 +292,7 @@ __global__ __launch_bounds__((seq_narrow_waves<T, D>() * 64), 1) void seq_narrow
         const unsigned char* kt = buf0 + buf * 2 * F::kTile;
         const int j0 = t.tile(e);
         const bool full = j0 + 31 <= t.pmin && (t.pmax - j0 < g.W || j0 + 31 < g.S);
-        if (full)
-            st.template tile<false>(f, kt, kt + F::kTile, lane, g.c, j0, pos, g.W, g.S);
-        else
-            st.template tile<true>(f, kt, kt + F::kTile, lane, g.c, j0, pos, g.W, g.S);
+        st.tile(f, kt, kt + F::kTile, lane, g.c, full, j0, pos, g.W, g.S);
         wait_lds();  // before the next loads into this buffer
     }
 

@@ -56,6 +56,41 @@ __device__ __forceinline__ f32x16 mma32(typename Tr<T>::x8 a, typename Tr<T>::x8
 // row (of 0..7) of entry i of a 32x32 result, without the lane's 4 (l / 32)
 __device__ __forceinline__ constexpr int entry_row(int i) { return 8 * (i >> 2) + (i & 3); }
 
+// Bits e of a lane's mask over the entries of a 32x32 result (entry i is row entry_row(i)):
+// below(x) has those with e < x (entries reach 27).
+__device__ __forceinline__ unsigned below(int x) { return (1u << min(max(x, 0), 31)) - 1u; }
+// y where the mask has the bit of entry i, else `other`: two instructions, where a comparison
+// per entry would take five.
+__device__ __forceinline__ float keep(unsigned mask, int i, float y, float other) {
+    const int t = (int)(mask << (31 - entry_row(i))) >> 31;
+    return __int_as_float((__float_as_int(y) & t) | (__float_as_int(other) & ~t));
+}
+// The entries of a tile of keys that a row at distance `dist` from its first one (of this
+// lane's half) sees; first: how many of them are first tokens.
+__device__ __forceinline__ unsigned seen_keys(int dist, int W, int first) {
+    return (below(dist + 1) & ~below(dist - W + 1)) | below(min(first, dist + 1));
+}
+
+// Ends the compiler's wait for the loads behind x here: it does not know that a written-out
+// wait covers them, and would wait again where x is used, in the loop, for every stage load
+// then in flight.
+template <typename V>
+__device__ __forceinline__ void settle(V& x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    if constexpr (sizeof(V) == 16) {
+        i32x4 u = __builtin_bit_cast(i32x4, x);
+        asm volatile("" : "+v"(u));
+        x = __builtin_bit_cast(V, u);
+    } else if constexpr (sizeof(V) == 32) {
+        f32x8 u = __builtin_bit_cast(f32x8, x);
+        asm volatile("" : "+v"(u));
+        x = __builtin_bit_cast(V, u);
+    } else {
+        asm volatile("" : "+v"(x));
+    }
+#endif
+}
+
 // Operands read from a staged tile of 32 rows (layout Rows<T, D>).
 template <typename T, int D>
 struct SeqFrags {
