@@ -73,7 +73,6 @@ void fill_common(na::SeqGeo& g, int64_t heads, int64_t kv_heads, int64_t kernel_
     g.chunk = INT32_MAX;
     g.fd_G.init(g.G);
     g.fd_kv.init(g.Hkv);
-    g.fd_split.init(1);
 }
 
 // ---- contiguous sequences ----
@@ -131,8 +130,8 @@ void fill_sink(const na_sink_problem& p, const int32_t* lengths, na::SeqGeo& g) 
 
 // The cut of dk, dv over workgroups, and the workspace: logsumexp and delta per row, then the
 // fp32 parts.  Fewer than 256 key tiles (a CU each) share the heads of a group among
-// workgroups.  The rows behind the windows of first tokens are cut into chunks of about a
-// window workgroup's length, no more of them than fill the GPU four times over.
+// workgroups.  The rows behind the windows of first tokens are cut into short chunks (their
+// tiles are staged one at a time), no more of them than fill the GPU four times over.
 // False: too large to launch.
 bool fill_backward(const na_sink_problem& p, const int32_t* lengths, na::SeqBwd& b, size_t& bytes) {
     std::memset(&b, 0, sizeof b);
@@ -145,9 +144,8 @@ bool fill_backward(const na_sink_problem& p, const int32_t* lengths, na::SeqBwd&
     int64_t blocks = 0, chunks = 1;
     if (g.S > 0 && n > g.W) {
         blocks = (std::min<int64_t>(g.S, n - g.W) + 31) / 32;
-        const int64_t window = (g.G + hsplit - 1) / hsplit * (std::min<int64_t>(n, g.W + 128L) / 32 + 1);
         const int64_t tiles = g.G * ((n - g.W) / 32 + 1);
-        const int64_t share = na::kFirstParts * std::max<int64_t>(16, window);
+        const int64_t share = 4 * 8;  // tiles of a workgroup: eight for each of four waves
         chunks = std::min((tiles + share - 1) / share,
                           std::max<int64_t>(1, 1024 / (slices * blocks)));
     }
@@ -166,7 +164,7 @@ bool fill_backward(const na_sink_problem& p, const int32_t* lengths, na::SeqBwd&
     const size_t key = 2 * (size_t)p.head_dim;
     const size_t part = (size_t)slices * key *
                         (hsplit > 1 ? (size_t)(hsplit * n) : (size_t)blocks * 32);
-    const size_t first = (size_t)(chunks * na::kFirstParts) * slices * blocks * 32 * key;
+    const size_t first = (size_t)chunks * slices * blocks * 32 * key;
     bytes = (2 * rows + part + first) * 4;
     return true;
 }
@@ -201,6 +199,9 @@ na_status check_attention(const na_cache_problem& p) {
         return NA_ERR_SHAPE;
     if (p.heads == 0 || p.tokens == 0 || p.requests == 0) return NA_OK;
     const int64_t G = p.heads / p.kv_heads;
+    // (a page's bytes, and a row's offset in it, fit 32 bits)
+    if (p.kv_heads * p.page_size * p.head_dim * elem_bytes(p.dtype) >= (int64_t(1) << 31))
+        return NA_ERR_SHAPE;
     if (p.tokens * G >= kMaxRows - 256 || (p.tokens * G / 32 + p.requests) >= kMaxGrid ||
         (p.tokens * G / 32 + p.requests) * p.kv_heads >= kMaxGrid)
         return NA_ERR_SHAPE;
@@ -217,8 +218,12 @@ bool cache_narrow(const na_cache_problem& p) {
     return most * (p.heads / p.kv_heads) <= 32;
 }
 
-// Splits the keys of a row tile when the row tiles alone would leave most of the 256 CUs idle.
-// A split has at least 16 key tiles (512 keys), so that joining costs less than it gains.
+// Splits the keys of a row tile when the row tiles alone would leave the 256 CUs idle (the wide
+// form: two workgroups a CU) or, in the narrow form, unevenly loaded: the bound is the longest
+// request's length, so requests of mixed lengths fill about half of the splits.  A split has at
+// least 32 key tiles (1024 keys), so that joining costs less than it gains.  Decoding over 8k
+// to 32k contexts (32 requests, 4 key heads, fp16 D = 128) with 512, 1024, 2048 and 4096 splits
+// aimed at: 254, 224, 236, 252 us.
 void fill_split(const na_cache_problem& p, bool narrow, na::SeqGeo& g) {
     const int64_t M = narrow ? 32 : 128;
     const int64_t rows = p.tokens * g.G;
@@ -228,13 +233,14 @@ void fill_split(const na_cache_problem& p, bool narrow, na::SeqGeo& g) {
     keys = std::min(keys, (int64_t)g.W + g.S + M + 64);
     const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32 + 1);
     const int64_t busy = std::max<int64_t>((rows + M - 1) / M, std::min(p.requests, p.tokens)) * g.Hkv;
-    int64_t split = std::min<int64_t>(na::kSeqMaxSplit, std::max<int64_t>(1, 1024 / busy));
+    int64_t split = std::min<int64_t>(na::kSeqMaxSplit,
+                                      std::max<int64_t>(1, (narrow ? 1024 : 512) / busy));
     split = std::min(split, std::max<int64_t>(1, (kMaxGrid - 1) / ((int64_t)g.ntiles * g.Hkv)));
-    int64_t chunk = std::max<int64_t>(16, (tiles + split - 1) / split);
+    int64_t chunk = std::max<int64_t>(32, (tiles + split - 1) / split);
     chunk = (chunk + 3) / 4 * 4;
     g.chunk = (int)chunk;
     g.nsplit = (int)((tiles + chunk - 1) / chunk);
-    g.fd_split.init(g.nsplit);
+    g.fd_tiles.init(g.ntiles * g.Hkv);
 }
 
 size_t split_bytes(const na_cache_problem& p, bool narrow, const na::SeqGeo& g) {

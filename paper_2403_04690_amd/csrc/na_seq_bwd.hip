@@ -80,7 +80,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dq_kernel(
 
     SeqStage<T, D, false, 4> ld;
     ld.init(g, t, kvh, lane, kg, vg);
-    auto issue_stage = [&](int e, int buf) {
+    auto issue_stage = [&](int e, int buf) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < SK; ++i)
             if (e + i < t.nT) ld.issue(g, t, e + i, wave, smem + buf * kBuf + i * 2 * F::kTile);
@@ -164,35 +164,43 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dq_kernel(
 }
 
 // ---- dk, dv: 32 keys a wave ----
+// A workgroup has 4 blocks of 32 keys and RS groups of four waves, one wave a block: the groups
+// take the row tiles in turn and add up their sums at the end, so that few key tiles still fill
+// the SIMDs (RS = 1 or 2).
 // A staged tile: 32 rows of q, the same of dout, then their lse2 and delta (256 bytes).
-template <typename T, int D>
-struct KvTile {
+// 16-bit types at D = 128 read the keys and values from LDS for each product: with their
+// fragments in registers beside 128 accumulators, tens of registers spill, and every reload
+// in the loop waits for the stage loads in flight too.
+template <typename T, int D, int RS>
+struct KvCfg {
     static constexpr int kRows = SeqFrags<T, D>::kTile;
     static constexpr int kBytes = 2 * kRows + 256;
-    static constexpr int kStage = sizeof(T) == 4 && D == 128 ? 1 : 2;  // tiles per stage
-    static constexpr int kLds = 2 * kStage * kBytes;
-    // waves of a workgroup of first tokens: one buffer each
-    static constexpr int kFirstWaves = kLds / kBytes;
-    static_assert(kFirstWaves <= kFirstParts, "parts of a chunk");
+    static constexpr bool kOwnLds = sizeof(T) == 2 && D == 128;
+    static constexpr int kPer = D == 128 ? 1 : 2;  // tiles of a group per stage
+    static constexpr int kBufs = 2 * kPer * RS;
+    static constexpr int kOwn = kBufs * kBytes;  // LDS offset of the keys and values
+    static constexpr int kLds = kOwn + (kOwnLds ? 8 * kRows : 0);
+    // waves of a workgroup of first tokens: a buffer each
+    static constexpr int kFirst = kBufs < 4 * RS ? kBufs : 4 * RS;
 };
 
 // OUT: kDk | kDv.  fp32 at D = 128 holds only one gradient's accumulators beside its
 // fragments, and forms dv and dk in two launches.
 enum { kDk = 1, kDv = 2 };
-template <typename T, int D, int OUT>
+template <typename T, int D, int OUT, bool LDS>
 struct KvState {
     using F = SeqFrags<T, D>;
     using x8 = typename Tr<T>::x8;
-    x8 kf[F::kKS], vf[OUT & kDk ? F::kKS : 1];
+    static constexpr bool kKf = !LDS, kVf = (OUT & kDk) && !LDS;
+    x8 kf[kKf ? F::kKS : 1], vf[kVf ? F::kKS : 1];
     f32x16 dk[OUT & kDk ? F::kDB : 1], dv[OUT & kDv ? F::kDB : 1];
 
     // Keys of this wave: lane l has key l % 32.
     __device__ __forceinline__ void init(const unsigned char* kp, const unsigned char* vp, int h) {
 #pragma unroll
         for (int s = 0; s < F::kKS; ++s) {
-            kf[s] = ld_x8<T>(reinterpret_cast<const T*>(kp) + s * 16 + 8 * h);
-            if constexpr (OUT & kDk)
-                vf[s] = ld_x8<T>(reinterpret_cast<const T*>(vp) + s * 16 + 8 * h);
+            if constexpr (kKf) kf[s] = ld_x8<T>(reinterpret_cast<const T*>(kp) + s * 16 + 8 * h);
+            if constexpr (kVf) vf[s] = ld_x8<T>(reinterpret_cast<const T*>(vp) + s * 16 + 8 * h);
         }
 #pragma unroll
         for (int db = 0; db < F::kDB; ++db) {
@@ -203,22 +211,24 @@ struct KvState {
     __device__ __forceinline__ void settle_keys() {
 #pragma unroll
         for (int s = 0; s < F::kKS; ++s) {
-            settle(kf[s]);
-            if constexpr (OUT & kDk) settle(vf[s]);
+            if constexpr (kKf) settle(kf[s]);
+            if constexpr (kVf) settle(vf[s]);
         }
     }
 
     // Rows i0 .. i0 + 31.  Unless `full` (uniform), row i0 + 4 h + e sees this lane's key when
     // (unsigned)(dist + e) < len.  (One body with a branch around the mask alone: two bodies
-    // meeting again in the accumulators spill them at D = 128.)
-    __device__ __forceinline__ void tile(const F& f, const unsigned char* qt, int lane, float c,
-                                         bool full, int dist, unsigned len) {
+    // meeting again in the accumulators spill them at D = 128.)  own: the wave's keys, then
+    // its values (LDS).
+    __device__ __forceinline__ void tile(const F& f, const unsigned char* qt, const unsigned char* own,
+                                         int lane, float c, bool full, int dist, int len) {
         const unsigned char* gt = qt + F::kTile;
         const float* stat = reinterpret_cast<const float*>(gt + F::kTile) + 4 * (lane >> 5);
         const int ro = opaque(f.ro), co = opaque(f.co);
         f32x16 s = f32x16{} * 0.f, dp = f32x16{} * 0.f;
 #pragma unroll
-        for (int st = 0; st < F::kKS; ++st) s = mma32<T>(F::row_at(qt, ro, st), kf[st], s);
+        for (int st = 0; st < F::kKS; ++st)
+            s = mma32<T>(F::row_at(qt, ro, st), LDS ? F::row_at(own, ro, st) : kf[kKf ? st : 0], s);
         x8 pf[2];
 #pragma unroll
         for (int i4 = 0; i4 < 4; ++i4) {
@@ -230,7 +240,7 @@ struct KvState {
             }
         }
         if (!full) {
-            const unsigned m = below((int)len - dist) & ~below(-dist);
+            const unsigned m = below(len - dist) & ~below(-dist);
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = keep(m, i, s[i], 0.f);
         }
@@ -238,30 +248,56 @@ struct KvState {
 #pragma unroll
             for (int i = 0; i < 16; ++i) pf[i >> 3][i & 7] = Tr<T>::cvt(s[i]);
 #pragma unroll
-            for (int db = 0; db < F::kDB; ++db)
+            for (int bi = 0; bi < 2; ++bi)
 #pragma unroll
-                for (int bi = 0; bi < 2; ++bi)
+                for (int db = 0; db < F::kDB; ++db)
                     dv[db] = mma32<T>(F::col_at(gt, co, db, bi, lane), pf[bi], dv[db]);
         }
-        if constexpr (!(OUT & kDk)) return;
+        if constexpr (OUT & kDk) {
 #pragma unroll
-        for (int st = 0; st < F::kKS; ++st)
-            if constexpr (OUT & kDk) dp = mma32<T>(F::row_at(gt, ro, st), vf[st], dp);
+            for (int st = 0; st < F::kKS; ++st)
+                dp = mma32<T>(F::row_at(gt, ro, st),
+                              LDS ? F::row_at(own + F::kTile, ro, st) : vf[kVf ? st : 0], dp);
 #pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-            const f32x4 delta = *reinterpret_cast<const f32x4*>(stat + 32 + 8 * i4);
+            for (int i4 = 0; i4 < 4; ++i4) {
+                const f32x4 delta = *reinterpret_cast<const f32x4*>(stat + 32 + 8 * i4);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 4 * i4 + r;
-                pf[i >> 3][i & 7] = Tr<T>::cvt(s[i] * (dp[i] - delta[r]));
+                for (int r = 0; r < 4; ++r) {
+                    const int i = 4 * i4 + r;
+                    pf[i >> 3][i & 7] = Tr<T>::cvt(s[i] * (dp[i] - delta[r]));
+                }
             }
-        }
-#pragma unroll
-        for (int db = 0; db < F::kDB; ++db)
 #pragma unroll
             for (int bi = 0; bi < 2; ++bi)
-                if constexpr (OUT & kDk)
+#pragma unroll
+                for (int db = 0; db < F::kDB; ++db)
                     dk[db] = mma32<T>(F::col_at(qt, co, db, bi, lane), pf[bi], dk[db]);
+        }
+    }
+
+    // Adds the accumulators of waves [half, 2 half) to those of waves [0, half), through LDS,
+    // one gradient at a time; every wave of the workgroup calls it.
+    __device__ __forceinline__ void add_waves(unsigned char* lds, int wave, int half, int lane) {
+        if constexpr (OUT & kDk) add_one(dk, lds, wave, half, lane);
+        if constexpr (OUT & kDv) add_one(dv, lds, wave, half, lane);
+    }
+    __device__ __forceinline__ static void add_one(f32x16* acc, unsigned char* lds, int wave,
+                                                   int half, int lane) {
+        f32x4* at = reinterpret_cast<f32x4*>(lds) + (wave % half) * (F::kDB * 4 * kWave) + lane;
+        __syncthreads();  // (what was there is read)
+        if (wave >= half && wave < 2 * half)
+#pragma unroll
+            for (int x = 0; x < F::kDB * 4; ++x)
+                at[x * kWave] = f32x4{acc[x >> 2][4 * (x & 3)], acc[x >> 2][4 * (x & 3) + 1],
+                                      acc[x >> 2][4 * (x & 3) + 2], acc[x >> 2][4 * (x & 3) + 3]};
+        __syncthreads();
+        if (wave < half)
+#pragma unroll
+            for (int x = 0; x < F::kDB * 4; ++x) {
+                const f32x4 y = at[x * kWave];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[x >> 2][4 * (x & 3) + r] += y[r];
+            }
     }
 };
 
@@ -272,18 +308,16 @@ template <typename T, int D, int STEP>
 struct KvStage {
     using R = SeqRows<T, D>;
     static constexpr int kCount = 2 * R::kInstr / STEP;
-    R rows;
-    uint32_t qlane, glane;
-    __device__ __forceinline__ void init(const SeqBwd& b, int lane) {
-        rows.init(lane);
-        qlane = rows.rowl * (uint32_t)b.g.qt;
-        glane = rows.rowl * (uint32_t)b.gt;
-    }
-    __device__ __forceinline__ void issue(const SeqBwd& b, const unsigned char* q,
+    __device__ __forceinline__ static void issue(const SeqBwd& b, const unsigned char* q,
                                           const unsigned char* dout, const float* lse2,
                                           const float* delta, int i0, int valid, int first,
-                                          int lane, unsigned char* dst) const {
+                                          int lane, unsigned char* dst) {
         const bool fast = i0 + 32 <= valid;
+        // (formed for each tile: kept, these would be registers that the accumulators need)
+        lane = opaque(lane);
+        R rows;
+        rows.init(lane);
+        const uint32_t qlane = rows.rowl * (uint32_t)b.g.qt, glane = rows.rowl * (uint32_t)b.gt;
 #pragma unroll
         for (int u = 0; u < kCount; ++u) {
             const int x = first + u * STEP;
@@ -322,28 +356,27 @@ __device__ __forceinline__ void each_four(const f32x16* acc, int h, float scale,
         }
 }
 // into fp32 parts ([key][dk, dv][D])
-template <typename T, int D, int OUT>
-__device__ __forceinline__ void store_part(const KvState<T, D, OUT>& st, float* p, int h,
-                                           float scale) {
+template <int D, int OUT, typename S>
+__device__ __forceinline__ void store_part(const S& st, float* p, int h, float scale) {
     auto put = [&](int d, f32x4 x) { st16<f32x4>(p + d, x); };
     if constexpr (OUT & kDk) each_four<D>(st.dk, h, scale, put);
     p += D;
     if constexpr (OUT & kDv) each_four<D>(st.dv, h, 1.f, put);
 }
 
-template <typename T, int D, int OUT>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dkv_kernel(
-    SeqBwd b, const T* __restrict__ qg, const T* __restrict__ kg, const T* __restrict__ vg,
-    const T* __restrict__ dog, T* __restrict__ dkg, T* __restrict__ dvg) {
-    using F = SeqFrags<T, D>;
-    using KT = KvTile<T, D>;
+template <typename T, int D, int OUT, int RS>
+__global__ __launch_bounds__((256 * RS), (sizeof(T) == 4 ? 1 : D == 32 ? 3 : 2)) void
+seq_dkv_kernel(SeqBwd b, const T* __restrict__ qg, const T* __restrict__ kg,
+               const T* __restrict__ vg, const T* __restrict__ dog, T* __restrict__ dkg,
+               T* __restrict__ dvg) {
+    using C = KvCfg<T, D, RS>;
     extern __shared__ __align__(16) unsigned char smem[];
     const SeqGeo& g = b.g;
     const int lane = threadIdx.x & 63, h = lane >> 5;
-    const int wave = uniform((threadIdx.x >> 6) & 3);
-    F f;
+    const int wave = uniform((threadIdx.x >> 6) & (4 * RS - 1));
+    KvState<T, D, OUT, C::kOwnLds> st;
+    SeqFrags<T, D> f;
     f.init(lane);
-    KvState<T, D, OUT> st;
 
     const bool first_role = (int)blockIdx.x < b.first_jobs;
     int slice, k0, part;  // part: chunk of rows (first tokens), or of heads
@@ -367,11 +400,30 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dkv_kernel(
                               (int64_t)kvh * g.G * b.gh;
     const int64_t stat = sb * g.lb + (int64_t)kvh * g.G * g.lh;
 
-    const int w0 = first_role ? k0 : k0 + wave * 32;  // this wave's first key
+    const int w0 = first_role ? k0 : k0 + (wave & 3) * 32;  // this wave's first key
     const int key = w0 + (lane & 31);
-    const int from = max(min(key, valid - 1), 0);
-    st.init(reinterpret_cast<const unsigned char*>(kg) + sb * g.kb + kvh * g.kh + from * g.kt,
-            reinterpret_cast<const unsigned char*>(vg) + sb * g.vb + kvh * g.vh + from * g.vt, h);
+    // (keys behind the length: the last one's rows, and no row sees them)
+    const unsigned char* krow = reinterpret_cast<const unsigned char*>(kg) + sb * g.kb + kvh * g.kh;
+    const unsigned char* vrow = reinterpret_cast<const unsigned char*>(vg) + sb * g.vb + kvh * g.vh;
+    const int last_key = max(valid - 1, 0);
+    unsigned char* own = smem + C::kOwn + (first_role ? 0 : (wave & 3) * 2 * C::kRows);
+    if constexpr (C::kOwnLds) {
+        if (wave < (first_role ? 1 : 4)) {
+            SeqRows<T, D> rows;
+            rows.init(lane);
+#pragma unroll
+            for (int n = 0; n < SeqRows<T, D>::kInstr; ++n) {
+                const int r = min(w0 + n * SeqRows<T, D>::kRpi + rows.rowl, last_key);
+                const uint32_t off = rows.off(n, 0u);
+                seq_load(krow + r * g.kt + off, own + n * 1024);
+                seq_load(vrow + r * g.vt + off, own + C::kRows + n * 1024);
+            }
+        }
+    }
+    {
+        const int from = min(key, last_key);
+        st.init(krow + from * g.kt, vrow + from * g.vt, h);
+    }
 
     if (first_role) {
         // rows W or more behind the key: tiles of every head in turn, this chunk's share of
@@ -380,24 +432,27 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dkv_kernel(
         const int nt = max(0, ((valid - 1) >> 5) - t0 + 1);
         const int all = nt * g.G, per = (all + b.chunks - 1) / b.chunks;
         const int end = min(all, (part + 1) * per);
-        if (wave >= KT::kFirstWaves) return;
-        KvStage<T, D, 1> ld;
-        ld.init(b, lane);
-        unsigned char* buf = smem + wave * KT::kBytes;
-        const unsigned len = key < g.S && valid - key > g.W ? valid - key - g.W : 0;
+        using Ld = KvStage<T, D, 1>;
+        unsigned char* buf = smem + wave * C::kBytes;
+        const int len = key < g.S && valid - key > g.W ? valid - key - g.W : 0;
         st.settle_keys();
-        for (int e = part * per + wave; e < end; e += KT::kFirstWaves) {
-            const int hd = e / nt, i0 = (t0 + e - hd * nt) * 32;
-            ld.issue(b, qs + hd * g.qh, gs + hd * b.gh, b.lse2 + stat + hd * g.lh,
-                     b.delta + stat + hd * g.lh, i0, valid, 0, lane, buf);
-            wait_vmem();
-            const bool full = i0 - (k0 + 31) >= g.W && i0 + 32 <= valid && k0 + 31 < g.S;
-            st.tile(f, buf, lane, g.c, full, i0 + 4 * h - key - g.W, len);
-            wait_lds();
+        stage_barrier();
+        if (wave < C::kFirst)
+            for (int e = part * per + wave; e < end; e += C::kFirst) {
+                const int hd = e / nt, i0 = (t0 + e - hd * nt) * 32;
+                Ld::issue(b, qs + hd * g.qh, gs + hd * b.gh, b.lse2 + stat + hd * g.lh,
+                         b.delta + stat + hd * g.lh, i0, valid, 0, lane, buf);
+                wait_vmem();
+                const bool full = i0 - (k0 + 31) >= g.W && i0 + 32 <= valid && k0 + 31 < g.S;
+                st.tile(f, buf, own, lane, g.c, full, i0 + 4 * h - key - g.W, len);
+                wait_lds();
+            }
+#pragma unroll
+        for (int half = C::kFirst / 2; half >= 1; half /= 2) st.add_waves(smem, wave, half, lane);
+        if (wave == 0) {
+            const int64_t row = ((int64_t)part * g.B * g.Hkv + slice) * (b.blocks * 32) + key;
+            store_part<D, OUT>(st, b.first_part + row * 2 * D, h, b.scale);
         }
-        const int64_t row = ((int64_t)(part * KT::kFirstWaves + wave) * g.B * g.Hkv + slice) *
-                                (b.blocks * 32) + key;
-        store_part<T, D, OUT>(st, b.first_part + row * 2 * D, h, b.scale);
         return;
     }
 
@@ -409,46 +464,65 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dkv_kernel(
     const int last = (int)min((int64_t)valid - 1, reach);
     const int nt = k0 < valid ? (last >> 5) - (k0 >> 5) + 1 : 0;
     const int all = nt * (h1 - h0);
-    KvStage<T, D, 4> ld;
-    ld.init(b, lane);
+    const int group = RS == 1 ? 0 : wave >> 2;
+    using Ld = KvStage<T, D, 4>;
+    // this group's tiles: group, group + RS, .. of the list; the tile to stage and the one to use
     struct Iter {
-        int hd, i;
-    } in{h0, 0}, at{h0, 0};
-    auto next = [&](Iter& x) {
-        if (++x.i == nt) {
-            x.i = 0;
+        int e, hd, i;
+    } in, at;
+    in.e = group;
+    in.hd = h0;
+    in.i = group;
+    auto wrap = [&](Iter& x) __attribute__((always_inline)) {
+        while (x.i >= nt && x.e < all) {
+            x.i -= nt;
             ++x.hd;
         }
     };
-    auto issue_stage = [&](int e, int buf) {
+    wrap(in);
+    at = in;
+    auto next = [&](Iter& x) __attribute__((always_inline)) {
+        x.e += RS;
+        x.i += RS;
+        wrap(x);
+    };
+    unsigned char* mine = smem + group * C::kPer * C::kBytes;
+    constexpr int kStage = RS * C::kPer * C::kBytes;
+    auto issue_stage = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < KT::kStage; ++i)
-            if (e + i < all) {
-                ld.issue(b, qs + in.hd * g.qh, gs + in.hd * b.gh, b.lse2 + stat + in.hd * g.lh,
-                         b.delta + stat + in.hd * g.lh, k0 + in.i * 32, valid, wave, lane,
-                         smem + (buf * KT::kStage + i) * KT::kBytes);
+        for (int i = 0; i < C::kPer; ++i)
+            if (in.e < all) {
+                Ld::issue(b, qs + in.hd * g.qh, gs + in.hd * b.gh, b.lse2 + stat + in.hd * g.lh,
+                         b.delta + stat + in.hd * g.lh, k0 + in.i * 32, valid, wave & 3, lane,
+                         mine + buf * kStage + i * C::kBytes);
                 next(in);
             }
     };
-    if (all > 0) issue_stage(0, 0);
-    const unsigned len = valid > key ? (unsigned)min(g.W, valid - key) : 0u;
+    issue_stage(0);
+    const int len = valid > key ? min(g.W, valid - key) : 0;
     st.settle_keys();
     stage_barrier();
-    for (int e = 0, buf = 0; e < all; e += KT::kStage, buf ^= 1) {
-        if (e + KT::kStage < all) issue_stage(e + KT::kStage, buf ^ 1);
+    constexpr int kStep = RS * C::kPer;
+    for (int e = 0, buf = 0; e < all; e += kStep, buf ^= 1) {
+        if (e + kStep < all) issue_stage(buf ^ 1);
 #pragma unroll
-        for (int i = 0; i < KT::kStage; ++i) {
-            if (e + i < all) {
+        for (int i = 0; i < C::kPer; ++i) {
+            if (at.e < all) {
                 const int i0 = k0 + at.i * 32;
                 next(at);
                 // some row sees some key of the wave; all see all
                 const bool some = i0 + 31 >= w0 && i0 - (w0 + 31) < g.W && w0 < valid;
                 const bool full = i0 >= w0 + 31 && i0 + 31 - w0 < g.W && i0 + 32 <= valid;
-                const unsigned char* qt = smem + (buf * KT::kStage + i) * KT::kBytes;
-                if (some) st.tile(f, qt, lane, g.c, full, i0 + 4 * h - key, len);
+                if (some)
+                    st.tile(f, mine + buf * kStage + i * C::kBytes, own, lane, g.c, full,
+                            i0 + 4 * h - key, len);
             }
         }
-        if (e + KT::kStage < all) stage_barrier();
+        if (e + kStep < all) stage_barrier();
+    }
+    if constexpr (RS == 2) {
+        st.add_waves(smem, wave, 4, lane);
+        if (wave >= 4) return;
     }
 
     if (key >= g.n) return;
@@ -456,7 +530,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dkv_kernel(
         // (with one part only the first tokens' blocks have parts)
         const int keys = b.hsplit > 1 ? g.n : b.blocks * 32;
         const int64_t row = ((int64_t)part * g.B * g.Hkv + slice) * keys + key;
-        store_part<T, D, OUT>(st, b.part + row * 2 * D, h, b.scale);
+        store_part<D, OUT>(st, b.part + row * 2 * D, h, b.scale);
         return;
     }
     T* dk = reinterpret_cast<T*>(reinterpret_cast<unsigned char*>(dkg) + sb * b.kb + kvh * b.kh +
@@ -514,25 +588,31 @@ static hipError_t launch_bwd(const SeqBwd& b, const T* q, const T* k, const T* v
     hipLaunchKernelGGL(kq, dim3(slices * g.ntiles), dim3(256), qlds, s, b, q, k, v, out, lse, dout,
                        dq);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    using KT = KvTile<T, D>;
-    auto launch_dkv = [&](auto kern) {
-        hipError_t r = seq_allow_lds(kern, KT::kLds);
+    const unsigned jobs = slices * b.ktiles * b.hsplit;
+    auto launch_dkv = [&](auto kern, int lds, int threads) {
+        hipError_t r = seq_allow_lds(kern, lds);
         if (r != hipSuccess) return r;
-        hipLaunchKernelGGL(kern, dim3(b.first_jobs + slices * b.ktiles * b.hsplit), dim3(256),
-                           KT::kLds, s, b, q, k, v, dout, dk, dv);
+        hipLaunchKernelGGL(kern, dim3(b.first_jobs + jobs), dim3(threads), lds, s, b, q, k, v, dout,
+                           dk, dv);
         return hipGetLastError();
     };
     if constexpr (sizeof(T) == 4 && D == 128) {
-        e = launch_dkv(seq_dkv_kernel<T, D, kDk>);
-        if (e == hipSuccess) e = launch_dkv(seq_dkv_kernel<T, D, kDv>);
-    } else {
-        e = launch_dkv(seq_dkv_kernel<T, D, kDk | kDv>);
+        e = launch_dkv(seq_dkv_kernel<T, D, kDk, 1>, KvCfg<T, D, 1>::kLds, 256);
+        if (e == hipSuccess) e = launch_dkv(seq_dkv_kernel<T, D, kDv, 1>, KvCfg<T, D, 1>::kLds, 256);
+    } else if constexpr (sizeof(T) == 4) {
+        e = launch_dkv(seq_dkv_kernel<T, D, kDk | kDv, 1>, KvCfg<T, D, 1>::kLds, 256);
+    } else if (D == 128 || jobs < 512) {
+        // (D = 128: one workgroup of eight waves a CU either way, by registers and LDS; below,
+        // fewer than two workgroups a CU)
+        e = launch_dkv(seq_dkv_kernel<T, D, kDk | kDv, 2>, KvCfg<T, D, 2>::kLds, 512);
+    } else if constexpr (D < 128) {
+        e = launch_dkv(seq_dkv_kernel<T, D, kDk | kDv, 1>, KvCfg<T, D, 1>::kLds, 256);
     }
     if (e != hipSuccess || (b.hsplit == 1 && b.blocks == 0)) return e;
     const int64_t units = (int64_t)slices * (b.hsplit > 1 ? g.n : b.blocks * 32) * (D / 2);
     const unsigned grid = (unsigned)std::min<int64_t>((units + 255) / 256, 1 << 16);
     hipLaunchKernelGGL((seq_dkv_join_kernel<T, D>), dim3(grid), dim3(256), 0, s, b,
-                       b.chunks * KT::kFirstWaves, dk, dv);
+                       b.chunks, dk, dv);
     return hipGetLastError();
 }
 

@@ -16,6 +16,7 @@
 //           every fourth key tile each, from LDS buffers of their own without barriers, and
 //           join their sums at the end: single tokens, where reading the cache is the work
 #include <cmath>
+#include <type_traits>
 
 #include "na_launch.h"
 #include "na_seq_kernels.h"
@@ -41,28 +42,63 @@ struct SeqState {
         for (int db = 0; db < F::kDB; ++db) o[db] = f32x16{} * 0.f;
     }
 
-    // One tile of 32 keys from position j0.  Unless `full` (uniform), some pair is not seen;
-    // pos: this lane's row.  (One body with a branch around the mask alone: two bodies that
-    // meet again in the accumulators cost registers.)
-    __device__ __forceinline__ void tile(const F& f, const unsigned char* kt,
-                                         const unsigned char* vt, int lane, float c, bool full,
-                                         int j0, int pos, int W, int S) {
-        f32x16 s = f32x16{} * 0.f;
+    // Folds N tiles of 32 keys into the state: K and V of tile n at tile[n] and tile[n] + kTile,
+    // from position j0[n].  Unless `full` (uniform), some pair is not seen, and of a tile that
+    // is not `on` none; pos: this lane's row.
+    //   With two tiles the matrix cores and the vector unit work side by side within a wave:
+    // the second tile's scores beside the scaling of the first's, the first's values beside
+    // the second's exponentials.  The compiler is told that order (sched_group_barrier).
+    //   (One body with a branch around the mask alone: two bodies that meet again in the
+    // accumulators cost registers.)
+    template <int N>
+    __device__ __forceinline__ void fold(const F& f, const unsigned char* (&tile)[N],
+                                         int lane, float c, bool full, const int (&j0)[N],
+                                         const bool (&on)[N], int pos, int W, int S) {
+        constexpr bool kHint = N == 2 && sizeof(T) == 2;
+        f32x16 s[N];
+        x8 kf[N][F::kKS];
 #pragma unroll
-        for (int st = 0; st < F::kKS; ++st) s = mma32<T>(f.row(kt, st), qf[st], s);
-        const float negm = mref == -INFINITY ? 0.f : -mref;
-        float y[16];
+        for (int n = 0; n < N; ++n) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) y[i] = fmaf(s[i], c, negm);
-        if (!full) {
-            const int base = j0 + 4 * (lane >> 5);  // entry i is key base + entry_row(i)
-            const unsigned m = seen_keys(pos - base, W, S - base);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) y[i] = keep(m, i, y[i], -INFINITY);
+            for (int st = 0; st < F::kKS; ++st) kf[n][st] = f.row(tile[n], st);
         }
-        float top = y[0];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, y[i]);
+        for (int n = 0; n < N; ++n) {
+            s[n] = f32x16{} * 0.f;
+#pragma unroll
+            for (int st = 0; st < F::kKS; ++st) s[n] = mma32<T>(kf[n][st], qf[st], s[n]);
+        }
+        const float negm = mref == -INFINITY ? 0.f : -mref;
+        float y[N][16];
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) y[n][i] = fmaf(s[n][i], c, negm);
+        if constexpr (kHint) {
+            __builtin_amdgcn_sched_group_barrier(0x100, F::kKS + 1, 0);  // K reads
+#pragma unroll
+            for (int st = 0; st < F::kKS; ++st) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                if (st < F::kKS - 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+#pragma unroll
+            for (int st = 0; st < F::kKS; ++st) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x2, 16 / F::kKS, 0);
+            }
+        }
+        if (!full) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int base = j0[n] + 4 * (lane >> 5);  // entry i is key base + entry_row(i)
+                const unsigned m = on[n] ? seen_keys(pos - base, W, S - base) : 0u;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) y[n][i] = keep(m, i, y[n][i], -INFINITY);
+            }
+        }
+        float top = y[0][0];
+#pragma unroll
+        for (int i = 1; i < 16 * N; ++i) top = fmaxf(top, y[i >> 4][i & 15]);
         // raise the reference on a row's first key, or when it grows by more than kSeqLazy
         if (__builtin_amdgcn_ballot_w64(top > thr)) {
             const float ymax = col_max<32>(top);
@@ -75,32 +111,65 @@ struct SeqState {
 #pragma unroll
             for (int db = 0; db < F::kDB; ++db) o[db] *= alpha;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) y[i] -= up;
+            for (int i = 0; i < 16 * N; ++i) y[i >> 4][i & 15] -= up;
         }
-        x8 pf[2];
-        float sum[2] = {0.f, 0.f};
+        x8 vf[N][2][F::kDB], pf[N][2];
+        float sum[2];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float p = fast_exp2(y[i]);
-            sum[i & 1] += p;
-            pf[i >> 3][i & 7] = Tr<T>::cvt(p);
-        }
-        l += sum[0] + sum[1];
-#pragma unroll
-        for (int db = 0; db < F::kDB; ++db)
+        for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int bi = 0; bi < 2; ++bi)
-                o[db] = mma32<T>(f.col(vt, db, bi, lane), pf[bi], o[db]);
+#pragma unroll
+                for (int db = 0; db < F::kDB; ++db)
+                    vf[n][bi][db] = f.col(tile[n] + F::kTile, db, bi, lane);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float p = fast_exp2(y[n][i]);
+                sum[i & 1] = n == 0 && i < 2 ? p : sum[i & 1] + p;
+                pf[n][i >> 3][i & 7] = Tr<T>::cvt(p);
+            }
+#pragma unroll
+            for (int bi = 0; bi < 2; ++bi)
+#pragma unroll
+                for (int db = 0; db < F::kDB; ++db)
+                    o[db] = mma32<T>(vf[n][bi][db], pf[n][bi], o[db]);
+        }
+        l += sum[0] + sum[1];
+        if constexpr (kHint) {
+            constexpr int kMM = 2 * F::kDB;  // products of a tile's values
+            __builtin_amdgcn_sched_group_barrier(0x100, 4 * F::kDB, 0);  // V reads of tile 0
+            __builtin_amdgcn_sched_group_barrier(0x402, 38, 0);          // its exponentials ..
+#pragma unroll
+            for (int x = 0; x < kMM; ++x) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x402, 40 / kMM, 0);
+            }
+        }
     }
 };
 
+// The wide form's ring of stages: tiles per stage, and stages (one read, the others in flight).
+template <typename T, int D>
+struct SeqRing {
+#ifndef TLV
+#define TLV (D == 128 && sizeof(T) == 2 ? 2 : 1)
+#endif
+    static constexpr int kTiles = TLV;
+    static constexpr int kStages = kTiles == 2 ? 2 : 3;
+    static constexpr int kStage = kTiles * 2 * SeqFrags<T, D>::kTile;
+    static constexpr int kLds = kStages * kStage;
+};
+
 template <typename T, int D, bool PAGED>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 3) : 1)) void seq_wide_kernel(
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 4) : 1)) void seq_wide_kernel(
     SeqGeo g, const T* __restrict__ qg, const T* __restrict__ kg, const T* __restrict__ vg,
     T* __restrict__ og, float* __restrict__ lseg, float* __restrict__ part) {
     using F = SeqFrags<T, D>;
-    constexpr int SK = seq_stage_tiles<T, D>();
-    constexpr int kBuf = SK * 2 * F::kTile;
+    using Ring = SeqRing<T, D>;
+    constexpr int SK = Ring::kTiles, NB = Ring::kStages;
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 63;
     const int wave = uniform((threadIdx.x >> 6) & 3);
@@ -109,11 +178,11 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 3) : 1)) voi
     SeqTile t;
     int split = 0, kvh, tile;
     if constexpr (PAGED) {
-        const int id = g.fd_split.div(blockIdx.x);
-        split = blockIdx.x - id * g.nsplit;
+        split = g.fd_tiles.div(blockIdx.x);
+        const int id = blockIdx.x - split * g.ntiles * g.Hkv;
         tile = g.fd_kv.div(id);
         kvh = id - tile * g.Hkv;
-        tile = g.ntiles - 1 - tile;
+        if (g.B > 64) tile = g.ntiles - 1 - tile;  // (long tiles of a request first, at least)
         if (!seq_locate(g, tile, 7, lane, t)) return;
     } else {
         const int id = xcd_remap(blockIdx.x, gridDim.x);
@@ -132,12 +201,13 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 3) : 1)) voi
 
     SeqStage<T, D, PAGED, 4> ld;
     ld.init(g, t, kvh, lane, kg, vg);
-    auto issue_stage = [&](int e, int buf) {
+    auto issue_stage = [&](int e, int buf) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < SK; ++i)
-            if (e + i < e1) ld.issue(g, t, e + i, wave, smem + buf * kBuf + i * 2 * F::kTile);
+        for (int i = 0; i < SK; ++i)  // (a tile behind the last one: zeros)
+            if (e < e1) ld.issue(g, t, e + i, wave, smem + buf * Ring::kStage + i * 2 * F::kTile);
     };
-    if (e0 < e1) issue_stage(e0, 0);
+#pragma unroll
+    for (int b = 0; b < NB - 1; ++b) issue_stage(e0 + b * SK, b);
 
     // ---- this lane's row, and the positions of the wave's rows ----
     const int m = wave * 32 + (lane & 31);
@@ -167,21 +237,44 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 3) : 1)) voi
 #pragma unroll
     for (int s = 0; s < F::kKS; ++s) settle(st.qf[s]);
 
-    stage_barrier();
-    for (int e = e0, buf = 0; e < e1; e += SK, buf ^= 1) {
-        if (e + SK < e1) issue_stage(e + SK, buf ^ 1);
+    // One stage, in buffer BUF (a constant, so that LDS addresses are the lane's offsets plus
+    // immediates).  Its loads have landed when no more than the later stages' are outstanding.
+    auto stage = [&](int e, auto BUF) __attribute__((always_inline)) {
+        constexpr int kBuf = decltype(BUF)::value;
+        if (NB > 2 && e + (NB - 2) * SK < e1)  // NB - 2 stages behind it
+            wait_vmem_but<(NB - 2) * SK * decltype(ld)::kCount>();
+        else
+            wait_vmem();
+        lds_barrier();  // for every wave; and the stage before is read
+        issue_stage(e + (NB - 1) * SK, (kBuf + NB - 1) % NB);
+        const unsigned char* base = smem + kBuf * Ring::kStage;
+        const unsigned char* tile[SK];
+        int j0[SK];
+        bool on[SK], out = true, full = true;
 #pragma unroll
         for (int i = 0; i < SK; ++i) {
-            const int j0 = t.tile(e + i);
+            tile[i] = base + i * 2 * F::kTile;
+            j0[i] = t.tile(e + i);
+            on[i] = i == 0 || e + i < e1;
             // outside every window of the wave's rows, and no first tokens
-            const bool out = j0 > wmax || (wmin - (j0 + 31) >= g.W && j0 >= g.S);
-            if (e + i < e1 && live && !out) {
-                const unsigned char* kt = smem + buf * kBuf + i * 2 * F::kTile;
-                const bool full = j0 + 31 <= wmin && (wmax - j0 < g.W || j0 + 31 < g.S);
-                st.tile(f, kt, kt + F::kTile, lane, g.c, full, j0, pos, g.W, g.S);
-            }
+            out = out && (!on[i] || j0[i] > wmax || (wmin - (j0[i] + 31) >= g.W && j0[i] >= g.S));
+            full = full && on[i] && j0[i] + 31 <= wmin && (wmax - j0[i] < g.W || j0[i] + 31 < g.S);
         }
-        if (e + SK < e1) stage_barrier();
+        if (live && !out) st.template fold<SK>(f, tile, lane, g.c, full, j0, on, pos, g.W, g.S);
+    };
+    for (int e = e0; e < e1;) {
+        stage(e, std::integral_constant<int, 0>{});
+        if ((e += SK) >= e1) break;
+        stage(e, std::integral_constant<int, 1>{});
+        if ((e += SK) >= e1) break;
+        if constexpr (NB > 2) {
+            stage(e, std::integral_constant<int, 2>{});
+            if ((e += SK) >= e1) break;
+        }
+        if constexpr (NB > 3) {
+            stage(e, std::integral_constant<int, 3>{});
+            e += SK;
+        }
     }
 
     // ---- epilogue ----
@@ -248,8 +341,8 @@ __global__ __launch_bounds__((seq_narrow_waves<T, D>() * 64), 1) void seq_narrow
     const int wave = uniform((threadIdx.x >> 6) & (W - 1));
 
     SeqTile t;
-    const int id = g.fd_split.div(blockIdx.x);
-    const int split = blockIdx.x - id * g.nsplit;
+    const int split = g.fd_tiles.div(blockIdx.x);
+    const int id = blockIdx.x - split * g.ntiles * g.Hkv;
     const int tile = g.fd_kv.div(id);
     const int kvh = id - tile * g.Hkv;
     if (!seq_locate(g, tile, 5, lane, t)) return;
@@ -289,10 +382,12 @@ __global__ __launch_bounds__((seq_narrow_waves<T, D>() * 64), 1) void seq_narrow
         } else {
             wait_vmem();
         }
-        const unsigned char* kt = buf0 + buf * 2 * F::kTile;
+        const unsigned char* ks[1] = {buf0 + buf * 2 * F::kTile};
         const int j0 = t.tile(e);
         const bool full = j0 + 31 <= t.pmin && (t.pmax - j0 < g.W || j0 + 31 < g.S);
-        st.tile(f, kt, kt + F::kTile, lane, g.c, full, j0, pos, g.W, g.S);
+        const int js[1] = {j0};
+        const bool on[1] = {true};
+        st.template fold<1>(f, ks, lane, g.c, full, js, on, pos, g.W, g.S);
         wait_lds();  // before the next loads into this buffer
     }
 
@@ -405,7 +500,7 @@ static hipError_t launch_fwd(const SeqGeo& g, bool paged, bool narrow, const T* 
         hipLaunchKernelGGL(kern, dim3(tiles * g.nsplit), dim3(N::W * 64), N::kLds, s, g, q, k, v,
                            out, lse, part);
     } else {
-        constexpr size_t lds = 2 * seq_stage_tiles<T, D>() * 2 * SeqFrags<T, D>::kTile;
+        constexpr size_t lds = SeqRing<T, D>::kLds;
         auto kern = paged ? seq_wide_kernel<T, D, true> : seq_wide_kernel<T, D, false>;
         if ((e = seq_allow_lds(kern, lds)) != hipSuccess) return e;
         hipLaunchKernelGGL(kern, dim3(tiles * g.nsplit), dim3(256), lds, s, g, q, k, v, out, lse,

@@ -17,6 +17,7 @@ namespace na {
 
 // Largest split of the pages of a request over workgroups (joined by a second launch).
 constexpr int kSeqMaxSplit = 64;
+constexpr int kSeqMaxTiles = 1 << 24;  // row tiles of a launch, at most
 
 struct SeqGeo {
     int n;          // tokens per sequence (contiguous form); all new tokens (paged form)
@@ -26,7 +27,9 @@ struct SeqGeo {
     int nsplit;     // key splits of a row tile (paged form; 1: none)
     int chunk;      // key tiles of a split
     int lgps, pages, max_pages;  // paged form: log2 page size, pages of the pool, table columns
-    FastDiv fd_G, fd_tiles, fd_kv, fd_split;
+    // fd_tiles divides by the row tiles of a (sequence, key/value head); paged: by those of all
+    // requests and heads
+    FastDiv fd_G, fd_tiles, fd_kv;
     // byte strides of batch, head, token (paged form: head, token of q and out)
     int64_t qb, qh, qt, kb, kh, kt, vb, vh, vt, ob, oh, ot;
     int64_t lb, lh, lt;  // logsumexp, in elements
@@ -59,10 +62,14 @@ __device__ __forceinline__ constexpr int entry_row(int i) { return 8 * (i >> 2) 
 // Bits e of a lane's mask over the entries of a 32x32 result (entry i is row entry_row(i)):
 // below(x) has those with e < x (entries reach 27).
 __device__ __forceinline__ unsigned below(int x) { return (1u << min(max(x, 0), 31)) - 1u; }
-// y where the mask has the bit of entry i, else `other`: two instructions, where a comparison
-// per entry would take five.
+// y where the mask has the bit of entry i, else `other`: the bit is spread over a word that
+// selects, two instructions.  (In assembly: the compiler makes a comparison and a select of it,
+// with the wait states between them.)
 __device__ __forceinline__ float keep(unsigned mask, int i, float y, float other) {
-    const int t = (int)(mask << (31 - entry_row(i))) >> 31;
+    int t = 0;
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm("v_bfe_i32 %0, %1, %2, 1" : "=v"(t) : "v"(mask), "i"(entry_row(i)));
+#endif
     return __int_as_float((__float_as_int(y) & t) | (__float_as_int(other) & ~t));
 }
 // The entries of a tile of keys that a row at distance `dist` from its first one (of this
@@ -91,10 +98,28 @@ __device__ __forceinline__ void settle(V& x) {
 #endif
 }
 
-// Operands read from a staged tile of 32 rows (layout Rows<T, D>).
+// LDS rows of the staged tiles: Rows<T, D>, with a swizzle of its own for rows of 256 bytes in
+// 16-bit types.  The transposed reads below take two 16-lane groups at a time, and here those
+// of a pair read four 16-byte segments of the same four rows (a 16x16 layout: two segments of
+// eight rows), which must fall on 16 different ones: rows 0..3 differ in the upper two bits of
+// the segment, rows 4 apart in bit 1, rows 8 apart in bit 0.  With Rows' swizzle a third of
+// the LDS cycles at D = 128 were conflicts.
+template <typename T, int D>
+struct SeqLay : Rows<T, D> {
+    using B = Rows<T, D>;
+    static constexpr bool kOwn = sizeof(T) == 2 && B::kSegs == 16;
+    __device__ __forceinline__ static constexpr int swz(int r) {
+        return kOwn ? (r & 1) << 2 ^ (r & 2) << 2 ^ (r & 4) >> 1 ^ (r & 8) >> 3 : B::swz(r);
+    }
+    __device__ __forceinline__ static int off(int r, int s) {
+        return r * B::kRowBytes + ((s ^ swz(r)) << 4);
+    }
+};
+
+// Operands read from a staged tile of 32 rows.
 template <typename T, int D>
 struct SeqFrags {
-    using L = Rows<T, D>;
+    using L = SeqLay<T, D>;
     using x8 = typename Tr<T>::x8;
     static constexpr int kKS = D / 16;  // contraction steps along D
     static constexpr int kDB = D / 32;  // blocks of 32 columns
@@ -114,6 +139,21 @@ struct SeqFrags {
         } else {
             co = h;
         }
+    }
+
+    // The fragments of a whole tile, all reads issued before any is used (the compiler, sparing
+    // registers, would put each right before its product and expose its latency every time).
+    __device__ __forceinline__ void rows(const unsigned char* tile, x8 (&x)[kKS]) const {
+#pragma unroll
+        for (int st = 0; st < kKS; ++st) x[st] = row(tile, st);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // (transposed: of 16-row half bi)
+    __device__ __forceinline__ void cols(const unsigned char* tile, int bi, int lane,
+                                         x8 (&x)[kDB]) const {
+#pragma unroll
+        for (int db = 0; db < kDB; ++db) x[db] = col(tile, db, bi, lane);
+        __builtin_amdgcn_sched_barrier(0);
     }
 
     // lane l: row l % 32, elements 16 st + 8 (l / 32) .. +7
@@ -173,7 +213,7 @@ struct SeqFrags {
 // swizzle of the first row.
 template <typename T, int D>
 struct SeqRows {
-    using L = Rows<T, D>;
+    using L = SeqLay<T, D>;
     static constexpr int kRowB = L::kRowBytes;
     static constexpr int kTile = 32 * kRowB;
     static constexpr int kInstr = kTile / 1024;
@@ -223,6 +263,10 @@ __device__ __forceinline__ void wait_vmem_but() {
 }
 // This wave's LDS reads are done (what they read may be overwritten).
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// This wave's LDS reads are done, and so are all waves'.
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
 // This wave's stage loads have landed and its LDS reads are done, and so for all waves.
 __device__ __forceinline__ void stage_barrier() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -253,26 +297,51 @@ struct SeqTile {
     }
 };
 
-// Paged form: row tile `tile` of M = 2^lgM rows -> its request.  Request r's tiles start at
-// floor(cu[r] G / M) + r, which leaves each at least as many as it has and needs no table;
-// the lanes of a wave search 64 requests at a time.  False: no such tile.
+// Paged form: row tile `tile` of M = 2^lgM rows -> its request and rows.  False: no such tile.
+//   With at most 64 requests the wide form takes them by descending length, and each from its
+// last rows on, so that the long tiles start first and the short ones fill the gaps at the end
+// (requests of 2 to 9 thousand tokens: see na_seq_fwd.hip).  Every lane holds a request and
+// adds up the tiles of those before it.
+//   Otherwise request r's tiles start at floor(cu[r] G / M) + r, which leaves each at least as
+// many as it has and needs no sum; the lanes search 64 requests at a time.
 __device__ __forceinline__ bool seq_locate(const SeqGeo& g, int tile, int lgM, int lane,
                                            SeqTile& t) {
-    auto first = [&](int r) { return (int)(((uint32_t)g.cu[r] * (uint32_t)g.G) >> lgM) + r; };
-    int lo = 0, span = g.B;  // the request is in [lo, lo + span)
-    while (span > 1) {
-        const int step = (span + 63) >> 6;
-        const int r = lo + lane * step;
-        const bool in = lane * step < span && first(min(r, g.B - 1)) <= tile;
-        const int below = __builtin_popcountll(__builtin_amdgcn_ballot_w64(in));
-        lo += (below > 0 ? below - 1 : 0) * step;
-        span = min(step, g.B - lo);
+    int r, at;
+    if (lgM == 7 && g.B <= 64) {
+        const int i = min(lane, g.B - 1);
+        const int start = g.cu[i], count = g.cu[i + 1] - start;
+        const bool ok = lane < g.B && start >= 0 && count > 0 && start <= g.n - count;
+        const int nt = ok ? (int)(((uint32_t)count * (uint32_t)g.G + 127u) >> 7) : 0;
+        const int key = max(g.context[i], 0) / 2 + (ok ? count / 2 : 0);
+        int before = 0;
+        for (int j = 0; j < g.B; ++j) {
+            const int kj = __builtin_amdgcn_readlane(key, j);
+            const int nj = __builtin_amdgcn_readlane(nt, j);
+            before += kj > key || (kj == key && j < lane) ? nj : 0;
+        }
+        const uint64_t here = __builtin_amdgcn_ballot_w64(tile >= before && tile - before < nt);
+        if (here == 0) return false;
+        r = __builtin_ctzll(here);
+        at = __builtin_amdgcn_readlane(nt, r) - 1 - (tile - __builtin_amdgcn_readlane(before, r));
+    } else {
+        auto first = [&](int x) { return (int)(((uint32_t)g.cu[x] * (uint32_t)g.G) >> lgM) + x; };
+        int lo = 0, span = g.B;  // the request is in [lo, lo + span)
+        while (span > 1) {
+            const int step = (span + 63) >> 6;
+            const int x = lo + lane * step;
+            const bool in = lane * step < span && first(min(x, g.B - 1)) <= tile;
+            const int below = __builtin_popcountll(__builtin_amdgcn_ballot_w64(in));
+            lo += (below > 0 ? below - 1 : 0) * step;
+            span = min(step, g.B - lo);
+        }
+        r = uniform(lo);
+        at = tile - first(r);
     }
-    const int r = uniform(lo);
     const int start = g.cu[r], n = g.cu[r + 1] - start;
     if (start < 0 || n <= 0 || start > g.n - n) return false;
     t.b = r;
-    t.row0 = (tile - first(r)) << lgM;
+    if (at < 0 || at >= kSeqMaxTiles) return false;
+    t.row0 = at << lgM;
     if (t.row0 < 0 || t.row0 >= n * g.G) return false;
     t.rows = min(n * g.G - t.row0, 1 << lgM);
     t.qtok = start;
@@ -303,16 +372,20 @@ __device__ __forceinline__ void seq_contiguous(const SeqGeo& g, int tile, int sl
     if (t.pmin < t.valid) t.span(g);
 }
 
-// Stages key tile `e` of the workgroup's tile (instructions first, first + step, ... of the
-// 2 kInstr of K and V).
+// Stages key tile `e` of the workgroup's tile: instructions first, first + STEP, ... of the
+// 2 kInstr of K and V (first < STEP).
 template <typename T, int D, bool PAGED, int STEP>
 struct SeqStage {
     using R = SeqRows<T, D>;
     static constexpr int kCount = 2 * R::kInstr / STEP;
     static_assert(2 * R::kInstr % STEP == 0, "equal shares");
-    const unsigned char *kb, *vb;  // head's rows (paged: of page 0)
+    // instructions of V: those from kInstr on, which is known at compile time where the waves
+    // divide K's evenly
+    static constexpr bool kEven = R::kInstr % STEP == 0;
+    const unsigned char *kb, *vb;  // the head's rows (paged: of page 0)
     R rows;
     uint32_t klane, vlane;  // rowl * token stride
+    int kt, vt;             // token strides (below 2^26 bytes)
 
     __device__ __forceinline__ void init(const SeqGeo& g, const SeqTile& t, int kvh, int lane,
                                          const void* k, const void* v) {
@@ -323,53 +396,73 @@ struct SeqStage {
             kb += t.b * g.kb;
             vb += t.b * g.vb;
         }
-        klane = rows.rowl * (uint32_t)g.kt;
-        vlane = rows.rowl * (uint32_t)g.vt;
+        kt = (int)g.kt;
+        vt = (int)g.vt;
+        klane = rows.rowl * (uint32_t)kt;
+        vlane = rows.rowl * (uint32_t)vt;
     }
 
     __device__ __forceinline__ void issue(const SeqGeo& g, const SeqTile& t, int e, int first,
                                           unsigned char* dst) const {
         const int j0 = t.tile(e);
         bool fast = j0 + 31 <= t.pmax && (j0 >= t.lo || j0 + 31 < g.S);
-        // of the tile's two 16-row blocks: byte offset from kb, vb, and whether it exists
-        int64_t ko[2], vo[2];
-        bool ok[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int j = j0 + 16 * i;
-            if constexpr (PAGED) {
-                const int col = j >> g.lgps;
-                int id = -1;
-                if (col < g.max_pages && j <= t.pmax)
-                    id = g.table[(int64_t)t.b * g.max_pages + col];
-                ok[i] = (unsigned)id < (unsigned)g.pages;
-                id = ok[i] ? id : 0;
-                const int in = j & ((1 << g.lgps) - 1);
-                ko[i] = id * g.kb + in * g.kt;
-                vo[i] = id * g.vb + in * g.vt;
-            } else {
-                ok[i] = true;
-                ko[i] = j * g.kt;
-                vo[i] = j * g.vt;
-            }
-            fast = fast && ok[i];
+        // byte offset of the first row of the tile's two 16-row blocks, and whether they exist
+        int64_t k0, k1, v0, v1;
+        bool ok0 = true, ok1 = true;
+        if constexpr (PAGED) {
+            // (pages hold whole blocks; a page of 16 rows ends inside the tile.  K and V pages
+            // are laid out alike, and a page's bytes fit 31 bits)
+            const int32_t* row = g.table + (int64_t)t.b * g.max_pages;
+            const int col = j0 >> g.lgps;
+            int id0 = -1, id1 = -1;
+            if (col < g.max_pages) id0 = row[col];
+            if (g.lgps != 4)
+                id1 = id0;
+            else if (col + 1 < g.max_pages && j0 + 16 <= t.pmax)
+                id1 = row[col + 1];
+            const int in = g.lgps == 4 ? 0 : (j0 & ((1 << g.lgps) - 1)) * kt;
+            ok0 = (unsigned)id0 < (unsigned)g.pages;
+            ok1 = (unsigned)id1 < (unsigned)g.pages;
+            k0 = (int64_t)(ok0 ? id0 : 0) * (int)g.kb + in;
+            k1 = (int64_t)(ok1 ? id1 : 0) * (int)g.kb + in + (g.lgps == 4 ? 0 : 16 * kt);
+            v0 = k0;
+            v1 = k1;
+            fast = fast && ok0 && ok1;
+        } else {
+            k0 = (int64_t)j0 * kt;
+            v0 = (int64_t)j0 * vt;
+            k1 = k0 + 16 * kt;
+            v1 = v0 + 16 * vt;
         }
+        if (fast)
+            load<true>(kb + k0, kb + k1, vb + v0, vb + v1, first, dst, true, true, t, g, j0);
+        else
+            load<false>(kb + k0, kb + k1, vb + v0, vb + v1, first, dst, ok0, ok1, t, g, j0);
+    }
+
+    // The loads themselves, from the first rows of the blocks; FAST: every row exists and is
+    // seen by some row.  (Everything by value: selects between captured references end up in
+    // scratch memory.)
+    template <bool FAST>
+    __device__ __forceinline__ void load(const unsigned char* k0, const unsigned char* k1,
+                                         const unsigned char* v0, const unsigned char* v1,
+                                         int first, unsigned char* dst, bool ok0, bool ok1,
+                                         const SeqTile& t, const SeqGeo& g, int j0) const {
 #pragma unroll
         for (int u = 0; u < kCount; ++u) {
             const int x = first + u * STEP;
-            const bool isv = x >= R::kInstr;
+            const bool isv = kEven ? u * STEP >= R::kInstr : x >= R::kInstr;
             const int n = isv ? x - R::kInstr : x;
             const int r0 = n * R::kRpi;
-            const int blk = r0 >> 4;
-            const int64_t in = (int64_t)(r0 & 15) * (isv ? g.vt : g.kt);
-            const unsigned char* base = (isv ? vb : kb) + (isv ? (blk ? vo[1] : vo[0])
-                                                               : (blk ? ko[1] : ko[0])) + in;
+            const bool blk = r0 >= 16;
+            const unsigned char* kx = blk ? k1 : k0;
+            const unsigned char* vx = blk ? v1 : v0;
+            const unsigned char* base = (isv ? vx : kx) + (r0 & 15) * (isv ? vt : kt);
             const uint32_t off = rows.off(n, isv ? vlane : klane);
-            if (fast) {
+            if constexpr (FAST) {
                 seq_load(base, off, dst + x * 1024);
             } else {
-                const int j = j0 + r0 + rows.rowl;
-                const bool see = (blk ? ok[1] : ok[0]) && t.sees(g, j);
+                const bool see = (blk ? ok1 : ok0) && t.sees(g, j0 + r0 + rows.rowl);
                 seq_load(see ? base + off : reinterpret_cast<const unsigned char*>(&kZeroRow),
                          dst + x * 1024);
             }
@@ -385,14 +478,13 @@ __device__ __forceinline__ void seq_row(const SeqGeo& g, const SeqTile& t, int m
     head = r - tok * g.G;
 }
 
-// Stage of the wide form: key tiles per stage.
+// Key tiles per stage of the row-major backward.
 template <typename T, int D>
 constexpr int seq_stage_tiles() {
-    return sizeof(T) == 4 && D == 128 ? 1 : 2;
+    return D == 128 ? 1 : 2;
 }
 
 // The backward's geometry: the forward's, the gradients' byte strides, and the cut of dk, dv.
-constexpr int kFirstParts = 4;  // parts that a chunk of the first tokens' rows leaves, at most
 struct SeqBwd {
     SeqGeo g;
     int64_t gb, gh, gt;  // dout
