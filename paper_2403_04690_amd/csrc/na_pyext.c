@@ -13,6 +13,9 @@
  *            head_dim, dtype, scale, q, k, v, out, logsumexp, dout, dq, dk, dv,
  *            stream) -> status
  *
+ *   call(fn, a0, a1, ..) -> status: any function whose arguments are all pointers
+ *            or 64-bit integers (at most 16; the entry points of na_seq.h)
+ *
  * Array arguments are the addresses of the problem's int64 / int32 arrays
  * (0 for a NULL causal array); the GIL is released for the call.
  */
@@ -102,11 +105,42 @@ static PyObject* na_fast_backward(PyObject* self, PyObject* const* args, Py_ssiz
     return PyLong_FromLong((long)st);
 }
 
+typedef int64_t i64;
+typedef na_status (*int_fn)(i64, i64, i64, i64, i64, i64, i64, i64, i64, i64, i64, i64, i64, i64,
+                            i64, i64);
+
+static PyObject* na_fast_call(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+    (void)self;
+    if (nargs < 1 || nargs > 17) {
+        PyErr_SetString(PyExc_TypeError, "call takes a function and at most 16 arguments");
+        return NULL;
+    }
+    int_fn fn = (int_fn)PyLong_AsVoidPtr(args[0]);
+    /* arguments that the function does not have are passed and not read: on this ABI the
+     * caller owns their registers and stack slots */
+    i64 a[16] = {0};
+    for (Py_ssize_t i = 1; i < nargs && !PyErr_Occurred(); ++i) {
+        a[i - 1] = (i64)PyLong_AsLongLong(args[i]);
+    }
+    if (PyErr_Occurred() || !fn) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "NULL function");
+        return NULL;
+    }
+    na_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = fn(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12], a[13],
+            a[14], a[15]);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong((long)st);
+}
+
 static PyMethodDef methods[] = {
     {"forward", (PyCFunction)(void (*)(void))na_fast_forward, METH_FASTCALL,
      "na_forward through a function address; returns the status"},
     {"backward", (PyCFunction)(void (*)(void))na_fast_backward, METH_FASTCALL,
      "na_backward through a function address; returns the status"},
+    {"call", (PyCFunction)(void (*)(void))na_fast_call, METH_FASTCALL,
+     "a function of pointers and 64-bit integers through its address; returns the status"},
     {NULL, NULL, 0, NULL},
 };
 

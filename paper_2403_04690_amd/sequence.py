@@ -58,6 +58,7 @@ class _CacheProblem(ctypes.Structure):
 
 
 _bound = None
+_entry = {}  # entry points by name: the ctypes function, and how to call it fast (or None)
 
 
 def _library():
@@ -76,48 +77,87 @@ def _library():
         lib.na_cache_attention_workspace.argtypes = [cache]
         lib.na_cache_attention_workspace.restype = ctypes.c_size_t
         _bound = lib
+        try:
+            from ._na_fast import call
+        except ImportError:
+            call = None
+        for name in ("na_sink_forward", "na_sink_backward", "na_cache_tables", "na_cache_write",
+                     "na_cache_attention"):
+            fn = getattr(lib, name)
+            if call is None:
+                # the problem goes by address in the fast form; ctypes takes it as a pointer
+                cast = fn.argtypes[0]
+                _entry[name] = fn if name == "na_cache_tables" else (
+                    lambda p, *args, fn=fn, cast=cast: fn(ctypes.cast(p, cast), *args))
+            else:
+                _entry[name] = functools.partial(call, ctypes.cast(fn, ctypes.c_void_p).value)
     return lib
 
 
-def _call(fn, device, *args):
-    """fn(args.., current stream of device), with that device current."""
-    if torch.cuda.current_device() == device.index:
-        _check(fn(*args, _stream(device)))
+# the current device without the checks of torch.cuda.current_device (where torch has it)
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _call(name, device, *args):
+    """The entry point with args.. and the current stream of device, that device current."""
+    if _device() == device.index:
+        status = _entry[name](*args, _stream(device))
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, _stream(device)))
+            status = _entry[name](*args, _stream(device))
+    if status:
+        _check(status)
 
 
-def _on_gpu(*tensors):
-    for t in tensors:
-        if not t.is_cuda:
+# Checks run once per combination of shapes, strides, types and devices (the functions below
+# that are cached take nothing else); addresses are checked by the library, on every call.
+
+def _meta(t):
+    return t.shape, t.stride(), t.dtype, t.device
+
+
+def _contiguous(shape, stride):
+    want = 1
+    for n, s in zip(reversed(shape), reversed(stride)):
+        if n != 1 and s != want:
+            return 0 in shape
+        want *= n
+    return True
+
+
+def _rows(*metas):
+    """Data tensors: of one supported type, with a contiguous last axis, on one GPU."""
+    dtype, device = metas[0][2:]
+    if dtype not in DTYPES:
+        raise TypeError(f"unsupported dtype {dtype}")
+    if any(m[2] != dtype for m in metas):
+        raise TypeError("data tensors must share a dtype")
+    for m in metas:
+        if 0 not in m[0] and m[1][-1] != 1:
+            raise ValueError("the last axis must be contiguous")
+    for m in metas:
+        if m[3].type != "cuda":
             raise ValueError("tensors must live on a GPU")
-        if t.device != tensors[0].device:
+        if m[3] != device:
             raise ValueError("tensors must share a device")
 
 
-def _rows(ref, *others):
-    """Data tensors: on one GPU, of one supported type, with a contiguous last axis."""
-    if ref.dtype not in DTYPES:
-        raise TypeError(f"unsupported dtype {ref.dtype}")
-    for t in others:
-        if t.dtype != ref.dtype:
-            raise TypeError("data tensors must share a dtype")
-    for t in (ref,) + others:
-        if t.numel() and t.stride(-1) != 1:
-            raise ValueError("the last axis must be contiguous")
-    _on_gpu(ref, *others)
-
-
-def _ints(ref, dtype, **tensors):
-    """Integer arrays beside ref: contiguous, on its device, of the given type."""
-    for name, t in tensors.items():
-        if t.dtype != dtype:
+def _ints(device, dtype, **metas):
+    """Integer arrays: contiguous, on the device, of the given type."""
+    for name, m in metas.items():
+        if m[2] != dtype:
             raise TypeError(f"{name} must be {dtype}")
-        if t.device != ref.device:
-            raise ValueError(f"{name} must live on {ref.device}")
-        if not t.is_contiguous():
+        if m[3] != device:
+            raise ValueError(f"{name} must live on {device}")
+        if not _contiguous(m[0], m[1]):
             raise ValueError(f"{name} must be contiguous")
+
+
+def _check_lse(lse, q):
+    if lse[2] != torch.float32 or lse[0] != q[0][:-1] or not _contiguous(lse[0], lse[1]):
+        raise ValueError("lse must be a contiguous fp32 tensor of shape q.shape[:-1]")
+    if lse[3] != q[3]:
+        raise ValueError("tensors must share a device")
 
 
 def _count(value, name, least):
@@ -134,40 +174,39 @@ def _like(t):
         t.shape, dtype=t.dtype, device=t.device)
 
 
+def _lse_for(q):
+    return torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
+
+
 # ---------------------------------------------------------------- contiguous sequences
 
 @functools.lru_cache(maxsize=256)
-def _sink_problem(shape, kv_heads, kernel_size, sinks, dtype, scale, strides):
-    """strides: of q, k, v, out[, dout, dq, dk, dv], each (batch, head, token, 1).  With the
-    backward's workspace size, where its strides are there."""
-    p = _SinkProblem(shape[0], shape[1], kv_heads, shape[2], shape[3], kernel_size, sinks)
-    for name, s in zip(("q", "k", "v", "out", "dout", "dq", "dk", "dv"), strides):
-        setattr(p, name, _Strides(*s[:3]))
-    p.dtype, p.scale = DTYPES[dtype], scale
-    return p, _library().na_sink_backward_workspace(p) if len(strides) > 4 else 0
-
-
-def _sink_args(q, k, v, kernel_size, sinks, scale, lengths):
-    if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape:
+def _sink_plan(kernel_size, sinks, scale, lengths, lse, q, k, v, *more):
+    """The problem (kept alive by the cache's entry), its address, and the backward's workspace.
+    Everything but the first three is a _meta; more: out[, dout, dq, dk, dv]."""
+    if len(q[0]) != 4 or len(k[0]) != 4 or k[0] != v[0]:
         raise ValueError("expected q [batch, heads, tokens, head_dim] and k, v of one shape")
-    if k.shape[0] != q.shape[0] or k.shape[2:] != q.shape[2:]:
+    (B, H, N, D), kv_heads = q[0], k[0][1]
+    if k[0][0] != B or k[0][2:] != q[0][2:]:
         raise ValueError("q, k and v must share batch, tokens and head_dim")
-    if q.shape[1] != k.shape[1] and (k.shape[1] == 0 or q.shape[1] % k.shape[1]):
+    if H != kv_heads and (kv_heads == 0 or H % kv_heads):
         raise ValueError("the heads of q must be a multiple of those of k and v")
-    _rows(q, k, v)
+    for m, ref in zip(more, (q, q, q, k, v)):
+        if m[0] != ref[0]:
+            raise ValueError("out, dout and the gradients must have the shapes of q, k and v")
+    _rows(q, k, v, *more)
+    _check_lse(lse, q)
     if lengths is not None:
-        _ints(q, torch.int32, lengths=lengths)
-        if lengths.shape != q.shape[:1]:
+        _ints(q[3], torch.int32, lengths=lengths)
+        if lengths[0] != (B,):
             raise ValueError("lengths needs one entry per sequence")
-    if scale is None:
-        scale = 1.0 / math.sqrt(q.shape[-1])
-    return _count(kernel_size, "kernel_size", 1), _count(sinks, "sinks", 0), float(scale)
-
-
-def _check_lse(lse, q):
-    if lse.dtype != torch.float32 or lse.shape != q.shape[:-1] or not lse.is_contiguous():
-        raise ValueError("lse must be a contiguous fp32 tensor of shape q.shape[:-1]")
-    _on_gpu(q, lse)
+    p = _SinkProblem(B, H, kv_heads, N, D, _count(kernel_size, "kernel_size", 1),
+                     _count(sinks, "sinks", 0))
+    for name, m in zip(("q", "k", "v", "out", "dout", "dq", "dk", "dv"), (q, k, v) + more):
+        setattr(p, name, _Strides(*m[1][:3]))
+    p.dtype, p.scale = DTYPES[q[2]], 1.0 / math.sqrt(D) if scale is None else float(scale)
+    need = _library().na_sink_backward_workspace(p) if len(more) > 1 else 0
+    return p, ctypes.addressof(p), need
 
 
 def sink_forward(q, k, v, kernel_size, sinks=0, scale=None, lengths=None, out=None, lse=None):
@@ -175,18 +214,12 @@ def sink_forward(q, k, v, kernel_size, sinks=0, scale=None, lengths=None, out=No
     [batch, kv_heads, tokens, head_dim]; lengths (int32, on the GPU): valid tokens of each
     sequence of a padded batch.  Returns (out, logsumexp); rows behind a length get 0 and
     -inf."""
-    lib = _library()
-    kernel_size, sinks, scale = _sink_args(q, k, v, kernel_size, sinks, scale, lengths)
+    _library()
     out = _like(q) if out is None else out
-    if lse is None:
-        lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
-    if out.shape != q.shape:
-        raise ValueError("out must have the shape of q")
-    _rows(q, out)
-    _check_lse(lse, q)
-    p, _ = _sink_problem(q.shape, k.shape[1], kernel_size, sinks, q.dtype, scale,
-                         (q.stride(), k.stride(), v.stride(), out.stride()))
-    _call(lib.na_sink_forward, q.device, p, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+    lse = _lse_for(q) if lse is None else lse
+    p = _sink_plan(kernel_size, sinks, scale, None if lengths is None else _meta(lengths),
+                   _meta(lse), _meta(q), _meta(k), _meta(v), _meta(out))
+    _call("na_sink_forward", q.device, p[1], q.data_ptr(), k.data_ptr(), v.data_ptr(),
           0 if lengths is None else lengths.data_ptr(), out.data_ptr(), lse.data_ptr())
     return out, lse
 
@@ -195,21 +228,16 @@ def sink_backward(q, k, v, out, lse, dout, kernel_size, sinks=0, scale=None, len
                   dq=None, dk=None, dv=None):
     """Gradients of sink_forward's out with respect to q, k and v, from the out and lse that it
     returned.  Returns (dq, dk, dv), 0 behind a length; the same inputs give the same bits."""
-    lib = _library()
-    kernel_size, sinks, scale = _sink_args(q, k, v, kernel_size, sinks, scale, lengths)
+    _library()
     dq = _like(q) if dq is None else dq
     dk = _like(k) if dk is None else dk
     dv = _like(v) if dv is None else dv
-    for t, ref in ((out, q), (dout, q), (dq, q), (dk, k), (dv, k)):
-        if t.shape != ref.shape:
-            raise ValueError("out, dout and the gradients must have the shapes of q, k and v")
-    _rows(q, out, dout, dq, dk, dv)
-    _check_lse(lse, q)
-    p, need = _sink_problem(q.shape, k.shape[1], kernel_size, sinks, q.dtype, scale,
-                            tuple(t.stride() for t in (q, k, v, out, dout, dq, dk, dv)))
+    p, at, need = _sink_plan(
+        kernel_size, sinks, scale, None if lengths is None else _meta(lengths), _meta(lse),
+        _meta(q), _meta(k), _meta(v), _meta(out), _meta(dout), _meta(dq), _meta(dk), _meta(dv))
     # (the allocator hands it out stream by stream, and to a captured graph from its own pool)
     work = torch.empty(need, dtype=torch.uint8, device=q.device)
-    _call(lib.na_sink_backward, q.device, p, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+    _call("na_sink_backward", q.device, at, q.data_ptr(), k.data_ptr(), v.data_ptr(),
           0 if lengths is None else lengths.data_ptr(), out.data_ptr(), lse.data_ptr(),
           dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), work.data_ptr(), need)
     return dq, dk, dv
@@ -247,24 +275,32 @@ def sink_attention(q, k, v, kernel_size, sinks=0, scale=None, lengths=None):
 # ---------------------------------------------------------------- the paged cache
 
 @functools.lru_cache(maxsize=256)
-def _cache_problem(requests, tokens, heads, kv_heads, head_dim, pages, page_size, max_pages,
-                   kernel_size, sinks, max_new, max_context, dtype, scale, strides):
-    """strides: of q, k, v, out, each (token, head, 1) or None.  With the workspace's size."""
-    p = _CacheProblem(requests, tokens, heads, kv_heads, head_dim, pages, page_size, max_pages,
-                      kernel_size, sinks, max_new, max_context)
-    for name, s in zip(("q", "k", "v", "out"), strides):
-        if s is not None:
-            setattr(p, name, _Strides(0, s[1], s[0]))
-    p.dtype, p.scale = DTYPES[dtype], scale
-    return p, _library().na_cache_attention_workspace(p)
-
-
-def _check_pages(ref, k_pages, v_pages):
-    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape:
-        raise ValueError("pages must be [pages, kv_heads, page_size, head_dim], k and v alike")
-    if not (k_pages.is_contiguous() and v_pages.is_contiguous()):
-        raise ValueError("pages must be contiguous")
-    _rows(ref, k_pages, v_pages)
+def _tables_plan(tokens, page_size, context, new, table, free, head, outs):
+    """Arguments of na_cache_tables up to the arrays.  outs: metas of cu_new, slots, positions
+    and new_head."""
+    if len(context[0]) != 1 or new[0] != context[0]:
+        raise ValueError("context_lens and new_lens need one entry per request")
+    if len(table[0]) != 2 or table[0][0] != context[0][0]:
+        raise ValueError("page_table must be [requests, max_pages]")
+    if len(free[0]) != 1:
+        raise ValueError("free_pages must be one list")
+    if context[3].type != "cuda":
+        raise ValueError("tensors must live on a GPU")
+    requests, device = context[0][0], context[3]
+    _ints(device, torch.int32, context_lens=context, new_lens=new, page_table=table,
+          free_pages=free)
+    if head is not None:
+        _ints(device, torch.int32, head=head)
+        if head[0].numel() != 1:
+            raise ValueError("head needs one entry")
+    for name, m, n, dtype in zip(("cu_new", "slots", "positions", "new_head"), outs,
+                                 (requests + 1, tokens, tokens, 1),
+                                 (torch.int32, torch.int64, torch.int32, torch.int32)):
+        if m is not None:
+            _ints(device, dtype, **{name: m})
+            if m[0] != (n,):
+                raise ValueError(f"{name} needs {n} entries")
+    return requests, _count(tokens, "tokens", 0), int(page_size), table[0][1], free[0][0]
 
 
 def cache_tables(context_lens, new_lens, page_table, free_pages, page_size, tokens, head=None,
@@ -276,61 +312,95 @@ def cache_tables(context_lens, new_lens, page_table, free_pages, page_size, toke
     Returns (cu_new [requests + 1] int32, slots [tokens] int64, positions [tokens] int32,
     new_head [1] int32); slots and positions behind the last token are -1, and so are the slots
     of tokens whose page the pool (new_head > len(free_pages)) or the table has no room for."""
-    lib = _library()
-    if context_lens.dim() != 1 or new_lens.shape != context_lens.shape:
-        raise ValueError("context_lens and new_lens need one entry per request")
-    if page_table.dim() != 2 or page_table.shape[0] != context_lens.shape[0]:
-        raise ValueError("page_table must be [requests, max_pages]")
-    if free_pages.dim() != 1:
-        raise ValueError("free_pages must be one list")
-    _on_gpu(context_lens)
-    requests, tokens, device = context_lens.shape[0], _count(tokens, "tokens", 0), context_lens.device
-
-    def room(t, n, dtype, name):
-        if t is None:
-            return torch.empty(n, dtype=dtype, device=device)
-        if t.shape != (n,):
-            raise ValueError(f"{name} needs {n} entries")
-        return t
-
-    cu_new = room(cu_new, requests + 1, torch.int32, "cu_new")
-    slots = room(slots, tokens, torch.int64, "slots")
-    positions = room(positions, tokens, torch.int32, "positions")
-    new_head = room(new_head, 1, torch.int32, "new_head")
-    _ints(context_lens, torch.int32, context_lens=context_lens, new_lens=new_lens,
-          page_table=page_table, free_pages=free_pages, cu_new=cu_new, positions=positions,
-          new_head=new_head)
-    _ints(context_lens, torch.int64, slots=slots)
-    if head is not None:
-        _ints(context_lens, torch.int32, head=head)
-        if head.numel() != 1:
-            raise ValueError("head needs one entry")
-    _call(lib.na_cache_tables, device, requests, tokens, int(page_size), page_table.shape[1],
-          free_pages.shape[0], context_lens.data_ptr(), new_lens.data_ptr(),
+    _library()
+    device = context_lens.device
+    outs = tuple(None if t is None else _meta(t) for t in (cu_new, slots, positions, new_head))
+    sizes = _tables_plan(tokens, page_size, _meta(context_lens), _meta(new_lens),
+                         _meta(page_table), _meta(free_pages),
+                         None if head is None else _meta(head), outs)
+    if cu_new is None:
+        cu_new = torch.empty(sizes[0] + 1, dtype=torch.int32, device=device)
+    if slots is None:
+        slots = torch.empty(sizes[1], dtype=torch.int64, device=device)
+    if positions is None:
+        positions = torch.empty(sizes[1], dtype=torch.int32, device=device)
+    if new_head is None:
+        new_head = torch.empty(1, dtype=torch.int32, device=device)
+    _call("na_cache_tables", device, *sizes, context_lens.data_ptr(), new_lens.data_ptr(),
           free_pages.data_ptr(), 0 if head is None else head.data_ptr(), page_table.data_ptr(),
           cu_new.data_ptr(), slots.data_ptr(), positions.data_ptr(), new_head.data_ptr())
     return cu_new, slots, positions, new_head
+
+
+def _check_pages(k_pages, v_pages):
+    if len(k_pages[0]) != 4 or k_pages[0] != v_pages[0]:
+        raise ValueError("pages must be [pages, kv_heads, page_size, head_dim], k and v alike")
+    if not (_contiguous(*k_pages[:2]) and _contiguous(*v_pages[:2])):
+        raise ValueError("pages must be contiguous")
+
+
+def _token_strides(m):
+    return _Strides(0, m[1][1], m[1][0])
+
+
+@functools.lru_cache(maxsize=256)
+def _write_plan(k, v, slots, k_pages, v_pages):
+    """The problem of na_cache_write (kept alive by the cache's entry) and its address."""
+    if len(k[0]) != 3 or k[0] != v[0]:
+        raise ValueError("expected k and v [tokens, kv_heads, head_dim]")
+    _check_pages(k_pages, v_pages)
+    _rows(k, v, k_pages, v_pages)
+    if k[0][1:] != k_pages[0][1::2]:
+        raise ValueError("k, v and the pages must share kv_heads and head_dim")
+    _ints(k[3], torch.int64, slots=slots)
+    if slots[0] != k[0][:1]:
+        raise ValueError("slots needs one entry per token")
+    p = _CacheProblem(0, k[0][0], 0, k[0][1], k[0][2], k_pages[0][0], k_pages[0][2], 0, 1, 0, 0, 0)
+    p.k, p.v = _token_strides(k), _token_strides(v)
+    p.dtype, p.scale = DTYPES[k[2]], 1.0
+    return p, ctypes.addressof(p)
 
 
 def cache_write(k, v, slots, k_pages, v_pages):
     """Writes row t of k and v [tokens, kv_heads, head_dim] into the pages [pages, kv_heads,
     page_size, head_dim] at slots[t] (page * page_size + offset, int64); slots outside the
     pages (-1) are skipped.  The slots of one call must differ."""
-    lib = _library()
-    if k.dim() != 3 or k.shape != v.shape:
-        raise ValueError("expected k and v [tokens, kv_heads, head_dim]")
-    _rows(k, v)
-    _check_pages(k, k_pages, v_pages)
-    if k.shape[1:] != k_pages.shape[1::2]:
-        raise ValueError("k, v and the pages must share kv_heads and head_dim")
-    _ints(k, torch.int64, slots=slots)
-    if slots.shape != k.shape[:1]:
-        raise ValueError("slots needs one entry per token")
-    p, _ = _cache_problem(0, k.shape[0], 0, k.shape[1], k.shape[2], k_pages.shape[0],
-                          k_pages.shape[2], 0, 1, 0, 0, 0, k.dtype, 1.0,
-                          (None, k.stride(), v.stride(), None))
-    _call(lib.na_cache_write, k.device, p, k.data_ptr(), v.data_ptr(), slots.data_ptr(),
+    _library()
+    p = _write_plan(_meta(k), _meta(v), _meta(slots), _meta(k_pages), _meta(v_pages))
+    _call("na_cache_write", k.device, p[1], k.data_ptr(), v.data_ptr(), slots.data_ptr(),
           k_pages.data_ptr(), v_pages.data_ptr())
+
+
+@functools.lru_cache(maxsize=256)
+def _attention_plan(kernel_size, sinks, scale, max_new, max_context, q, k_pages, v_pages, table,
+                    context, cu_new, out, lse):
+    """The problem of na_cache_attention (kept alive by the cache's entry), its address and its
+    workspace's size."""
+    if len(q[0]) != 3:
+        raise ValueError("expected q [tokens, heads, head_dim]")
+    _check_pages(k_pages, v_pages)
+    (T, H, D), (P, kv_heads, page_size, _) = q[0], k_pages[0]
+    if D != k_pages[0][3]:
+        raise ValueError("q and the pages must share head_dim")
+    if H != kv_heads and (kv_heads == 0 or H % kv_heads):
+        raise ValueError("the heads of q must be a multiple of those of the pages")
+    if len(context[0]) != 1 or len(table[0]) != 2 or table[0][0] != context[0][0]:
+        raise ValueError("expected context_lens [requests] and page_table [requests, max_pages]")
+    if cu_new[0] != (context[0][0] + 1,):
+        raise ValueError("cu_new needs one entry more than there are requests")
+    if out[0] != q[0]:
+        raise ValueError("out must have the shape of q")
+    _rows(q, k_pages, v_pages, out)
+    _check_lse(lse, q)
+    _ints(q[3], torch.int32, page_table=table, context_lens=context, cu_new=cu_new)
+    p = _CacheProblem(
+        context[0][0], T, H, kv_heads, D, P, page_size, table[0][1],
+        _WHOLE if kernel_size is None else _count(kernel_size, "kernel_size", 1),
+        _count(sinks, "sinks", 0), 0 if max_new is None else _count(max_new, "max_new", 0),
+        0 if max_context is None else _count(max_context, "max_context", 0))
+    p.q, p.out = _token_strides(q), _token_strides(out)
+    p.dtype, p.scale = DTYPES[q[2]], 1.0 / math.sqrt(D) if scale is None else float(scale)
+    return p, ctypes.addressof(p), _library().na_cache_attention_workspace(p)
 
 
 def cache_attention(q, k_pages, v_pages, page_table, context_lens, cu_new, kernel_size=None,
@@ -341,40 +411,15 @@ def cache_attention(q, k_pages, v_pages, page_table, context_lens, cu_new, kerne
     of the new tokens and of the whole tokens of any request where the caller knows them, only
     choose how the work is split.  Returns (out, logsumexp [tokens, heads] fp32); rows from
     cu_new[requests] on are left as they were.  A page id outside the pages reads as zeros."""
-    lib = _library()
-    if q.dim() != 3:
-        raise ValueError("expected q [tokens, heads, head_dim]")
-    _check_pages(q, k_pages, v_pages)
-    kv_heads = k_pages.shape[1]
-    if q.shape[2] != k_pages.shape[3]:
-        raise ValueError("q and the pages must share head_dim")
-    if q.shape[1] != kv_heads and (kv_heads == 0 or q.shape[1] % kv_heads):
-        raise ValueError("the heads of q must be a multiple of those of the pages")
-    if context_lens.dim() != 1 or page_table.dim() != 2 \
-            or page_table.shape[0] != context_lens.shape[0]:
-        raise ValueError("expected context_lens [requests] and page_table [requests, max_pages]")
-    if cu_new.shape != (context_lens.shape[0] + 1,):
-        raise ValueError("cu_new needs one entry more than there are requests")
+    _library()
     out = _like(q) if out is None else out
-    if lse is None:
-        lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
-    if out.shape != q.shape:
-        raise ValueError("out must have the shape of q")
-    _rows(q, out)
-    _check_lse(lse, q)
-    _ints(q, torch.int32, page_table=page_table, context_lens=context_lens, cu_new=cu_new)
-    if scale is None:
-        scale = 1.0 / math.sqrt(q.shape[-1])
-    p, need = _cache_problem(
-        context_lens.shape[0], q.shape[0], q.shape[1], kv_heads, q.shape[2], k_pages.shape[0],
-        k_pages.shape[2], page_table.shape[1],
-        _WHOLE if kernel_size is None else _count(kernel_size, "kernel_size", 1),
-        _count(sinks, "sinks", 0), 0 if max_new is None else _count(max_new, "max_new", 0),
-        0 if max_context is None else _count(max_context, "max_context", 0), q.dtype,
-        float(scale), (q.stride(), None, None, out.stride()))
+    lse = _lse_for(q) if lse is None else lse
+    p, at, need = _attention_plan(
+        kernel_size, sinks, scale, max_new, max_context, _meta(q), _meta(k_pages), _meta(v_pages),
+        _meta(page_table), _meta(context_lens), _meta(cu_new), _meta(out), _meta(lse))
     # (the allocator hands it out stream by stream, and to a captured graph from its own pool)
     work = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    _call(lib.na_cache_attention, q.device, p, q.data_ptr(), k_pages.data_ptr(),
+    _call("na_cache_attention", q.device, at, q.data_ptr(), k_pages.data_ptr(),
           v_pages.data_ptr(), page_table.data_ptr(), context_lens.data_ptr(), cu_new.data_ptr(),
           out.data_ptr(), lse.data_ptr(), work.data_ptr() if need else 0, need)
     return out, lse
