@@ -150,7 +150,7 @@ bool fill_backward(const na_sink_problem& p, const int32_t* lengths, na::SeqBwd&
                           std::max<int64_t>(1, 1024 / (slices * blocks)));
     }
     const int64_t first_jobs = slices * blocks * chunks;
-    if (first_jobs + base * hsplit >= kMaxGrid) return false;
+    if (first_jobs + base * hsplit >= kMaxGrid / 2) return false;  // (up to 512 threads each)
     b.ktiles = (int)ktiles;
     b.hsplit = (int)hsplit;
     b.blocks = (int)blocks;
@@ -221,7 +221,8 @@ bool cache_narrow(const na_cache_problem& p) {
 // Splits the keys of a row tile when the row tiles alone would leave the 256 CUs idle (the wide
 // form: two workgroups a CU) or, in the narrow form, unevenly loaded: the bound is the longest
 // request's length, so requests of mixed lengths fill about half of the splits.  A split has at
-// least 32 key tiles (1024 keys), so that joining costs less than it gains.  Decoding over 8k
+// least 32 key tiles (8 in fp32, whose products take sixteen times as long), so that joining
+// costs less than it gains.  Decoding over 8k
 // to 32k contexts (32 requests, 4 key heads, fp16 D = 128) with 512, 1024, 2048 and 4096 splits
 // aimed at: 254, 224, 236, 252 us.
 void fill_split(const na_cache_problem& p, bool narrow, na::SeqGeo& g) {
@@ -235,8 +236,11 @@ void fill_split(const na_cache_problem& p, bool narrow, na::SeqGeo& g) {
     const int64_t busy = std::max<int64_t>((rows + M - 1) / M, std::min(p.requests, p.tokens)) * g.Hkv;
     int64_t split = std::min<int64_t>(na::kSeqMaxSplit,
                                       std::max<int64_t>(1, (narrow ? 1024 : 512) / busy));
-    split = std::min(split, std::max<int64_t>(1, (kMaxGrid - 1) / ((int64_t)g.ntiles * g.Hkv)));
-    int64_t chunk = std::max<int64_t>(32, (tiles + split - 1) / split);
+    // (the joining launch has four workgroups a row tile)
+    split = std::min(split, std::max<int64_t>(1, (kMaxGrid - 1) / (4 * (int64_t)g.ntiles * g.Hkv)));
+    if (4 * (int64_t)g.ntiles * g.Hkv >= kMaxGrid) split = 1;
+    const int64_t least = p.dtype == NA_FP32 ? 8 : 32;
+    int64_t chunk = split == 1 ? tiles : std::max<int64_t>(least, (tiles + split - 1) / split);
     chunk = (chunk + 3) / 4 * 4;
     g.chunk = (int)chunk;
     g.nsplit = (int)((tiles + chunk - 1) / chunk);

@@ -18,6 +18,8 @@
 //   join    sums the fp32 parts that split heads and first tokens leave
 // P and dA are rounded once to the tensors' type for their matrix products (16-bit types);
 // everything else is fp32.
+#include <type_traits>
+
 #include "na_launch.h"
 #include "na_seq_kernels.h"
 
@@ -36,10 +38,14 @@ struct DqState {
                                          const unsigned char* vt, int lane, float c, bool full,
                                          int j0, int pos, int W, int S) {
         f32x16 s = f32x16{} * 0.f, dp = f32x16{} * 0.f;
+        x8 kf[F::kKS], vf[F::kKS], kc[2][F::kDB];
+        f.rows(kt, kf);
+        if constexpr (sizeof(T) == 2) f.rows(vt, vf);
 #pragma unroll
-        for (int st = 0; st < F::kKS; ++st) s = mma32<T>(f.row(kt, st), qf[st], s);
+        for (int st = 0; st < F::kKS; ++st) s = mma32<T>(kf[st], qf[st], s);
+        if constexpr (sizeof(T) == 4) f.rows(vt, vf);
 #pragma unroll
-        for (int st = 0; st < F::kKS; ++st) dp = mma32<T>(f.row(vt, st), gf[st], dp);
+        for (int st = 0; st < F::kKS; ++st) dp = mma32<T>(vf[st], gf[st], dp);
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = fast_exp2(fmaf(s[i], c, -lse2));
         if (!full) {
@@ -48,25 +54,27 @@ struct DqState {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = keep(m, i, s[i], 0.f);
         }
+        f.cols(kt, 0, lane, kc[0]);
+        if constexpr (sizeof(T) == 2) f.cols(kt, 1, lane, kc[1]);
         x8 pf[2];
 #pragma unroll
         for (int i = 0; i < 16; ++i) pf[i >> 3][i & 7] = Tr<T>::cvt(s[i] * (dp[i] - delta));
 #pragma unroll
-        for (int db = 0; db < F::kDB; ++db)
+        for (int db = 0; db < F::kDB; ++db) dq[db] = mma32<T>(kc[0][db], pf[0], dq[db]);
+        if constexpr (sizeof(T) == 4) f.cols(kt, 1, lane, kc[1]);
 #pragma unroll
-            for (int bi = 0; bi < 2; ++bi)
-                dq[db] = mma32<T>(f.col(kt, db, bi, lane), pf[bi], dq[db]);
+        for (int db = 0; db < F::kDB; ++db) dq[db] = mma32<T>(kc[1][db], pf[1], dq[db]);
     }
 };
 
+// (a ring of three stages of a key tile, as the forward's)
 template <typename T, int D>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dq_kernel(
+__global__ __launch_bounds__(256, (sizeof(T) == 4 ? 1 : D == 128 ? 2 : 3)) void seq_dq_kernel(
     SeqBwd b, const T* __restrict__ qg, const T* __restrict__ kg, const T* __restrict__ vg,
     const T* __restrict__ og, const float* __restrict__ lseg, const T* __restrict__ dog,
     T* __restrict__ dqg) {
     using F = SeqFrags<T, D>;
-    constexpr int SK = seq_stage_tiles<T, D>();
-    constexpr int kBuf = SK * 2 * F::kTile;
+    constexpr int kBuf = 2 * F::kTile;
     extern __shared__ __align__(16) unsigned char smem[];
     const SeqGeo& g = b.g;
     const int lane = threadIdx.x & 63;
@@ -80,12 +88,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dq_kernel(
 
     SeqStage<T, D, false, 4> ld;
     ld.init(g, t, kvh, lane, kg, vg);
-    auto issue_stage = [&](int e, int buf) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < SK; ++i)
-            if (e + i < t.nT) ld.issue(g, t, e + i, wave, smem + buf * kBuf + i * 2 * F::kTile);
-    };
-    if (t.nT > 0) issue_stage(0, 0);
+    if (t.nT > 0) ld.issue(g, t, 0, wave, smem);
+    if (t.nT > 1) ld.issue(g, t, 1, wave, smem + kBuf);
 
     const int m = wave * 32 + (lane & 31), h = lane >> 5;
     int tok, head;
@@ -132,20 +136,25 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? 2 : 1)) void seq_dq_kernel(
     settle(st.lse2);
     settle(st.delta);
 
-    stage_barrier();
-    for (int e = 0, buf = 0; e < t.nT; e += SK, buf ^= 1) {
-        if (e + SK < t.nT) issue_stage(e + SK, buf ^ 1);
-#pragma unroll
-        for (int i = 0; i < SK; ++i) {
-            const int j0 = t.tile(e + i);
-            const bool out = j0 > wmax || (wmin - (j0 + 31) >= g.W && j0 >= g.S);
-            if (e + i < t.nT && live && !out) {
-                const unsigned char* kt = smem + buf * kBuf + i * 2 * F::kTile;
-                const bool full = j0 + 31 <= wmin && (wmax - j0 < g.W || j0 + 31 < g.S);
-                st.tile(f, kt, kt + F::kTile, lane, g.c, full, j0, tok, g.W, g.S);
-            }
-        }
-        if (e + SK < t.nT) stage_barrier();
+    auto stage = [&](int e, auto BUF) __attribute__((always_inline)) {
+        constexpr int kAt = decltype(BUF)::value;
+        if (e + 1 < t.nT)
+            wait_vmem_but<decltype(ld)::kCount>();
+        else
+            wait_vmem();
+        lds_barrier();
+        if (e + 2 < t.nT) ld.issue(g, t, e + 2, wave, smem + (kAt + 2) % 3 * kBuf);
+        const int j0 = t.tile(e);
+        const bool out = j0 > wmax || (wmin - (j0 + 31) >= g.W && j0 >= g.S);
+        const bool full = j0 + 31 <= wmin && (wmax - j0 < g.W || j0 + 31 < g.S);
+        const unsigned char* kt = smem + kAt * kBuf;
+        if (live && !out) st.tile(f, kt, kt + F::kTile, lane, g.c, full, j0, tok, g.W, g.S);
+    };
+    wait_vmem();  // (the row's own loads and stores too: from here on only stage loads count)
+    for (int e = 0; e < t.nT; e += 3) {
+        stage(e, std::integral_constant<int, 0>{});
+        if (e + 1 < t.nT) stage(e + 1, std::integral_constant<int, 1>{});
+        if (e + 2 < t.nT) stage(e + 2, std::integral_constant<int, 2>{});
     }
 
     if (m >= t.rows) return;
@@ -561,9 +570,11 @@ __global__ __launch_bounds__(256) void seq_dkv_join_kernel(SeqBwd b, int first_p
         const int slice = (int)(row / keys), key = (int)(row % keys);
         const int64_t slices = (int64_t)g.B * g.Hkv;
         f32x4 sum{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
         for (int p = 0; p < b.hsplit; ++p)
             sum += ld16<f32x4>(b.part + ((p * slices + slice) * stride + key) * 2 * D + d);
         if (key < b.blocks * 32)
+#pragma unroll 16
             for (int p = 0; p < first_parts; ++p)
                 sum += ld16<f32x4>(b.first_part +
                                    ((p * slices + slice) * (b.blocks * 32) + key) * 2 * D + d);
@@ -582,7 +593,7 @@ static hipError_t launch_bwd(const SeqBwd& b, const T* q, const T* k, const T* v
     const SeqGeo& g = b.g;
     const unsigned slices = (unsigned)g.B * g.Hkv;
     hipError_t e;
-    constexpr size_t qlds = 2 * seq_stage_tiles<T, D>() * 2 * SeqFrags<T, D>::kTile;
+    constexpr size_t qlds = 3 * 2 * SeqFrags<T, D>::kTile;
     auto kq = seq_dq_kernel<T, D>;
     if ((e = seq_allow_lds(kq, qlds)) != hipSuccess) return e;
     hipLaunchKernelGGL(kq, dim3(slices * g.ntiles), dim3(256), qlds, s, b, q, k, v, out, lse, dout,

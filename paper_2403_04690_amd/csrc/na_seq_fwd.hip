@@ -449,30 +449,35 @@ __global__ __launch_bounds__((seq_narrow_waves<T, D>() * 64), 1) void seq_narrow
 }
 
 // Joins the splits of each row: out = sum_s 2^(lse_s - lse) out_s, in a fixed order.  One
-// workgroup per (row tile, key/value head); D / 4 threads a row.
+// workgroup per 32 rows of a (row tile, key/value head); D / 4 threads a row.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void seq_join_kernel(SeqGeo g, int lgM, T* __restrict__ og,
                                                        float* __restrict__ lseg,
                                                        const float* __restrict__ part) {
-    const int tile = g.fd_kv.div(blockIdx.x);
-    const int kvh = blockIdx.x - tile * g.Hkv;
+    const int id = blockIdx.x >> (lgM - 5), r0 = (blockIdx.x & ((1 << (lgM - 5)) - 1)) * 32;
+    int tile = g.fd_kv.div(id);
+    const int kvh = id - tile * g.Hkv;
+    const int64_t row0 = (int64_t)(tile * g.Hkv + kvh) * g.nsplit << lgM;
     SeqTile t;
     if (!seq_locate(g, tile, lgM, threadIdx.x & 63, t)) return;
     const int splits = seq_splits(g, t.nT);
     if (splits == 1) return;  // written by the only split
-    const int64_t row0 = (int64_t)(tile * g.Hkv + kvh) * g.nsplit << lgM;
     const float* pl = part + ((int64_t)g.ntiles * g.Hkv * g.nsplit << lgM) * D + row0;
-    for (int x = threadIdx.x; x < t.rows * (D / 4); x += 256) {
-        const int row = x / (D / 4), d = x % (D / 4) * 4;
-        float mx = -INFINITY;
-        for (int s = 0; s < splits; ++s) mx = fmaxf(mx, pl[(s << lgM) + row]);
-        float sum = 0.f;
+    const int end = min(32, t.rows - r0) * (D / 4);
+    for (int x = threadIdx.x; x < end; x += 256) {
+        const int row = r0 + x / (D / 4), d = x % (D / 4) * 4;
+        float mx = -INFINITY, sum = 0.f;
         f32x4 acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
         for (int s = 0; s < splits; ++s) {
             const float e = pl[(s << lgM) + row];
-            const float w = e == -INFINITY ? 0.f : fast_exp2(e - mx);
-            sum += w;
-            acc += ld16<f32x4>(part + (row0 + (s << lgM) + row) * D + d) * w;
+            const f32x4 y = ld16<f32x4>(part + (row0 + (s << lgM) + row) * D + d);
+            const float top = fmaxf(mx, e);
+            const float a = mx == -INFINITY ? 0.f : fast_exp2(mx - top);
+            const float w = e == -INFINITY ? 0.f : fast_exp2(e - top);
+            sum = sum * a + w;
+            acc = acc * a + y * w;
+            mx = top;
         }
         const bool some = sum > 0.f;
         int tk, hd;
@@ -507,8 +512,8 @@ static hipError_t launch_fwd(const SeqGeo& g, bool paged, bool narrow, const T* 
                            part);
     }
     if ((e = hipGetLastError()) != hipSuccess || g.nsplit == 1) return e;
-    hipLaunchKernelGGL((seq_join_kernel<T, D>), dim3(tiles), dim3(256), 0, s, g, narrow ? 5 : 7,
-                       out, lse, part);
+    hipLaunchKernelGGL((seq_join_kernel<T, D>), dim3(tiles * (narrow ? 1 : 4)), dim3(256), 0, s, g,
+                       narrow ? 5 : 7, out, lse, part);
     return hipGetLastError();
 }
 

@@ -478,12 +478,6 @@ __device__ __forceinline__ void seq_row(const SeqGeo& g, const SeqTile& t, int m
     head = r - tok * g.G;
 }
 
-// Key tiles per stage of the row-major backward.
-template <typename T, int D>
-constexpr int seq_stage_tiles() {
-    return D == 128 ? 1 : 2;
-}
-
 // The backward's geometry: the forward's, the gradients' byte strides, and the cut of dk, dv.
 struct SeqBwd {
     SeqGeo g;

@@ -425,6 +425,33 @@ def cache_attention(q, k_pages, v_pages, page_table, context_lens, cu_new, kerne
     return out, lse
 
 
+@functools.lru_cache(maxsize=256)
+def _step_plan(kernel_size, sinks, scale, max_new, max_context, data, out, lse, new, free, head,
+               tables):
+    """The problem of both the write and the attention of a step (kept alive by the cache's
+    entry), its address, its workspace's size, and the arguments of na_cache_tables; the checks
+    are those of the three functions."""
+    q, k, v, k_pages, v_pages, page_table, context = data
+    if len(q[0]) != 3 or len(k[0]) != 3 or q[0][0] != k[0][0]:
+        raise ValueError("q, k and v need the same new tokens")
+    T, device = q[0][0], q[3]
+    sizes, requests = None, context[0][0] if len(context[0]) == 1 else 0
+    _check_pages(k_pages, v_pages)
+    if tables is None:
+        sizes = _tables_plan.__wrapped__(T, k_pages[0][2], context, new, page_table, free, head,
+                                         (None,) * 4)
+        ints = lambda n, dtype: (torch.Size((n,)), (1,), dtype, device)  # noqa: E731
+        tables = ints(requests + 1, torch.int32), ints(T, torch.int64)
+    cu_new, slots = tables
+    _write_plan.__wrapped__(k, v, slots, k_pages, v_pages)
+    p, at, need = _attention_plan.__wrapped__(kernel_size, sinks, scale, max_new, max_context, q,
+                                              k_pages, v_pages, page_table, context, cu_new, out,
+                                              lse)
+    _rows(q, k)
+    p.k, p.v = _token_strides(k), _token_strides(v)
+    return p, at, need, sizes
+
+
 def cache_step(q, k, v, k_pages, v_pages, page_table, context_lens, new_lens, free_pages,
                kernel_size=None, sinks=0, scale=None, head=None, max_new=None, max_context=None,
                tables=None):
@@ -433,13 +460,36 @@ def cache_step(q, k, v, k_pages, v_pages, page_table, context_lens, new_lens, fr
     kv_heads, head_dim] hold the requests' new tokens one after another.  `tables`: what
     cache_tables returned for this step (the layers of a model share it); None builds it.
     Returns (out, logsumexp, new_head)."""
-    if q.dim() != 3 or q.shape[0] != k.shape[0]:
-        raise ValueError("q, k and v need the same new tokens")
+    _library()
+    device = q.device
+    out, lse = _like(q), _lse_for(q)
+    metas = (_meta(q), _meta(k), _meta(v), _meta(k_pages), _meta(v_pages), _meta(page_table),
+             _meta(context_lens))
     if tables is None:
-        tables = cache_tables(context_lens, new_lens, page_table, free_pages, k_pages.shape[2],
-                              q.shape[0], head)
-    cu_new, slots, _, new_head = tables
-    cache_write(k, v, slots, k_pages, v_pages)
-    out, lse = cache_attention(q, k_pages, v_pages, page_table, context_lens, cu_new, kernel_size,
-                               sinks, scale, max_new, max_context)
+        plan = _step_plan(kernel_size, sinks, scale, max_new, max_context, metas, _meta(out),
+                          _meta(lse), _meta(new_lens), _meta(free_pages),
+                          None if head is None else _meta(head), None)
+        # slots, positions and cu_new live in one buffer (only the new head is handed out)
+        sizes = plan[3]
+        tokens = sizes[1]
+        ints = torch.empty(3 * tokens + sizes[0] + 1, dtype=torch.int32, device=device)
+        new_head = torch.empty(1, dtype=torch.int32, device=device)
+        slots = ints.data_ptr()
+        positions, cu_new = slots + 8 * tokens, slots + 12 * tokens
+    else:
+        cu_new, slots, _, new_head = tables
+        plan = _step_plan(kernel_size, sinks, scale, max_new, max_context, metas, _meta(out),
+                          _meta(lse), None, None, None, (_meta(cu_new), _meta(slots)))
+        cu_new, slots = cu_new.data_ptr(), slots.data_ptr()
+    p, at, need, sizes = plan
+    work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    context, table = context_lens.data_ptr(), page_table.data_ptr()
+    kp, vp = k_pages.data_ptr(), v_pages.data_ptr()
+    if tables is None:
+        _call("na_cache_tables", device, *sizes, context, new_lens.data_ptr(),
+              free_pages.data_ptr(), 0 if head is None else head.data_ptr(), table, cu_new, slots,
+              positions, new_head.data_ptr())
+    _call("na_cache_write", device, at, k.data_ptr(), v.data_ptr(), slots, kp, vp)
+    _call("na_cache_attention", device, at, q.data_ptr(), kp, vp, table, context, cu_new,
+          out.data_ptr(), lse.data_ptr(), work.data_ptr() if need else 0, need)
     return out, lse, new_head
