@@ -113,6 +113,7 @@ void fill_sink(const na_sink_problem& p, const int32_t* lengths, na::SeqGeo& g) 
     g.B = (int)p.batch;
     g.ntiles = (int)((p.tokens * g.G + 127) / 128);
     g.fd_tiles.init(g.ntiles);
+    g.runs = 2 * (int64_t)g.W < p.tokens || p.batch * p.kv_heads % 8 == 0;
     auto put = [&](const na_strides& s, int64_t& b, int64_t& h, int64_t& t) {
         b = s.batch * es;
         h = s.head * es;
@@ -129,9 +130,11 @@ void fill_sink(const na_sink_problem& p, const int32_t* lengths, na::SeqGeo& g) 
 }
 
 // The cut of dk, dv over workgroups, and the workspace: logsumexp and delta per row, then the
-// fp32 parts.  Fewer than 256 key tiles (a CU each) share the heads of a group among
-// workgroups.  The rows behind the windows of first tokens are cut into short chunks (their
-// tiles are staged one at a time), no more of them than fill the GPU four times over.
+// fp32 parts.  Key tiles share the heads of a group among workgroups where they are fewer than
+// the CUs, or, where windows are so long that the first key tiles have many times the rows of
+// the last (1024 workgroups even that out: 16 heads on 4, 8192 tokens, full causal, bf16 D = 128
+// 1500 us without).  The rows behind the windows of first tokens are cut into short chunks, no
+// more of them than fill the GPU four times over.
 // False: too large to launch.
 bool fill_backward(const na_sink_problem& p, const int32_t* lengths, na::SeqBwd& b, size_t& bytes) {
     std::memset(&b, 0, sizeof b);
@@ -140,12 +143,13 @@ bool fill_backward(const na_sink_problem& p, const int32_t* lengths, na::SeqBwd&
     const int64_t n = p.tokens, slices = p.batch * p.kv_heads;
     b.scale = p.scale;
     const int64_t ktiles = (n + 127) / 128, base = slices * ktiles;
-    const int64_t hsplit = base >= 256 ? 1 : std::min<int64_t>(g.G, (511 + base) / base);
+    const int64_t want = 2 * (int64_t)g.W >= n ? 1024 : 256;
+    const int64_t hsplit = std::min<int64_t>(g.G, (want + base - 1) / base);
     int64_t blocks = 0, chunks = 1;
     if (g.S > 0 && n > g.W) {
         blocks = (std::min<int64_t>(g.S, n - g.W) + 31) / 32;
         const int64_t tiles = g.G * ((n - g.W) / 32 + 1);
-        const int64_t share = 4 * 8;  // tiles of a workgroup: eight for each of four waves
+        const int64_t share = 8 * 4;  // tiles of a workgroup: four for each of eight waves
         chunks = std::min((tiles + share - 1) / share,
                           std::max<int64_t>(1, 1024 / (slices * blocks)));
     }

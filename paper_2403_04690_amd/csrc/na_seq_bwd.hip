@@ -14,7 +14,7 @@
 //           head by head, so that staged rows are consecutive tokens.  Few key tiles (short
 //           sequences, many heads a group) split the heads over workgroups.  The first tokens
 //           are attended by every later row: those pairs (outside the window) are cut over
-//           rows into workgroups of their own, in the same launch, ahead of the others
+//           rows into workgroups of their own, in the same launch, behind the others
 //   join    sums the fp32 parts that split heads and first tokens leave
 // P and dA are rounded once to the tensors' type for their matrix products (16-bit types);
 // everything else is fp32.
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 ? 1 : D == 128 ? 2 : 3)) void 
     const int wave = uniform((threadIdx.x >> 6) & 3);
 
     SeqTile t;
-    const int id = xcd_remap(blockIdx.x, gridDim.x);
+    const int id = seq_job(g, blockIdx.x, gridDim.x);
     const int slice = g.fd_tiles.div(id);
     seq_contiguous(g, g.ntiles - 1 - (id - slice * g.ntiles), slice, t);
     const int kvh = slice - t.b * g.Hkv;
@@ -188,14 +188,25 @@ struct KvCfg {
     static constexpr int kPer = D == 128 ? 1 : 2;  // tiles of a group per stage
     static constexpr int kBufs = 2 * kPer * RS;
     static constexpr int kOwn = kBufs * kBytes;  // LDS offset of the keys and values
-    static constexpr int kLds = kOwn + (kOwnLds ? 8 * kRows : 0);
-    // waves of a workgroup of first tokens: a buffer each
-    static constexpr int kFirst = kBufs < 4 * RS ? kBufs : 4 * RS;
+    // a workgroup of first tokens: a buffer for each wave, and one block's keys and values
+    static constexpr int kFirst = 4 * RS;
+    static constexpr int kFirstOwn = kFirst * kBytes;
+    static constexpr int kMain = kOwn + (kOwnLds ? 8 * kRows : 0);
+    static constexpr int kFirstLds = kFirstOwn + (kOwnLds ? 2 * kRows : 0);
+    static constexpr int kLds = kMain > kFirstLds ? kMain : kFirstLds;
+    static_assert(kLds <= 160 * 1024, "LDS of a CU");
 };
 
 // OUT: kDk | kDv.  fp32 at D = 128 holds only one gradient's accumulators beside its
 // fragments, and forms dv and dk in two launches.
 enum { kDk = 1, kDv = 2 };
+
+// The next N instructions of a kind in the order of a block that the compiler is asked to
+// keep: 0x8 matrix, 0x100 LDS reads, 0x2 vector, 0x400 transcendental.
+template <int KIND, int N>
+__device__ __forceinline__ void sched_group() {
+    __builtin_amdgcn_sched_group_barrier(KIND, N, 0);
+}
 template <typename T, int D, int OUT, bool LDS>
 struct KvState {
     using F = SeqFrags<T, D>;
@@ -234,11 +245,17 @@ struct KvState {
         const unsigned char* gt = qt + F::kTile;
         const float* stat = reinterpret_cast<const float*>(gt + F::kTile) + 4 * (lane >> 5);
         const int ro = opaque(f.ro), co = opaque(f.co);
+        constexpr bool kHint = sizeof(T) == 2 && OUT == (kDk | kDv);
+        constexpr int kKS = F::kKS, kDB = F::kDB;
         f32x16 s = f32x16{} * 0.f, dp = f32x16{} * 0.f;
 #pragma unroll
-        for (int st = 0; st < F::kKS; ++st)
+        for (int st = 0; st < kKS; ++st)
             s = mma32<T>(F::row_at(qt, ro, st), LDS ? F::row_at(own, ro, st) : kf[kKf ? st : 0], s);
-        x8 pf[2];
+        if constexpr (OUT & kDk)
+#pragma unroll
+            for (int st = 0; st < kKS; ++st)
+                dp = mma32<T>(F::row_at(gt, ro, st),
+                              LDS ? F::row_at(own + F::kTile, ro, st) : vf[kVf ? st : 0], dp);
 #pragma unroll
         for (int i4 = 0; i4 < 4; ++i4) {
             const f32x4 lse2 = *reinterpret_cast<const f32x4*>(stat + 8 * i4);
@@ -248,39 +265,76 @@ struct KvState {
                 s[i] = fast_exp2(fmaf(s[i], c, -lse2[r]));
             }
         }
+        if constexpr (kHint) {
+            // Half of the operands are read before the first product, the others behind each;
+            // the exponentials stand between the products of dp, which do not need them.
+            constexpr int kR = LDS ? 2 : 1, kH = kKS / 2;  // reads a product
+            sched_group<0x100, (kH * kR)>();
+#pragma unroll
+            for (int x = 0; x < kH; ++x) {
+                sched_group<0x8, 1>();
+                sched_group<0x100, kR>();
+            }
+            sched_group<0x100, 4>();
+#pragma unroll
+            for (int x = 0; x < kH; ++x) {
+                sched_group<0x8, 1>();
+                sched_group<0x100, kR>();
+            }
+#pragma unroll
+            for (int x = 0; x < kKS; ++x) {
+                sched_group<0x8, 1>();
+                if (x < kH) sched_group<0x100, kR>();
+                sched_group<0x402, (32 / kKS)>();
+            }
+        }
         if (!full) {
             const unsigned m = below(len - dist) & ~below(-dist);
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = keep(m, i, s[i], 0.f);
         }
+        x8 pf[2], df[2];
         if constexpr (OUT & kDv) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) pf[i >> 3][i & 7] = Tr<T>::cvt(s[i]);
 #pragma unroll
             for (int bi = 0; bi < 2; ++bi)
 #pragma unroll
-                for (int db = 0; db < F::kDB; ++db)
+                for (int db = 0; db < kDB; ++db)
                     dv[db] = mma32<T>(F::col_at(gt, co, db, bi, lane), pf[bi], dv[db]);
         }
         if constexpr (OUT & kDk) {
-#pragma unroll
-            for (int st = 0; st < F::kKS; ++st)
-                dp = mma32<T>(F::row_at(gt, ro, st),
-                              LDS ? F::row_at(own + F::kTile, ro, st) : vf[kVf ? st : 0], dp);
 #pragma unroll
             for (int i4 = 0; i4 < 4; ++i4) {
                 const f32x4 delta = *reinterpret_cast<const f32x4*>(stat + 32 + 8 * i4);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int i = 4 * i4 + r;
-                    pf[i >> 3][i & 7] = Tr<T>::cvt(s[i] * (dp[i] - delta[r]));
+                    df[i >> 3][i & 7] = Tr<T>::cvt(s[i] * (dp[i] - delta[r]));
                 }
             }
 #pragma unroll
             for (int bi = 0; bi < 2; ++bi)
 #pragma unroll
-                for (int db = 0; db < F::kDB; ++db)
-                    dk[db] = mma32<T>(F::col_at(qt, co, db, bi, lane), pf[bi], dk[db]);
+                for (int db = 0; db < kDB; ++db)
+                    dk[db] = mma32<T>(F::col_at(qt, co, db, bi, lane), df[bi], dk[db]);
+        }
+        if constexpr (kHint) {
+            // dv's products with the forming of dA between them, then dk's
+            sched_group<0x100, (2 * kDB)>();
+            sched_group<0x2, 8>();
+            sched_group<0x100, 4>();
+#pragma unroll
+            for (int x = 0; x < 2 * kDB; ++x) {
+                sched_group<0x8, 1>();
+                sched_group<0x100, 2>();
+                sched_group<0x2, (40 / (2 * kDB))>();
+            }
+#pragma unroll
+            for (int x = 0; x < kDB; ++x) {
+                sched_group<0x8, 1>();
+                sched_group<0x100, 2>();
+            }
         }
     }
 
@@ -387,15 +441,16 @@ seq_dkv_kernel(SeqBwd b, const T* __restrict__ qg, const T* __restrict__ kg,
     SeqFrags<T, D> f;
     f.init(lane);
 
-    const bool first_role = (int)blockIdx.x < b.first_jobs;
+    const int jobs = gridDim.x - b.first_jobs;
+    const bool first_role = (int)blockIdx.x >= jobs;
     int slice, k0, part;  // part: chunk of rows (first tokens), or of heads
     if (first_role) {
-        const int id = b.fd_chunks.div(blockIdx.x);
-        part = blockIdx.x - id * b.chunks;
+        const int id = b.fd_chunks.div(blockIdx.x - jobs);
+        part = blockIdx.x - jobs - id * b.chunks;
         slice = b.fd_blocks.div(id);
         k0 = (id - slice * b.blocks) * 32;
     } else {
-        const int job = xcd_remap(blockIdx.x - b.first_jobs, gridDim.x - b.first_jobs);
+        const int job = seq_job(g, blockIdx.x, jobs);
         const int id = b.fd_hsplit.div(job);
         part = job - id * b.hsplit;
         slice = b.fd_ktiles.div(id);
@@ -415,7 +470,7 @@ seq_dkv_kernel(SeqBwd b, const T* __restrict__ qg, const T* __restrict__ kg,
     const unsigned char* krow = reinterpret_cast<const unsigned char*>(kg) + sb * g.kb + kvh * g.kh;
     const unsigned char* vrow = reinterpret_cast<const unsigned char*>(vg) + sb * g.vb + kvh * g.vh;
     const int last_key = max(valid - 1, 0);
-    unsigned char* own = smem + C::kOwn + (first_role ? 0 : (wave & 3) * 2 * C::kRows);
+    unsigned char* own = smem + (first_role ? C::kFirstOwn : C::kOwn + (wave & 3) * 2 * C::kRows);
     if constexpr (C::kOwnLds) {
         if (wave < (first_role ? 1 : 4)) {
             SeqRows<T, D> rows;
@@ -446,16 +501,15 @@ seq_dkv_kernel(SeqBwd b, const T* __restrict__ qg, const T* __restrict__ kg,
         const int len = key < g.S && valid - key > g.W ? valid - key - g.W : 0;
         st.settle_keys();
         stage_barrier();
-        if (wave < C::kFirst)
-            for (int e = part * per + wave; e < end; e += C::kFirst) {
-                const int hd = e / nt, i0 = (t0 + e - hd * nt) * 32;
-                Ld::issue(b, qs + hd * g.qh, gs + hd * b.gh, b.lse2 + stat + hd * g.lh,
-                         b.delta + stat + hd * g.lh, i0, valid, 0, lane, buf);
-                wait_vmem();
-                const bool full = i0 - (k0 + 31) >= g.W && i0 + 32 <= valid && k0 + 31 < g.S;
-                st.tile(f, buf, own, lane, g.c, full, i0 + 4 * h - key - g.W, len);
-                wait_lds();
-            }
+        for (int e = part * per + wave; e < end; e += C::kFirst) {
+            const int hd = e / nt, i0 = (t0 + e - hd * nt) * 32;
+            Ld::issue(b, qs + hd * g.qh, gs + hd * b.gh, b.lse2 + stat + hd * g.lh,
+                      b.delta + stat + hd * g.lh, i0, valid, 0, lane, buf);
+            wait_vmem();
+            const bool full = i0 - (k0 + 31) >= g.W && i0 + 32 <= valid && k0 + 31 < g.S;
+            st.tile(f, buf, own, lane, g.c, full, i0 + 4 * h - key - g.W, len);
+            wait_lds();
+        }
 #pragma unroll
         for (int half = C::kFirst / 2; half >= 1; half /= 2) st.add_waves(smem, wave, half, lane);
         if (wave == 0) {
@@ -552,8 +606,9 @@ seq_dkv_kernel(SeqBwd b, const T* __restrict__ qg, const T* __restrict__ kg,
         each_four<D>(st.dv, h, 1.f, [&](int d, f32x4 x) { st_x4<T>(dv + d, x); });
 }
 
-// Sums the parts of each key (heads, then first tokens' chunks) and rounds once: a thread per
-// four columns of dk or dv.
+// Sums the parts of each key (heads, then first tokens' chunks) and rounds once: four lanes per
+// four columns of dk or dv, each with every fourth part, so that the loads of tens of parts are
+// in flight together; a fixed order.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void seq_dkv_join_kernel(SeqBwd b, int first_parts,
                                                            T* __restrict__ dkg,
@@ -562,22 +617,28 @@ __global__ __launch_bounds__(256) void seq_dkv_join_kernel(SeqBwd b, int first_p
     const int keys = b.hsplit > 1 ? g.n : min(g.n, b.blocks * 32);
     const int stride = b.hsplit > 1 ? g.n : b.blocks * 32;  // keys of a slice's parts
     constexpr int kPer = 2 * D / 4;
-    const int64_t total = (int64_t)g.B * g.Hkv * keys * kPer;
-    for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < total;
-         x += (int64_t)gridDim.x * 256) {
+    const int64_t slices = (int64_t)g.B * g.Hkv, total = slices * keys * kPer;
+    const int q = threadIdx.x & 3;
+    // (whole quads of lanes leave the loop together)
+    for (int64_t x = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 2; x < total;
+         x += (int64_t)gridDim.x * 64) {
         const int64_t row = x / kPer;
         const int d = (int)(x % kPer) * 4;
         const int slice = (int)(row / keys), key = (int)(row % keys);
-        const int64_t slices = (int64_t)g.B * g.Hkv;
         f32x4 sum{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-        for (int p = 0; p < b.hsplit; ++p)
+        for (int p = q; p < b.hsplit; p += 4)
             sum += ld16<f32x4>(b.part + ((p * slices + slice) * stride + key) * 2 * D + d);
         if (key < b.blocks * 32)
-#pragma unroll 16
-            for (int p = 0; p < first_parts; ++p)
+#pragma unroll 8
+            for (int p = q; p < first_parts; p += 4)
                 sum += ld16<f32x4>(b.first_part +
                                    ((p * slices + slice) * (b.blocks * 32) + key) * 2 * D + d);
+#pragma unroll
+        for (int m = 1; m <= 2; m *= 2)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum[r] += __shfl_xor(sum[r], m, kWave);
+        if (q != 0) continue;
         const int sb = g.fd_kv.div(slice), kvh = slice - sb * g.Hkv;
         unsigned char* to =
             d < D ? reinterpret_cast<unsigned char*>(dkg) + sb * b.kb + kvh * b.kh + key * b.kt
@@ -621,7 +682,7 @@ static hipError_t launch_bwd(const SeqBwd& b, const T* q, const T* k, const T* v
     }
     if (e != hipSuccess || (b.hsplit == 1 && b.blocks == 0)) return e;
     const int64_t units = (int64_t)slices * (b.hsplit > 1 ? g.n : b.blocks * 32) * (D / 2);
-    const unsigned grid = (unsigned)std::min<int64_t>((units + 255) / 256, 1 << 16);
+    const unsigned grid = (unsigned)std::min<int64_t>((units + 63) / 64, 1 << 16);
     hipLaunchKernelGGL((seq_dkv_join_kernel<T, D>), dim3(grid), dim3(256), 0, s, b,
                        b.chunks, dk, dv);
     return hipGetLastError();

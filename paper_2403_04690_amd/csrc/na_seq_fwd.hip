@@ -185,7 +185,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 4) : 1)) voi
         if (g.B > 64) tile = g.ntiles - 1 - tile;  // (long tiles of a request first, at least)
         if (!seq_locate(g, tile, 7, lane, t)) return;
     } else {
-        const int id = xcd_remap(blockIdx.x, gridDim.x);
+        const int id = seq_job(g, blockIdx.x, gridDim.x);
         const int slice = g.fd_tiles.div(id);
         tile = g.ntiles - 1 - (id - slice * g.ntiles);
         seq_contiguous(g, tile, slice, t);

@@ -34,6 +34,7 @@ struct SeqGeo {
     int64_t qb, qh, qt, kb, kh, kt, vb, vh, vt, ob, oh, ot;
     int64_t lb, lh, lt;  // logsumexp, in elements
     float c;             // scale * log2(e)
+    int runs;            // contiguous form: each XCD takes a run of neighbouring tiles
     const int32_t* lengths;  // contiguous form: valid tokens per sequence, or null
     const int32_t *context, *cu, *table;  // paged form
 };
@@ -357,6 +358,13 @@ __device__ __forceinline__ bool seq_locate(const SeqGeo& g, int tile, int lgM, i
 // last one whatever is left (the host sizes chunk by a bound that it is told).
 __device__ __forceinline__ int seq_splits(const SeqGeo& g, int nT) {
     return max(1, min(g.nsplit, (nT + g.chunk - 1) / g.chunk));
+}
+
+// Contiguous form: workgroup -> job.  Runs of neighbouring tiles on one XCD share what its L2
+// holds; where windows are long the tiles of a sequence differ in length, and a run of less
+// than whole sequences would give one XCD the long ones and another the short ones.
+__device__ __forceinline__ int seq_job(const SeqGeo& g, int bid, int jobs) {
+    return g.runs ? xcd_remap(bid, jobs) : bid;
 }
 
 // Contiguous form: row tile `tile` of (sequence, key/value head) `slice`.
