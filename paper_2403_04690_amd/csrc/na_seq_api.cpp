@@ -113,7 +113,8 @@ void fill_sink(const na_sink_problem& p, const int32_t* lengths, na::SeqGeo& g) 
     g.B = (int)p.batch;
     g.ntiles = (int)((p.tokens * g.G + 127) / 128);
     g.fd_tiles.init(g.ntiles);
-    g.runs = 2 * (int64_t)g.W < p.tokens || p.batch * p.kv_heads % 8 == 0;
+    g.fd_slices.init((int)(p.batch * p.kv_heads));
+    g.runs = 2 * (int64_t)g.W < p.tokens;
     auto put = [&](const na_strides& s, int64_t& b, int64_t& h, int64_t& t) {
         b = s.batch * es;
         h = s.head * es;

@@ -81,9 +81,9 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 ? 1 : D == 128 ? 2 : 3)) void 
     const int wave = uniform((threadIdx.x >> 6) & 3);
 
     SeqTile t;
-    const int id = seq_job(g, blockIdx.x, gridDim.x);
-    const int slice = g.fd_tiles.div(id);
-    seq_contiguous(g, g.ntiles - 1 - (id - slice * g.ntiles), slice, t);
+    int tile, slice;
+    seq_job(g, blockIdx.x, gridDim.x, tile, slice);
+    seq_contiguous(g, tile, slice, t);
     const int kvh = slice - t.b * g.Hkv;
 
     SeqStage<T, D, false, 4> ld;
@@ -200,13 +200,6 @@ struct KvCfg {
 // OUT: kDk | kDv.  fp32 at D = 128 holds only one gradient's accumulators beside its
 // fragments, and forms dv and dk in two launches.
 enum { kDk = 1, kDv = 2 };
-
-// The next N instructions of a kind in the order of a block that the compiler is asked to
-// keep: 0x8 matrix, 0x100 LDS reads, 0x2 vector, 0x400 transcendental.
-template <int KIND, int N>
-__device__ __forceinline__ void sched_group() {
-    __builtin_amdgcn_sched_group_barrier(KIND, N, 0);
-}
 template <typename T, int D, int OUT, bool LDS>
 struct KvState {
     using F = SeqFrags<T, D>;
@@ -245,7 +238,6 @@ struct KvState {
         const unsigned char* gt = qt + F::kTile;
         const float* stat = reinterpret_cast<const float*>(gt + F::kTile) + 4 * (lane >> 5);
         const int ro = opaque(f.ro), co = opaque(f.co);
-        constexpr bool kHint = sizeof(T) == 2 && OUT == (kDk | kDv);
         constexpr int kKS = F::kKS, kDB = F::kDB;
         f32x16 s = f32x16{} * 0.f, dp = f32x16{} * 0.f;
 #pragma unroll
@@ -263,29 +255,6 @@ struct KvState {
             for (int r = 0; r < 4; ++r) {
                 const int i = 4 * i4 + r;
                 s[i] = fast_exp2(fmaf(s[i], c, -lse2[r]));
-            }
-        }
-        if constexpr (kHint) {
-            // Half of the operands are read before the first product, the others behind each;
-            // the exponentials stand between the products of dp, which do not need them.
-            constexpr int kR = LDS ? 2 : 1, kH = kKS / 2;  // reads a product
-            sched_group<0x100, (kH * kR)>();
-#pragma unroll
-            for (int x = 0; x < kH; ++x) {
-                sched_group<0x8, 1>();
-                sched_group<0x100, kR>();
-            }
-            sched_group<0x100, 4>();
-#pragma unroll
-            for (int x = 0; x < kH; ++x) {
-                sched_group<0x8, 1>();
-                sched_group<0x100, kR>();
-            }
-#pragma unroll
-            for (int x = 0; x < kKS; ++x) {
-                sched_group<0x8, 1>();
-                if (x < kH) sched_group<0x100, kR>();
-                sched_group<0x402, (32 / kKS)>();
             }
         }
         if (!full) {
@@ -318,23 +287,6 @@ struct KvState {
 #pragma unroll
                 for (int db = 0; db < kDB; ++db)
                     dk[db] = mma32<T>(F::col_at(qt, co, db, bi, lane), df[bi], dk[db]);
-        }
-        if constexpr (kHint) {
-            // dv's products with the forming of dA between them, then dk's
-            sched_group<0x100, (2 * kDB)>();
-            sched_group<0x2, 8>();
-            sched_group<0x100, 4>();
-#pragma unroll
-            for (int x = 0; x < 2 * kDB; ++x) {
-                sched_group<0x8, 1>();
-                sched_group<0x100, 2>();
-                sched_group<0x2, (40 / (2 * kDB))>();
-            }
-#pragma unroll
-            for (int x = 0; x < kDB; ++x) {
-                sched_group<0x8, 1>();
-                sched_group<0x100, 2>();
-            }
         }
     }
 
@@ -450,11 +402,21 @@ seq_dkv_kernel(SeqBwd b, const T* __restrict__ qg, const T* __restrict__ kg,
         slice = b.fd_blocks.div(id);
         k0 = (id - slice * b.blocks) * 32;
     } else {
-        const int job = seq_job(g, blockIdx.x, jobs);
-        const int id = b.fd_hsplit.div(job);
-        part = job - id * b.hsplit;
-        slice = b.fd_ktiles.div(id);
-        k0 = (id - slice * b.ktiles) * 128;
+        // (the orders of seq_job; the first keys have the most rows)
+        int tile;
+        if (g.runs) {
+            const int job = xcd_remap(blockIdx.x, jobs);
+            const int id = b.fd_hsplit.div(job);
+            part = job - id * b.hsplit;
+            slice = b.fd_ktiles.div(id);
+            tile = id - slice * b.ktiles;
+        } else {
+            const int id = g.fd_slices.div(blockIdx.x);
+            slice = blockIdx.x - id * g.B * g.Hkv;
+            tile = b.fd_hsplit.div(id);
+            part = id - tile * b.hsplit;
+        }
+        k0 = tile * 128;
     }
     const int sb = g.fd_kv.div(slice), kvh = slice - sb * g.Hkv;
     const int valid = g.lengths ? min(max(g.lengths[sb], 0), g.n) : g.n;

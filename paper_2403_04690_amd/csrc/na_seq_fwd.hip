@@ -45,16 +45,16 @@ struct SeqState {
     // Folds N tiles of 32 keys into the state: K and V of tile n at tile[n] and tile[n] + kTile,
     // from position j0[n].  Unless `full` (uniform), some pair is not seen, and of a tile that
     // is not `on` none; pos: this lane's row.
-    //   With two tiles the matrix cores and the vector unit work side by side within a wave:
+    //   With two tiles the matrix cores and the vector unit can work side by side within a wave:
     // the second tile's scores beside the scaling of the first's, the first's values beside
-    // the second's exponentials.  The compiler is told that order (sched_group_barrier).
+    // the second's exponentials.  (Asking for that order instruction by instruction, with
+    // scheduling groups, was 1 to 8 % slower than leaving it to the compiler.)
     //   (One body with a branch around the mask alone: two bodies that meet again in the
     // accumulators cost registers.)
     template <int N>
     __device__ __forceinline__ void fold(const F& f, const unsigned char* (&tile)[N],
                                          int lane, float c, bool full, const int (&j0)[N],
                                          const bool (&on)[N], int pos, int W, int S) {
-        constexpr bool kHint = N == 2 && sizeof(T) == 2;
         f32x16 s[N];
         x8 kf[N][F::kKS];
 #pragma unroll
@@ -74,19 +74,6 @@ struct SeqState {
         for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) y[n][i] = fmaf(s[n][i], c, negm);
-        if constexpr (kHint) {
-            __builtin_amdgcn_sched_group_barrier(0x100, F::kKS + 1, 0);  // K reads
-#pragma unroll
-            for (int st = 0; st < F::kKS; ++st) {
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                if (st < F::kKS - 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            }
-#pragma unroll
-            for (int st = 0; st < F::kKS; ++st) {
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x2, 16 / F::kKS, 0);
-            }
-        }
         if (!full) {
 #pragma unroll
             for (int n = 0; n < N; ++n) {
@@ -137,27 +124,13 @@ struct SeqState {
                     o[db] = mma32<T>(vf[n][bi][db], pf[n][bi], o[db]);
         }
         l += sum[0] + sum[1];
-        if constexpr (kHint) {
-            constexpr int kMM = 2 * F::kDB;  // products of a tile's values
-            __builtin_amdgcn_sched_group_barrier(0x100, 4 * F::kDB, 0);  // V reads of tile 0
-            __builtin_amdgcn_sched_group_barrier(0x402, 38, 0);          // its exponentials ..
-#pragma unroll
-            for (int x = 0; x < kMM; ++x) {
-                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-                __builtin_amdgcn_sched_group_barrier(0x402, 40 / kMM, 0);
-            }
-        }
     }
 };
 
 // The wide form's ring of stages: tiles per stage, and stages (one read, the others in flight).
 template <typename T, int D>
 struct SeqRing {
-#ifndef TLV
-#define TLV (D == 128 && sizeof(T) == 2 ? 2 : 1)
-#endif
-    static constexpr int kTiles = TLV;
+    static constexpr int kTiles = D == 128 && sizeof(T) == 2 ? 2 : 1;
     static constexpr int kStages = kTiles == 2 ? 2 : 3;
     static constexpr int kStage = kTiles * 2 * SeqFrags<T, D>::kTile;
     static constexpr int kLds = kStages * kStage;
@@ -185,9 +158,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 4) : 1)) voi
         if (g.B > 64) tile = g.ntiles - 1 - tile;  // (long tiles of a request first, at least)
         if (!seq_locate(g, tile, 7, lane, t)) return;
     } else {
-        const int id = seq_job(g, blockIdx.x, gridDim.x);
-        const int slice = g.fd_tiles.div(id);
-        tile = g.ntiles - 1 - (id - slice * g.ntiles);
+        int slice;
+        seq_job(g, blockIdx.x, gridDim.x, tile, slice);
         seq_contiguous(g, tile, slice, t);
         kvh = slice - t.b * g.Hkv;
     }
