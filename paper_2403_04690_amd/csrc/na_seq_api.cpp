@@ -404,9 +404,9 @@ na_status na_cache_attention(const na_cache_problem* problem, const void* q, con
     const na_status st = check_attention(p);
     if (st != NA_OK) return st;
     if (p.heads == 0 || p.tokens == 0 || p.requests == 0) return NA_OK;
-    const bool cached = p.pages > 0 && p.max_pages > 0;  // (else every page reads as zeros)
+    // (a pool or a table without entries is never read)
     if (!q || !context_lens || !cu_new || !out || !logsumexp ||
-        (cached && (!k_pages || !v_pages || !page_table)))
+        (p.pages > 0 && (!k_pages || !v_pages)) || (p.max_pages > 0 && !page_table))
         return NA_ERR_NULL;
     if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16) ||
         !aligned(logsumexp, 16) || !aligned(workspace, 16) || !aligned(page_table, 4) ||
@@ -422,8 +422,8 @@ na_status na_cache_attention(const na_cache_problem* problem, const void* q, con
     const int64_t es = elem_bytes(p.dtype);
     g.n = (int)p.tokens;
     g.B = (int)p.requests;
-    g.pages = cached ? (int)p.pages : 0;
-    g.max_pages = cached ? (int)p.max_pages : 0;
+    g.pages = (int)p.pages;
+    g.max_pages = (int)p.max_pages;
     g.lgps = __builtin_ctzll(p.page_size);
     g.qh = p.q.head * es;
     g.qt = p.q.token * es;

@@ -25,6 +25,7 @@ stream of the tensors' device.
 import ctypes
 import functools
 import math
+from operator import index
 
 import torch
 
@@ -160,8 +161,24 @@ def _check_lse(lse, q):
         raise ValueError("tensors must share a device")
 
 
+def _window(kernel_size, sinks, scale):
+    """Plain numbers (the plans are looked up by value, never by a tensor's identity)."""
+    return (None if kernel_size is None else index(kernel_size), index(sinks),
+            None if scale is None else float(scale))
+
+
+def _bounds(max_new, max_context):
+    """The caller's bounds, the second rounded up by at most a tile of 32 keys or 3 %: one that
+    grows by a token a step needs a new plan every 32 steps, not every step."""
+    if max_context is not None:
+        max_context = index(max_context)
+        if max_context > 0:
+            step = max(5, max_context.bit_length() - 6)
+            max_context = -(-max_context >> step) << step
+    return None if max_new is None else index(max_new), max_context
+
+
 def _count(value, name, least):
-    value = int(value)
     if value < least:
         raise ValueError(f"{name} must be at least {least}")
     return min(value, _WHOLE)
@@ -217,8 +234,9 @@ def sink_forward(q, k, v, kernel_size, sinks=0, scale=None, lengths=None, out=No
     _library()
     out = _like(q) if out is None else out
     lse = _lse_for(q) if lse is None else lse
-    p = _sink_plan(kernel_size, sinks, scale, None if lengths is None else _meta(lengths),
-                   _meta(lse), _meta(q), _meta(k), _meta(v), _meta(out))
+    p = _sink_plan(*_window(kernel_size, sinks, scale),
+                   None if lengths is None else _meta(lengths), _meta(lse), _meta(q), _meta(k),
+                   _meta(v), _meta(out))
     _call("na_sink_forward", q.device, p[1], q.data_ptr(), k.data_ptr(), v.data_ptr(),
           0 if lengths is None else lengths.data_ptr(), out.data_ptr(), lse.data_ptr())
     return out, lse
@@ -233,8 +251,9 @@ def sink_backward(q, k, v, out, lse, dout, kernel_size, sinks=0, scale=None, len
     dk = _like(k) if dk is None else dk
     dv = _like(v) if dv is None else dv
     p, at, need = _sink_plan(
-        kernel_size, sinks, scale, None if lengths is None else _meta(lengths), _meta(lse),
-        _meta(q), _meta(k), _meta(v), _meta(out), _meta(dout), _meta(dq), _meta(dk), _meta(dv))
+        *_window(kernel_size, sinks, scale), None if lengths is None else _meta(lengths),
+        _meta(lse), _meta(q), _meta(k), _meta(v), _meta(out), _meta(dout), _meta(dq), _meta(dk),
+        _meta(dv))
     # (the allocator hands it out stream by stream, and to a captured graph from its own pool)
     work = torch.empty(need, dtype=torch.uint8, device=q.device)
     _call("na_sink_backward", q.device, at, q.data_ptr(), k.data_ptr(), v.data_ptr(),
@@ -268,7 +287,10 @@ class _SinkFunction(torch.autograd.Function):
 
 
 def sink_attention(q, k, v, kernel_size, sinks=0, scale=None, lengths=None):
-    """Autograd-aware window attention with visible first tokens (see sink_forward)."""
+    """Autograd-aware window attention with visible first tokens (see sink_forward).  Capture
+    its forward and backward into one graph with no eager autograd graph of the same leaves
+    alive: torch runs a leaf's accumulation on the stream of the oldest such graph, which a
+    capture of another stream cannot join."""
     return _SinkFunction.apply(q, k, v, kernel_size, sinks, scale, lengths)
 
 
@@ -300,7 +322,7 @@ def _tables_plan(tokens, page_size, context, new, table, free, head, outs):
             _ints(device, dtype, **{name: m})
             if m[0] != (n,):
                 raise ValueError(f"{name} needs {n} entries")
-    return requests, _count(tokens, "tokens", 0), int(page_size), table[0][1], free[0][0]
+    return requests, _count(tokens, "tokens", 0), page_size, table[0][1], free[0][0]
 
 
 def cache_tables(context_lens, new_lens, page_table, free_pages, page_size, tokens, head=None,
@@ -315,7 +337,7 @@ def cache_tables(context_lens, new_lens, page_table, free_pages, page_size, toke
     _library()
     device = context_lens.device
     outs = tuple(None if t is None else _meta(t) for t in (cu_new, slots, positions, new_head))
-    sizes = _tables_plan(tokens, page_size, _meta(context_lens), _meta(new_lens),
+    sizes = _tables_plan(index(tokens), index(page_size), _meta(context_lens), _meta(new_lens),
                          _meta(page_table), _meta(free_pages),
                          None if head is None else _meta(head), outs)
     if cu_new is None:
@@ -415,8 +437,8 @@ def cache_attention(q, k_pages, v_pages, page_table, context_lens, cu_new, kerne
     out = _like(q) if out is None else out
     lse = _lse_for(q) if lse is None else lse
     p, at, need = _attention_plan(
-        kernel_size, sinks, scale, max_new, max_context, _meta(q), _meta(k_pages), _meta(v_pages),
-        _meta(page_table), _meta(context_lens), _meta(cu_new), _meta(out), _meta(lse))
+        *_window(kernel_size, sinks, scale), *_bounds(max_new, max_context), _meta(q),
+        _meta(k_pages), _meta(v_pages), _meta(page_table), _meta(context_lens), _meta(cu_new), _meta(out), _meta(lse))
     # (the allocator hands it out stream by stream, and to a captured graph from its own pool)
     work = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     _call("na_cache_attention", q.device, at, q.data_ptr(), k_pages.data_ptr(),
@@ -465,8 +487,9 @@ def cache_step(q, k, v, k_pages, v_pages, page_table, context_lens, new_lens, fr
     out, lse = _like(q), _lse_for(q)
     metas = (_meta(q), _meta(k), _meta(v), _meta(k_pages), _meta(v_pages), _meta(page_table),
              _meta(context_lens))
+    rule = *_window(kernel_size, sinks, scale), *_bounds(max_new, max_context)
     if tables is None:
-        plan = _step_plan(kernel_size, sinks, scale, max_new, max_context, metas, _meta(out),
+        plan = _step_plan(*rule, metas, _meta(out),
                           _meta(lse), _meta(new_lens), _meta(free_pages),
                           None if head is None else _meta(head), None)
         # slots, positions and cu_new live in one buffer (only the new head is handed out)
@@ -478,8 +501,8 @@ def cache_step(q, k, v, k_pages, v_pages, page_table, context_lens, new_lens, fr
         positions, cu_new = slots + 8 * tokens, slots + 12 * tokens
     else:
         cu_new, slots, _, new_head = tables
-        plan = _step_plan(kernel_size, sinks, scale, max_new, max_context, metas, _meta(out),
-                          _meta(lse), None, None, None, (_meta(cu_new), _meta(slots)))
+        plan = _step_plan(*rule, metas, _meta(out), _meta(lse), None, None, None,
+                          (_meta(cu_new), _meta(slots)))
         cu_new, slots = cu_new.data_ptr(), slots.data_ptr()
     p, at, need, sizes = plan
     work = torch.empty(need, dtype=torch.uint8, device=device) if need else None

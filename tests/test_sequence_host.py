@@ -258,6 +258,24 @@ def test_binding_refuses_before_launch(lib):
             f()
 
 
+def test_plans_are_looked_up_by_numbers(lib):
+    # a tensor's value counts, not its identity; numbers that are not whole are refused
+    w = torch.tensor(5)
+    assert sequence._window(w, 2, torch.tensor(0.5)) == (5, 2, 0.5)
+    w += 1
+    assert sequence._window(w, 2, None) == (6, 2, None)
+    with pytest.raises(TypeError):
+        sequence._window(5.0, 2, None)
+    with pytest.raises(TypeError):
+        sequence._bounds(None, 100.5)
+    # a growing bound: never below itself, at most a tile or 1/32 above, few distinct ones
+    assert sequence._bounds(3, None) == (3, None)
+    assert sequence._bounds(None, 0)[1] == 0 and sequence._bounds(None, -4)[1] == -4
+    got = [sequence._bounds(None, n)[1] for n in range(1, 20000)]
+    assert all(n <= x <= max(n + 31, n + n // 32) for n, x in enumerate(got, 1))
+    assert len(set(got)) < 300
+
+
 def test_cache_binding_refuses_before_launch(lib):
     pages = torch.zeros(4, 2, 16, 32)
     q, k = torch.zeros(3, 4, 32), torch.zeros(3, 2, 32)
