@@ -34,11 +34,12 @@ struct DqState {
     f32x16 dq[F::kDB];
     float lse2, delta;
 
-    __device__ __forceinline__ void tile(const F& f, const unsigned char* kt,
-                                         const unsigned char* vt, int lane, float c, bool full,
-                                         int j0, int pos, int W, int S) {
-        f32x16 s = f32x16{} * 0.f, dp = f32x16{} * 0.f;
-        x8 kf[F::kKS], vf[F::kKS], kc[2][F::kDB];
+    // P and dout . v of a tile of keys; full, j0, pos: as in the forward.
+    __device__ __forceinline__ void weights(const F& f, const unsigned char* kt,
+                                            const unsigned char* vt, int lane, float c, bool full,
+                                            int j0, int pos, int W, int S, f32x16& s, f32x16& dp) {
+        x8 kf[F::kKS], vf[F::kKS];
+        s = dp = f32x16{} * 0.f;
         f.rows(kt, kf);
         if constexpr (sizeof(T) == 2) f.rows(vt, vf);
 #pragma unroll
@@ -54,6 +55,14 @@ struct DqState {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = keep(m, i, s[i], 0.f);
         }
+    }
+
+    __device__ __forceinline__ void tile(const F& f, const unsigned char* kt,
+                                         const unsigned char* vt, int lane, float c, bool full,
+                                         int j0, int pos, int W, int S) {
+        f32x16 s, dp;
+        weights(f, kt, vt, lane, c, full, j0, pos, W, S, s, dp);
+        x8 kc[2][F::kDB];
         f.cols(kt, 0, lane, kc[0]);
         if constexpr (sizeof(T) == 2) f.cols(kt, 1, lane, kc[1]);
         x8 pf[2];
@@ -67,7 +76,17 @@ struct DqState {
     }
 };
 
+// Rows of fewer keys than this form delta themselves (see seq_dq_kernel).
+constexpr int kFewKeys = 128;
+
 // (a ring of three stages of a key tile, as the forward's)
+//   delta_i = dout_i . out_i takes out as the forward rounded it.  Where a row has few keys, out
+// is as large as a value, and that rounding is most of what dq is off by besides its own and
+// dA's: in 16-bit types the row tiles with such rows (the first tokens', or all of a short
+// window) pass over their keys twice, and first sum delta_i = sum_j P_ij dout_i . v_j
+// unrounded.  (Error of dq, in errors of one rounding of it: 1.45 to 1.65 without, 1.40 to 1.47
+// with.  Gradients of 16 heads on 4, 8192 tokens, bf16 D = 128: window 120, every tile twice,
+// 86 and 96 us; window 512, the first ones only, 206 and 207.)
 template <typename T, int D>
 __global__ __launch_bounds__(256, (sizeof(T) == 4 ? 1 : D == 128 ? 2 : 3)) void seq_dq_kernel(
     SeqBwd b, const T* __restrict__ qg, const T* __restrict__ kg, const T* __restrict__ vg,
@@ -119,13 +138,6 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 ? 1 : D == 128 ? 2 : 3)) void 
         st.delta = col_sum<32>(d);
         st.lse2 = lseg[t.b * g.lb + hq * g.lh + from] * kLog2e;
     }
-#pragma unroll
-    for (int db = 0; db < F::kDB; ++db) st.dq[db] = f32x16{} * 0.f;
-    if (m < t.rows && h == 0) {
-        const int64_t at = t.b * g.lb + hq * g.lh + tok;
-        b.lse2[at] = st.lse2;
-        b.delta[at] = st.delta;
-    }
     F f;
     f.init(lane);
 #pragma unroll
@@ -136,7 +148,8 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 ? 1 : D == 128 ? 2 : 3)) void 
     settle(st.lse2);
     settle(st.delta);
 
-    auto stage = [&](int e, auto BUF) __attribute__((always_inline)) {
+    float own = 0.f;  // this lane's share of delta
+    auto stage = [&](int e, auto BUF, auto FIRST) __attribute__((always_inline)) {
         constexpr int kAt = decltype(BUF)::value;
         if (e + 1 < t.nT)
             wait_vmem_but<decltype(ld)::kCount>();
@@ -148,14 +161,41 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 ? 1 : D == 128 ? 2 : 3)) void 
         const bool out = j0 > wmax || (wmin - (j0 + 31) >= g.W && j0 >= g.S);
         const bool full = j0 + 31 <= wmin && (wmax - j0 < g.W || j0 + 31 < g.S);
         const unsigned char* kt = smem + kAt * kBuf;
-        if (live && !out) st.tile(f, kt, kt + F::kTile, lane, g.c, full, j0, tok, g.W, g.S);
+        if (!live || out) return;
+        if constexpr (decltype(FIRST)::value) {
+            f32x16 s, dp;
+            st.weights(f, kt, kt + F::kTile, lane, g.c, full, j0, tok, g.W, g.S, s, dp);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) own = fmaf(s[i], dp[i], own);
+        } else {
+            st.tile(f, kt, kt + F::kTile, lane, g.c, full, j0, tok, g.W, g.S);
+        }
     };
-    wait_vmem();  // (the row's own loads and stores too: from here on only stage loads count)
-    for (int e = 0; e < t.nT; e += 3) {
-        stage(e, std::integral_constant<int, 0>{});
-        if (e + 1 < t.nT) stage(e + 1, std::integral_constant<int, 1>{});
-        if (e + 2 < t.nT) stage(e + 2, std::integral_constant<int, 2>{});
+    auto pass = [&](auto FIRST) __attribute__((always_inline)) {
+        wait_vmem();  // (the row's own loads and stores too: from here on only stage loads count)
+        for (int e = 0; e < t.nT; e += 3) {
+            stage(e, std::integral_constant<int, 0>{}, FIRST);
+            if (e + 1 < t.nT) stage(e + 1, std::integral_constant<int, 1>{}, FIRST);
+            if (e + 2 < t.nT) stage(e + 2, std::integral_constant<int, 2>{}, FIRST);
+        }
+    };
+    if constexpr (sizeof(T) == 2) {
+        if (t.nT > 0 && min(t.pmin + 1, min(g.W, kFewKeys) + min(g.S, kFewKeys)) < kFewKeys) {
+            pass(std::true_type{});
+            st.delta = col_sum<32>(own);
+            lds_barrier();  // (the last stages are read)
+            ld.issue(g, t, 0, wave, smem);
+            if (t.nT > 1) ld.issue(g, t, 1, wave, smem + kBuf);
+        }
     }
+    if (m < t.rows && h == 0) {
+        const int64_t at = t.b * g.lb + hq * g.lh + tok;
+        b.lse2[at] = st.lse2;
+        b.delta[at] = st.delta;
+    }
+#pragma unroll
+    for (int db = 0; db < F::kDB; ++db) st.dq[db] = f32x16{} * 0.f;
+    pass(std::false_type{});
 
     if (m >= t.rows) return;
     const bool some = tok < t.valid;

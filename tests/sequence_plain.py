@@ -13,9 +13,12 @@ Bounds.  A kernel works from the same (already rounded) inputs.  u is half a ste
   * out is a P-weighted mean, so each relative error of P moves it by at most that times
     (P |V|), once from the numerator and once from the sum, and it is rounded once more.
 
-Gradients start from the out and logsumexp that the forward stored, like the kernels:
-P = exp(s - lse), delta = dout . out.
-  * dout . v and delta are sums of D products in fp32: off by (D + 2) U of their absolute sums;
+Gradients start from the logsumexp that the forward stored, like the kernels: P = exp(s - lse).
+  * dout . v is a sum of D products in fp32: off by (D + 2) U of its absolute sum;
+  * delta is sum_j P_j dout . v_j.  A kernel sums that (off by P's relative error of each term
+    and by P times the error of dout . v), or takes dout . out of the stored out, a sum of D
+    products too: off by (D + 2) U of its absolute sum, and by dout . (out - sum_j P_j v_j),
+    which is known;
   * dA = P (dout . v - delta) is off by the relative errors of P (its score's, exp2's) and by P
     times those sums' errors, then rounded to the type (u, and 2^-25 absolute in fp16);
   * dq, dk and dv sum n such terms in fp32, at most n U of their absolute sum more, and are
@@ -100,9 +103,13 @@ def sink_grad(q, k, v, out, lse, dout, kernel_size, sinks, scale, lengths=None):
             p = torch.where(seen, torch.exp(s - lse[b, h, :n, None]), torch.zeros_like(s))
             e = (D + 4) * U * abs(scale) * (qq.abs() @ kk.abs().T) \
                 + 2 * U * (s.abs() + lse[b, h, :n, None].abs()) + 2.0 ** -21
-            da = p * (g @ vv.T - (g * o).sum(-1, keepdim=True))
-            e_da = (e + u_p) * da.abs() + tiny * seen + (1 + e) * p * (D + 2) * U * (
-                g.abs() @ vv.abs().T + (g * o).abs().sum(-1, keepdim=True))
+            dp, size = g @ vv.T, g.abs() @ vv.abs().T
+            da = p * (dp - (p * dp).sum(-1, keepdim=True))
+            e_delta = (p * (e * dp.abs() + (D + 2) * U * size)).sum(-1, keepdim=True) \
+                + (g * (o - p @ vv)).sum(-1, keepdim=True).abs() \
+                + (D + 2) * U * (g * o).abs().sum(-1, keepdim=True)
+            e_da = (e + u_p) * da.abs() + tiny * seen + (1 + e) * p * (
+                (D + 2) * U * size + e_delta)
             e_p = p * (e + u_p) + tiny * seen
             grads[0][b, h, :n] = scale * da @ kk
             tols[0][b, h, :n] = abs(scale) * (e_da + n * U * da.abs()) @ kk.abs()
