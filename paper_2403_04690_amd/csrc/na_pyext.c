@@ -15,6 +15,8 @@
  *
  *   call(fn, a0, a1, ..) -> status: any function whose arguments are all pointers
  *            or 64-bit integers (at most 16; the entry points of na_seq.h)
+ *   metas(t0, t1, ..) -> ((t0.shape, t0.stride(), t0.dtype, t0.device), ..), None for None:
+ *            what the binding's checks depend on, the keys of its cached plans
  *
  * Array arguments are the addresses of the problem's int64 / int32 arrays
  * (0 for a NULL causal array); the GIL is released for the call.
@@ -134,6 +136,41 @@ static PyObject* na_fast_call(PyObject* self, PyObject* const* args, Py_ssize_t 
     return PyLong_FromLong((long)st);
 }
 
+static PyObject* names[4]; /* "shape", "stride", "dtype", "device" */
+
+static PyObject* meta_of(PyObject* t) {
+    PyObject* m = PyTuple_New(4);
+    if (!m) return NULL;
+    for (Py_ssize_t i = 0; i < 4; ++i) {
+        PyObject* x = i == 1 ? PyObject_CallMethodNoArgs(t, names[i])
+                             : PyObject_GetAttr(t, names[i]);
+        if (!x) {
+            Py_DECREF(m);
+            return NULL;
+        }
+        PyTuple_SET_ITEM(m, i, x);
+    }
+    return m;
+}
+
+static PyObject* na_fast_metas(PyObject* self, PyObject* const* args, Py_ssize_t nargs) {
+    (void)self;
+    PyObject* all = PyTuple_New(nargs);
+    if (!all) return NULL;
+    for (Py_ssize_t i = 0; i < nargs; ++i) {
+        PyObject* m;
+        if (args[i] == Py_None) {
+            Py_INCREF(Py_None);
+            m = Py_None;
+        } else if (!(m = meta_of(args[i]))) {
+            Py_DECREF(all);
+            return NULL;
+        }
+        PyTuple_SET_ITEM(all, i, m);
+    }
+    return all;
+}
+
 static PyMethodDef methods[] = {
     {"forward", (PyCFunction)(void (*)(void))na_fast_forward, METH_FASTCALL,
      "na_forward through a function address; returns the status"},
@@ -141,6 +178,8 @@ static PyMethodDef methods[] = {
      "na_backward through a function address; returns the status"},
     {"call", (PyCFunction)(void (*)(void))na_fast_call, METH_FASTCALL,
      "a function of pointers and 64-bit integers through its address; returns the status"},
+    {"metas", (PyCFunction)(void (*)(void))na_fast_metas, METH_FASTCALL,
+     "shape, strides, type and device of each tensor (None: None)"},
     {NULL, NULL, 0, NULL},
 };
 
@@ -148,4 +187,10 @@ static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_na_fast",
                                     "Argument marshalling for libna.so's hot calls", -1, methods,
                                     NULL, NULL, NULL, NULL};
 
-PyMODINIT_FUNC PyInit__na_fast(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__na_fast(void) {
+    static const char* const text[4] = {"shape", "stride", "dtype", "device"};
+    for (int i = 0; i < 4; ++i) {
+        if (!names[i] && !(names[i] = PyUnicode_InternFromString(text[i]))) return NULL;
+    }
+    return PyModule_Create(&module);
+}

@@ -134,8 +134,8 @@ void fill_sink(const na_sink_problem& p, const int32_t* lengths, na::SeqGeo& g) 
 // fp32 parts.  Key tiles share the heads of a group among workgroups where they are fewer than
 // the CUs, or, where windows are so long that the first key tiles have many times the rows of
 // the last (1024 workgroups even that out: gradients of 16 heads on 4, 8192 tokens, full causal,
-// bf16 D = 128 in 1000 us, with 256 aimed at 1370).  The rows behind the windows of first tokens are cut into short chunks, no
-// more of them than fill the GPU four times over.
+// bf16 D = 128 in 1000 us, with 256 aimed at 1370).  The rows behind the windows of first
+// tokens are cut into short chunks, no more of them than fill the GPU four times over.
 // False: too large to launch.
 bool fill_backward(const na_sink_problem& p, const int32_t* lengths, na::SeqBwd& b, size_t& bytes) {
     std::memset(&b, 0, sizeof b);
@@ -227,9 +227,8 @@ bool cache_narrow(const na_cache_problem& p) {
 // form: two workgroups a CU) or, in the narrow form, unevenly loaded: the bound is the longest
 // request's length, so requests of mixed lengths fill about half of the splits.  A split has at
 // least 32 key tiles (8 in fp32, whose products take sixteen times as long), so that joining
-// costs less than it gains.  Decoding over 8k
-// to 32k contexts (32 requests, 4 key heads, fp16 D = 128) with 512, 1024, 2048 and 4096 splits
-// aimed at: 254, 224, 236, 252 us.
+// costs less than it gains.  Decoding over 8k to 32k contexts (32 requests, 4 key heads, fp16
+// D = 128) with 512, 1024, 2048 and 4096 splits aimed at: 254, 224, 236, 252 us.
 void fill_split(const na_cache_problem& p, bool narrow, na::SeqGeo& g) {
     const int64_t M = narrow ? 32 : 128;
     const int64_t rows = p.tokens * g.G;

@@ -113,8 +113,15 @@ def _call(name, device, *args):
 # Checks run once per combination of shapes, strides, types and devices (the functions below
 # that are cached take nothing else); addresses are checked by the library, on every call.
 
-def _meta(t):
-    return t.shape, t.stride(), t.dtype, t.device
+def _metas_plain(*tensors):
+    """What the checks of each tensor depend on (None: None)."""
+    return tuple(None if t is None else (t.shape, t.stride(), t.dtype, t.device) for t in tensors)
+
+
+try:
+    from ._na_fast import metas as _metas
+except ImportError:  # (also a build of it without this function)
+    _metas = _metas_plain
 
 
 def _contiguous(shape, stride):
@@ -155,6 +162,8 @@ def _ints(device, dtype, **metas):
 
 
 def _check_lse(lse, q):
+    if lse is None:
+        return
     if lse[2] != torch.float32 or lse[0] != q[0][:-1] or not _contiguous(lse[0], lse[1]):
         raise ValueError("lse must be a contiguous fp32 tensor of shape q.shape[:-1]")
     if lse[3] != q[3]:
@@ -184,23 +193,32 @@ def _count(value, name, least):
     return min(value, _WHOLE)
 
 
-def _like(t):
-    """An output of t's shape and axis order."""
-    out = torch.empty_like(t)
-    return out if out.stride(-1) == 1 or not out.numel() else torch.empty(
-        t.shape, dtype=t.dtype, device=t.device)
+def _layout(m):
+    """Shape and strides of an output of a tensor's shape and axis order (plain tuples, which
+    torch reads faster than its own sizes)."""
+    t = torch.empty_like(torch.empty_strided(m[0], m[1], dtype=m[2], device="meta"))
+    if t.stride(-1) != 1 and t.numel():
+        t = torch.empty(t.shape, device="meta")
+    return tuple(t.shape), t.stride()
 
 
-def _lse_for(q):
-    return torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
+def _filled(m, ref):
+    """The meta of an output: what the caller gave, or what is made for it."""
+    return (*_layout(ref), *ref[2:]) if m is None else m
+
+
+def _lse_shape(q):
+    return tuple(q[0][:-1])
 
 
 # ---------------------------------------------------------------- contiguous sequences
 
 @functools.lru_cache(maxsize=256)
-def _sink_plan(kernel_size, sinks, scale, lengths, lse, q, k, v, *more):
-    """The problem (kept alive by the cache's entry), its address, and the backward's workspace.
-    Everything but the first three is a _meta; more: out[, dout, dq, dk, dv]."""
+def _sink_plan(kernel_size, sinks, scale, metas):
+    """The problem (kept alive by the cache's entry), its address, the layouts of out or of dq,
+    dk and dv where the call makes them, and the logsumexp's shape or the backward's workspace.
+    metas: of lengths, lse, q, k, v, out[, dout, dq, dk, dv]."""
+    lengths, lse, q, k, v, *more = metas
     if len(q[0]) != 4 or len(k[0]) != 4 or k[0] != v[0]:
         raise ValueError("expected q [batch, heads, tokens, head_dim] and k, v of one shape")
     (B, H, N, D), kv_heads = q[0], k[0][1]
@@ -208,10 +226,12 @@ def _sink_plan(kernel_size, sinks, scale, lengths, lse, q, k, v, *more):
         raise ValueError("q, k and v must share batch, tokens and head_dim")
     if H != kv_heads and (kv_heads == 0 or H % kv_heads):
         raise ValueError("the heads of q must be a multiple of those of k and v")
-    for m, ref in zip(more, (q, q, q, k, v)):
+    _rows(q, k, v, *(m for m in more if m is not None))
+    like = (q, q, q, k, v)
+    more = [_filled(m, ref) for m, ref in zip(more, like)]
+    for m, ref in zip(more, like):
         if m[0] != ref[0]:
             raise ValueError("out, dout and the gradients must have the shapes of q, k and v")
-    _rows(q, k, v, *more)
     _check_lse(lse, q)
     if lengths is not None:
         _ints(q[3], torch.int32, lengths=lengths)
@@ -219,11 +239,13 @@ def _sink_plan(kernel_size, sinks, scale, lengths, lse, q, k, v, *more):
             raise ValueError("lengths needs one entry per sequence")
     p = _SinkProblem(B, H, kv_heads, N, D, _count(kernel_size, "kernel_size", 1),
                      _count(sinks, "sinks", 0))
-    for name, m in zip(("q", "k", "v", "out", "dout", "dq", "dk", "dv"), (q, k, v) + more):
+    for name, m in zip(("q", "k", "v", "out", "dout", "dq", "dk", "dv"), (q, k, v, *more)):
         setattr(p, name, _Strides(*m[1][:3]))
     p.dtype, p.scale = DTYPES[q[2]], 1.0 / math.sqrt(D) if scale is None else float(scale)
-    need = _library().na_sink_backward_workspace(p) if len(more) > 1 else 0
-    return p, ctypes.addressof(p), need
+    if len(more) == 1:
+        return p, ctypes.addressof(p), _layout(q), _lse_shape(q)
+    return (p, ctypes.addressof(p), tuple(_layout(m) for m in (q, k, v)),
+            _library().na_sink_backward_workspace(p))
 
 
 def sink_forward(q, k, v, kernel_size, sinks=0, scale=None, lengths=None, out=None, lse=None):
@@ -232,12 +254,11 @@ def sink_forward(q, k, v, kernel_size, sinks=0, scale=None, lengths=None, out=No
     sequence of a padded batch.  Returns (out, logsumexp); rows behind a length get 0 and
     -inf."""
     _library()
-    out = _like(q) if out is None else out
-    lse = _lse_for(q) if lse is None else lse
-    p = _sink_plan(*_window(kernel_size, sinks, scale),
-                   None if lengths is None else _meta(lengths), _meta(lse), _meta(q), _meta(k),
-                   _meta(v), _meta(out))
-    _call("na_sink_forward", q.device, p[1], q.data_ptr(), k.data_ptr(), v.data_ptr(),
+    p, at, layout, rows = _sink_plan(*_window(kernel_size, sinks, scale),
+                                     _metas(lengths, lse, q, k, v, out))
+    out = q.new_empty_strided(*layout) if out is None else out
+    lse = q.new_empty(rows, dtype=torch.float32) if lse is None else lse
+    _call("na_sink_forward", q.device, at, q.data_ptr(), k.data_ptr(), v.data_ptr(),
           0 if lengths is None else lengths.data_ptr(), out.data_ptr(), lse.data_ptr())
     return out, lse
 
@@ -247,13 +268,11 @@ def sink_backward(q, k, v, out, lse, dout, kernel_size, sinks=0, scale=None, len
     """Gradients of sink_forward's out with respect to q, k and v, from the out and lse that it
     returned.  Returns (dq, dk, dv), 0 behind a length; the same inputs give the same bits."""
     _library()
-    dq = _like(q) if dq is None else dq
-    dk = _like(k) if dk is None else dk
-    dv = _like(v) if dv is None else dv
-    p, at, need = _sink_plan(
-        *_window(kernel_size, sinks, scale), None if lengths is None else _meta(lengths),
-        _meta(lse), _meta(q), _meta(k), _meta(v), _meta(out), _meta(dout), _meta(dq), _meta(dk),
-        _meta(dv))
+    p, at, layouts, need = _sink_plan(*_window(kernel_size, sinks, scale),
+                                      _metas(lengths, lse, q, k, v, out, dout, dq, dk, dv))
+    dq = q.new_empty_strided(*layouts[0]) if dq is None else dq
+    dk = q.new_empty_strided(*layouts[1]) if dk is None else dk
+    dv = q.new_empty_strided(*layouts[2]) if dv is None else dv
     # (the allocator hands it out stream by stream, and to a captured graph from its own pool)
     work = torch.empty(need, dtype=torch.uint8, device=q.device)
     _call("na_sink_backward", q.device, at, q.data_ptr(), k.data_ptr(), v.data_ptr(),
@@ -297,9 +316,10 @@ def sink_attention(q, k, v, kernel_size, sinks=0, scale=None, lengths=None):
 # ---------------------------------------------------------------- the paged cache
 
 @functools.lru_cache(maxsize=256)
-def _tables_plan(tokens, page_size, context, new, table, free, head, outs):
-    """Arguments of na_cache_tables up to the arrays.  outs: metas of cu_new, slots, positions
-    and new_head."""
+def _tables_plan(tokens, page_size, metas):
+    """Arguments of na_cache_tables up to the arrays.  metas: of context_lens, new_lens,
+    page_table, free_pages, head, cu_new, slots, positions and new_head."""
+    context, new, table, free, head, *outs = metas
     if len(context[0]) != 1 or new[0] != context[0]:
         raise ValueError("context_lens and new_lens need one entry per request")
     if len(table[0]) != 2 or table[0][0] != context[0][0]:
@@ -335,20 +355,19 @@ def cache_tables(context_lens, new_lens, page_table, free_pages, page_size, toke
     new_head [1] int32); slots and positions behind the last token are -1, and so are the slots
     of tokens whose page the pool (new_head > len(free_pages)) or the table has no room for."""
     _library()
-    device = context_lens.device
-    outs = tuple(None if t is None else _meta(t) for t in (cu_new, slots, positions, new_head))
-    sizes = _tables_plan(index(tokens), index(page_size), _meta(context_lens), _meta(new_lens),
-                         _meta(page_table), _meta(free_pages),
-                         None if head is None else _meta(head), outs)
+    sizes = _tables_plan(index(tokens), index(page_size),
+                         _metas(context_lens, new_lens, page_table, free_pages, head, cu_new,
+                                slots, positions, new_head))
+    # (like context_lens: int32)
     if cu_new is None:
-        cu_new = torch.empty(sizes[0] + 1, dtype=torch.int32, device=device)
+        cu_new = context_lens.new_empty(sizes[0] + 1)
     if slots is None:
-        slots = torch.empty(sizes[1], dtype=torch.int64, device=device)
+        slots = context_lens.new_empty(sizes[1], dtype=torch.int64)
     if positions is None:
-        positions = torch.empty(sizes[1], dtype=torch.int32, device=device)
+        positions = context_lens.new_empty(sizes[1])
     if new_head is None:
-        new_head = torch.empty(1, dtype=torch.int32, device=device)
-    _call("na_cache_tables", device, *sizes, context_lens.data_ptr(), new_lens.data_ptr(),
+        new_head = context_lens.new_empty(1)
+    _call("na_cache_tables", context_lens.device, *sizes, context_lens.data_ptr(), new_lens.data_ptr(),
           free_pages.data_ptr(), 0 if head is None else head.data_ptr(), page_table.data_ptr(),
           cu_new.data_ptr(), slots.data_ptr(), positions.data_ptr(), new_head.data_ptr())
     return cu_new, slots, positions, new_head
@@ -366,8 +385,10 @@ def _token_strides(m):
 
 
 @functools.lru_cache(maxsize=256)
-def _write_plan(k, v, slots, k_pages, v_pages):
-    """The problem of na_cache_write (kept alive by the cache's entry) and its address."""
+def _write_plan(metas):
+    """The problem of na_cache_write (kept alive by the cache's entry) and its address.  metas:
+    of k, v, slots, k_pages and v_pages."""
+    k, v, slots, k_pages, v_pages = metas
     if len(k[0]) != 3 or k[0] != v[0]:
         raise ValueError("expected k and v [tokens, kv_heads, head_dim]")
     _check_pages(k_pages, v_pages)
@@ -388,16 +409,17 @@ def cache_write(k, v, slots, k_pages, v_pages):
     page_size, head_dim] at slots[t] (page * page_size + offset, int64); slots outside the
     pages (-1) are skipped.  The slots of one call must differ."""
     _library()
-    p = _write_plan(_meta(k), _meta(v), _meta(slots), _meta(k_pages), _meta(v_pages))
-    _call("na_cache_write", k.device, p[1], k.data_ptr(), v.data_ptr(), slots.data_ptr(),
+    p, at = _write_plan(_metas(k, v, slots, k_pages, v_pages))
+    _call("na_cache_write", k.device, at, k.data_ptr(), v.data_ptr(), slots.data_ptr(),
           k_pages.data_ptr(), v_pages.data_ptr())
 
 
 @functools.lru_cache(maxsize=256)
-def _attention_plan(kernel_size, sinks, scale, max_new, max_context, q, k_pages, v_pages, table,
-                    context, cu_new, out, lse):
-    """The problem of na_cache_attention (kept alive by the cache's entry), its address and its
-    workspace's size."""
+def _attention_plan(kernel_size, sinks, scale, max_new, max_context, metas):
+    """The problem of na_cache_attention (kept alive by the cache's entry), its address, its
+    workspace's size, and the layout of out and the logsumexp's shape where the call makes them.
+    metas: of q, k_pages, v_pages, page_table, context_lens, cu_new, out and lse."""
+    q, k_pages, v_pages, table, context, cu_new, out, lse = metas
     if len(q[0]) != 3:
         raise ValueError("expected q [tokens, heads, head_dim]")
     _check_pages(k_pages, v_pages)
@@ -410,9 +432,10 @@ def _attention_plan(kernel_size, sinks, scale, max_new, max_context, q, k_pages,
         raise ValueError("expected context_lens [requests] and page_table [requests, max_pages]")
     if cu_new[0] != (context[0][0] + 1,):
         raise ValueError("cu_new needs one entry more than there are requests")
-    if out[0] != q[0]:
+    if out is not None and out[0] != q[0]:
         raise ValueError("out must have the shape of q")
-    _rows(q, k_pages, v_pages, out)
+    _rows(q, k_pages, v_pages, *(() if out is None else (out,)))
+    out = _filled(out, q)
     _check_lse(lse, q)
     _ints(q[3], torch.int32, page_table=table, context_lens=context, cu_new=cu_new)
     p = _CacheProblem(
@@ -422,7 +445,8 @@ def _attention_plan(kernel_size, sinks, scale, max_new, max_context, q, k_pages,
         0 if max_context is None else _count(max_context, "max_context", 0))
     p.q, p.out = _token_strides(q), _token_strides(out)
     p.dtype, p.scale = DTYPES[q[2]], 1.0 / math.sqrt(D) if scale is None else float(scale)
-    return p, ctypes.addressof(p), _library().na_cache_attention_workspace(p)
+    return (p, ctypes.addressof(p), _library().na_cache_attention_workspace(p), _layout(q),
+            _lse_shape(q))
 
 
 def cache_attention(q, k_pages, v_pages, page_table, context_lens, cu_new, kernel_size=None,
@@ -434,11 +458,11 @@ def cache_attention(q, k_pages, v_pages, page_table, context_lens, cu_new, kerne
     choose how the work is split.  Returns (out, logsumexp [tokens, heads] fp32); rows from
     cu_new[requests] on are left as they were.  A page id outside the pages reads as zeros."""
     _library()
-    out = _like(q) if out is None else out
-    lse = _lse_for(q) if lse is None else lse
-    p, at, need = _attention_plan(
-        *_window(kernel_size, sinks, scale), *_bounds(max_new, max_context), _meta(q),
-        _meta(k_pages), _meta(v_pages), _meta(page_table), _meta(context_lens), _meta(cu_new), _meta(out), _meta(lse))
+    p, at, need, layout, rows = _attention_plan(
+        *_window(kernel_size, sinks, scale), *_bounds(max_new, max_context),
+        _metas(q, k_pages, v_pages, page_table, context_lens, cu_new, out, lse))
+    out = q.new_empty_strided(*layout) if out is None else out
+    lse = q.new_empty(rows, dtype=torch.float32) if lse is None else lse
     # (the allocator hands it out stream by stream, and to a captured graph from its own pool)
     work = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     _call("na_cache_attention", q.device, at, q.data_ptr(), k_pages.data_ptr(),
@@ -448,30 +472,32 @@ def cache_attention(q, k_pages, v_pages, page_table, context_lens, cu_new, kerne
 
 
 @functools.lru_cache(maxsize=256)
-def _step_plan(kernel_size, sinks, scale, max_new, max_context, data, out, lse, new, free, head,
-               tables):
+def _step_plan(kernel_size, sinks, scale, max_new, max_context, metas):
     """The problem of both the write and the attention of a step (kept alive by the cache's
-    entry), its address, its workspace's size, and the arguments of na_cache_tables; the checks
-    are those of the three functions."""
-    q, k, v, k_pages, v_pages, page_table, context = data
+    entry), its address, its workspace's size, the layout of out and the logsumexp's shape, and
+    the arguments of na_cache_tables; the checks are those of the three functions.  metas: of
+    q, k, v, k_pages, v_pages, page_table, context_lens, then of new_lens, free_pages and head,
+    or of the cu_new and slots that the caller has."""
+    q, k, v, k_pages, v_pages, page_table, context, *more = metas
     if len(q[0]) != 3 or len(k[0]) != 3 or q[0][0] != k[0][0]:
         raise ValueError("q, k and v need the same new tokens")
     T, device = q[0][0], q[3]
     sizes, requests = None, context[0][0] if len(context[0]) == 1 else 0
     _check_pages(k_pages, v_pages)
-    if tables is None:
-        sizes = _tables_plan.__wrapped__(T, k_pages[0][2], context, new, page_table, free, head,
-                                         (None,) * 4)
+    if len(more) == 3:
+        new, free, head = more
+        sizes = _tables_plan.__wrapped__(T, k_pages[0][2], (context, new, page_table, free, head)
+                                         + (None,) * 4)
         ints = lambda n, dtype: (torch.Size((n,)), (1,), dtype, device)  # noqa: E731
-        tables = ints(requests + 1, torch.int32), ints(T, torch.int64)
-    cu_new, slots = tables
-    _write_plan.__wrapped__(k, v, slots, k_pages, v_pages)
-    p, at, need = _attention_plan.__wrapped__(kernel_size, sinks, scale, max_new, max_context, q,
-                                              k_pages, v_pages, page_table, context, cu_new, out,
-                                              lse)
+        more = ints(requests + 1, torch.int32), ints(T, torch.int64)
+    cu_new, slots = more
+    _write_plan.__wrapped__((k, v, slots, k_pages, v_pages))
+    p, at, need, layout, rows = _attention_plan.__wrapped__(
+        kernel_size, sinks, scale, max_new, max_context,
+        (q, k_pages, v_pages, page_table, context, cu_new, None, None))
     _rows(q, k)
     p.k, p.v = _token_strides(k), _token_strides(v)
-    return p, at, need, sizes
+    return p, at, need, layout, rows, sizes
 
 
 def cache_step(q, k, v, k_pages, v_pages, page_table, context_lens, new_lens, free_pages,
@@ -484,34 +510,31 @@ def cache_step(q, k, v, k_pages, v_pages, page_table, context_lens, new_lens, fr
     Returns (out, logsumexp, new_head)."""
     _library()
     device = q.device
-    out, lse = _like(q), _lse_for(q)
-    metas = (_meta(q), _meta(k), _meta(v), _meta(k_pages), _meta(v_pages), _meta(page_table),
-             _meta(context_lens))
-    rule = *_window(kernel_size, sinks, scale), *_bounds(max_new, max_context)
     if tables is None:
-        plan = _step_plan(*rule, metas, _meta(out),
-                          _meta(lse), _meta(new_lens), _meta(free_pages),
-                          None if head is None else _meta(head), None)
-        # slots, positions and cu_new live in one buffer (only the new head is handed out)
-        sizes = plan[3]
-        tokens = sizes[1]
-        ints = torch.empty(3 * tokens + sizes[0] + 1, dtype=torch.int32, device=device)
-        new_head = torch.empty(1, dtype=torch.int32, device=device)
-        slots = ints.data_ptr()
-        positions, cu_new = slots + 8 * tokens, slots + 12 * tokens
+        metas = _metas(q, k, v, k_pages, v_pages, page_table, context_lens, new_lens, free_pages,
+                       head)
     else:
         cu_new, slots, _, new_head = tables
-        plan = _step_plan(*rule, metas, _meta(out), _meta(lse), None, None, None,
-                          (_meta(cu_new), _meta(slots)))
-        cu_new, slots = cu_new.data_ptr(), slots.data_ptr()
-    p, at, need, sizes = plan
+        metas = _metas(q, k, v, k_pages, v_pages, page_table, context_lens, cu_new, slots)
+    p, at, need, layout, rows, sizes = _step_plan(
+        *_window(kernel_size, sinks, scale), *_bounds(max_new, max_context), metas)
+    out = q.new_empty_strided(*layout)
+    lse = q.new_empty(rows, dtype=torch.float32)
     work = torch.empty(need, dtype=torch.uint8, device=device) if need else None
     context, table = context_lens.data_ptr(), page_table.data_ptr()
     kp, vp = k_pages.data_ptr(), v_pages.data_ptr()
     if tables is None:
+        # slots, positions and cu_new live in one buffer (only the new head is handed out)
+        tokens = sizes[1]
+        ints = context_lens.new_empty(3 * tokens + sizes[0] + 1)
+        new_head = context_lens.new_empty(1)
+        slots = ints.data_ptr()
+        positions, cu_new = slots + 8 * tokens, slots + 12 * tokens
         _call("na_cache_tables", device, *sizes, context, new_lens.data_ptr(),
               free_pages.data_ptr(), 0 if head is None else head.data_ptr(), table, cu_new, slots,
               positions, new_head.data_ptr())
+    else:
+        cu_new, slots = cu_new.data_ptr(), slots.data_ptr()
     _call("na_cache_write", device, at, k.data_ptr(), v.data_ptr(), slots, kp, vp)
     _call("na_cache_attention", device, at, q.data_ptr(), kp, vp, table, context, cu_new,
           out.data_ptr(), lse.data_ptr(), work.data_ptr() if need else 0, need)
