@@ -225,10 +225,16 @@ bool cache_narrow(const na_cache_problem& p) {
 
 // Splits the keys of a row tile when the row tiles alone would leave the 256 CUs idle (the wide
 // form: two workgroups a CU) or, in the narrow form, unevenly loaded: the bound is the longest
-// request's length, so requests of mixed lengths fill about half of the splits.  A split has at
-// least 32 key tiles (8 in fp32, whose products take sixteen times as long), so that joining
-// costs less than it gains.  Decoding over 8k to 32k contexts (32 requests, 4 key heads, fp16
-// D = 128) with 512, 1024, 2048 and 4096 splits aimed at: 254, 224, 236, 252 us.
+// request's length, so requests of mixed lengths fill about half of the splits.
+//   A split costs a second launch (4 us) that joins, so 16-bit types have at least 8 key tiles a
+// split and split no fewer than 24 (narrow, whose four waves share a split's tiles: 12 and 40);
+// the products of fp32 take sixteen times as long, and 2 (8) tiles are enough.  bf16, 16 heads
+// on 4, D = 128, 64 new tokens over 8000: 37 us with 32 tiles a split at least, 27 with 16, 21
+// with 8, 24 with 4; one new token for each of 8 requests of 3000: 19 with 32, 15 with 12, 17
+// with 8.  fp32, 6 heads on 1, D = 64, 100 tokens of 5 requests, window 255: 32, 22 and 18 us
+// with 8, 4 and 2.
+//   Decoding over 8k to 32k contexts (32 requests, 4 key heads, fp16 D = 128) with 512, 1024,
+// 2048 and 4096 splits aimed at: 254, 224, 236, 252 us.
 void fill_split(const na_cache_problem& p, bool narrow, na::SeqGeo& g) {
     const int64_t M = narrow ? 32 : 128;
     const int64_t rows = p.tokens * g.G;
@@ -243,9 +249,12 @@ void fill_split(const na_cache_problem& p, bool narrow, na::SeqGeo& g) {
     // (the joining launch has four workgroups a row tile)
     split = std::min(split, std::max<int64_t>(1, (kMaxGrid - 1) / (4 * (int64_t)g.ntiles * g.Hkv)));
     if (4 * (int64_t)g.ntiles * g.Hkv >= kMaxGrid) split = 1;
-    const int64_t least = p.dtype == NA_FP32 ? 8 : 32;
+    const bool half = p.dtype != NA_FP32;
+    const int64_t least = half ? (narrow ? 12 : 8) : (narrow ? 8 : 2);
+    if (half && tiles < (narrow ? 40 : 24)) split = 1;
+    const int64_t step = narrow ? 4 : 2;
     int64_t chunk = split == 1 ? tiles : std::max<int64_t>(least, (tiles + split - 1) / split);
-    chunk = (chunk + 3) / 4 * 4;
+    chunk = (chunk + step - 1) / step * step;
     g.chunk = (int)chunk;
     g.nsplit = (int)((tiles + chunk - 1) / chunk);
     g.fd_tiles.init(g.ntiles * g.Hkv);
