@@ -1,6 +1,7 @@
 /*
  * na.h -- C ABI of the fused neighborhood-attention (NA) library for MI355X
- * (gfx950).  Shared object: paper_2403_04690_amd/libna.so.
+ * (gfx950).  Shared object: paper_2403_04690_amd/libna.so.  (Its sequence operators, attention
+ * of a causal window and the first tokens and a paged cache, are declared in na_seq.h.)
  *
  * Operation (Faster Neighborhood Attention, arXiv 2403.04690):
  *   Each query token of a rank-r token space (r = 1, 2, 3) attends to its

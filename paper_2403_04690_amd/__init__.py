@@ -11,6 +11,9 @@ each query attends to its k_a nearest same-group tokens along every axis a
 dilation d_a splitting each axis into d_a interleaved sub-lattices.  Axes can
 be causal (``causal``, one flag per axis): there a query attends only to the
 k nearest positions not after it.
+
+The sequence operators (causal window attention with first tokens that stay visible, its
+gradient, and a paged cache; ``include/na_seq.h``) are in ``sequence.py``.
 """
 import ctypes
 import functools

@@ -13,6 +13,8 @@ from tests import test_sanitizers as san
 
 @pytest.fixture(scope="module")
 def driver(tmp_path_factory):
+    if "libclang_rt.asan" in os.environ.get("LD_PRELOAD", ""):
+        pytest.skip("the whole suite runs under a sanitizer already; a second runtime cannot load")
     hipcc = shutil.which("hipcc")
     if not (hipcc and os.path.exists(san.CLANGXX)):
         pytest.skip("ROCm clang and hipcc are needed for the sanitizer builds")
