@@ -289,6 +289,15 @@ def _readable(t):
     return t.contiguous()
 
 
+def _gradients(ctx, dout):
+    q, k, v, out, lse, lengths = ctx.saved_tensors
+    return sink_backward(q, k, v, out, lse, _readable(dout), *ctx.cfg, lengths) + (None,) * 4
+
+
+# (with create_graph: a second derivative raises; the wrapper costs 10 us that others need not pay)
+_gradients_once = torch.autograd.function.once_differentiable(_gradients)
+
+
 class _SinkFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, kernel_size, sinks, scale, lengths):
@@ -298,11 +307,8 @@ class _SinkFunction(torch.autograd.Function):
         return out
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, dout):
-        q, k, v, out, lse, lengths = ctx.saved_tensors
-        grads = sink_backward(q, k, v, out, lse, _readable(dout), *ctx.cfg, lengths)
-        return grads + (None,) * 4
+        return (_gradients_once if torch.is_grad_enabled() else _gradients)(ctx, dout)
 
 
 def sink_attention(q, k, v, kernel_size, sinks=0, scale=None, lengths=None):
