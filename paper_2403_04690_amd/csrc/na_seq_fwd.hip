@@ -248,10 +248,6 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 4) : 1)) voi
         if ((e += SK) >= e1) break;
         if constexpr (NB > 2) {
             stage(e, std::integral_constant<int, 2>{});
-            if ((e += SK) >= e1) break;
-        }
-        if constexpr (NB > 3) {
-            stage(e, std::integral_constant<int, 3>{});
             e += SK;
         }
     }
