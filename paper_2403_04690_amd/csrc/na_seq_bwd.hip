@@ -17,13 +17,58 @@
 //           rows into workgroups of their own, in the same launch, behind the others
 //   join    sums the fp32 parts that split heads and first tokens leave
 // P and dA are rounded once to the tensors' type for their matrix products (16-bit types);
-// everything else is fp32.
+// everything else is fp32.  fp16 has too few exponents for both as they are: over thousands of
+// keys P falls below its normal range, and dA goes with the size of dout, which small or large
+// loss scales take below it or above its largest number.  So in fp16
+//   P  enters dv times 2^15 (P <= 1), which the logsumexp that the dq launch leaves contains
+//   dA is scaled by a power of two of its own per row (dq) or key (dk), a column of the products
+//      and so a lane: lowered, with the accumulators, when a tile brings a value above 2^15, to
+//      where the largest is at 2^11 to 2^12 (DaScale)
+// and both are undone, exactly, in the fp32 sums.  Without, dv over 128k keys was off by twice what
+// its roundings are, and dq with output gradients of 2^-14 by seven times; it costs 5 to 6 % of
+// the gradient (16 heads on 4, 8192 tokens, D = 128: window 512 198 us without and 204 with, full
+// causal 5.4 and 10.7 % above bf16; short sequences 31 and 33 us).
 #include <type_traits>
 
 #include "na_launch.h"
 #include "na_seq_kernels.h"
 
 namespace na {
+
+// fp16 only; the other types have fp32's exponents.
+template <typename T>
+constexpr bool kHalf = std::is_same<T, _Float16>::value;
+constexpr float kPExp = 15.f;  // base-2 exponent that P has in the dk, dv launch
+
+// The power of two that a lane's dA is scaled by.  It starts so high that whatever is not lost in
+// fp16's gradients anyway is in fp16's normal range (dout, v and P of 2^-24: 2^-72 in all), and
+// the largest (dout, v of 2^16, D = 128, P of 2^kPExp: 2^56) still far from fp32's end.
+struct DaScale {
+    static constexpr float kStart = 0x1p+58f, kMost = 0x1p+15f;
+    float by;
+    __device__ __forceinline__ void init() { by = kStart; }
+    // exactly 1 / by
+    __device__ __forceinline__ float undo() const {
+        return __int_as_float((254 << 23) - __float_as_int(by));
+    }
+    // x: the scaled values of a tile, two lanes a column; acc: what they are added to.  Returns
+    // what `by` was multiplied with.
+    template <int N>
+    __device__ __forceinline__ float fit(float (&x)[16], f32x16 (&acc)[N]) {
+        float top = fabsf(x[0]);
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
+        if (!__builtin_amdgcn_ballot_w64(top > kMost)) return 1.f;
+        top = col_max<32>(top);
+        const float f = top > kMost ? ldexpf(1.f, 12 - __builtin_amdgcn_frexp_expf(top)) : 1.f;
+        by *= f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] *= f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) acc[n] *= f;
+        return f;
+    }
+};
 
 // ---- dq: 32 rows a wave ----
 template <typename T, int D>
@@ -33,6 +78,8 @@ struct DqState {
     x8 qf[F::kKS], gf[F::kKS];
     f32x16 dq[F::kDB];
     float lse2, delta;
+    DaScale scale;  // (fp16) and delta under it
+    float sdelta;
 
     // P and dout . v of a tile of keys; full, j0, pos: as in the forward.
     __device__ __forceinline__ void weights(const F& f, const unsigned char* kt,
@@ -66,8 +113,18 @@ struct DqState {
         f.cols(kt, 0, lane, kc[0]);
         if constexpr (sizeof(T) == 2) f.cols(kt, 1, lane, kc[1]);
         x8 pf[2];
+        float x[16];
+        if constexpr (kHalf<T>) {
+            // (scaling by a power of two and the difference: one rounding, in one instruction)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) pf[i >> 3][i & 7] = Tr<T>::cvt(s[i] * (dp[i] - delta));
+            for (int i = 0; i < 16; ++i) x[i] = s[i] * fmaf(dp[i], scale.by, -sdelta);
+            sdelta *= scale.fit(x, dq);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = s[i] * (dp[i] - delta);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) pf[i >> 3][i & 7] = Tr<T>::cvt(x[i]);
 #pragma unroll
         for (int db = 0; db < F::kDB; ++db) dq[db] = mma32<T>(kc[0][db], pf[0], dq[db]);
         if constexpr (sizeof(T) == 4) f.cols(kt, 1, lane, kc[1]);
@@ -190,8 +247,13 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 ? 1 : D == 128 ? 2 : 3)) void 
     }
     if (m < t.rows && h == 0) {
         const int64_t at = t.b * g.lb + hq * g.lh + tok;
-        b.lse2[at] = st.lse2;
+        b.lse2[at] = kHalf<T> ? st.lse2 - kPExp : st.lse2;
         b.delta[at] = st.delta;
+    }
+    float scale = b.scale;
+    if constexpr (kHalf<T>) {
+        st.scale.init();
+        st.sdelta = st.delta * st.scale.by;
     }
 #pragma unroll
     for (int db = 0; db < F::kDB; ++db) st.dq[db] = f32x16{} * 0.f;
@@ -199,6 +261,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 ? 1 : D == 128 ? 2 : 3)) void 
 
     if (m >= t.rows) return;
     const bool some = tok < t.valid;
+    if constexpr (kHalf<T>) scale *= st.scale.undo();
     T* dp = reinterpret_cast<T*>(reinterpret_cast<unsigned char*>(dqg) + t.b * b.qb + hq * b.qh +
                                  (int64_t)tok * b.qt);
 #pragma unroll
@@ -207,7 +270,7 @@ __global__ __launch_bounds__(256, (sizeof(T) == 4 ? 1 : D == 128 ? 2 : 3)) void 
         for (int i = 0; i < 4; ++i) {
             f32x4 x;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = some ? st.dq[db][4 * i + r] * b.scale : 0.f;
+            for (int r = 0; r < 4; ++r) x[r] = some ? st.dq[db][4 * i + r] * scale : 0.f;
             st_x4<T>(dp + db * 32 + i * 8 + h * 4, x);
         }
 }
@@ -247,6 +310,7 @@ struct KvState {
     static constexpr bool kKf = !LDS, kVf = (OUT & kDk) && !LDS;
     x8 kf[kKf ? F::kKS : 1], vf[kVf ? F::kKS : 1];
     f32x16 dk[OUT & kDk ? F::kDB : 1], dv[OUT & kDv ? F::kDB : 1];
+    DaScale scale;  // (fp16)
 
     // Keys of this wave: lane l has key l % 32.
     __device__ __forceinline__ void init(const unsigned char* kp, const unsigned char* vp, int h) {
@@ -259,6 +323,20 @@ struct KvState {
         for (int db = 0; db < F::kDB; ++db) {
             if constexpr (OUT & kDk) dk[db] = f32x16{} * 0.f;
             if constexpr (OUT & kDv) dv[db] = f32x16{} * 0.f;
+        }
+        if constexpr (kHalf<T>) scale.init();
+    }
+    // The sums without the powers of two of P and dA; before they meet other waves'.
+    __device__ __forceinline__ void finish() {
+        if constexpr (kHalf<T>) {
+            constexpr float p = 1.f / (1 << 15);
+            static_assert(kPExp == 15.f, "p is its inverse");
+            const float a = scale.undo() * p;
+#pragma unroll
+            for (int db = 0; db < F::kDB; ++db) {
+                if constexpr (OUT & kDk) dk[db] *= a;
+                if constexpr (OUT & kDv) dv[db] *= p;
+            }
         }
     }
     __device__ __forceinline__ void settle_keys() {
@@ -313,15 +391,20 @@ struct KvState {
                     dv[db] = mma32<T>(F::col_at(gt, co, db, bi, lane), pf[bi], dv[db]);
         }
         if constexpr (OUT & kDk) {
+            float x[16];
 #pragma unroll
             for (int i4 = 0; i4 < 4; ++i4) {
                 const f32x4 delta = *reinterpret_cast<const f32x4*>(stat + 32 + 8 * i4);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int i = 4 * i4 + r;
-                    df[i >> 3][i & 7] = Tr<T>::cvt(s[i] * (dp[i] - delta[r]));
+                    x[i] = s[i] * (dp[i] - delta[r]);
+                    if constexpr (kHalf<T>) x[i] *= scale.by;
                 }
             }
+            if constexpr (kHalf<T>) scale.fit(x, dk);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) df[i >> 3][i & 7] = Tr<T>::cvt(x[i]);
 #pragma unroll
             for (int bi = 0; bi < 2; ++bi)
 #pragma unroll
@@ -516,6 +599,7 @@ seq_dkv_kernel(SeqBwd b, const T* __restrict__ qg, const T* __restrict__ kg,
             st.tile(f, buf, own, lane, g.c, full, i0 + 4 * h - key - g.W, len);
             wait_lds();
         }
+        st.finish();
 #pragma unroll
         for (int half = C::kFirst / 2; half >= 1; half /= 2) st.add_waves(smem, wave, half, lane);
         if (wave == 0) {
@@ -589,6 +673,7 @@ seq_dkv_kernel(SeqBwd b, const T* __restrict__ qg, const T* __restrict__ kg,
         }
         if (e + kStep < all) stage_barrier();
     }
+    st.finish();
     if constexpr (RS == 2) {
         st.add_waves(smem, wave, 4, lane);
         if (wave >= 4) return;

@@ -1,0 +1,149 @@
+"""Calls of the sequence operators that the header allows at its edges: axes of one entry, offsets
+that lie outside the new tokens.  (Bounds: tests/sequence_plain.py.)"""
+import pytest
+import torch
+
+from tests import sequence_plain as plain
+
+pytestmark = pytest.mark.gpu
+
+DT = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def na():
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible")
+    import paper_2403_04690_amd as lib
+
+    lib.load_library()
+    return lib
+
+
+def _randn(shape, dtype, seed):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(DT[dtype]).cuda()
+
+
+def _odd(t, *axes):
+    """t, its axes (of one entry) with a stride that no axis of more could have."""
+    strides = list(t.stride())
+    for i, x in enumerate(axes):
+        assert t.shape[x] == 1
+        strides[x] = (3, (1 << 26) + 5, 7)[i]
+    return t.as_strided(t.shape, strides)
+
+
+# ---------------------------------------------------------------- axes of one entry
+
+@pytest.mark.parametrize("dtype", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("B,H,Hkv,N,axes,kv_axes", [
+    (1, 4, 2, 70, (0,), (0,)), (2, 1, 1, 70, (1,), (1,)), (2, 4, 1, 70, (), (1,)),
+    (2, 4, 2, 1, (2,), (2,)), (1, 1, 1, 1, (0, 2, 1), (1, 2, 0)),
+])
+def test_strides_of_axes_of_one_entry_do_not_matter(na, B, H, Hkv, N, axes, kv_axes, dtype):
+    q, k, v, g = (_randn((B, h, N, 64), dtype, i) for i, h in enumerate((H, Hkv, Hkv, H)))
+    want = na.sink_forward(q, k, v, 30, 4)
+    want += na.sink_backward(q, k, v, *want, g, 30, 4)
+    q, g = _odd(q, *axes), _odd(g, *axes)
+    k, v = _odd(k, *kv_axes), _odd(v, *kv_axes)
+    room = [torch.full(t.shape, 7.0, dtype=DT[dtype], device="cuda") for t in (q, q, k, v)]
+    out, dq = (_odd(t, *axes) for t in room[:2])
+    dk, dv = (_odd(t, *kv_axes) for t in room[2:])
+    for own in ({}, {"out": out}):
+        got = na.sink_forward(q, k, v, 30, 4, **own)
+        for into in ({}, {"dq": dq, "dk": dk, "dv": dv}):
+            for a, b in zip(got + na.sink_backward(q, k, v, *got, g, 30, 4, **into), want):
+                assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("T,H,Hkv,axes,kv_axes", [
+    (1, 4, 2, (0,), (0,)), (5, 1, 1, (1,), (1,)), (5, 4, 1, (), (1,)), (1, 1, 1, (1, 0), (0, 1)),
+])
+def test_cache_strides_of_axes_of_one_entry_do_not_matter(na, T, H, Hkv, axes, kv_axes, dtype):
+    q, k, v = (_randn((T, h, 64), dtype, i) for i, h in enumerate((H, Hkv, Hkv)))
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+
+    def serve(q, k, v, **own):
+        pages = [torch.zeros(4, Hkv, 16, 64, dtype=DT[dtype], device="cuda") for _ in range(2)]
+        table = ints(2, -1, -1)[None]
+        out, lse, head = na.cache_step(q, k, v, *pages, table, ints(13), ints(T), ints(3, 0, 1))
+        res = [out, lse, head, table] + pages
+        if own:
+            res += na.cache_attention(q, *pages, table, ints(13), ints(0, T), **own)
+        return res
+
+    want = serve(q, k, v)
+    out = _odd(torch.full_like(q, 7.0), *axes)
+    got = serve(_odd(q, *axes), _odd(k, *kv_axes), _odd(v, *kv_axes), out=out)
+    for a, b in zip(got, want + want[:2]):
+        assert torch.equal(a, b)
+    # a request's last token, far away from the one before it
+    far = torch.zeros((1 << 25) + H * 64, dtype=DT[dtype], device="cuda")
+    last = far.as_strided((2, H, 64), (1 << 25, 64, 1))[1:]
+    last.copy_(q[-1:])
+    pages = [t.clone() for t in want[4:6]]
+    a, b = (na.cache_attention(x, *pages, want[3], ints(12 + T), ints(0, 1)) for x in (last, q[-1:]))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+# ---------------------------------------------------------------- offsets
+
+def _offsets(na, cu, T, H, Hkv, context, **hints):
+    """Rows that a valid request owns hold its attention where the offsets increase; every other
+    row, and the memory around the outputs, stays as it was."""
+    D, page, R = 32, 16, len(cu) - 1
+    q = _randn((T, H, D), "fp32", 1)
+    kp, vp = (_randn((9, Hkv, page, D), "fp32", 2 + i) for i in range(2))
+    table = torch.randint(0, 9, (R, 3), generator=torch.Generator().manual_seed(5)).int()
+    margin = 200
+    room = torch.full(((T + 2 * margin), H, D), 7.0, device="cuda")
+    lroom = torch.full(((T + 2 * margin), H), 7.0, device="cuda")
+    out, lse = room[margin:margin + T], lroom[margin:margin + T]
+    na.cache_attention(q, kp, vp, table.cuda(), torch.tensor(context, dtype=torch.int32).cuda(),
+                       torch.tensor(cu, dtype=torch.int64).int().cuda(), out=out, lse=lse, **hints)
+    torch.cuda.synchronize()
+    owned = torch.zeros(T, dtype=torch.bool)
+    ordered = all(a <= b for a, b in zip(cu, cu[1:]))
+    for r in range(R):
+        a, b = cu[r], cu[r + 1]
+        if not 0 <= a < b <= T:
+            continue
+        owned[a:b] = True
+        if ordered:
+            c = min(max(context[r], 0), 3 * page)
+            want = plain.cache(q[a:b], kp, vp, [table[r].tolist()], [c], [b - a], 2 ** 31 - 1, 0,
+                               D ** -0.5)
+            plain.close(out[a:b], want[0], want[2], f"out of request {r}")
+            plain.close(lse[a:b], want[1], want[3], f"lse of request {r}")
+    keep = torch.ones(T + 2 * margin, dtype=torch.bool)
+    keep[margin:margin + T] = ~owned
+    assert bool((room.cpu()[keep] == 7).all()) and bool((lroom.cpu()[keep] == 7).all())
+
+
+BAD = [
+    [0, 2, 1, 6], [-5, 0, 2, 2], [0, 100, 200, 300], [2 ** 31 - 1, -2 ** 31, 0, 6],
+    [-2 ** 31, -2 ** 31, 3, 5], [2, 4, 2 ** 31 - 1, 2 ** 31 - 1],
+]
+
+
+@pytest.mark.parametrize("cu", BAD)
+@pytest.mark.parametrize("T,H,Hkv", [(6, 4, 2), (40, 4, 2), (6, 4, 1)])
+def test_requests_outside_the_new_tokens_have_no_rows(na, cu, T, H, Hkv):
+    for context in ([0, 5, 31], [-9, 2 ** 31 - 1, -2 ** 31]):
+        for hints in ({}, {"max_new": 1}):
+            _offsets(na, cu, T, H, Hkv, context, **hints)
+
+
+def test_requests_beyond_the_room_do_not_hide_the_others(na):
+    """More new tokens than there is room for (as cache_tables counts them, up to 2^31 - 1): the
+    requests that fit have their rows."""
+    far = 2 ** 30
+    for cu in ([0, 500, 600, far, far + 1, 2 ** 31 - 1], [0, 599, 600, 2 ** 30 + 2 ** 29, 2 ** 31 - 1],
+               [0, 590, 600, far - 1, far, far + 1, 2 ** 31 - 1, 2 ** 31 - 1]):
+        for hints in ({}, {"max_new": 1}):
+            _offsets(na, cu, 600, 4, 1, [5] * (len(cu) - 1), **hints)
+    # more requests than the wide form sorts
+    cu = list(range(0, 400, 5)) + [far + 7 * i for i in range(9)]
+    for hints in ({}, {"max_new": 1}):
+        _offsets(na, cu, 400, 4, 1, [3] * (len(cu) - 1), **hints)
