@@ -25,6 +25,14 @@ namespace na {
 
 constexpr float kSeqLazy = 8.f;  // base-2 headroom before the running maximum is raised
 
+// How far (base 2) below a row's maximum the reference of its scores is put when it is raised.  In
+// fp16 the weights then reach up to 2^15, and are in the normal range down to 2^-21 of the largest
+// instead of 2^-14: beside a first token that takes most of the weight, thousands of keys have less
+// than that, and may be all of the output.  (A first token of score 12 above 65k others, its value
+// 0: off by twice the bound of the roundings with 0 here.)
+template <typename T>
+constexpr float kSeqBelow = std::is_same<T, _Float16>::value ? 7.f : 0.f;
+
 // Running state of 32 rows: lane l holds row l % 32, and of the keys those of its half.
 template <typename T, int D>
 struct SeqState {
@@ -90,10 +98,10 @@ struct SeqState {
         if (__builtin_amdgcn_ballot_w64(top > thr)) {
             const float ymax = col_max<32>(top);
             const bool raise = ymax > thr;
-            const float up = raise ? ymax : 0.f;
+            const float up = raise ? ymax - kSeqBelow<T> : 0.f;
             const float alpha = thr == -INFINITY ? 0.f : fast_exp2(-up);
             mref = raise ? up - negm : mref;
-            thr = mref != -INFINITY ? kSeqLazy : -INFINITY;
+            thr = mref != -INFINITY ? kSeqLazy + kSeqBelow<T> : -INFINITY;
             l *= alpha;
 #pragma unroll
             for (int db = 0; db < F::kDB; ++db) o[db] *= alpha;

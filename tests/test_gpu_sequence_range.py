@@ -153,3 +153,41 @@ def test_gradients_over_a_long_context(na):
         # (values are stored in fp16: 2^-25 at most below its normal range)
         bound += 2.0 ** -25 / math.sqrt(3)
         assert _rms(got.double() - want) < bound, (name, _rms(got.double() - want) / bound)
+
+
+@pytest.mark.parametrize("form", ["sequence", "cache"])
+def test_forward_beside_a_key_that_takes_most_of_the_weight(na, form):
+    """A first token with score 12 above the others and little in its value (as sinks come out of
+    training): the others' weights are e^-12 of it, and are what the output is made of.  Errors
+    as above: P and out are rounded once."""
+    N, D = 2 ** 16 - 5, 64
+    gen = torch.Generator().manual_seed(6)
+    q, k, v = (torch.randn(1, 1, N, D, generator=gen) for _ in range(3))
+    q[..., 0] = 8.0
+    k[..., 0] = 0.0
+    k[0, 0, 0] = 0.0
+    k[0, 0, 0, 0] = 12.0                     # 8 * 12 / sqrt(64)
+    v[0, 0, 0] = 0.0
+    q, k, v = (t.half().cuda() for t in (q, k, v))
+    rows = torch.arange(N - 64, N, device="cuda")
+    if form == "sequence":
+        out = na.sink_forward(q, k, v, N)[0][0, 0, rows]
+    else:
+        pages = -(-N // 16)
+        kp, vp = (torch.nn.functional.pad(t[0, 0], (0, 0, 0, 16 * pages - N)).reshape(pages, 1, 16, D)
+                  for t in (k, v))
+        table = torch.arange(pages, dtype=torch.int32, device="cuda")[None]
+        ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+        out = na.cache_attention(q[0, 0, rows][:, None].contiguous(), kp, vp, table, ints(N - 64),
+                                 ints(0, 64))[0][:, 0]
+        one = na.cache_attention(q[0, 0, rows[-1:]][:, None].contiguous(), kp, vp, table, ints(N - 1),
+                                 ints(0, 1), max_new=1)[0][:, 0]
+        out = torch.cat([out, one])
+        rows = torch.cat([rows, rows[-1:]])
+    s = D ** -0.5 * q[0, 0, rows].double() @ k[0, 0].double().T
+    s = s.masked_fill(torch.arange(N, device="cuda")[None, :] > rows[:, None], -math.inf)
+    p = torch.softmax(s, -1)
+    want = p @ v[0, 0].double()
+    each = HALF / math.sqrt(3) * ((p ** 2 @ v[0, 0].double() ** 2) + want ** 2).sqrt()
+    bound = 1.1 * _rms(each) + 2.0 ** -20 * _rms(p @ v[0, 0].double().abs()) + 2.0 ** -25
+    assert _rms(out.double() - want) < bound, _rms(out.double() - want) / bound
