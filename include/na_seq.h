@@ -50,8 +50,8 @@ typedef struct {
  * Forward.  lengths: valid tokens per sequence (int32 [batch], clamped to [0, tokens]), or
  * NULL where all are; rows behind a length get out 0 and logsumexp -inf, and their keys are
  * not read.  logsumexp: contiguous [batch, heads, tokens] fp32, natural log.
- * NA_ERR_SHAPE: kv_heads does not divide heads, an extent is negative, a stride breaks the
- * rules above, sinks is negative, or tokens * (heads / kv_heads) reaches 2^30.
+ * NA_ERR_SHAPE: kv_heads does not divide heads, only one of the two is 0, an extent is negative,
+ * a stride breaks the rules above, sinks is negative, or tokens * (heads / kv_heads) reaches 2^30.
  */
 na_status na_sink_forward(const na_sink_problem* problem, const void* q, const void* k,
                           const void* v, const int32_t* lengths, void* out, float* logsumexp,

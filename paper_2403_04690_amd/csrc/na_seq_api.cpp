@@ -27,10 +27,12 @@ na_status check_types(int64_t head_dim, int32_t dtype, float scale) {
     return std::isfinite(scale) ? NA_OK : NA_ERR_SCALE;
 }
 
-// Heads in whole groups, a window and first tokens that are counts.
+// Heads in whole groups (a key head without a query head has none: its gradients would be 0 that
+// no launch writes), a window and first tokens that are counts.
 na_status check_heads(int64_t heads, int64_t kv_heads, int64_t kernel_size, int64_t sinks) {
     if (heads < 0 || kv_heads < 0 || heads >= kMaxRows) return NA_ERR_SHAPE;
-    if (heads > 0 && (kv_heads == 0 || heads % kv_heads != 0)) return NA_ERR_SHAPE;
+    if ((heads == 0) != (kv_heads == 0)) return NA_ERR_SHAPE;
+    if (heads > 0 && heads % kv_heads != 0) return NA_ERR_SHAPE;
     if (kernel_size < 1) return NA_ERR_KERNEL_SIZE;
     return sinks < 0 ? NA_ERR_SHAPE : NA_OK;
 }

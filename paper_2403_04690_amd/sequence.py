@@ -224,7 +224,7 @@ def _sink_plan(kernel_size, sinks, scale, metas):
     (B, H, N, D), kv_heads = q[0], k[0][1]
     if k[0][0] != B or k[0][2:] != q[0][2:]:
         raise ValueError("q, k and v must share batch, tokens and head_dim")
-    if H != kv_heads and (kv_heads == 0 or H % kv_heads):
+    if H != kv_heads and (H == 0 or kv_heads == 0 or H % kv_heads):
         raise ValueError("the heads of q must be a multiple of those of k and v")
     _rows(q, k, v, *(m for m in more if m is not None))
     like = (q, q, q, k, v)
@@ -432,7 +432,7 @@ def _attention_plan(kernel_size, sinks, scale, max_new, max_context, metas):
     (T, H, D), (P, kv_heads, page_size, _) = q[0], k_pages[0]
     if D != k_pages[0][3]:
         raise ValueError("q and the pages must share head_dim")
-    if H != kv_heads and (kv_heads == 0 or H % kv_heads):
+    if H != kv_heads and (H == 0 or kv_heads == 0 or H % kv_heads):
         raise ValueError("the heads of q must be a multiple of those of the pages")
     if len(context[0]) != 1 or len(table[0]) != 2 or table[0][0] != context[0][0]:
         raise ValueError("expected context_lens [requests] and page_table [requests, max_pages]")

@@ -1,0 +1,32 @@
+"""Edges of the sequence operators that need no GPU: refusals, and first use by several threads."""
+import pytest
+import torch
+
+import paper_2403_04690_amd as na
+from paper_2403_04690_amd import sequence
+from tests import test_sequence_host as host
+
+SHAPE, NULL = host.SHAPE, host.NULL
+lib = host.lib  # (a fixture)
+
+
+# ---------------------------------------------------------------- no query heads
+
+def test_key_heads_without_query_heads_are_refused(lib):
+    """Gradients of keys that no query head reads would be left unwritten."""
+    p = host._sink(heads=0, kv_heads=2)
+    assert host._forward(lib, p) == SHAPE and host._backward(lib, p) == SHAPE
+    assert lib.na_sink_backward_workspace(p) == 0
+    assert host._attend(lib, host._cache(heads=0, kv_heads=2)) == SHAPE
+    q, k = torch.zeros(1, 0, 5, 32), torch.zeros(1, 2, 5, 32)
+    lse = torch.zeros(1, 0, 5)
+    with pytest.raises(ValueError, match="multiple"):
+        na.sink_forward(q, k, k, 3)
+    with pytest.raises(ValueError, match="multiple"):
+        na.sink_backward(q, k, k, q, lse, q, 3)
+    with pytest.raises(ValueError, match="multiple"):
+        na.sink_attention(q, k.requires_grad_(True), k, 3)
+    pages, ints = torch.zeros(4, 2, 16, 32), torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="multiple"):
+        na.cache_attention(torch.zeros(3, 0, 32), pages, pages, torch.zeros(2, 3, dtype=torch.int32),
+                           ints, torch.zeros(3, dtype=torch.int32))
