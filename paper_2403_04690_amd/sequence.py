@@ -64,7 +64,7 @@ _entry = {}  # entry points by name: the ctypes function, and how to call it fas
 
 def _library():
     """libna.so with the argument types of na_seq.h."""
-    global _bound
+    global _bound, _entry
     lib = load_library()
     if _bound is not lib:
         sink, cache = ctypes.POINTER(_SinkProblem), ctypes.POINTER(_CacheProblem)
@@ -77,21 +77,25 @@ def _library():
         lib.na_cache_attention.argtypes = ([cache] + [_vp] * 9 + [ctypes.c_size_t, _vp])
         lib.na_cache_attention_workspace.argtypes = [cache]
         lib.na_cache_attention_workspace.restype = ctypes.c_size_t
-        _bound = lib
         try:
             from ._na_fast import call
         except ImportError:
             call = None
+        entry = {}
         for name in ("na_sink_forward", "na_sink_backward", "na_cache_tables", "na_cache_write",
                      "na_cache_attention"):
             fn = getattr(lib, name)
             if call is None:
                 # the problem goes by address in the fast form; ctypes takes it as a pointer
                 cast = fn.argtypes[0]
-                _entry[name] = fn if name == "na_cache_tables" else (
+                entry[name] = fn if name == "na_cache_tables" else (
                     lambda p, *args, fn=fn, cast=cast: fn(ctypes.cast(p, cast), *args))
             else:
-                _entry[name] = functools.partial(call, ctypes.cast(fn, ctypes.c_void_p).value)
+                entry[name] = functools.partial(call, ctypes.cast(fn, ctypes.c_void_p).value)
+        # (another thread may come here at any time: it sees the entries complete, and _bound
+        # only after them; two threads that both come first make the same)
+        _entry = entry
+        _bound = lib
     return lib
 
 

@@ -30,3 +30,38 @@ def test_key_heads_without_query_heads_are_refused(lib):
     with pytest.raises(ValueError, match="multiple"):
         na.cache_attention(torch.zeros(3, 0, 32), pages, pages, torch.zeros(2, 3, dtype=torch.int32),
                            ints, torch.zeros(3, dtype=torch.int32))
+
+
+# ---------------------------------------------------------------- first use
+
+def test_first_use_by_many_threads_while_the_extension_is_imported(lib, monkeypatch):
+    """A thread that comes while another one binds the library finds every entry point."""
+    import builtins
+    import threading
+    import time
+
+    names = {"na_sink_forward", "na_sink_backward", "na_cache_tables", "na_cache_write",
+             "na_cache_attention"}
+    monkeypatch.setattr(sequence, "_bound", None)
+    monkeypatch.setattr(sequence, "_entry", {})
+    real = builtins.__import__
+
+    def slow(name, *args, **kwargs):
+        if name.endswith("_na_fast"):
+            time.sleep(0.2)
+        return real(name, *args, **kwargs)
+
+    monkeypatch.setattr(builtins, "__import__", slow)
+    wrong = []
+
+    def use():
+        sequence._library()
+        wrong.extend(names - set(sequence._entry))
+
+    threads = [threading.Thread(target=use) for _ in range(8)]
+    for t in threads:
+        t.start()
+        time.sleep(0.01)
+    for t in threads:
+        t.join(20)
+    assert wrong == []
