@@ -14,7 +14,8 @@
  * Conventions, beside those of na.h (streams, statuses, ownership):
  *   - Strides count elements; the last axis is contiguous.  Every stride of an input may be 0
  *     (a broadcast axis); outputs must not overlap themselves.  A stride is a multiple of 16
- *     bytes, and a token stride below 2^26 bytes.
+ *     bytes, and a token stride below 2^26 bytes.  The stride of an axis of one entry does not
+ *     matter.
  *   - Data pointers (q, k, v, out, gradients, pages, logsumexp, workspaces) are 16-byte
  *     aligned, integer arrays by their element.  Integer arrays are device memory.
  *   - Keys and values of the tokens that a sequence has are finite.  What lies behind a

@@ -37,10 +37,16 @@ na_status check_heads(int64_t heads, int64_t kv_heads, int64_t kernel_size, int6
     return sinks < 0 ? NA_ERR_SHAPE : NA_OK;
 }
 
-// Strides of a [batch, heads, tokens, head_dim] tensor (see na_seq.h).  Outputs: the axes of
-// more than one entry, ordered by stride, do not overlap.
-bool good_strides(const na_strides& s, int es, int64_t batch, int64_t heads, int64_t tokens,
+// Strides as they are used: 0 on axes of one entry, whatever the caller has there.
+na_strides used(const na_strides& s, int64_t batch, int64_t heads, int64_t tokens) {
+    return {batch == 1 ? 0 : s.batch, heads == 1 ? 0 : s.head, tokens == 1 ? 0 : s.token};
+}
+
+// Strides of a [batch, heads, tokens, head_dim] tensor (see na_seq.h), its axes of more than one
+// entry.  Outputs: those, ordered by stride, do not overlap.
+bool good_strides(const na_strides& all, int es, int64_t batch, int64_t heads, int64_t tokens,
                   int64_t head_dim, bool output) {
+    const na_strides s = used(all, batch, heads, tokens);
     const int64_t st[3] = {s.batch, s.head, s.token}, n[3] = {batch, heads, tokens};
     for (int i = 0; i < 3; ++i) {
         if (st[i] < 0 || st[i] >= (int64_t(1) << 40) || (st[i] * es) % 16 != 0) return false;
@@ -108,24 +114,28 @@ na_status check_sink(const na_sink_problem& p, bool backward) {
 
 bool empty_sink(const na_sink_problem& p) { return p.batch == 0 || p.heads == 0 || p.tokens == 0; }
 
+// Byte strides of one tensor of the problem.
+void put_strides(const na_sink_problem& p, const na_strides& all, int64_t heads, int64_t& b,
+                 int64_t& h, int64_t& t) {
+    const na_strides s = used(all, p.batch, heads, p.tokens);
+    const int64_t es = elem_bytes(p.dtype);
+    b = s.batch * es;
+    h = s.head * es;
+    t = s.token * es;
+}
+
 void fill_sink(const na_sink_problem& p, const int32_t* lengths, na::SeqGeo& g) {
     fill_common(g, p.heads, p.kv_heads, p.kernel_size, p.sinks, p.scale);
-    const int64_t es = elem_bytes(p.dtype);
     g.n = (int)p.tokens;
     g.B = (int)p.batch;
     g.ntiles = (int)((p.tokens * g.G + 127) / 128);
     g.fd_tiles.init(g.ntiles);
     g.fd_slices.init((int)(p.batch * p.kv_heads));
     g.runs = 2 * (int64_t)g.W < p.tokens;
-    auto put = [&](const na_strides& s, int64_t& b, int64_t& h, int64_t& t) {
-        b = s.batch * es;
-        h = s.head * es;
-        t = s.token * es;
-    };
-    put(p.q, g.qb, g.qh, g.qt);
-    put(p.k, g.kb, g.kh, g.kt);
-    put(p.v, g.vb, g.vh, g.vt);
-    put(p.out, g.ob, g.oh, g.ot);
+    put_strides(p, p.q, p.heads, g.qb, g.qh, g.qt);
+    put_strides(p, p.k, p.kv_heads, g.kb, g.kh, g.kt);
+    put_strides(p, p.v, p.kv_heads, g.vb, g.vh, g.vt);
+    put_strides(p, p.out, p.heads, g.ob, g.oh, g.ot);
     g.lb = p.heads * p.tokens;
     g.lh = p.tokens;
     g.lt = 1;
@@ -322,16 +332,10 @@ na_status na_sink_backward(const na_sink_problem* problem, const void* q, const 
     if (workspace_bytes < need) return NA_ERR_WORKSPACE;
     if (!workspace) return NA_ERR_NULL;
     place_workspace(p, static_cast<float*>(workspace), b);
-    const int64_t es = elem_bytes(p.dtype);
-    auto put = [&](const na_strides& s, int64_t& x, int64_t& h, int64_t& t) {
-        x = s.batch * es;
-        h = s.head * es;
-        t = s.token * es;
-    };
-    put(p.dout, b.gb, b.gh, b.gt);
-    put(p.dq, b.qb, b.qh, b.qt);
-    put(p.dk, b.kb, b.kh, b.kt);
-    put(p.dv, b.vb, b.vh, b.vt);
+    put_strides(p, p.dout, p.heads, b.gb, b.gh, b.gt);
+    put_strides(p, p.dq, p.heads, b.qb, b.qh, b.qt);
+    put_strides(p, p.dk, p.kv_heads, b.kb, b.kh, b.kt);
+    put_strides(p, p.dv, p.kv_heads, b.vb, b.vh, b.vt);
     return na::launch_seq_backward(b, (int)p.head_dim, p.dtype, q, k, v, out, logsumexp, dout, dq,
                                    dk, dv, reinterpret_cast<hipStream_t>(stream)) == hipSuccess
                ? NA_OK
@@ -385,10 +389,11 @@ na_status na_cache_write(const na_cache_problem* problem, const void* k, const v
     if (!aligned(k, 16) || !aligned(v, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) ||
         !aligned(slots, 8))
         return NA_ERR_ALIGNMENT;
+    const na_strides ks = used(p.k, 1, p.kv_heads, p.tokens), vs = used(p.v, 1, p.kv_heads, p.tokens);
     return na::launch_cache_write((int)p.tokens, (int)p.kv_heads, (int)row,
                                   __builtin_ctzll(p.page_size), p.pages * p.page_size,
-                                  p.k.token * es, p.k.head * es, p.v.token * es, p.v.head * es, k,
-                                  v, slots, k_pages, v_pages,
+                                  ks.token * es, ks.head * es, vs.token * es, vs.head * es, k, v,
+                                  slots, k_pages, v_pages,
                                   reinterpret_cast<hipStream_t>(stream)) == hipSuccess
                ? NA_OK
                : NA_ERR_HIP;
@@ -435,10 +440,11 @@ na_status na_cache_attention(const na_cache_problem* problem, const void* q, con
     g.pages = (int)p.pages;
     g.max_pages = (int)p.max_pages;
     g.lgps = __builtin_ctzll(p.page_size);
-    g.qh = p.q.head * es;
-    g.qt = p.q.token * es;
-    g.oh = p.out.head * es;
-    g.ot = p.out.token * es;
+    const na_strides qs = used(p.q, 1, p.heads, p.tokens), os = used(p.out, 1, p.heads, p.tokens);
+    g.qh = qs.head * es;
+    g.qt = qs.token * es;
+    g.oh = os.head * es;
+    g.ot = os.token * es;
     g.kt = g.vt = p.head_dim * es;
     g.kh = g.vh = g.kt << g.lgps;
     g.kb = g.vb = g.kh * p.kv_heads;

@@ -32,6 +32,33 @@ def test_key_heads_without_query_heads_are_refused(lib):
                            ints, torch.zeros(3, dtype=torch.int32))
 
 
+# ---------------------------------------------------------------- axes of one entry
+
+@pytest.mark.parametrize("size,stride", [
+    ({"batch": 1}, lambda b, h, t: (3, h, t)), ({"batch": 1}, lambda b, h, t: (-8, h, t)),
+    ({"tokens": 1}, lambda b, h, t: (b, h, 2 ** 40)), ({"heads": 2, "kv_heads": 1}, None),
+    ({"heads": 1, "kv_heads": 1}, lambda b, h, t: (b, 5, t)),
+])
+def test_strides_of_axes_of_one_entry_are_not_looked_at(lib, size, stride):
+    p = host._sink(**size)
+    for name in host.STRIDED:
+        s = getattr(p, name)
+        if stride is not None:
+            setattr(p, name, sequence._Strides(*stride(s.batch, s.head, s.token)))
+        elif name in ("k", "v", "dk", "dv"):
+            s.head = 7
+    # (a valid problem: the pointer is what is refused)
+    assert host._forward(lib, p, q=None) == NULL and host._backward(lib, p, q=None) == NULL
+    assert lib.na_sink_backward_workspace(p) > 0
+
+
+def test_cache_strides_of_axes_of_one_entry_are_not_looked_at(lib):
+    for size, odd in (({"tokens": 1}, (0, 64, 2 ** 40 + 1)),
+                      ({"heads": 1, "kv_heads": 1}, (0, 3, 64))):
+        p = host._cache(q=odd, k=odd, v=odd, out=odd, **size)
+        assert host._attend(lib, p, q=None) == NULL and host._write(lib, p, k=None) == NULL
+
+
 # ---------------------------------------------------------------- first use
 
 def test_first_use_by_many_threads_while_the_extension_is_imported(lib, monkeypatch):
