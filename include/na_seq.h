@@ -121,7 +121,8 @@ na_status na_cache_write(const na_cache_problem* problem, const void* k, const v
  * logsumexp: contiguous [tokens, heads] fp32.  Rows from cu_new[requests] on are left as they
  * were.  A page id outside [0, pages), or a column beyond max_pages, reads as a page of zero
  * keys and values; context lengths are clamped to [0, max_pages * page_size].  A request whose
- * range of rows is not inside [0, tokens) has no rows.
+ * range of rows is not inside [0, tokens) has no rows.  (Where cu_new decreases somewhere, it is
+ * left open which of the requests that have rows get them.)
  * max_new, max_context: bounds of new_lens and of context + new that the caller knows (0:
  * unknown).  They choose how the work is split, and are not relied on for the result.
  * workspace: na_cache_attention_workspace(problem) bytes (it may be 0: then NULL is fine);

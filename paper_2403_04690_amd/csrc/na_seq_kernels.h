@@ -310,10 +310,11 @@ __device__ __forceinline__ bool seq_locate(const SeqGeo& g, int tile, int lgM, i
     int r, at;
     if (lgM == 7 && g.B <= 64) {
         const int i = min(lane, g.B - 1);
-        const int start = g.cu[i], count = g.cu[i + 1] - start;
-        const bool ok = lane < g.B && start >= 0 && count > 0 && start <= g.n - count;
+        const int start = g.cu[i], end = g.cu[i + 1];
+        const bool ok = lane < g.B && start >= 0 && start < end && end <= g.n;
+        const int count = ok ? end - start : 0;
         const int nt = ok ? (int)(((uint32_t)count * (uint32_t)g.G + 127u) >> 7) : 0;
-        const int key = max(g.context[i], 0) / 2 + (ok ? count / 2 : 0);
+        const int key = max(g.context[i], 0) / 2 + count / 2;
         int before = 0;
         for (int j = 0; j < g.B; ++j) {
             const int kj = __builtin_amdgcn_readlane(key, j);
@@ -325,7 +326,8 @@ __device__ __forceinline__ bool seq_locate(const SeqGeo& g, int tile, int lgM, i
         r = __builtin_ctzll(here);
         at = __builtin_amdgcn_readlane(nt, r) - 1 - (tile - __builtin_amdgcn_readlane(before, r));
     } else {
-        auto first = [&](int x) { return (int)(((uint32_t)g.cu[x] * (uint32_t)g.G) >> lgM) + x; };
+        // (offsets outside the rows, which have none, stay in order and below 2^30 this way)
+        auto first = [&](int x) { return (min(max(g.cu[x], 0), g.n) * g.G >> lgM) + x; };
         int lo = 0, span = g.B;  // the request is in [lo, lo + span)
         while (span > 1) {
             const int step = (span + 63) >> 6;
@@ -338,8 +340,9 @@ __device__ __forceinline__ bool seq_locate(const SeqGeo& g, int tile, int lgM, i
         r = uniform(lo);
         at = tile - first(r);
     }
-    const int start = g.cu[r], n = g.cu[r + 1] - start;
-    if (start < 0 || n <= 0 || start > g.n - n) return false;
+    const int start = g.cu[r], end = g.cu[r + 1];
+    if (start < 0 || start >= end || end > g.n) return false;
+    const int n = end - start;
     t.b = r;
     if (at < 0 || at >= kSeqMaxTiles) return false;
     t.row0 = at << lgM;

@@ -1,6 +1,9 @@
-"""Calls of the sequence operators that the header allows at its edges."""
+"""Calls of the sequence operators that the header allows at its edges.  (Bounds:
+tests/sequence_plain.py.)"""
 import pytest
 import torch
+
+from tests import sequence_plain as plain
 
 pytestmark = pytest.mark.gpu
 
@@ -82,3 +85,65 @@ def test_cache_strides_of_axes_of_one_entry_do_not_matter(na, T, H, Hkv, axes, k
     pages = [t.clone() for t in want[4:6]]
     a, b = (na.cache_attention(x, *pages, want[3], ints(12 + T), ints(0, 1)) for x in (last, q[-1:]))
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+# ---------------------------------------------------------------- offsets
+
+def _offsets(na, cu, T, H, Hkv, context, **hints):
+    """Rows that a valid request owns hold its attention where the offsets increase; every other
+    row, and the memory around the outputs, stays as it was."""
+    D, page, R = 32, 16, len(cu) - 1
+    q = _randn((T, H, D), "fp32", 1)
+    kp, vp = (_randn((9, Hkv, page, D), "fp32", 2 + i) for i in range(2))
+    table = torch.randint(0, 9, (R, 3), generator=torch.Generator().manual_seed(5)).int()
+    margin = 200
+    room = torch.full(((T + 2 * margin), H, D), 7.0, device="cuda")
+    lroom = torch.full(((T + 2 * margin), H), 7.0, device="cuda")
+    out, lse = room[margin:margin + T], lroom[margin:margin + T]
+    na.cache_attention(q, kp, vp, table.cuda(), torch.tensor(context, dtype=torch.int32).cuda(),
+                       torch.tensor(cu, dtype=torch.int64).int().cuda(), out=out, lse=lse, **hints)
+    torch.cuda.synchronize()
+    owned = torch.zeros(T, dtype=torch.bool)
+    ordered = all(a <= b for a, b in zip(cu, cu[1:]))
+    for r in range(R):
+        a, b = cu[r], cu[r + 1]
+        if not 0 <= a < b <= T:
+            continue
+        owned[a:b] = True
+        if ordered:
+            c = min(max(context[r], 0), 3 * page)
+            want = plain.cache(q[a:b], kp, vp, [table[r].tolist()], [c], [b - a], 2 ** 31 - 1, 0,
+                               D ** -0.5)
+            plain.close(out[a:b], want[0], want[2], f"out of request {r}")
+            plain.close(lse[a:b], want[1], want[3], f"lse of request {r}")
+    keep = torch.ones(T + 2 * margin, dtype=torch.bool)
+    keep[margin:margin + T] = ~owned
+    assert bool((room.cpu()[keep] == 7).all()) and bool((lroom.cpu()[keep] == 7).all())
+
+
+BAD = [
+    [0, 2, 1, 6], [-5, 0, 2, 2], [0, 100, 200, 300], [2 ** 31 - 1, -2 ** 31, 0, 6],
+    [-2 ** 31, -2 ** 31, 3, 5], [2, 4, 2 ** 31 - 1, 2 ** 31 - 1],
+]
+
+
+@pytest.mark.parametrize("cu", BAD)
+@pytest.mark.parametrize("T,H,Hkv", [(6, 4, 2), (40, 4, 2), (6, 4, 1)])
+def test_requests_outside_the_new_tokens_have_no_rows(na, cu, T, H, Hkv):
+    for context in ([0, 5, 31], [-9, 2 ** 31 - 1, -2 ** 31]):
+        for hints in ({}, {"max_new": 1}):
+            _offsets(na, cu, T, H, Hkv, context, **hints)
+
+
+def test_requests_beyond_the_room_do_not_hide_the_others(na):
+    """More new tokens than there is room for (as cache_tables counts them, up to 2^31 - 1): the
+    requests that fit have their rows."""
+    far = 2 ** 30
+    for cu in ([0, 500, 600, far, far + 1, 2 ** 31 - 1], [0, 599, 600, 2 ** 30 + 2 ** 29, 2 ** 31 - 1],
+               [0, 590, 600, far - 1, far, far + 1, 2 ** 31 - 1, 2 ** 31 - 1]):
+        for hints in ({}, {"max_new": 1}):
+            _offsets(na, cu, 600, 4, 1, [5] * (len(cu) - 1), **hints)
+    # more requests than the wide form sorts
+    cu = list(range(0, 400, 5)) + [far + 7 * i for i in range(9)]
+    for hints in ({}, {"max_new": 1}):
+        _offsets(na, cu, 400, 4, 1, [3] * (len(cu) - 1), **hints)
