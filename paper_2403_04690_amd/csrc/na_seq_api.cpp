@@ -65,8 +65,9 @@ bool good_strides(const na_strides& all, int es, int64_t batch, int64_t heads, i
 }
 
 // A window in 32 bits.  Positions stay below kMaxRows + kMaxRows - 256, so the clamp keeps every
-// distance inside it, and the kernels may add the entries of a tile to it.
-int clamp_window(int64_t x) { return (int)std::min<int64_t>(x, INT32_MAX - 64); }
+// distance inside it, and the masks may take it from a distance down to -127 (a row lies at most
+// 31 before its wave's last, that one 32 before a stage's second tile, entries start 4 later).
+int clamp_window(int64_t x) { return (int)std::min<int64_t>(x, INT32_MAX - 128); }
 
 // The fields that both forms of the attention share.
 void fill_common(na::SeqGeo& g, int64_t heads, int64_t kv_heads, int64_t kernel_size,
