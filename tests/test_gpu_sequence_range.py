@@ -191,3 +191,31 @@ def test_forward_beside_a_key_that_takes_most_of_the_weight(na, form):
     each = HALF / math.sqrt(3) * ((p ** 2 @ v[0, 0].double() ** 2) + want ** 2).sqrt()
     bound = 1.1 * _rms(each) + 2.0 ** -20 * _rms(p @ v[0, 0].double().abs()) + 2.0 ** -25
     assert _rms(out.double() - want) < bound, _rms(out.double() - want) / bound
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("H,Hkv,N,D,W,S", SHAPES)
+def test_an_overflowed_output_gradient_shows(na, dtype, H, Hkv, N, D, W, S):
+    """An infinite dout (a loss scale that was too high) makes every gradient that it reaches
+    infinite or NaN, so that a training program can skip the step, and none of another key head's.
+    (Keys of its own that the row does not see may be hit too: their P is 0, and 0 times infinity
+    is NaN in the plain form as well.)"""
+    q, k, v, g = (_normal((1, h, N, D), 30 + i).to(dtype).cuda()
+                  for i, h in enumerate((H, Hkv, Hkv, H)))
+    out, lse = na.sink_forward(q, k, v, W, S)
+    want = na.sink_backward(q, k, v, out, lse, g, W, S)
+    row, head = 2 * N // 3, H - 1
+    g = g.clone()
+    g[0, head, row, 7] = math.inf
+    got = na.sink_backward(q, k, v, out, lse, g, W, S)
+    seen = plain.visible(torch.tensor([row]), torch.arange(N), W, S)[0].cuda()
+    hit = [torch.zeros(t.shape[:3], dtype=torch.bool, device="cuda") for t in want]
+    hit[0][0, head, row] = True
+    hit[1][0, Hkv - 1, seen] = True
+    hit[2][0, Hkv - 1, seen] = True
+    for name, a, w, h in zip(("dq", "dk", "dv"), got, want, hit):
+        # (dv takes dout itself: only its column; dq and dk its product with every value)
+        bad = ~a[..., 7].isfinite() if name == "dv" else (~a.isfinite()).all(-1)
+        assert bool(bad[h].all()), name
+        others = slice(0, head) if name == "dq" else slice(0, Hkv - 1)
+        assert torch.equal(a[:, others], w[:, others]), name
