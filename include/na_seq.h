@@ -18,9 +18,11 @@
  *     matter.
  *   - Data pointers (q, k, v, out, gradients, pages, logsumexp, workspaces) are 16-byte
  *     aligned, integer arrays by their element.  Integer arrays are device memory.
- *   - Keys and values of the tokens that a sequence has are finite.  What lies behind a
- *     sequence's length, on unused pages, or on pages that no new token sees, may hold
- *     anything, NaN included.
+ *   - Queries, keys and values of the tokens that a sequence has are finite.  What lies behind
+ *     a sequence's length, on unused pages, or on pages that no new token sees, may hold
+ *     anything, NaN included.  An output gradient that is not finite makes the gradients that
+ *     it reaches infinite or NaN.
+ *   - Outputs overlap neither the inputs nor each other.
  *   - A workspace belongs to one call until that call's work on the stream is done; calls
  *     that may run at once need one each.
  */
@@ -52,7 +54,8 @@ typedef struct {
  * NULL where all are; rows behind a length get out 0 and logsumexp -inf, and their keys are
  * not read.  logsumexp: contiguous [batch, heads, tokens] fp32, natural log.
  * NA_ERR_SHAPE: kv_heads does not divide heads, only one of the two is 0, an extent is negative,
- * a stride breaks the rules above, sinks is negative, or tokens * (heads / kv_heads) reaches 2^30.
+ * a stride breaks the rules above, sinks is negative, tokens * (heads / kv_heads) reaches 2^30, or
+ * batch * kv_heads * ceil(tokens * (heads / kv_heads) / 128) reaches 2^24.
  */
 na_status na_sink_forward(const na_sink_problem* problem, const void* q, const void* k,
                           const void* v, const int32_t* lengths, void* out, float* logsumexp,
@@ -65,6 +68,9 @@ na_status na_sink_forward(const na_sink_problem* problem, const void* q, const v
  * each other.  Deterministic: the same inputs give bit-identical gradients.
  * workspace: na_sink_backward_workspace(problem) bytes; NA_ERR_WORKSPACE if workspace_bytes is
  * less.  (0 for a problem that is empty or not valid.)
+ * NA_ERR_SHAPE also where dk and dv would take 2^23 workgroups or more: one for 128 keys of a
+ * key/value head, and one for 32 of its first tokens that rows outside their window see (up to
+ * 1024 in all where those are fewer).
  */
 size_t na_sink_backward_workspace(const na_sink_problem* problem);
 na_status na_sink_backward(const na_sink_problem* problem, const void* q, const void* k,
@@ -89,7 +95,8 @@ typedef struct {
 
 /*
  * Tables of a step, from request lengths: request r has context_lens[r] tokens in the cache
- * and gets new_lens[r] more (device int32 arrays; negative counts as 0).
+ * and gets new_lens[r] more (device int32 arrays; negative counts as 0,
+ * more than 2^30 as 2^30).
  *   cu_new[requests + 1]  offsets of the requests' new tokens, exclusive sums of new_lens
  *   positions[tokens]     int32, position of each new token in its request
  *   slots[tokens]         int64, page * page_size + offset in the page; -1 without a page
@@ -97,6 +104,8 @@ typedef struct {
  *                         request from free_pages[*head], [*head + 1], ..; others are left
  *   new_head[1]           *head plus the pages taken.  Above num_free the pool ran dry: the
  *                         last tokens' pages are -1, their slots too
+ * NA_ERR_SHAPE: requests, tokens or num_free reach 2^30, page_size and the table's size as in
+ * na_cache_attention, or new_head is head.
  * head may be NULL (0); new_head must be other memory than head.  `tokens` is the room in
  * slots and positions: entries behind the last new token get -1; new tokens beyond the room
  * get no entry, as those beyond max_pages pages get no page.
@@ -111,6 +120,8 @@ na_status na_cache_tables(int64_t requests, int64_t tokens, int64_t page_size, i
  * Writes row t of k and v ([tokens, kv_heads, head_dim], strided) into the pages at slots[t].
  * Slots outside [0, pages * page_size) are skipped.  Slots of one call must differ: two equal
  * ones leave a mixture of both rows.
+ * NA_ERR_SHAPE: page_size as below, kv_heads or a stride out of range, tokens * kv_heads reaches
+ * 2^30, or the 16-byte pieces of k do 2^31.
  */
 na_status na_cache_write(const na_cache_problem* problem, const void* k, const void* v,
                          const int64_t* slots, void* k_pages, void* v_pages, na_stream_t stream);
@@ -126,7 +137,12 @@ na_status na_cache_write(const na_cache_problem* problem, const void* k, const v
  * max_new, max_context: bounds of new_lens and of context + new that the caller knows (0:
  * unknown).  They choose how the work is split, and are not relied on for the result.
  * workspace: na_cache_attention_workspace(problem) bytes (it may be 0: then NULL is fine);
- * NA_ERR_WORKSPACE if workspace_bytes is less.
+ * NA_ERR_WORKSPACE if workspace_bytes is less.  It grows with the requests, those without new
+ * tokens among them.
+ * NA_ERR_SHAPE: what na_sink_forward refuses of heads, sinks and strides; page_size is no power of
+ * two from 16 to 2^20; requests reach 2^24, max_pages * page_size passes 2^30, requests * max_pages
+ * reaches 2^31 or a page's bytes do, tokens * (heads / kv_heads) reaches 2^30 - 256, or
+ * (tokens * (heads / kv_heads) / 32 + requests) * kv_heads reaches 2^24.
  */
 size_t na_cache_attention_workspace(const na_cache_problem* problem);
 na_status na_cache_attention(const na_cache_problem* problem, const void* q, const void* k_pages,

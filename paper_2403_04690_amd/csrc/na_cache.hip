@@ -129,7 +129,8 @@ __global__ __launch_bounds__(kTabThreads) void cache_tables_kernel(
 
 // A thread per 16 bytes of a key row and its value row; consecutive threads run along a row,
 // so loads and stores are whole rows.  Bound by memory: 32k tokens of 8 heads, bf16 D = 128,
-// 258 MB in 49.5 us (5.2 TB/s); 64 tokens 2.7 us.
+// 258 MB in 49 us a call on changing buffers (5.2 TB/s; 41 us of kernel time on the same ones
+// again, part of which caches may hold); 64 tokens 2.6 us.
 __global__ __launch_bounds__(256) void cache_write_kernel(
     uint32_t units, int lgseg, int Hkv, FastDiv fd_kv, int lgps, int64_t slots_end, int64_t kt,
     int64_t kh, int64_t vt, int64_t vh, const unsigned char* __restrict__ k,

@@ -246,6 +246,15 @@ bool cache_narrow(const na_cache_problem& p) {
 // with 8, 24 with 4; one new token for each of 8 requests of 3000: 19 with 32, 15 with 12, 17
 // with 8.  fp32, 6 heads on 1, D = 64, 100 tokens of 5 requests, window 255: 32, 22 and 18 us
 // with 8, 4 and 2.
+//   fp32 over its range (captured; 4 requests of 64 new tokens or 8 of one, 6 heads on 1; wide with 2,
+// 4, 8 tiles a split at least, unsplit): 3 tiles, D = 32 11.0, 12.4, 10.6, 10.6 us, D = 128 25.9, 33.3,
+// 31.5, 31.4; 8 tiles 11.1, 14.3, 20.2, 18.3 and 27, 39, 60, 60; 38 tiles 17, 16, 21, 67 and 55, 44, 63,
+// 241.  Narrow with 4, 8, 16: 19 tiles, D = 32 8.3, 9.9, 12.9, D = 128 21, 33, 57; 75 tiles at 16
+// heads on 4 14.9, 13.1, 13.3 and 57, 64, 61.
+//   The bounds of 24 and 40 tiles, bf16 (split, unsplit): wide, 21 tiles 13.4 and 18.7 us at D = 32, 21
+// and 26 at D = 128, 40 tiles 13 and 32, 21 and 43; narrow, 38 tiles 8.1 and 10.2, 10.4 and 16, 75 tiles
+// 9 and 16, 11.5 and 27.  (So lower ones would pay; those of half the size were right at 9 tiles,
+// where nothing was split either way.)
 //   Decoding over 8k to 32k contexts (32 requests, 4 key heads, fp16 D = 128) with 512, 1024,
 // 2048 and 4096 splits aimed at: 254, 224, 236, 252 us.
 void fill_split(const na_cache_problem& p, bool narrow, na::SeqGeo& g) {

@@ -502,10 +502,10 @@ __device__ __forceinline__ void store_part(const S& st, float* p, int h, float s
     if constexpr (OUT & kDv) each_four<D>(st.dv, h, 1.f, put);
 }
 
-//   Five products a pair from one pass over the rows: bound by the matrix cores and the vector
-// unit in turn.  16 heads on 4, 8192 tokens, window 512, 4 first tokens, bf16 D = 128: 125 us
-// (dq, three products a pair: 84 us); full causal: dq, dk and dv together 995 us, 0.69 PFLOP/s
-// of the five products counted.
+//   Five products a pair from one pass over the rows: the matrix cores are busy 26 % of the cycles,
+// the vector unit 22 %, LDS 24 %, in turn, with two waves a SIMD.  16 heads on 4, 8192 tokens,
+// window 512, 4 first tokens, bf16 D = 128: 125 to 129 us (dq, three products a pair: 84 to 86);
+// full causal: dq, dk and dv together 1000 to 1050 us, 0.65 to 0.69 PFLOP/s of the five counted.
 template <typename T, int D, int OUT, int RS>
 __global__ __launch_bounds__((256 * RS), (sizeof(T) == 4 ? 1 : D == 32 ? 3 : 2)) void
 seq_dkv_kernel(SeqBwd b, const T* __restrict__ qg, const T* __restrict__ kg,

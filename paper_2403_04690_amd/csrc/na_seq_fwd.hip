@@ -147,10 +147,13 @@ struct SeqRing {
     static constexpr int kLds = kStages * kStage;
 };
 
-// Bound by the matrix cores and the vector unit in turn (the cache and the windows come from L2).
-//   16 heads on 4, 8192 tokens, bf16 D = 128: window 512 and 4 first tokens 61 us, full causal
-// 290 us (0.95 PFLOP/s); 16 heads, 32768 tokens, window 1023, fp16 D = 64 200 us (0.68 PFLOP/s);
-// chunks of 512 to 2048 tokens over 2k to 8k cached ones, 4 requests, bf16 D = 128 320 us (0.83).
+// Bound by the matrix cores and the vector unit in turn (the cache and the windows come from L2): at
+// D = 64 the cores are busy 34 % of the cycles and the vector unit 60 %, so little of one overlaps
+// the other; at D = 128, with two waves a SIMD, 26 to 33 % and 28 %, the rest waits.
+//   16 heads on 4, 8192 tokens, bf16 D = 128: window 512 and 4 first tokens 55 to 62 us, full causal
+// 284 to 297 us (0.93 to 0.97 PFLOP/s); 16 heads, 32768 tokens, window 1023, fp16 D = 64 203 to 208
+// us (0.67); chunks of 512 to 2048 tokens over 2k to 8k cached ones, 4 requests, bf16 D = 128 317
+// to 341 us (0.80).
 template <typename T, int D, bool PAGED>
 __global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 4) : 1)) void seq_wide_kernel(
     SeqGeo g, const T* __restrict__ qg, const T* __restrict__ kg, const T* __restrict__ vg,

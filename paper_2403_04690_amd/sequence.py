@@ -517,7 +517,7 @@ def cache_step(q, k, v, k_pages, v_pages, page_table, context_lens, new_lens, fr
     values into the pages, and their attention.  q [tokens, heads, head_dim], k and v [tokens,
     kv_heads, head_dim] hold the requests' new tokens one after another.  `tables`: what
     cache_tables returned for this step (the layers of a model share it); None builds it.
-    Returns (out, logsumexp, new_head)."""
+    Returns (out, logsumexp, new_head); rows of out behind the last new token are not written."""
     _library()
     device = q.device
     if tables is None:
