@@ -1,7 +1,8 @@
 /*
  * na_seq.h -- C ABI of the sequence operators of libna.so: the attention of a causal 1-D
  * neighbourhood with first tokens that stay visible, its gradient, and the paged cache that
- * serves it one step at a time.
+ * serves it one step at a time, whose requests may share first tokens and are cut back to a
+ * budget by the attention weight that their keys gathered.
  *
  * Attention.  Token i of a sequence attends to token j when
  *     j <= i   and   (i - j < kernel_size   or   j < sinks):
@@ -150,6 +151,118 @@ na_status na_cache_attention(const na_cache_problem* problem, const void* q, con
                              const int32_t* context_lens, const int32_t* cu_new, void* out,
                              float* logsumexp, void* workspace, size_t workspace_bytes,
                              na_stream_t stream);
+
+/* ---- long contexts: shared first tokens, gathered weights, eviction ---- */
+
+/* Groups of requests that share their first tokens. */
+typedef struct {
+    na_cache_problem cache;      /* max_context unused */
+    int64_t groups;
+    int64_t max_shared, max_own; /* see na_cache_shared_attention */
+} na_shared_problem;
+
+/*
+ * Attention of new tokens over a cache in which groups of requests share their first tokens: what
+ * na_cache_attention computes, with the shared keys read once for all rows of a group.
+ *   cu_groups[groups + 1]   group g holds the requests cu_groups[g] .. cu_groups[g + 1] - 1; the
+ *                           offsets do not decrease (otherwise it is left open which requests
+ *                           are in which group).  Requests outside of all groups share nothing.
+ *   shared_lens[groups]     the first shared_lens[g] tokens of each request of group g are the
+ *                           same, on the pages that the group's first request lists: a key
+ *                           before shared_lens[g] is read there, one from it on on the request's
+ *                           own pages (clamped to [0, max_pages * page_size]).  It need not fill
+ *                           whole pages, and may reach past a request's context.
+ * Both are int32 device arrays (they may be NULL where groups is 0).  max_new bounds the new tokens
+ * of a request, max_shared the shared ones of a group, max_own those of a request behind the
+ * shared ones, the new ones among them (0: unknown): they choose how the work is split, and are
+ * not relied on for the result.
+ * workspace: na_cache_shared_attention_workspace(problem) bytes; NA_ERR_WORKSPACE if
+ * workspace_bytes is less.  (0 for a problem that is empty or not valid.)
+ * NA_ERR_SHAPE: what na_cache_attention refuses; groups is negative or reaches 2^24; a bound is
+ * negative; or (tokens * (heads / kv_heads) / 32 + 4 * requests + groups) * kv_heads reaches 2^24.
+ */
+size_t na_cache_shared_attention_workspace(const na_shared_problem* problem);
+na_status na_cache_shared_attention(const na_shared_problem* problem, const void* q,
+                                    const void* k_pages, const void* v_pages,
+                                    const int32_t* page_table, const int32_t* context_lens,
+                                    const int32_t* cu_new, const int32_t* cu_groups,
+                                    const int32_t* shared_lens, void* out, float* logsumexp,
+                                    void* workspace, size_t workspace_bytes, na_stream_t stream);
+
+/* Gathered attention weights: fp32 [requests, kv_heads, capacity], contiguous; entry j belongs to
+ * the token at position j of the request.  A capacity may be less than the tokens of a request:
+ * those behind it gather nothing. */
+typedef struct {
+    na_cache_problem cache;  /* v, out unused */
+    int64_t capacity;
+} na_weights_problem;
+
+/*
+ * Adds to weights[r, c, j] the attention weights that the new tokens of request r gave key j:
+ *     sum over new tokens i that see j, and query heads h of key/value head c, of
+ *     exp(scale q_ih . k_jc - logsumexp_ih),
+ * with the logsumexp ([tokens, heads], 4-byte aligned) that na_cache_attention (or the form above)
+ * returned for the same tokens.  The keys of the new tokens are in the cache.  Entries before
+ * first[r] (int32 [requests] or NULL: none), of keys that no new token sees, and of requests
+ * without new tokens are left as they were.  A page outside the pool reads as zero keys.
+ * Deterministic: the same inputs give the same bits.  Weights must overlap no input.
+ * NA_ERR_SHAPE: what na_cache_attention refuses of these arguments; capacity is negative,
+ * or requests * kv_heads * capacity reaches 2^40; or requests * kv_heads reaches 2^20.
+ */
+na_status na_cache_weights(const na_weights_problem* problem, const void* q,
+                           const float* logsumexp, const void* k_pages, const int32_t* page_table,
+                           const int32_t* context_lens, const int32_t* cu_new,
+                           const int32_t* first, float* weights, na_stream_t stream);
+
+typedef struct {
+    int64_t requests, kv_heads, head_dim;
+    int64_t pages, page_size, max_pages, num_free;
+    int64_t capacity;        /* of weights and new_weights */
+    int64_t budget, recent;  /* tokens that stay, and how many of them the last ones */
+    int32_t dtype;
+} na_evict_problem;
+
+/*
+ * Cuts the requests of a cache back to `budget` tokens a key/value head.  A request with
+ * context_lens[r] <= budget stays as it is.  Of the others each key/value head keeps
+ *   the first f = min(first[r], budget) tokens (first: int32 [requests], or NULL: 0),
+ *   the last l = min(recent, budget - f), and
+ *   of those between the budget - f - l of largest weight (of equal ones those of lower position;
+ *   NaN is below all, and so the weights behind the capacity count as 0),
+ * and the request's first `budget` positions then hold, key/value head by key/value head:
+ *   the first tokens, and at their own positions those of largest weight that lie before
+ *   end = budget - l;
+ *   at the other positions before end, in order, those of largest weight from end on;
+ *   from end on the last l tokens, in order.
+ * Rows of k_pages and v_pages move in place, on the request's own pages of the first `budget`
+ * positions.  Positions before f are neither read nor written, so requests may share the pages
+ * of their first f tokens; a page that holds other positions belongs to one request.  A row
+ * from a page outside the pool is zeros, and one to such a page goes nowhere.
+ *   kept[requests, kv_heads, budget]         position at which what is there now was; -1 behind
+ *                                            the tokens of a request below the budget
+ *   new_weights[requests, kv_heads, capacity] the weights of what is there now, 0 behind it
+ *   new_context[requests]                    min(context_lens[r], budget)
+ *   new_head[1], free_pages[num_free]        pages of the positions from budget on return to the
+ *                                            list that na_cache_tables takes from: new_head is
+ *                                            *head minus their number (not below 0), and they are
+ *                                            entered from there on, request by request; entries
+ *                                            outside [0, num_free) are dropped.  The page table is
+ *                                            left as it is.
+ * Outputs overlap neither the inputs nor each other.  All of it is exact, and the same inputs give
+ * the same bits.
+ * workspace: na_cache_evict_workspace(problem) bytes; NA_ERR_WORKSPACE if workspace_bytes is less.
+ * NA_ERR_SHAPE: page_size and the table's size as in na_cache_attention; kv_heads is below 1 or
+ * requests * kv_heads reaches 2^20; budget is below 1, recent or capacity negative, one of
+ * budget and num_free reaches 2^30, requests * kv_heads * capacity reaches 2^40; a page's bytes
+ * reach 2^31; or new_head is head, or new_context is context_lens.
+ */
+size_t na_cache_evict_workspace(const na_evict_problem* problem);
+na_status na_cache_evict(const na_evict_problem* problem, const float* weights,
+                         const int32_t* context_lens, const int32_t* first,
+                         const int32_t* page_table, const int32_t* head, int32_t* free_pages,
+                         void* k_pages, void* v_pages, int32_t* new_context, float* new_weights,
+                         int32_t* kept, int32_t* new_head, void* workspace,
+                         size_t workspace_bytes, na_stream_t stream);
 
 #ifdef __cplusplus
 }

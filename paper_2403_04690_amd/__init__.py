@@ -13,7 +13,8 @@ be causal (``causal``, one flag per axis): there a query attends only to the
 k nearest positions not after it.
 
 The sequence operators (causal window attention with first tokens that stay visible, its
-gradient, and a paged cache; ``include/na_seq.h``) are in ``sequence.py``.
+gradient, and a paged cache; ``include/na_seq.h``) are in ``sequence.py``, those for long contexts
+over that cache (shared first tokens, gathered attention weights, eviction) in ``serving.py``.
 """
 import ctypes
 import functools
@@ -518,6 +519,8 @@ def unfused_backward(q, k, v, probs, dout, kernel_size, dilation=1, scale=None, 
 # ---------------------------------------------------------------- sequence operators
 from .sequence import (cache_attention, cache_step, cache_tables, cache_write,  # noqa: E402
                        sink_attention, sink_backward, sink_forward)
+from .serving import cache_evict, cache_shared_attention, cache_weights  # noqa: E402
 
 __all__ += ["sink_forward", "sink_backward", "sink_attention", "cache_tables", "cache_write",
-            "cache_attention", "cache_step"]
+            "cache_attention", "cache_step", "cache_shared_attention", "cache_weights",
+            "cache_evict"]

@@ -1,0 +1,285 @@
+// na_long_api.cpp -- the C ABI of the cache operators for long contexts (na_seq.h): attention with
+// shared first tokens, gathered weights, eviction.  Validation, the split of the work and
+// dispatch; nothing allocates, synchronises or keeps state.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <cstring>
+
+#include "na_launch.h"
+#include "na_seq_host.h"
+#include "na_shared.h"
+
+namespace {
+
+using namespace na::host;
+
+bool nothing(const na_cache_problem& p) {
+    return p.heads == 0 || p.tokens == 0 || p.requests == 0;
+}
+
+// ---- attention with shared first tokens ----
+na_status check_shared(const na_shared_problem& s) {
+    const na_cache_problem& p = s.cache;
+    const na_status st = check_attention(p);
+    if (st != NA_OK) return st;
+    if (s.groups < 0 || s.groups >= kMaxGrid || s.max_shared < 0 || s.max_own < 0)
+        return NA_ERR_SHAPE;
+    if (nothing(p)) return NA_OK;
+    const int64_t G = p.heads / p.kv_heads;
+    const int64_t tiles = p.tokens * G / 32 + 4 * p.requests + s.groups;
+    if (tiles >= kMaxGrid || tiles * p.kv_heads >= kMaxGrid) return NA_ERR_SHAPE;
+    return NA_OK;
+}
+
+// The cut of the keys of one side over workgroups.  keys: the most that a row tile has;
+// busy: row tiles that are expected to have rows.
+void cut_side(na::SharedSide& side, int64_t keys, int64_t busy, int64_t Hkv, bool half) {
+    const bool narrow = side.narrow;
+    const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32 + 1);
+    int64_t split = std::max<int64_t>(1, (narrow ? 1024 : 512) / std::max<int64_t>(1, busy * Hkv));
+    split = std::min<int64_t>(split, na::kSeqMaxSplit);
+    split = std::min(split, std::max<int64_t>(1, (kMaxGrid - 1) / ((int64_t)side.ntiles * Hkv)));
+    const int64_t least = half ? (narrow ? 12 : 8) : (narrow ? 8 : 2);
+    const int64_t step = narrow ? 4 : 2;
+    int64_t chunk = split == 1 ? tiles : std::max<int64_t>(least, (tiles + split - 1) / split);
+    chunk = (chunk + step - 1) / step * step;
+    side.chunk = (int)chunk;
+    side.nsplit = (int)((tiles + chunk - 1) / chunk);
+    side.fd_tiles.init((int)(side.ntiles * Hkv));
+}
+
+void fill_shared(const na_shared_problem& s, na::SharedGeo& x) {
+    const na_cache_problem& p = s.cache;
+    std::memset(&x, 0, sizeof x);
+    na::SeqGeo& g = x.g;
+    fill_common(g, p.heads, p.kv_heads, p.kernel_size, p.sinks, p.scale);
+    fill_paged(p, g);
+    const int64_t rows = p.tokens * g.G, room = p.max_pages * p.page_size;
+    const bool half = p.dtype != NA_FP32;
+    x.groups = (int)s.groups;
+
+    na::SharedSide& own = x.own_side;
+    own.narrow = cache_narrow(p);
+    const int64_t M = own.narrow ? 32 : 128;
+    own.ntiles = g.ntiles = (int)(rows / M + p.requests);
+    int64_t keys = s.max_own > 0 ? std::min(s.max_own, room) : room;
+    keys = std::min(keys, (int64_t)g.W + g.S + M + 64);
+    cut_side(own, keys, std::max((rows + M - 1) / M, std::min(p.requests, p.tokens)), g.Hkv, half);
+
+    na::SharedSide& shared = x.shared_side;
+    shared.fd_tiles.init(1);
+    if (s.groups == 0) return;
+    // (the narrow form where a group's rows are expected to fill one block of 32)
+    shared.narrow = rows <= 32 * s.groups;
+    const int64_t Ms = shared.narrow ? 32 : 128;
+    shared.ntiles = (int)(rows / Ms + s.groups);
+    keys = s.max_shared > 0 ? std::min(s.max_shared, room) : room;
+    cut_side(shared, keys, std::max((rows + Ms - 1) / Ms, std::min(s.groups, p.tokens)), g.Hkv,
+             half);
+}
+
+size_t shared_bytes(const na_shared_problem& s, const na::SharedGeo& x) {
+    return (size_t)(x.shared_side.nsplit + x.own_side.nsplit) * s.cache.tokens * s.cache.heads *
+           (s.cache.head_dim + 1) * 4;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t na_cache_shared_attention_workspace(const na_shared_problem* problem) {
+    if (!problem || check_shared(*problem) != NA_OK || nothing(problem->cache)) return 0;
+    na::SharedGeo x;
+    fill_shared(*problem, x);
+    return shared_bytes(*problem, x);
+}
+
+na_status na_cache_shared_attention(const na_shared_problem* problem, const void* q,
+                                    const void* k_pages, const void* v_pages,
+                                    const int32_t* page_table, const int32_t* context_lens,
+                                    const int32_t* cu_new, const int32_t* cu_groups,
+                                    const int32_t* shared_lens, void* out, float* logsumexp,
+                                    void* workspace, size_t workspace_bytes, na_stream_t stream) {
+    if (!problem) return NA_ERR_NULL;
+    const na_cache_problem& p = problem->cache;
+    const na_status st = check_shared(*problem);
+    if (st != NA_OK) return st;
+    if (nothing(p)) return NA_OK;
+    if (!q || !context_lens || !cu_new || !out || !logsumexp ||
+        (problem->groups > 0 && (!cu_groups || !shared_lens)) ||
+        (p.pages > 0 && (!k_pages || !v_pages)) || (p.max_pages > 0 && !page_table))
+        return NA_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(out, 16) ||
+        !aligned(logsumexp, 16) || !aligned(workspace, 16) || !aligned(page_table, 4) ||
+        !aligned(context_lens, 4) || !aligned(cu_new, 4) || !aligned(cu_groups, 4) ||
+        !aligned(shared_lens, 4))
+        return NA_ERR_ALIGNMENT;
+    na::SharedGeo x;
+    fill_shared(*problem, x);
+    const size_t need = shared_bytes(*problem, x);
+    if (workspace_bytes < need) return NA_ERR_WORKSPACE;
+    if (!workspace) return NA_ERR_NULL;
+    x.g.context = context_lens;
+    x.g.cu = cu_new;
+    x.g.table = page_table;
+    x.cu_groups = cu_groups;
+    x.shared = shared_lens;
+    x.part = static_cast<float*>(workspace);
+    x.part_lse = x.part + (size_t)(x.shared_side.nsplit + x.own_side.nsplit) * p.tokens * p.heads *
+                              p.head_dim;
+    return na::launch_shared_attention(x, (int)p.head_dim, p.dtype, q, k_pages, v_pages, out,
+                                       logsumexp, reinterpret_cast<hipStream_t>(stream)) ==
+                   hipSuccess
+               ? NA_OK
+               : NA_ERR_HIP;
+}
+
+na_status na_cache_weights(const na_weights_problem* problem, const void* q,
+                           const float* logsumexp, const void* k_pages, const int32_t* page_table,
+                           const int32_t* context_lens, const int32_t* cu_new,
+                           const int32_t* first, float* weights, na_stream_t stream) {
+    if (!problem) return NA_ERR_NULL;
+    const na_cache_problem& p = problem->cache;
+    const na_status st = check_attention(p, false);
+    if (st != NA_OK) return st;
+    const int64_t slices = p.requests * p.kv_heads;
+    if (problem->capacity < 0 || problem->capacity >= (int64_t(1) << 40) ||
+        slices >= (int64_t(1) << 20) ||
+        (__int128)slices * problem->capacity >= ((__int128)1 << 40))
+        return NA_ERR_SHAPE;
+    if (nothing(p) || problem->capacity == 0) return NA_OK;
+    if (!q || !logsumexp || !context_lens || !cu_new || !weights || (p.pages > 0 && !k_pages) ||
+        (p.max_pages > 0 && !page_table))
+        return NA_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(logsumexp, 4) ||
+        !aligned(weights, 4) || !aligned(page_table, 4) || !aligned(context_lens, 4) ||
+        !aligned(cu_new, 4) || !aligned(first, 4))
+        return NA_ERR_ALIGNMENT;
+    na::WeightsGeo w;
+    std::memset(&w, 0, sizeof w);
+    na::SeqGeo& g = w.g;
+    fill_common(g, p.heads, p.kv_heads, p.kernel_size, p.sinks, p.scale);
+    fill_paged(p, g);
+    w.form = cache_narrow(p) ? 0 : 1;
+    w.capacity = problem->capacity;
+    w.first = first;
+    w.lse = logsumexp;
+    w.weights = weights;
+    g.context = context_lens;
+    g.cu = cu_new;
+    g.table = page_table;
+    // Key tiles of a request over workgroups.
+    const int64_t room = p.max_pages * p.page_size;
+    const int64_t most = p.max_new > 0 ? std::min(p.max_new, p.tokens) : p.tokens;
+    int64_t keys = p.max_context > 0 ? std::min(p.max_context, room) : room;
+    keys = std::min(keys, (int64_t)g.W + g.S + most + 64);
+    const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32 + 1);
+    int64_t chunk;
+    if (w.form == 0) {
+        const int64_t split = std::max<int64_t>(1, 2048 / slices);
+        chunk = std::max<int64_t>(8, (tiles + split - 1) / split);
+    } else {
+        chunk = 8;
+    }
+    chunk = std::max(chunk, (tiles * slices + kMaxGrid / 2 - 1) / (kMaxGrid / 2));
+    chunk = (chunk + 7) / 8 * 8;
+    g.chunk = (int)chunk;
+    g.nsplit = (int)((tiles + chunk - 1) / chunk);
+    g.fd_tiles.init(g.nsplit);
+    return na::launch_cache_weights(w, (int)p.head_dim, p.dtype, q, k_pages,
+                                    reinterpret_cast<hipStream_t>(stream)) == hipSuccess
+               ? NA_OK
+               : NA_ERR_HIP;
+}
+
+// ---- eviction ----
+static na_status check_evict(const na_evict_problem& p) {
+    const na_status st = check_types(p.head_dim, p.dtype, 1.f);
+    if (st != NA_OK) return st;
+    if (p.requests < 0 || p.requests >= kMaxGrid || p.kv_heads < 1 || p.kv_heads >= kMaxGrid ||
+        p.requests * p.kv_heads >= (int64_t(1) << 20))
+        return NA_ERR_SHAPE;
+    if (p.pages < 0 || p.pages >= kMaxRows || p.page_size < 16 || p.page_size > (1 << 20) ||
+        (p.page_size & (p.page_size - 1)) || p.max_pages < 0 || p.max_pages >= kMaxRows ||
+        p.max_pages * p.page_size > kMaxRows || p.requests * p.max_pages >= (int64_t(1) << 31) ||
+        p.num_free < 0 || p.num_free >= kMaxRows)
+        return NA_ERR_SHAPE;
+    if (p.budget < 1 || p.budget >= kMaxRows || p.recent < 0 || p.capacity < 0 ||
+        p.capacity >= (int64_t(1) << 40) ||
+        (__int128)p.requests * p.kv_heads * p.capacity >= ((__int128)1 << 40))
+        return NA_ERR_SHAPE;
+    if (p.kv_heads * p.page_size * p.head_dim * elem_bytes(p.dtype) >= (int64_t(1) << 31))
+        return NA_ERR_SHAPE;
+    return NA_OK;
+}
+
+size_t na_cache_evict_workspace(const na_evict_problem* problem) {
+    if (!problem || check_evict(*problem) != NA_OK) return 0;
+    const size_t slices = (size_t)(problem->requests * problem->kv_heads);
+    return slices * (2 * (size_t)problem->budget + 1) * 4;
+}
+
+na_status na_cache_evict(const na_evict_problem* problem, const float* weights,
+                         const int32_t* context_lens, const int32_t* first,
+                         const int32_t* page_table, const int32_t* head, int32_t* free_pages,
+                         void* k_pages, void* v_pages, int32_t* new_context, float* new_weights,
+                         int32_t* kept, int32_t* new_head, void* workspace,
+                         size_t workspace_bytes, na_stream_t stream) {
+    if (!problem) return NA_ERR_NULL;
+    const na_evict_problem& p = *problem;
+    const na_status st = check_evict(p);
+    if (st != NA_OK) return st;
+    if (!head || !new_head || (p.num_free && !free_pages)) return NA_ERR_NULL;
+    const bool some = p.requests > 0;
+    if (some && (!context_lens || !new_context || !kept || (p.max_pages && !page_table) ||
+                 (p.capacity && (!weights || !new_weights)) ||
+                 (p.pages && (!k_pages || !v_pages))))
+        return NA_ERR_NULL;
+    const void* words[] = {weights, context_lens, first,       page_table, head,
+                           free_pages, new_context, new_weights, kept,       new_head};
+    for (const void* x : words)
+        if (!aligned(x, 4)) return NA_ERR_ALIGNMENT;
+    if (!aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(workspace, 4))
+        return NA_ERR_ALIGNMENT;
+    if (head == new_head || (some && new_context == context_lens)) return NA_ERR_SHAPE;
+    const size_t need = na_cache_evict_workspace(problem);
+    if (workspace_bytes < need) return NA_ERR_WORKSPACE;
+    if (need && !workspace) return NA_ERR_NULL;
+    na::EvictGeo v;
+    std::memset(&v, 0, sizeof v);
+    v.R = (int)p.requests;
+    v.Hkv = (int)p.kv_heads;
+    v.budget = (int)p.budget;
+    v.recent = (int)std::min(p.recent, p.budget);
+    v.lgps = __builtin_ctzll(p.page_size);
+    v.pages = (int)p.pages;
+    v.max_pages = (int)p.max_pages;
+    v.num_free = (int)p.num_free;
+    const int64_t row = p.head_dim * elem_bytes(p.dtype);
+    v.lgrow = v.lgslice = __builtin_ctzll(row);
+    const int64_t slices = p.requests * p.kv_heads;
+    while (v.lgslice > 6 && (slices * 2 << (v.lgrow - v.lgslice)) < 1024) --v.lgslice;
+    v.capacity = p.capacity;
+    v.fd_kv.init(v.Hkv);
+    v.weights = reinterpret_cast<const uint32_t*>(weights);
+    v.context = context_lens;
+    v.first = first;
+    v.table = page_table;
+    v.head = head;
+    v.free_pages = free_pages;
+    v.new_context = new_context;
+    v.kept = kept;
+    v.new_head = new_head;
+    v.new_weights = reinterpret_cast<uint32_t*>(new_weights);
+    v.moves = static_cast<int32_t*>(workspace);
+    v.to = v.moves + slices;
+    v.from = v.to + slices * p.budget;
+    return na::launch_cache_evict(v, k_pages, v_pages, reinterpret_cast<hipStream_t>(stream)) ==
+                   hipSuccess
+               ? NA_OK
+               : NA_ERR_HIP;
+}
+
+}  // extern "C"

@@ -296,6 +296,10 @@ struct SeqTile {
     __device__ __forceinline__ bool sees(const SeqGeo& g, int j) const {
         return (j >= lo || j < g.S) && j <= pmax;
     }
+    // whether some row may see each of the 32 positions from j0 on
+    __device__ __forceinline__ bool whole(const SeqGeo& g, int j0) const {
+        return j0 + 31 <= pmax && (j0 >= lo || j0 + 31 < g.S);
+    }
 };
 
 // Paged form: row tile `tile` of M = 2^lgM rows -> its request and rows.  False: no such tile.
@@ -395,7 +399,7 @@ __device__ __forceinline__ void seq_contiguous(const SeqGeo& g, int tile, int sl
 }
 
 // Stages key tile `e` of the workgroup's tile: instructions first, first + STEP, ... of the
-// 2 kInstr of K and V (first < STEP).
+// 2 kInstr of K and V (first < STEP).  Tile: a SeqTile, or one with the same members.
 template <typename T, int D, bool PAGED, int STEP>
 struct SeqStage {
     using R = SeqRows<T, D>;
@@ -409,7 +413,8 @@ struct SeqStage {
     uint32_t klane, vlane;  // rowl * token stride
     int kt, vt;             // token strides (below 2^26 bytes)
 
-    __device__ __forceinline__ void init(const SeqGeo& g, const SeqTile& t, int kvh, int lane,
+    template <typename Tile>
+    __device__ __forceinline__ void init(const SeqGeo& g, const Tile& t, int kvh, int lane,
                                          const void* k, const void* v) {
         rows.init(lane);
         kb = static_cast<const unsigned char*>(k) + kvh * g.kh;
@@ -424,10 +429,11 @@ struct SeqStage {
         vlane = rows.rowl * (uint32_t)vt;
     }
 
-    __device__ __forceinline__ void issue(const SeqGeo& g, const SeqTile& t, int e, int first,
+    template <typename Tile>
+    __device__ __forceinline__ void issue(const SeqGeo& g, const Tile& t, int e, int first,
                                           unsigned char* dst) const {
         const int j0 = t.tile(e);
-        bool fast = j0 + 31 <= t.pmax && (j0 >= t.lo || j0 + 31 < g.S);
+        bool fast = t.whole(g, j0);
         // byte offset of the first row of the tile's two 16-row blocks, and whether they exist
         int64_t k0, k1, v0, v1;
         bool ok0 = true, ok1 = true;
@@ -465,11 +471,11 @@ struct SeqStage {
     // The loads themselves, from the first rows of the blocks; FAST: every row exists and is
     // seen by some row.  (Everything by value: selects between captured references end up in
     // scratch memory.)
-    template <bool FAST>
+    template <bool FAST, typename Tile>
     __device__ __forceinline__ void load(const unsigned char* k0, const unsigned char* k1,
                                          const unsigned char* v0, const unsigned char* v1,
                                          int first, unsigned char* dst, bool ok0, bool ok1,
-                                         const SeqTile& t, const SeqGeo& g, int j0) const {
+                                         const Tile& t, const SeqGeo& g, int j0) const {
 #pragma unroll
         for (int u = 0; u < kCount; ++u) {
             const int x = first + u * STEP;

@@ -1,0 +1,576 @@
+// na_shared.hip -- attention of new tokens over a paged cache in which groups of requests share their
+// first tokens: the shared keys are read once for all rows of a group (gfx950).
+//
+//   With a row's keys in two sets A and B, lse = log(e^lse_A + e^lse_B) and
+//   out = e^(lse_A - lse) out_A + e^(lse_B - lse) out_B,
+// so the shared keys are one problem of all the rows of a group (every request's new tokens times
+// the heads of a key/value head), the keys behind them one problem a request, and a second
+// launch joins the parts.  Each of the problems is cut into splits of its keys; every
+// split of every row leaves a logsumexp (-inf where the row sees nothing of it) and, unless it
+// is -inf, its mean of the values, both in fp32.
+#include <cmath>
+#include <type_traits>
+
+#include "na_launch.h"
+#include "na_seq_state.h"
+#include "na_shared.h"
+
+namespace na {
+
+namespace {
+
+// A tile of rows against the keys [from, end) of a request, or of those that a group shares.
+// (The members that SeqStage reads are SeqTile's.)
+struct SharedTile : SeqTile {
+    int r0, r1;       // requests that its rows belong to
+    int from, end;    // keys of this side
+    int s0;           // first tile of the first tokens
+    // Requests stand at different positions: with a window shorter than they are apart there may be
+    // keys between lo and end that no row sees.  Then `seen` has those of the tile that is staged
+    // next (bit e: its key e), otherwise all bits.
+    bool gaps;
+    unsigned seen;
+
+    // Rows at positions rmin .. rmax, keys [from, to).
+    __device__ __forceinline__ void span(const SeqGeo& g, int rmin, int rmax, int to) {
+        end = min(to, rmax + 1);
+        pmax = end - 1;
+        lo = max(rmin - g.W + 1, from);
+        w0 = lo >> 5;
+        s0 = from >> 5;
+        gaps = rmax - rmin >= g.W;
+        seen = ~0u;
+        nS = nT = 0;
+        if (end <= from) return;
+        // (first tokens in the window's first tile come with it, if there is a window here)
+        const bool window = lo < end;
+        const int stop = (min(g.S, end) + 31) >> 5;
+        nS = max(0, (window ? min(stop, w0) : stop) - s0);
+        nT = nS + (window ? (pmax >> 5) - w0 + 1 : 0);
+    }
+    __device__ __forceinline__ int tile(int e) const { return (e < nS ? s0 + e : w0 + e - nS) << 5; }
+    __device__ __forceinline__ bool sees(const SeqGeo& g, int j) const {
+        return (j >= lo || j < g.S) && j >= from && j < end && (seen >> (j & 31) & 1);
+    }
+    __device__ __forceinline__ bool whole(const SeqGeo& g, int j0) const {
+        return j0 >= from && j0 + 31 < end && (j0 >= lo || j0 + 31 < g.S) && seen == ~0u;
+    }
+    // Keys of the tile from j0 on that the rows at positions pos (N a lane) of the wave see.
+    template <int N>
+    __device__ __forceinline__ void look(const SeqGeo& g, int j0, const int (&pos)[N]) {
+        unsigned m = 0;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int d = pos[n] - j0;
+            m |= below32(d + 1) & (~below32(d - g.W + 1) | below32(g.S - j0));
+        }
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) m |= __shfl_xor(m, x, kWave);
+        seen = uniform((int)m);
+    }
+    __device__ __forceinline__ static unsigned below32(int x) {
+        return x >= 32 ? ~0u : (1u << max(x, 0)) - 1u;
+    }
+};
+
+// The last x of [lo, lo + span) with at(x) <= v (at does not decrease; lo where there is none): the
+// lanes probe 64 places at a time.
+template <typename At>
+__device__ __forceinline__ int last_at(int lo, int span, int v, int lane, At at) {
+    while (span > 1) {
+        const int step = (span + 63) >> 6;
+        const bool in = lane * step < span && at(lo + lane * step) <= v;
+        const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(in));
+        const int skip = (n > 0 ? n - 1 : 0) * step;
+        lo += skip;
+        span = min(step, span - skip);
+    }
+    return uniform(lo);
+}
+
+__device__ __forceinline__ int context_of(const SeqGeo& g, int c) {
+    return min(max(c, 0), g.max_pages << g.lgps);
+}
+__device__ __forceinline__ int shared_of(const SharedGeo& s, int x) {
+    return context_of(s.g, s.shared[x]);
+}
+
+// Row tile `tile` of M = 2^lgM rows of the groups -> its rows.  False: no such tile.  Group x has
+// tiles from floor(first row / M) + x on, at least as many as it needs.
+__device__ __forceinline__ bool locate_group(const SharedGeo& s, int tile, int lgM, int lane,
+                                             SharedTile& t, int& to) {
+    const SeqGeo& g = s.g;
+    auto request = [&](int x) { return min(max(s.cu_groups[x], 0), g.B); };
+    auto token = [&](int x) { return min(max(g.cu[request(x)], 0), g.n); };
+    const int x = last_at(0, s.groups, tile, lane,
+                          [&](int i) { return (token(i) * g.G >> lgM) + i; });
+    t.r0 = uniform(request(x));
+    t.r1 = uniform(request(x + 1));
+    const int start = uniform(token(x)), n = uniform(token(x + 1)) - start;
+    if (t.r0 >= t.r1 || n <= 0) return false;
+    const int at = tile - (start * g.G >> lgM) - x;
+    if (at < 0 || at >= kSeqMaxTiles) return false;
+    t.row0 = at << lgM;
+    if (t.row0 < 0 || t.row0 >= n * g.G) return false;
+    t.b = t.r0;
+    t.rows = min(n * g.G - t.row0, 1 << lgM);
+    t.qtok = start;
+    t.pos0 = 0;
+    t.valid = n;
+    t.from = 0;
+    to = uniform(shared_of(s, x));
+    return true;
+}
+
+// Group of request r, or -1.
+__device__ __forceinline__ int group_of(const SharedGeo& s, int r, int lane) {
+    if (s.groups == 0) return -1;
+    const int x = last_at(0, s.groups, r, lane, [&](int i) { return s.cu_groups[i]; });
+    return uniform(s.cu_groups[x] <= r && r < s.cu_groups[x + 1] ? x : -1);
+}
+
+// Position of row `tok` of q (each lane its own; `least` the wave's least) among the requests
+// [r0, r1), whose offsets do not decrease.
+__device__ __forceinline__ int position_of(const SeqGeo& g, int r0, int r1, int least, int tok,
+                                           int lane) {
+    int base = r0, pos = 0;
+    if (r1 - r0 > 64)
+        base = last_at(r0, r1 - r0, least, lane, [&](int i) { return g.cu[i]; });
+    for (;;) {
+        const int r = min(base + lane, r1 - 1);
+        const int c = g.context[r];
+        const int start = base + lane < r1 ? max(g.cu[r], 0) : INT32_MAX;
+        int i = 0;  // the last of these requests that begins at or before tok
+#pragma unroll
+        for (int bit = 32; bit > 0; bit >>= 1) {
+            const int at = __shfl(start, i + bit, kWave);
+            i += at <= tok ? bit : 0;
+        }
+        const int begin = __shfl(start, i, kWave), cached = __shfl(c, i, kWave);
+        if (begin <= tok) pos = context_of(g, cached) + tok - begin;
+        base += 64;
+        if (base >= r1 ||
+            __builtin_amdgcn_ballot_w64(max(g.cu[base], 0) <= tok) == 0)
+            return pos;
+    }
+}
+
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) x = min(x, __shfl_xor(x, d, kWave));
+    return uniform(x);
+}
+__device__ __forceinline__ int wave_max(int x) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) x = max(x, __shfl_xor(x, d, kWave));
+    return uniform(x);
+}
+
+// The rows of a workgroup of one side: where they are, and the keys [e0, e1) of its split.
+// GROUP: of the shared keys; otherwise of a request's own ones.
+template <bool GROUP, int LGM>
+struct SharedJob {
+    SharedTile t;
+    int tile, kvh, split, part;  // part: place among all parts of a row
+    int to, group;
+
+    __device__ __forceinline__ bool locate(const SharedGeo& s, int bid, int lane) {
+        const SeqGeo& g = s.g;
+        const SharedSide& side = GROUP ? s.shared_side : s.own_side;
+        split = side.fd_tiles.div(bid);
+        const int id = bid - split * side.ntiles * g.Hkv;
+        tile = g.fd_kv.div(id);
+        kvh = id - tile * g.Hkv;
+        part = split + (GROUP ? 0 : s.shared_side.nsplit);
+        if constexpr (GROUP) {
+            return locate_group(s, tile, LGM, lane, t, to);
+        } else {
+            if (!seq_locate(g, tile, LGM, lane, t)) return false;
+            group = group_of(s, t.b, lane);
+            t.from = group < 0 ? 0 : uniform(shared_of(s, group));
+            t.span(g, t.pmin, t.pmax, INT32_MAX);
+            return true;
+        }
+    }
+    __device__ __forceinline__ void keys(const SharedGeo& s, int& e0, int& e1) const {
+        const SharedSide& side = GROUP ? s.shared_side : s.own_side;
+        e0 = min(split * side.chunk, t.nT);
+        e1 = split == side.nsplit - 1 ? t.nT : min(e0 + side.chunk, t.nT);
+    }
+};
+
+// Place of a row's part: its logsumexp (base 2); D times that its mean of the values.
+__device__ __forceinline__ int64_t part_row(const SharedGeo& s, int part, int tok, int64_t head) {
+    return ((int64_t)part * s.g.n + tok) * ((int64_t)s.g.Hkv * s.g.G) + head;
+}
+
+// Requests without a group have no shared part: their rows' places there say so.
+template <typename Job>
+__device__ __forceinline__ void no_shared_part(const SharedGeo& s, const Job& job, int m, int tok,
+                                               int head) {
+    if (job.group >= 0 || job.split != 0 || m >= job.t.rows) return;
+    for (int x = 0; x < s.shared_side.nsplit; ++x)
+        s.part_lse[part_row(s, x, job.t.qtok + tok, (int64_t)job.kvh * s.g.G + head)] = -INFINITY;
+}
+
+// Many rows: four waves of 32 rows each share the staged key tiles (as the wide form of
+// na_seq_fwd.hip).
+template <typename T, int D, bool GROUP>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 4) : 1)) void shared_wide_kernel(
+    SharedGeo s, const T* __restrict__ qg, const T* __restrict__ kg, const T* __restrict__ vg) {
+    using F = SeqFrags<T, D>;
+    using Ring = SeqRing<T, D>;
+    constexpr int SK = Ring::kTiles, NB = Ring::kStages;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const SeqGeo& g = s.g;
+    const int lane = threadIdx.x & 63;
+    const int wave = uniform((threadIdx.x >> 6) & 3);
+    SharedJob<GROUP, 7> job;
+    if (!job.locate(s, blockIdx.x, lane)) return;
+    SharedTile& t = job.t;
+
+    // ---- this lane's row, and the positions of the wave's rows ----
+    const int m = wave * 32 + (lane & 31);
+    int tok, head, pos;
+    seq_row(g, t, m, tok, head);
+    int tf, hh;
+    seq_row(g, t, wave * 32, tf, hh);
+    int wmin, wmax;
+    int all[GROUP ? 4 : 1];  // positions of rows lane % 32 of every wave
+    if constexpr (GROUP) {
+        pos = position_of(g, t.r0, t.r1, t.qtok + tf, t.qtok + tok, lane);
+        wmin = wave_min(pos);
+        wmax = wave_max(pos);
+        int* rows = reinterpret_cast<int*>(smem);  // (before the stages use the LDS)
+        if (lane < 32) rows[m] = pos;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) all[w] = rows[w * 32 + (lane & 31)];
+        t.span(g, wave_min(min(min(all[0], all[1]), min(all[2], all[3]))),
+               wave_max(max(max(all[0], all[1]), max(all[2], all[3]))), job.to);
+        __syncthreads();
+    } else {
+        pos = t.pos0 + tok;
+        wmin = wave_min(pos);
+        wmax = wave_max(pos);
+    }
+    int e0, e1;
+    job.keys(s, e0, e1);
+
+    SeqStage<T, D, true, 4> ld;
+    ld.init(g, t, job.kvh, lane, kg, vg);
+    auto issue_stage = [&](int e, int buf) __attribute__((always_inline)) {
+        if (e >= e1) return;
+#pragma unroll
+        for (int i = 0; i < SK; ++i) {  // (a tile behind the last one: zeros)
+            if (GROUP && t.gaps) t.look(g, t.tile(e + i), all);
+            ld.issue(g, t, e + i, wave, smem + buf * Ring::kStage + i * 2 * F::kTile);
+        }
+    };
+#pragma unroll
+    for (int b = 0; b < NB - 1; ++b) issue_stage(e0 + b * SK, b);
+
+    const bool live = wave * 32 < t.rows;
+    const int64_t hq = (int64_t)job.kvh * g.G + head;
+    SeqState<T, D> st;
+    st.init();
+    {
+        const unsigned char* qp = reinterpret_cast<const unsigned char*>(qg) + hq * g.qh +
+                                  (int64_t)(t.qtok + tok) * g.qt;
+#pragma unroll
+        for (int x = 0; x < F::kKS; ++x)
+            st.qf[x] = ld_x8<T>(reinterpret_cast<const T*>(qp) + x * 16 + 8 * (lane >> 5));
+    }
+    F f;
+    f.init(lane);
+#pragma unroll
+    for (int x = 0; x < F::kKS; ++x) settle(st.qf[x]);
+    auto seen = [&](int base) __attribute__((always_inline)) {
+        return seen_keys(pos - base, g.W, g.S - base) & below(t.end - base) & ~below(t.from - base);
+    };
+
+    // One stage, in buffer BUF (see na_seq_fwd.hip).
+    auto stage = [&](int e, auto BUF) __attribute__((always_inline)) {
+        constexpr int kBuf = decltype(BUF)::value;
+        if (NB > 2 && e + (NB - 2) * SK < e1)
+            wait_vmem_but<(NB - 2) * SK * decltype(ld)::kCount>();
+        else
+            wait_vmem();
+        lds_barrier();
+        issue_stage(e + (NB - 1) * SK, (kBuf + NB - 1) % NB);
+        const unsigned char* base = smem + kBuf * Ring::kStage;
+        const unsigned char* tile[SK];
+        int j0[SK];
+        bool on[SK], out = true, full = true;
+#pragma unroll
+        for (int i = 0; i < SK; ++i) {
+            tile[i] = base + i * 2 * F::kTile;
+            j0[i] = t.tile(e + i);
+            on[i] = i == 0 || e + i < e1;
+            out = out && (!on[i] || j0[i] > wmax || (wmin - (j0[i] + 31) >= g.W && j0[i] >= g.S));
+            full = full && on[i] && j0[i] + 31 <= wmin && (wmax - j0[i] < g.W || j0[i] + 31 < g.S) &&
+                   j0[i] >= t.from && j0[i] + 31 < t.end;
+        }
+        if (live && !out) st.template fold<SK>(f, tile, lane, g.c, full, j0, on, seen);
+    };
+    for (int e = e0; e < e1;) {
+        stage(e, std::integral_constant<int, 0>{});
+        if ((e += SK) >= e1) break;
+        stage(e, std::integral_constant<int, 1>{});
+        if ((e += SK) >= e1) break;
+        if constexpr (NB > 2) {
+            stage(e, std::integral_constant<int, 2>{});
+            e += SK;
+        }
+    }
+
+    // ---- this split's part of the rows ----
+    if constexpr (!GROUP) {
+        if (lane < 32) no_shared_part(s, job, m, tok, head);
+    }
+    const float l = col_sum<32>(st.l);
+    if (m >= t.rows) return;
+    const bool some = l > 0.f;
+    const float inv = some ? 1.f / l : 0.f;
+    const int h = lane >> 5;
+    const int64_t row = part_row(s, job.part, t.qtok + tok, hq);
+    if (h == 0) s.part_lse[row] = some ? st.mref + __log2f(l) : -INFINITY;
+    if (!some) return;
+    float* po = s.part + row * D;
+#pragma unroll
+    for (int db = 0; db < F::kDB; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            st16<f32x4>(po + db * 32 + i * 8 + h * 4,
+                        f32x4{st.o[db][4 * i], st.o[db][4 * i + 1], st.o[db][4 * i + 2],
+                              st.o[db][4 * i + 3]} * inv);
+}
+
+// Few rows (one block of 32): the waves take every fourth key tile each and join (as the narrow
+// form of na_seq_fwd.hip).
+template <typename T, int D, bool GROUP>
+__global__ __launch_bounds__((seq_narrow_waves<T, D>() * 64), 1) void shared_narrow_kernel(
+    SharedGeo s, const T* __restrict__ qg, const T* __restrict__ kg, const T* __restrict__ vg) {
+    using F = SeqFrags<T, D>;
+    using N = SeqNarrow<T, D>;
+    constexpr int W = N::W;
+    extern __shared__ __align__(16) unsigned char smem[];
+    const SeqGeo& g = s.g;
+    const int lane = threadIdx.x & 63;
+    const int wave = uniform((threadIdx.x >> 6) & (W - 1));
+    SharedJob<GROUP, 5> job;
+    if (!job.locate(s, blockIdx.x, lane)) return;
+    SharedTile& t = job.t;
+    int tok, head, pos;
+    seq_row(g, t, lane & 31, tok, head);
+    if constexpr (GROUP) {
+        int tf, hh;
+        seq_row(g, t, 0, tf, hh);
+        pos = position_of(g, t.r0, t.r1, t.qtok + tf, t.qtok + tok, lane);
+    } else {
+        pos = t.pos0 + tok;
+    }
+    const int wmin = wave_min(pos), wmax = wave_max(pos);
+    if constexpr (GROUP) t.span(g, wmin, wmax, job.to);
+    int e0, e1;
+    job.keys(s, e0, e1);
+
+    SeqStage<T, D, true, 1> ld;
+    ld.init(g, t, job.kvh, lane, kg, vg);
+    unsigned char* buf0 = smem + wave * 4 * F::kTile;
+    const int all[1] = {pos};
+    auto issue = [&](int e, unsigned char* dst) __attribute__((always_inline)) {
+        if (GROUP && t.gaps) t.look(g, t.tile(e), all);
+        ld.issue(g, t, e, 0, dst);
+    };
+    int e = e0 + wave;
+    if (e < e1) issue(e, buf0);
+    const int64_t hq = (int64_t)job.kvh * g.G + head;
+    SeqState<T, D> st;
+    st.init();
+    {
+        const unsigned char* qp = reinterpret_cast<const unsigned char*>(qg) + hq * g.qh +
+                                  (int64_t)(t.qtok + tok) * g.qt;
+#pragma unroll
+        for (int x = 0; x < F::kKS; ++x)
+            st.qf[x] = ld_x8<T>(reinterpret_cast<const T*>(qp) + x * 16 + 8 * (lane >> 5));
+    }
+    F f;
+    f.init(lane);
+#pragma unroll
+    for (int x = 0; x < F::kKS; ++x) settle(st.qf[x]);
+    wait_vmem();  // (the first tile too: from here on only stage loads are outstanding)
+    auto seen = [&](int base) __attribute__((always_inline)) {
+        return seen_keys(pos - base, g.W, g.S - base) & below(t.end - base) & ~below(t.from - base);
+    };
+    for (int buf = 0; e < e1; e += W, buf ^= 1) {
+        if (e + W < e1) {
+            issue(e + W, buf0 + (buf ^ 1) * 2 * F::kTile);
+            wait_vmem_but<2 * SeqRows<T, D>::kInstr>();
+        } else {
+            wait_vmem();
+        }
+        const unsigned char* ks[1] = {buf0 + buf * 2 * F::kTile};
+        const int j0 = t.tile(e);
+        const bool full = j0 + 31 <= wmin && (wmax - j0 < g.W || j0 + 31 < g.S) && j0 >= t.from &&
+                          j0 + 31 < t.end;
+        const int js[1] = {j0};
+        const bool on[1] = {true};
+        st.template fold<1>(f, ks, lane, g.c, full, js, on, seen);
+        wait_lds();  // before the next loads into this buffer
+    }
+
+    // ---- join the waves: every sum relative to the largest reference ----
+    const float l = col_sum<32>(st.l);
+    float* stat = reinterpret_cast<float*>(smem + N::kStat);  // [wave][32] of (reference, sum)
+    if (lane < 32) {
+        stat[(wave * 32 + lane) * 2] = st.mref;
+        stat[(wave * 32 + lane) * 2 + 1] = l;
+        if constexpr (!GROUP) {
+            if (wave == 0) no_shared_part(s, job, lane, tok, head);
+        }
+    }
+    __syncthreads();
+    const int col = lane & 31, h = lane >> 5;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < W; ++w) top = fmaxf(top, stat[(w * 32 + col) * 2]);
+    const float scale = st.mref == -INFINITY ? 0.f : fast_exp2(st.mref - top);
+    {
+        float* mine = reinterpret_cast<float*>(smem + (wave * 32 + col) * N::kRow);
+#pragma unroll
+        for (int db = 0; db < F::kDB; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                st16<f32x4>(mine + db * 32 + i * 8 + h * 4,
+                            f32x4{st.o[db][4 * i], st.o[db][4 * i + 1], st.o[db][4 * i + 2],
+                                  st.o[db][4 * i + 3]} * scale);
+    }
+    __syncthreads();
+    // each thread: four columns of a row
+    for (int x = threadIdx.x; x < t.rows * (D / 4); x += W * 64) {
+        const int row = x / (D / 4), d = x % (D / 4) * 4;
+        float mx = -INFINITY, sum = 0.f;
+        f32x4 acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < W; ++w) mx = fmaxf(mx, stat[(w * 32 + row) * 2]);
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float m = stat[(w * 32 + row) * 2];
+            sum += m == -INFINITY ? 0.f : fast_exp2(m - mx) * stat[(w * 32 + row) * 2 + 1];
+            acc += *reinterpret_cast<const f32x4*>(smem + (w * 32 + row) * N::kRow + d * 4);
+        }
+        const bool some = sum > 0.f;
+        int tk, hd;
+        seq_row(g, t, row, tk, hd);
+        const int64_t pr = part_row(s, job.part, t.qtok + tk, (int64_t)job.kvh * g.G + hd);
+        if (some) st16(s.part + pr * D + d, acc * (1.f / sum));
+        if (d == 0) s.part_lse[pr] = some ? mx + __log2f(sum) : -INFINITY;
+    }
+}
+
+// Joins the parts of each row in a fixed order.  One workgroup per 32 rows of a (row tile of the
+// requests, key/value head); D / 4 threads a row.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void shared_join_kernel(SharedGeo s, int lgM, T* __restrict__ og,
+                                                          float* __restrict__ lseg) {
+    const SeqGeo& g = s.g;
+    const int id = blockIdx.x >> (lgM - 5), r0 = (blockIdx.x & ((1 << (lgM - 5)) - 1)) * 32;
+    const int tile = g.fd_kv.div(id);
+    const int kvh = id - tile * g.Hkv;
+    SeqTile t;
+    if (!seq_locate(g, tile, lgM, threadIdx.x & 63, t)) return;
+    const int parts = s.shared_side.nsplit + s.own_side.nsplit;
+    const int64_t apart = (int64_t)g.n * g.Hkv * g.G;
+    const int end = min(32, t.rows - r0) * (D / 4);
+    for (int x = threadIdx.x; x < end; x += 256) {
+        const int row = r0 + x / (D / 4), d = x % (D / 4) * 4;
+        int tok, head;
+        seq_row(g, t, row, tok, head);
+        const int64_t hr = (int64_t)kvh * g.G + head;
+        const int64_t at = part_row(s, 0, t.qtok + tok, hr);
+        float mx = -INFINITY, sum = 0.f;
+        for (int p = 0; p < parts; ++p) mx = fmaxf(mx, s.part_lse[at + p * apart]);
+        f32x4 acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int p = 0; p < parts; ++p) {
+            const float e = s.part_lse[at + p * apart];
+            if (e == -INFINITY) continue;
+            const float w = fast_exp2(e - mx);
+            sum += w;
+            acc += ld16<f32x4>(s.part + (at + p * apart) * D + d) * w;
+        }
+        const bool some = sum > 0.f;
+        T* op = reinterpret_cast<T*>(reinterpret_cast<unsigned char*>(og) + hr * g.oh +
+                                     (int64_t)(t.qtok + tok) * g.ot);
+        st_x4<T>(op + d, acc * (some ? 1.f / sum : 0.f));
+        if (d == 0)
+            lseg[hr * g.lh + (int64_t)(t.qtok + tok) * g.lt] =
+                some ? (mx + __log2f(sum)) * kLn2 : -INFINITY;
+    }
+}
+
+// ---- host ----
+template <typename T, int D, bool GROUP>
+hipError_t launch_side(const SharedGeo& s, bool narrow, const T* q, const T* k, const T* v,
+                       hipStream_t st) {
+    const SharedSide& side = GROUP ? s.shared_side : s.own_side;
+    const unsigned grid = (unsigned)side.ntiles * s.g.Hkv * side.nsplit;
+    hipError_t e;
+    if (narrow) {
+        using N = SeqNarrow<T, D>;
+        auto kern = shared_narrow_kernel<T, D, GROUP>;
+        if ((e = seq_allow_lds(kern, N::kLds)) != hipSuccess) return e;
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(N::W * 64), N::kLds, st, s, q, k, v);
+    } else {
+        constexpr size_t lds = SeqRing<T, D>::kLds;
+        auto kern = shared_wide_kernel<T, D, GROUP>;
+        if ((e = seq_allow_lds(kern, lds)) != hipSuccess) return e;
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, st, s, q, k, v);
+    }
+    return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t launch_shared(const SharedGeo& s, const void* q, const void* k, const void* v, void* out,
+                         float* lse, hipStream_t st) {
+    auto q_ = static_cast<const T*>(q);
+    auto k_ = static_cast<const T*>(k);
+    auto v_ = static_cast<const T*>(v);
+    hipError_t e;
+    if (s.shared_side.nsplit > 0 &&
+        (e = launch_side<T, D, true>(s, s.shared_side.narrow, q_, k_, v_, st)) != hipSuccess)
+        return e;
+    if ((e = launch_side<T, D, false>(s, s.own_side.narrow, q_, k_, v_, st)) != hipSuccess) return e;
+    const bool narrow = s.own_side.narrow;
+    hipLaunchKernelGGL((shared_join_kernel<T, D>),
+                       dim3((unsigned)s.g.ntiles * s.g.Hkv * (narrow ? 1 : 4)), dim3(256), 0, st, s,
+                       narrow ? 5 : 7, static_cast<T*>(out), lse);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_shared_d(const SharedGeo& s, int D, const void* q, const void* k, const void* v,
+                           void* out, float* lse, hipStream_t st) {
+    switch (D) {
+        case 32: return launch_shared<T, 32>(s, q, k, v, out, lse, st);
+        case 64: return launch_shared<T, 64>(s, q, k, v, out, lse, st);
+        case 128: return launch_shared<T, 128>(s, q, k, v, out, lse, st);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_shared_attention(const SharedGeo& s, int D, int dtype, const void* q,
+                                   const void* k, const void* v, void* out, float* lse,
+                                   hipStream_t st) {
+    switch (dtype) {
+        case 0: return launch_shared_d<float>(s, D, q, k, v, out, lse, st);
+        case 1: return launch_shared_d<_Float16>(s, D, q, k, v, out, lse, st);
+        case 2: return launch_shared_d<__bf16>(s, D, q, k, v, out, lse, st);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace na

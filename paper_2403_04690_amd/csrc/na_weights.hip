@@ -1,0 +1,402 @@
+// na_weights.hip -- the attention weight that every key of a paged cache gathers from new tokens
+// (gfx950):
+//
+//   w[r, c, j] += sum over the new tokens i of request r and the query heads h of key/value head c of
+//                 exp(scale q_ih . k_jc - lse_ih),   j seen by i,
+//
+// from the logsumexp that the tokens' attention returned.  A key's sum is one workgroup's alone, so
+// nothing is joined and the order of every sum is fixed.
+//
+//   S = Q K^T (32 rows x 32 keys a step) leaves a key in one lane column (two lanes), whose entries
+// are rows: a lane adds up its own exponentials, and the two halves meet once at the end.
+// Scores, exponentials and sums are fp32; nothing is rounded on the way.
+#include <type_traits>
+
+#include "na_launch.h"
+#include "na_seq_kernels.h"
+#include "na_shared.h"
+
+namespace na {
+
+namespace {
+
+constexpr float kNever = INFINITY;  // logsumexp of a row that does not exist: its weights are 0
+__device__ const float kNeverRow = INFINITY;
+
+// Bits e of the rows row + e (row: of the request's rows, token row / G) that see key j.
+__device__ __forceinline__ unsigned seen_rows(const SeqGeo& g, int pos0, int row, int j) {
+    const int f = g.fd_G.div(row);
+    const int o = row - f * g.G;  // heads of token f that lie before the row
+    const int d = j - (pos0 + f);  // the first token that sees the key, from token f on
+    const int64_t lo = (int64_t)min(d, 33) * g.G - o;
+    const int64_t hi = min((int64_t)d + g.W, (int64_t)33) * g.G - o;
+    const unsigned from = ~below((int)max(min(lo, (int64_t)32), (int64_t)0));
+    return j < g.S ? from : from & below((int)max(min(hi, (int64_t)32), (int64_t)0));
+}
+
+// Request r's new tokens.  False: it has none.
+__device__ __forceinline__ bool weights_request(const SeqGeo& g, int r, SeqTile& t) {
+    const int start = g.cu[r], end = g.cu[r + 1];
+    if (start < 0 || start >= end || end > g.n) return false;
+    t.b = r;
+    t.row0 = 0;
+    t.rows = (end - start) * g.G;
+    t.qtok = start;
+    t.pos0 = min(max(g.context[r], 0), g.max_pages << g.lgps);
+    t.valid = end - start;
+    t.pmin = t.pos0;
+    t.pmax = t.pos0 + t.valid - 1;
+    t.span(g);
+    return true;
+}
+
+// Bytes of key j's row from the head's rows of page 0, or -1: no such page.
+__device__ __forceinline__ int64_t key_offset(const SeqGeo& g, int r, int j) {
+    const int col = j >> g.lgps;
+    const int id = col < g.max_pages ? g.table[(int64_t)r * g.max_pages + col] : -1;
+    if ((unsigned)id >= (unsigned)g.pages) return -1;
+    return (int64_t)id * (int)g.kb + (int64_t)(j & ((1 << g.lgps) - 1)) * (int)g.kt;
+}
+
+__device__ __forceinline__ int64_t weights_at(const WeightsGeo& w, int r, int kvh) {
+    return ((int64_t)r * w.g.Hkv + kvh) * w.capacity;
+}
+
+// The rows of a block of 32 as an operand: lane l has row l % 32.
+template <typename T, int D>
+__device__ __forceinline__ void load_rows(const SeqGeo& g, const SeqTile& t, int kvh, int row0,
+                                          const T* qg, int lane,
+                                          typename Tr<T>::x8 (&qf)[D / 16]) {
+    const int m = min(row0 + (lane & 31), t.rows - 1);
+    const int tok = g.fd_G.div(m), head = m - tok * g.G;
+    const unsigned char* qp = reinterpret_cast<const unsigned char*>(qg) +
+                              ((int64_t)kvh * g.G + head) * g.qh +
+                              (int64_t)(t.qtok + tok) * g.qt;
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x)
+        qf[x] = ld_x8<T>(reinterpret_cast<const T*>(qp) + x * 16 + 8 * (lane >> 5));
+}
+
+// Logsumexp of row m, base 2.
+__device__ __forceinline__ float row_lse(const WeightsGeo& w, const SeqTile& t, int kvh, int m) {
+    if (m >= t.rows) return kNever;
+    const SeqGeo& g = w.g;
+    const int tok = g.fd_G.div(m), head = m - tok * g.G;
+    return w.lse[(int64_t)(t.qtok + tok) * g.lt + (int64_t)kvh * g.G + head] * kLog2e;
+}
+
+constexpr int kFewWaves = 4;
+constexpr int kFewTiles = 64;  // key tiles whose sums are in LDS at a time
+
+// Few rows (one block of 32: single tokens): each wave takes every fourth key tile of the split,
+// from LDS buffers of its own.  Bound by reading the keys once.
+template <typename T, int D>
+__global__ __launch_bounds__(kFewWaves * 64, 1) void weights_few_kernel(
+    WeightsGeo w, const T* __restrict__ qg, const T* __restrict__ kg) {
+    using F = SeqFrags<T, D>;
+    using R = SeqRows<T, D>;
+    constexpr int W = kFewWaves;
+    extern __shared__ __align__(16) unsigned char smem[];
+    float* sums = reinterpret_cast<float*>(smem + W * 2 * F::kTile);
+    const SeqGeo& g = w.g;
+    const int lane = threadIdx.x & 63;
+    const int wave = uniform((threadIdx.x >> 6) & (W - 1));
+    const int slice = g.fd_tiles.div(blockIdx.x);
+    const int split = blockIdx.x - slice * g.nsplit;
+    const int r = g.fd_kv.div(slice), kvh = slice - r * g.Hkv;
+    SeqTile t;
+    if (!weights_request(g, r, t)) return;
+    const int splits = seq_splits(g, t.nT);
+    if (split >= splits) return;
+    const int e0 = split * g.chunk, e1 = split == splits - 1 ? t.nT : e0 + g.chunk;
+    const int first = w.first ? max(w.first[r], 0) : 0;
+
+    R rows;
+    rows.init(lane);
+    const unsigned char* kb = reinterpret_cast<const unsigned char*>(kg) + kvh * g.kh;
+    const uint32_t klane = rows.rowl * (uint32_t)g.kt;
+    auto issue = [&](int e, unsigned char* dst) __attribute__((always_inline)) {
+        const int j0 = t.tile(e);
+        // (pages hold whole blocks of 16 keys)
+        const int64_t at0 = key_offset(g, r, j0), at1 = key_offset(g, r, j0 + 16);
+#pragma unroll
+        for (int n = 0; n < R::kInstr; ++n) {
+            const int r0 = n * R::kRpi;
+            const int64_t at = r0 >= 16 ? at1 : at0;
+            const bool see = at >= 0 && t.sees(g, j0 + r0 + rows.rowl);
+            const unsigned char* base = kb + (at >= 0 ? at : 0) + (r0 & 15) * (int)g.kt;
+            seq_load(see ? base + rows.off(n, klane)
+                         : reinterpret_cast<const unsigned char*>(&kZeroRow),
+                     dst + n * 1024);
+        }
+    };
+    F f;
+    f.init(lane);
+    const int h = lane >> 5;
+    typename Tr<T>::x8 qf[F::kKS];
+    float lse[16];
+    load_rows<T, D>(g, t, kvh, 0, qg, lane, qf);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) lse[i] = row_lse(w, t, kvh, entry_row(i) + 4 * h);
+#pragma unroll
+    for (int x = 0; x < F::kKS; ++x) settle(qf[x]);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(lse[i]));
+    unsigned char* buf0 = smem + wave * 2 * F::kTile;
+
+    for (int pass = e0; pass < e1; pass += kFewTiles) {
+        const int end = min(pass + kFewTiles, e1);
+        int e = pass + wave;
+        if (e < end) issue(e, buf0);
+        for (int buf = 0; e < end; e += W, buf ^= 1) {
+            if (e + W < end) {
+                issue(e + W, buf0 + (buf ^ 1) * F::kTile);
+                wait_vmem_but<R::kInstr>();
+            } else {
+                wait_vmem();
+            }
+            const unsigned char* tile = buf0 + buf * F::kTile;
+            typename Tr<T>::x8 kf[F::kKS];
+            f.rows(tile, kf);
+            const int j0 = t.tile(e), j = j0 + (lane & 31);
+            float sum = 0.f;
+            for (int row0 = 0; row0 < t.rows; row0 += 32) {
+                if (row0 > 0) {  // (more rows than the caller's bound says)
+                    load_rows<T, D>(g, t, kvh, row0, qg, lane, qf);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        lse[i] = row_lse(w, t, kvh, row0 + entry_row(i) + 4 * h);
+                }
+                f32x16 s = f32x16{} * 0.f;
+#pragma unroll
+                for (int x = 0; x < F::kKS; ++x) s = mma32<T>(qf[x], kf[x], s);
+                const unsigned m = seen_rows(g, t.pos0, row0 + 4 * h, j);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    if (row0 + 8 * b >= t.rows) break;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int i = 4 * b + x;
+                        sum += fast_exp2(keep(m, i, fmaf(s[i], g.c, -lse[i]), -INFINITY));
+                    }
+                }
+            }
+            if (t.rows > 32) {  // the first block again
+                load_rows<T, D>(g, t, kvh, 0, qg, lane, qf);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) lse[i] = row_lse(w, t, kvh, entry_row(i) + 4 * h);
+            }
+            sum = col_sum<32>(sum);
+            if (h == 0) sums[(e - pass) * 32 + lane] = sum;
+            wait_lds();  // before the next loads into this buffer
+        }
+        __syncthreads();
+        float* out = w.weights + weights_at(w, r, kvh);
+        for (int x = threadIdx.x; x < (end - pass) * 32; x += W * 64) {
+            const int j = t.tile(pass + (x >> 5)) + (x & 31);
+            if (j >= first && j < w.capacity && t.sees(g, j)) out[j] += sums[x];
+        }
+        __syncthreads();
+    }
+}
+
+// Key tiles of a wave in the form for many rows: two while their operands fit the registers of
+// two waves a SIMD.
+template <typename T, int D>
+struct WeightsMany {
+    static constexpr int kTiles = sizeof(T) == 4 && D == 128 ? 1 : 2;
+    static constexpr int kStages = 3;
+    static constexpr int kTile = SeqFrags<T, D>::kTile;
+    static constexpr int kStage = kTile + 4 * 256;  // rows, and each wave's copy of their lse
+    static constexpr int kLds = kStages * kStage;
+};
+
+// Many rows (chunks of prompts): four waves of kTiles x 32 keys each, whose operands stay in registers,
+// share blocks of 32 staged rows.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsGeo w,
+                                                             const T* __restrict__ qg,
+                                                             const T* __restrict__ kg) {
+    using F = SeqFrags<T, D>;
+    using R = SeqRows<T, D>;
+    using M = WeightsMany<T, D>;
+    constexpr int KT = M::kTiles, NB = M::kStages;
+    constexpr int kShare = (R::kInstr + 3) / 4, kCount = kShare + 1;
+    static_assert(R::kInstr % 4 == 0 || R::kInstr < 4, "equal shares");
+    extern __shared__ __align__(16) unsigned char smem[];
+    const SeqGeo& g = w.g;
+    const int lane = threadIdx.x & 63;
+    const int wave = uniform((threadIdx.x >> 6) & 3);
+    const int id = xcd_remap(blockIdx.x, gridDim.x);
+    const int slice = g.fd_tiles.div(id);
+    const int split = id - slice * g.nsplit;
+    const int r = g.fd_kv.div(slice), kvh = slice - r * g.Hkv;
+    SeqTile t;
+    if (!weights_request(g, r, t)) return;
+    const int splits = seq_splits(g, t.nT);
+    if (split >= splits) return;
+    const int c1 = split == splits - 1 ? t.nT : (split + 1) * g.chunk;
+    const int first = w.first ? max(w.first[r], 0) : 0;
+    const int h = lane >> 5;
+    F f;
+    f.init(lane);
+    R rows;
+    rows.init(lane);
+    const unsigned char* kb = reinterpret_cast<const unsigned char*>(kg) + kvh * g.kh;
+
+    // Rows of block b, and their logsumexps, into stage `buf`: this wave's share.
+    auto issue = [&](int b, int buf) __attribute__((always_inline)) {
+        unsigned char* dst = smem + buf * M::kStage;
+#pragma unroll
+        for (int u = 0; u < kShare; ++u) {
+            // (fewer than four: two waves bring the same)
+            const int n = R::kInstr < 4 ? wave % R::kInstr : wave + 4 * u;
+            const int m = min(b * 32 + n * R::kRpi + rows.rowl, t.rows - 1);
+            const int tok = g.fd_G.div(m), head = m - tok * g.G;
+            seq_load(reinterpret_cast<const unsigned char*>(qg) +
+                         ((int64_t)kvh * g.G + head) * g.qh + (int64_t)(t.qtok + tok) * g.qt +
+                         rows.off(n, 0),
+                     dst + n * 1024);
+        }
+        const int m = b * 32 + (lane & 31);
+        const int mc = min(m, t.rows - 1);
+        const int tok = g.fd_G.div(mc), head = mc - tok * g.G;
+        const float* p = w.lse + (int64_t)(t.qtok + tok) * g.lt + (int64_t)kvh * g.G + head;
+        seq_load4(reinterpret_cast<const unsigned char*>(m < t.rows ? p : &kNeverRow),
+                  dst + M::kTile + wave * 256);
+    };
+
+    for (int pass = split * g.chunk; pass < c1; pass += 4 * KT) {
+        // ---- this wave's keys ----
+        const int e = pass + wave * KT;
+        typename Tr<T>::x8 kf[KT][F::kKS];
+        int j0[KT];
+        bool on[KT];
+        float sum[KT];
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+            on[k] = e + k < c1;
+            j0[k] = t.tile(on[k] ? e + k : pass);
+            // (keys that nobody gathers for)
+            on[k] = on[k] && j0[k] + 31 >= first;
+            sum[k] = 0.f;
+            const int j = j0[k] + (lane & 31);
+            const int64_t at = t.sees(g, j) ? key_offset(g, r, j) : -1;
+#pragma unroll
+            for (int x = 0; x < F::kKS; ++x) {
+                kf[k][x] = zero_x8<T>();
+                if (at >= 0)
+                    kf[k][x] = ld_x8<T>(reinterpret_cast<const T*>(kb + at) + x * 16 + 8 * h);
+            }
+        }
+        // ---- the rows that see any of the workgroup's keys ----
+        const int ja = t.tile(pass), jb = t.tile(min(pass + 4 * KT, c1) - 1) + 31;
+        const int ta = max(ja - t.pos0, 0);
+        const int tb = (int)min((int64_t)t.valid, ja < g.S ? (int64_t)t.valid
+                                                           : (int64_t)jb - t.pos0 + g.W);
+        const int b0 = ta < tb ? ta * g.G >> 5 : 0;
+        const int b1 = ta < tb && jb >= first ? (tb * g.G + 31) >> 5 : b0;
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+            for (int x = 0; x < F::kKS; ++x) settle(kf[k][x]);
+        lds_barrier();  // (the stages of the pass before are read)
+#pragma unroll
+        for (int x = 0; x < NB - 1; ++x)
+            if (b0 + x < b1) issue(b0 + x, x);
+        int buf = 0;
+        for (int b = b0; b < b1; ++b, buf = buf == NB - 1 ? 0 : buf + 1) {
+            if (b + NB - 2 < b1)
+                wait_vmem_but<(NB - 2) * kCount>();
+            else
+                wait_vmem();
+            lds_barrier();  // for every wave; and the stage before is read
+            if (b + NB - 1 < b1) issue(b + NB - 1, buf == 0 ? NB - 1 : buf - 1);
+            const unsigned char* tile = smem + buf * M::kStage;
+            typename Tr<T>::x8 qf[F::kKS];
+            f.rows(tile, qf);
+            float lse[16];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(tile + M::kTile + wave * 256 +
+                                                                (8 * x + 4 * h) * 4);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) lse[4 * x + y] = v[y] * kLog2e;
+            }
+            const int pa = t.pos0 + g.fd_G.div(b * 32);
+            const int pb = t.pos0 + g.fd_G.div(min(b * 32 + 31, t.rows - 1));
+#pragma unroll
+            for (int k = 0; k < KT; ++k) {
+                if (!on[k] || pb < j0[k] || (pa - (j0[k] + 31) >= g.W && j0[k] >= g.S)) continue;
+                f32x16 s = f32x16{} * 0.f;
+#pragma unroll
+                for (int x = 0; x < F::kKS; ++x) s = mma32<T>(qf[x], kf[k][x], s);
+                float y[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) y[i] = fmaf(s[i], g.c, -lse[i]);
+                if (!(pa >= j0[k] + 31 && (pb - j0[k] < g.W || j0[k] + 31 < g.S))) {
+                    const unsigned m = seen_rows(g, t.pos0, b * 32 + 4 * h, j0[k] + (lane & 31));
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) y[i] = keep(m, i, y[i], -INFINITY);
+                }
+                float part[2] = {0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < 16; ++i) part[i & 1] += fast_exp2(y[i]);
+                sum[k] += part[0] + part[1];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < KT; ++k) {
+            const float total = col_sum<32>(sum[k]);
+            const int j = j0[k] + lane;
+            if (on[k] && h == 0 && j >= first && j < w.capacity && t.sees(g, j))
+                w.weights[weights_at(w, r, kvh) + j] += total;
+        }
+    }
+}
+
+// ---- host ----
+template <typename T, int D>
+hipError_t launch_weights(const WeightsGeo& w, const void* q, const void* k, hipStream_t st) {
+    auto q_ = static_cast<const T*>(q);
+    auto k_ = static_cast<const T*>(k);
+    const unsigned grid = (unsigned)w.g.B * w.g.Hkv * w.g.nsplit;
+    hipError_t e;
+    if (w.form == 0) {
+        constexpr size_t lds = kFewWaves * 2 * SeqFrags<T, D>::kTile + kFewTiles * 32 * 4;
+        auto kern = weights_few_kernel<T, D>;
+        if ((e = seq_allow_lds(kern, lds)) != hipSuccess) return e;
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(kFewWaves * 64), lds, st, w, q_, k_);
+    } else {
+        constexpr size_t lds = WeightsMany<T, D>::kLds;
+        auto kern = weights_many_kernel<T, D>;
+        if ((e = seq_allow_lds(kern, lds)) != hipSuccess) return e;
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, st, w, q_, k_);
+    }
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_weights_d(const WeightsGeo& w, int D, const void* q, const void* k,
+                            hipStream_t st) {
+    switch (D) {
+        case 32: return launch_weights<T, 32>(w, q, k, st);
+        case 64: return launch_weights<T, 64>(w, q, k, st);
+        case 128: return launch_weights<T, 128>(w, q, k, st);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_cache_weights(const WeightsGeo& w, int D, int dtype, const void* q, const void* k,
+                                hipStream_t st) {
+    switch (dtype) {
+        case 0: return launch_weights_d<float>(w, D, q, k, st);
+        case 1: return launch_weights_d<_Float16>(w, D, q, k, st);
+        case 2: return launch_weights_d<__bf16>(w, D, q, k, st);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace na

@@ -19,8 +19,8 @@ Serving, one step of a batch of requests over a paged cache:
     cache_write(k, v, slots, k_pages, v_pages)
     out, lse = cache_attention(q, k_pages, v_pages, page_table, context_lens, cu)
 
-or the three at once, ``cache_step``.  Nothing here synchronises; all work is on the current
-stream of the tensors' device.
+or the three at once, ``cache_step``; ``serving.py`` has more for long contexts.  Nothing here
+synchronises; all work is on the current stream of the tensors' device.
 """
 import ctypes
 import functools
@@ -58,6 +58,40 @@ class _CacheProblem(ctypes.Structure):
                 + [("dtype", ctypes.c_int32), ("scale", ctypes.c_float)])
 
 
+class _SharedProblem(ctypes.Structure):
+    _fields_ = [("cache", _CacheProblem), ("groups", _i64), ("max_shared", _i64),
+                ("max_own", _i64)]
+
+
+class _WeightsProblem(ctypes.Structure):
+    _fields_ = [("cache", _CacheProblem), ("capacity", _i64)]
+
+
+class _EvictProblem(ctypes.Structure):
+    _fields_ = ([(n, _i64) for n in ("requests", "kv_heads", "head_dim", "pages", "page_size",
+                                     "max_pages", "num_free", "capacity", "budget", "recent")]
+                + [("dtype", ctypes.c_int32)])
+
+
+# argument types of the entry points, without the workspace sizes (ctypes; the problem by pointer)
+_SIGNATURES = {
+    "na_sink_forward": [ctypes.POINTER(_SinkProblem)] + [_vp] * 7,
+    "na_sink_backward": [ctypes.POINTER(_SinkProblem)] + [_vp] * 11 + [ctypes.c_size_t, _vp],
+    "na_cache_tables": [_i64] * 5 + [_vp] * 10,
+    "na_cache_write": [ctypes.POINTER(_CacheProblem)] + [_vp] * 6,
+    "na_cache_attention": [ctypes.POINTER(_CacheProblem)] + [_vp] * 9 + [ctypes.c_size_t, _vp],
+    "na_cache_shared_attention": ([ctypes.POINTER(_SharedProblem)] + [_vp] * 11
+                                  + [ctypes.c_size_t, _vp]),
+    "na_cache_weights": [ctypes.POINTER(_WeightsProblem)] + [_vp] * 9,
+    "na_cache_evict": [ctypes.POINTER(_EvictProblem)] + [_vp] * 13 + [ctypes.c_size_t, _vp],
+}
+_WORKSPACES = {
+    "na_sink_backward_workspace": _SinkProblem,
+    "na_cache_attention_workspace": _CacheProblem,
+    "na_cache_shared_attention_workspace": _SharedProblem,
+    "na_cache_evict_workspace": _EvictProblem,
+}
+
 _bound = None
 _entry = {}  # entry points by name: the ctypes function, and how to call it fast (or None)
 
@@ -67,23 +101,17 @@ def _library():
     global _bound, _entry
     lib = load_library()
     if _bound is not lib:
-        sink, cache = ctypes.POINTER(_SinkProblem), ctypes.POINTER(_CacheProblem)
-        lib.na_sink_forward.argtypes = [sink] + [_vp] * 7
-        lib.na_sink_backward.argtypes = [sink] + [_vp] * 11 + [ctypes.c_size_t, _vp]
-        lib.na_sink_backward_workspace.argtypes = [sink]
-        lib.na_sink_backward_workspace.restype = ctypes.c_size_t
-        lib.na_cache_tables.argtypes = [_i64] * 5 + [_vp] * 10
-        lib.na_cache_write.argtypes = [cache] + [_vp] * 6
-        lib.na_cache_attention.argtypes = ([cache] + [_vp] * 9 + [ctypes.c_size_t, _vp])
-        lib.na_cache_attention_workspace.argtypes = [cache]
-        lib.na_cache_attention_workspace.restype = ctypes.c_size_t
+        for name, types in _SIGNATURES.items():
+            getattr(lib, name).argtypes = types
+        for name, problem in _WORKSPACES.items():
+            fn = getattr(lib, name)
+            fn.argtypes, fn.restype = [ctypes.POINTER(problem)], ctypes.c_size_t
         try:
             from ._na_fast import call
         except ImportError:
             call = None
         entry = {}
-        for name in ("na_sink_forward", "na_sink_backward", "na_cache_tables", "na_cache_write",
-                     "na_cache_attention"):
+        for name in _SIGNATURES:
             fn = getattr(lib, name)
             if call is None:
                 # the problem goes by address in the fast form; ctypes takes it as a pointer
@@ -429,6 +457,14 @@ def _attention_plan(kernel_size, sinks, scale, max_new, max_context, metas):
     """The problem of na_cache_attention (kept alive by the cache's entry), its address, its
     workspace's size, and the layout of out and the logsumexp's shape where the call makes them.
     metas: of q, k_pages, v_pages, page_table, context_lens, cu_new, out and lse."""
+    p = _attention_problem(kernel_size, sinks, scale, max_new, max_context, metas)
+    q = metas[0]
+    return (p, ctypes.addressof(p), _library().na_cache_attention_workspace(p), _layout(q),
+            _lse_shape(q))
+
+
+def _attention_problem(kernel_size, sinks, scale, max_new, max_context, metas):
+    """The checks of new tokens against the cache, and their problem."""
     q, k_pages, v_pages, table, context, cu_new, out, lse = metas
     if len(q[0]) != 3:
         raise ValueError("expected q [tokens, heads, head_dim]")
@@ -455,8 +491,7 @@ def _attention_plan(kernel_size, sinks, scale, max_new, max_context, metas):
         0 if max_context is None else _count(max_context, "max_context", 0))
     p.q, p.out = _token_strides(q), _token_strides(out)
     p.dtype, p.scale = DTYPES[q[2]], 1.0 / math.sqrt(D) if scale is None else float(scale)
-    return (p, ctypes.addressof(p), _library().na_cache_attention_workspace(p), _layout(q),
-            _lse_shape(q))
+    return p
 
 
 def cache_attention(q, k_pages, v_pages, page_table, context_lens, cu_new, kernel_size=None,
