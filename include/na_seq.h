@@ -206,13 +206,18 @@ typedef struct {
  * first[r] (int32 [requests] or NULL: none), of keys that no new token sees, and of requests
  * without new tokens are left as they were.  A page outside the pool reads as zero keys.
  * Deterministic: the same inputs give the same bits.  Weights must overlap no input.
+ * max_new and max_context as in na_cache_attention.
+ * workspace: na_cache_weights_workspace(problem) bytes (it may be 0: then NULL is fine);
+ * NA_ERR_WORKSPACE if workspace_bytes is less.
  * NA_ERR_SHAPE: what na_cache_attention refuses of these arguments; capacity is negative,
  * or requests * kv_heads * capacity reaches 2^40; or requests * kv_heads reaches 2^20.
  */
+size_t na_cache_weights_workspace(const na_weights_problem* problem);
 na_status na_cache_weights(const na_weights_problem* problem, const void* q,
                            const float* logsumexp, const void* k_pages, const int32_t* page_table,
                            const int32_t* context_lens, const int32_t* cu_new,
-                           const int32_t* first, float* weights, na_stream_t stream);
+                           const int32_t* first, float* weights, void* workspace,
+                           size_t workspace_bytes, na_stream_t stream);
 
 typedef struct {
     int64_t requests, kv_heads, head_dim;

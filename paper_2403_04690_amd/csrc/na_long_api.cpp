@@ -136,58 +136,101 @@ na_status na_cache_shared_attention(const na_shared_problem* problem, const void
                : NA_ERR_HIP;
 }
 
-na_status na_cache_weights(const na_weights_problem* problem, const void* q,
-                           const float* logsumexp, const void* k_pages, const int32_t* page_table,
-                           const int32_t* context_lens, const int32_t* cu_new,
-                           const int32_t* first, float* weights, na_stream_t stream) {
-    if (!problem) return NA_ERR_NULL;
-    const na_cache_problem& p = problem->cache;
+static na_status check_weights(const na_weights_problem& w) {
+    const na_cache_problem& p = w.cache;
     const na_status st = check_attention(p, false);
     if (st != NA_OK) return st;
     const int64_t slices = p.requests * p.kv_heads;
-    if (problem->capacity < 0 || problem->capacity >= (int64_t(1) << 40) ||
-        slices >= (int64_t(1) << 20) ||
-        (__int128)slices * problem->capacity >= ((__int128)1 << 40))
+    if (w.capacity < 0 || w.capacity >= (int64_t(1) << 40) || slices >= (int64_t(1) << 20) ||
+        (__int128)slices * w.capacity >= ((__int128)1 << 40))
         return NA_ERR_SHAPE;
-    if (nothing(p) || problem->capacity == 0) return NA_OK;
-    if (!q || !logsumexp || !context_lens || !cu_new || !weights || (p.pages > 0 && !k_pages) ||
-        (p.max_pages > 0 && !page_table))
-        return NA_ERR_NULL;
-    if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(logsumexp, 4) ||
-        !aligned(weights, 4) || !aligned(page_table, 4) || !aligned(context_lens, 4) ||
-        !aligned(cu_new, 4) || !aligned(first, 4))
-        return NA_ERR_ALIGNMENT;
-    na::WeightsGeo w;
+    return NA_OK;
+}
+
+// The cut of the work.  Few rows: chunks of 8 to 64 key tiles (what a workgroup sums up at a time),
+// 2048 workgroups or more.  Many: 8 key tiles to a workgroup, whose rows are shared by as many as
+// leave each 32 blocks of 32 rows, or 8 where there would be fewer than 1024 workgroups.
+static void fill_weights(const na_weights_problem& problem, na::WeightsGeo& w) {
+    const na_cache_problem& p = problem.cache;
     std::memset(&w, 0, sizeof w);
     na::SeqGeo& g = w.g;
     fill_common(g, p.heads, p.kv_heads, p.kernel_size, p.sinks, p.scale);
     fill_paged(p, g);
     w.form = cache_narrow(p) ? 0 : 1;
-    w.capacity = problem->capacity;
-    w.first = first;
-    w.lse = logsumexp;
-    w.weights = weights;
-    g.context = context_lens;
-    g.cu = cu_new;
-    g.table = page_table;
-    // Key tiles of a request over workgroups.
+    w.capacity = problem.capacity;
+    const int64_t slices = p.requests * p.kv_heads, busy = std::min(p.requests, p.tokens) * p.kv_heads;
     const int64_t room = p.max_pages * p.page_size;
     const int64_t most = p.max_new > 0 ? std::min(p.max_new, p.tokens) : p.tokens;
     int64_t keys = p.max_context > 0 ? std::min(p.max_context, room) : room;
     keys = std::min(keys, (int64_t)g.W + g.S + most + 64);
     const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32 + 1);
-    int64_t chunk;
+    int64_t chunk = 8;
     if (w.form == 0) {
-        const int64_t split = std::max<int64_t>(1, 2048 / slices);
-        chunk = std::max<int64_t>(8, (tiles + split - 1) / split);
-    } else {
-        chunk = 8;
+        const int64_t split = std::max<int64_t>(1, 2048 / busy);
+        chunk = std::min<int64_t>(64, std::max<int64_t>(8, (tiles + split - 1) / split));
     }
     chunk = std::max(chunk, (tiles * slices + kMaxGrid / 2 - 1) / (kMaxGrid / 2));
     chunk = (chunk + 7) / 8 * 8;
     g.chunk = (int)chunk;
     g.nsplit = (int)((tiles + chunk - 1) / chunk);
     g.fd_tiles.init(g.nsplit);
+    int64_t shares = 1;
+    if (w.form == 1) {
+        // (rows that see any of the 256 keys of a workgroup)
+        const int64_t rows = std::min(most, (int64_t)g.W + 256) * g.G, blocks = (rows + 31) / 32;
+        shares = blocks / 32;
+        const int64_t fill = 1024 / (busy * g.nsplit);
+        shares = std::max(shares, std::min(fill, blocks / 8));
+        shares = std::min<int64_t>(std::max<int64_t>(shares, 1), 32);
+        shares = std::min(shares, std::max<int64_t>(1, (kMaxGrid - 1) / (slices * g.nsplit)));
+    }
+    w.shares = (int)shares;
+    w.fd_shares.init(w.shares);
+    w.part_keys = (int64_t)g.nsplit * g.chunk * 32;
+    w.joins = (int)((int64_t)g.nsplit * g.chunk / 8);
+    w.fd_joins.init(w.joins);
+}
+
+static size_t weights_bytes(const na::WeightsGeo& w) {
+    return w.shares == 1 ? 0 : (size_t)w.shares * w.g.B * w.g.Hkv * w.part_keys * 4;
+}
+
+size_t na_cache_weights_workspace(const na_weights_problem* problem) {
+    if (!problem || check_weights(*problem) != NA_OK || nothing(problem->cache)) return 0;
+    na::WeightsGeo w;
+    fill_weights(*problem, w);
+    return weights_bytes(w);
+}
+
+na_status na_cache_weights(const na_weights_problem* problem, const void* q,
+                           const float* logsumexp, const void* k_pages, const int32_t* page_table,
+                           const int32_t* context_lens, const int32_t* cu_new,
+                           const int32_t* first, float* weights, void* workspace,
+                           size_t workspace_bytes, na_stream_t stream) {
+    if (!problem) return NA_ERR_NULL;
+    const na_cache_problem& p = problem->cache;
+    const na_status st = check_weights(*problem);
+    if (st != NA_OK) return st;
+    if (nothing(p) || problem->capacity == 0) return NA_OK;
+    if (!q || !logsumexp || !context_lens || !cu_new || !weights || (p.pages > 0 && !k_pages) ||
+        (p.max_pages > 0 && !page_table))
+        return NA_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(k_pages, 16) || !aligned(logsumexp, 4) ||
+        !aligned(weights, 4) || !aligned(page_table, 4) || !aligned(context_lens, 4) ||
+        !aligned(cu_new, 4) || !aligned(first, 4) || !aligned(workspace, 4))
+        return NA_ERR_ALIGNMENT;
+    na::WeightsGeo w;
+    fill_weights(*problem, w);
+    const size_t need = weights_bytes(w);
+    if (workspace_bytes < need) return NA_ERR_WORKSPACE;
+    if (need && !workspace) return NA_ERR_NULL;
+    w.first = first;
+    w.lse = logsumexp;
+    w.weights = weights;
+    w.part = static_cast<float*>(workspace);
+    w.g.context = context_lens;
+    w.g.cu = cu_new;
+    w.g.table = page_table;
     return na::launch_cache_weights(w, (int)p.head_dim, p.dtype, q, k_pages,
                                     reinterpret_cast<hipStream_t>(stream)) == hipSuccess
                ? NA_OK
@@ -218,7 +261,7 @@ static na_status check_evict(const na_evict_problem& p) {
 size_t na_cache_evict_workspace(const na_evict_problem* problem) {
     if (!problem || check_evict(*problem) != NA_OK) return 0;
     const size_t slices = (size_t)(problem->requests * problem->kv_heads);
-    return slices * (2 * (size_t)problem->budget + 1) * 4;
+    return slices * (2 * (size_t)problem->budget + 2) * 4;
 }
 
 na_status na_cache_evict(const na_evict_problem* problem, const float* weights,
@@ -261,6 +304,12 @@ na_status na_cache_evict(const na_evict_problem* problem, const float* weights,
     v.lgrow = v.lgslice = __builtin_ctzll(row);
     const int64_t slices = p.requests * p.kv_heads;
     while (v.lgslice > 6 && (slices * 2 << (v.lgrow - v.lgslice)) < 1024) --v.lgslice;
+    // (2048 workgroups, most of which may find nothing to move)
+    const int64_t most = std::max<int64_t>(1, std::min(p.budget, p.max_pages * p.page_size));
+    const int64_t chunks = std::min((most + 127) / 128, std::max<int64_t>(1, 1024 / std::max<int64_t>(1, slices)));
+    v.chunk = (int)((most + chunks - 1) / chunks);
+    v.chunks = (int)((most + v.chunk - 1) / v.chunk);
+    v.fd_chunks.init(v.chunks);
     v.capacity = p.capacity;
     v.fd_kv.init(v.Hkv);
     v.weights = reinterpret_cast<const uint32_t*>(weights);
@@ -274,7 +323,7 @@ na_status na_cache_evict(const na_evict_problem* problem, const float* weights,
     v.new_head = new_head;
     v.new_weights = reinterpret_cast<uint32_t*>(new_weights);
     v.moves = static_cast<int32_t*>(workspace);
-    v.to = v.moves + slices;
+    v.to = v.moves + 2 * slices;
     v.from = v.to + slices * p.budget;
     return na::launch_cache_evict(v, k_pages, v_pages, reinterpret_cast<hipStream_t>(stream)) ==
                    hipSuccess

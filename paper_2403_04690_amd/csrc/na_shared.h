@@ -32,7 +32,12 @@ hipError_t launch_shared_attention(const SharedGeo& s, int D, int dtype, const v
 struct WeightsGeo {
     SeqGeo g;
     int64_t capacity;      // weights of a (request, key/value head)
-    int form;              // see na_weights.hip
+    int form;              // 0: few rows, 1: many
+    int shares;            // workgroups that share the rows of the same keys (form 1)
+    int joins;             // workgroups that add up the shares of a (request, key/value head)
+    FastDiv fd_shares, fd_joins;
+    int64_t part_keys;     // sums of a (request, key/value head) in part[shares][..][part_keys]
+    float* part;
     const int32_t* first;  // keys before it gather nothing, or null
     const float* lse;
     float* weights;
@@ -44,15 +49,16 @@ hipError_t launch_cache_weights(const WeightsGeo& w, int D, int dtype, const voi
 struct EvictGeo {
     int R, Hkv, budget, recent, lgps, pages, max_pages, num_free;
     int lgrow;    // log2 of a key's bytes
-    int lgslice;  // log2 of the bytes of a row that a workgroup moves
+    int lgslice;  // log2 of the bytes of a row that a workgroup moves in order
+    int chunk, chunks;  // rows that a workgroup moves in any order, such workgroups of K or V
     int64_t capacity;
-    FastDiv fd_kv;
+    FastDiv fd_kv, fd_chunks;
     const uint32_t* weights;  // (the bits of fp32)
     uint32_t* new_weights;
     const int32_t *context, *first, *table, *head;
     int32_t *free_pages, *new_context, *kept, *new_head;
-    // by (request, key/value head): how many rows move to the place of another, [.][budget] the
-    // places that they get and where they are
+    // by (request, key/value head): how many rows move to the place of another, and how many of
+    // them from positions below the budget; [.][budget] the places that they get, where they are
     int32_t *moves, *to, *from;
 };
 

@@ -4,8 +4,9 @@
 //   w[r, c, j] += sum over the new tokens i of request r and the query heads h of key/value head c of
 //                 exp(scale q_ih . k_jc - lse_ih),   j seen by i,
 //
-// from the logsumexp that the tokens' attention returned.  A key's sum is one workgroup's alone, so
-// nothing is joined and the order of every sum is fixed.
+// from the logsumexp that the tokens' attention returned.  A key's sum is one workgroup's alone, or
+// where few keys meet many rows that of a few, each with a share of the rows, whose sums a second
+// launch adds up: the order of every sum is fixed.
 //
 //   S = Q K^T (32 rows x 32 keys a step) leaves a key in one lane column (two lanes), whose entries
 // are rows: a lane adds up its own exponentials, and the two halves meet once at the end.
@@ -170,14 +171,18 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void weights_few_kernel(
                 f32x16 s = f32x16{} * 0.f;
 #pragma unroll
                 for (int x = 0; x < F::kKS; ++x) s = mma32<T>(qf[x], kf[x], s);
-                const unsigned m = seen_rows(g, t.pos0, row0 + 4 * h, j);
+                // (rows in order of their positions; the tile's keys seen by all of them)
+                const int pa = t.pos0 + g.fd_G.div(row0);
+                const bool full = pa >= j0 + 31 && (t.pmax - j0 < g.W || j0 + 31 < g.S);
+                const unsigned m = full ? ~0u : seen_rows(g, t.pos0, row0 + 4 * h, j);
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
-                    if (row0 + 8 * b >= t.rows) break;
+                    if (row0 + 8 * b >= t.rows) continue;
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
                         const int i = 4 * b + x;
-                        sum += fast_exp2(keep(m, i, fmaf(s[i], g.c, -lse[i]), -INFINITY));
+                        const float y = fmaf(s[i], g.c, -lse[i]);
+                        sum += fast_exp2(full ? y : keep(m, i, y, -INFINITY));
                     }
                 }
             }
@@ -227,7 +232,8 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsGeo w,
     const SeqGeo& g = w.g;
     const int lane = threadIdx.x & 63;
     const int wave = uniform((threadIdx.x >> 6) & 3);
-    const int id = xcd_remap(blockIdx.x, gridDim.x);
+    const int id = w.fd_shares.div(xcd_remap(blockIdx.x, gridDim.x));
+    const int share = xcd_remap(blockIdx.x, gridDim.x) - id * w.shares;
     const int slice = g.fd_tiles.div(id);
     const int split = id - slice * g.nsplit;
     const int r = g.fd_kv.div(slice), kvh = slice - r * g.Hkv;
@@ -294,8 +300,16 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsGeo w,
         const int ta = max(ja - t.pos0, 0);
         const int tb = (int)min((int64_t)t.valid, ja < g.S ? (int64_t)t.valid
                                                            : (int64_t)jb - t.pos0 + g.W);
-        const int b0 = ta < tb ? ta * g.G >> 5 : 0;
-        const int b1 = ta < tb && jb >= first ? (tb * g.G + 31) >> 5 : b0;
+        int b0 = ta < tb ? ta * g.G >> 5 : 0;
+        int b1 = ta < tb && jb >= first ? (tb * g.G + 31) >> 5 : b0;
+        const bool shared = w.shares > 1 && pass < g.nsplit * g.chunk;
+        if (shared) {  // this workgroup's share of them
+            const int each = (b1 - b0 + w.shares - 1) / w.shares;
+            b0 = min(b0 + share * each, b1);
+            b1 = min(b0 + each, b1);
+        } else if (share > 0) {  // (keys behind the caller's bound: one workgroup's)
+            break;
+        }
 #pragma unroll
         for (int k = 0; k < KT; ++k)
 #pragma unroll
@@ -349,10 +363,32 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsGeo w,
         for (int k = 0; k < KT; ++k) {
             const float total = col_sum<32>(sum[k]);
             const int j = j0[k] + lane;
-            if (on[k] && h == 0 && j >= first && j < w.capacity && t.sees(g, j))
+            if (shared) {
+                if (e + k < c1 && h == 0)
+                    w.part[((int64_t)share * g.B * g.Hkv + slice) * w.part_keys + (e + k) * 32 + lane] =
+                        total;
+            } else if (on[k] && h == 0 && j >= first && j < w.capacity && t.sees(g, j))
                 w.weights[weights_at(w, r, kvh) + j] += total;
         }
     }
+}
+
+// Adds up the row shares of each key: a workgroup for 256 keys.
+__global__ __launch_bounds__(256) void weights_join_kernel(WeightsGeo w) {
+    const SeqGeo& g = w.g;
+    const int slice = w.fd_joins.div(blockIdx.x);
+    const int e = (blockIdx.x - slice * w.joins) * 8 + (threadIdx.x >> 5);
+    const int r = g.fd_kv.div(slice), kvh = slice - r * g.Hkv;
+    SeqTile t;
+    if (!weights_request(g, r, t) || e >= min(t.nT, g.nsplit * g.chunk)) return;
+    const int first = w.first ? max(w.first[r], 0) : 0;
+    const int j = t.tile(e) + (threadIdx.x & 31);
+    if (j < first || j >= w.capacity || !t.sees(g, j)) return;
+    const float* part = w.part + slice * w.part_keys + e * 32 + (threadIdx.x & 31);
+    float sum = 0.f;
+#pragma unroll 8
+    for (int x = 0; x < w.shares; ++x) sum += part[(int64_t)x * g.B * g.Hkv * w.part_keys];
+    w.weights[weights_at(w, r, kvh) + j] += sum;
 }
 
 // ---- host ----
@@ -360,7 +396,7 @@ template <typename T, int D>
 hipError_t launch_weights(const WeightsGeo& w, const void* q, const void* k, hipStream_t st) {
     auto q_ = static_cast<const T*>(q);
     auto k_ = static_cast<const T*>(k);
-    const unsigned grid = (unsigned)w.g.B * w.g.Hkv * w.g.nsplit;
+    const unsigned slices = (unsigned)w.g.B * w.g.Hkv, grid = slices * w.g.nsplit * w.shares;
     hipError_t e;
     if (w.form == 0) {
         constexpr size_t lds = kFewWaves * 2 * SeqFrags<T, D>::kTile + kFewTiles * 32 * 4;
@@ -372,6 +408,10 @@ hipError_t launch_weights(const WeightsGeo& w, const void* q, const void* k, hip
         auto kern = weights_many_kernel<T, D>;
         if ((e = seq_allow_lds(kern, lds)) != hipSuccess) return e;
         hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, st, w, q_, k_);
+        if (w.shares > 1) {
+            if ((e = hipGetLastError()) != hipSuccess) return e;
+            hipLaunchKernelGGL(weights_join_kernel, dim3(slices * w.joins), dim3(256), 0, st, w);
+        }
     }
     return hipGetLastError();
 }

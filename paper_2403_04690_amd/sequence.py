@@ -82,13 +82,14 @@ _SIGNATURES = {
     "na_cache_attention": [ctypes.POINTER(_CacheProblem)] + [_vp] * 9 + [ctypes.c_size_t, _vp],
     "na_cache_shared_attention": ([ctypes.POINTER(_SharedProblem)] + [_vp] * 11
                                   + [ctypes.c_size_t, _vp]),
-    "na_cache_weights": [ctypes.POINTER(_WeightsProblem)] + [_vp] * 9,
+    "na_cache_weights": [ctypes.POINTER(_WeightsProblem)] + [_vp] * 9 + [ctypes.c_size_t, _vp],
     "na_cache_evict": [ctypes.POINTER(_EvictProblem)] + [_vp] * 13 + [ctypes.c_size_t, _vp],
 }
 _WORKSPACES = {
     "na_sink_backward_workspace": _SinkProblem,
     "na_cache_attention_workspace": _CacheProblem,
     "na_cache_shared_attention_workspace": _SharedProblem,
+    "na_cache_weights_workspace": _WeightsProblem,
     "na_cache_evict_workspace": _EvictProblem,
 }
 

@@ -100,8 +100,8 @@ def _check_first(first, requests, device):
 
 @functools.lru_cache(maxsize=256)
 def _weights_plan(kernel_size, sinks, scale, max_new, max_context, metas):
-    """The problem of na_cache_weights (kept alive by the cache's entry) and its address.  metas:
-    of q, lse, k_pages, page_table, context_lens, cu_new, weights and first."""
+    """The problem of na_cache_weights (kept alive by the cache's entry), its address and its
+    workspace's size.  metas: of q, lse, k_pages, page_table, context_lens, cu_new, weights and first."""
     q, lse, k_pages, table, context, cu_new, weights, first = metas
     if lse is None:
         raise ValueError("lse is needed")
@@ -110,7 +110,7 @@ def _weights_plan(kernel_size, sinks, scale, max_new, max_context, metas):
     _check_weights("weights", weights, context[0][0], k_pages[0][1], q[3])
     _check_first(first, context[0][0], q[3])
     p = _WeightsProblem(problem, weights[0][2])
-    return p, ctypes.addressof(p)
+    return p, ctypes.addressof(p), _library().na_cache_weights_workspace(p)
 
 
 def cache_weights(q, lse, k_pages, page_table, context_lens, cu_new, weights, kernel_size=None,
@@ -123,12 +123,14 @@ def cache_weights(q, lse, k_pages, page_table, context_lens, cu_new, weights, ke
     sinks and scale.  Entries before first[r] (int32 [requests]; None: 0) are left as they
     were.  Start a request's entries at 0."""
     _library()
-    p, at = _weights_plan(*_window(kernel_size, sinks, scale), *_bounds(max_new, max_context),
+    p, at, need = _weights_plan(*_window(kernel_size, sinks, scale), *_bounds(max_new, max_context),
                           _metas(q, lse, k_pages, page_table, context_lens, cu_new, weights,
                                  first))
+    work = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     _call("na_cache_weights", q.device, at, q.data_ptr(), lse.data_ptr(), k_pages.data_ptr(),
           page_table.data_ptr(), context_lens.data_ptr(), cu_new.data_ptr(),
-          0 if first is None else first.data_ptr(), weights.data_ptr())
+          0 if first is None else first.data_ptr(), weights.data_ptr(),
+          work.data_ptr() if need else 0, need)
 
 
 @functools.lru_cache(maxsize=256)

@@ -506,17 +506,17 @@ def test_evict(na, context, Hkv, D, page, dtype, budget, recent, first, ties):
 
 @pytest.mark.parametrize("n,budget,recent", [
     (9000, 100, 10), (9000, 8500, 600), (5000, 4097, 4000), (4096, 4095, 0), (12289, 4096, 4096),
-    (30000, 1, 0)])
+    (30000, 1, 0), (32768, 20000, 0), (40000, 5000, 100), (33001, 33000, 1), (70001, 40000, 7)])
 def test_evict_of_long_contexts(na, n, budget, recent):
     _evict_check(na, _weights(2, 1, n, ties=n % 2 == 0), [n, n - 1], 32, 64, "fp16", budget, recent,
                  [3, 0])
 
 
 def test_evict_of_equal_weights_keeps_the_first(na):
-    for value in (0.0, 1.0, -2.5, math.inf, -math.inf, math.nan):
-        w = torch.full((1, 1, 9000), value)
-        got = _evict_check(na, w, [9000], 32, 64, "fp32", 5000, 7)
-        assert got[2][0, 0].tolist() == list(range(4993)) + list(range(8993, 9000))
+    for value, n in ((v, n) for v in (0.0, 1.0, -2.5, math.inf, -math.inf, math.nan) for n in (9000, 36000)):
+        w = torch.full((1, 1, n), value)
+        got = _evict_check(na, w, [n], 32, 64, "fp32", 5000, 7)
+        assert got[2][0, 0].tolist() == list(range(4993)) + list(range(n - 7, n))
 
 
 def test_evict_of_weights_that_are_no_numbers(na):
@@ -526,7 +526,7 @@ def test_evict_of_weights_that_are_no_numbers(na):
     odd = torch.tensor([math.nan, -math.nan, math.inf, -math.inf, 0.0, -0.0, 1e-45, -1e-45,
                         torch.finfo(torch.float32).max, -torch.finfo(torch.float32).max, 1.0,
                         1.0 + 2.0 ** -23, 1.0 - 2.0 ** -24, -1.0, -1.0 - 2.0 ** -23])
-    for n, budget in ((40, 20), (300, 100), (300, 290), (5000, 2500)):
+    for n, budget in ((40, 20), (300, 100), (300, 290), (5000, 2500), (40000, 11111)):
         w = odd[torch.randint(0, odd.numel(), (2, 2, n), generator=gen)]
         _evict_check(na, w, [n, n - 3], 32, 16, "fp32", budget, 3)
 
