@@ -148,8 +148,8 @@ static na_status check_weights(const na_weights_problem& w) {
 }
 
 // The cut of the work.  Few rows: chunks of 8 to 64 key tiles (what a workgroup sums up at a time),
-// 2048 workgroups or more.  Many: 8 key tiles to a workgroup, whose rows are shared by as many as
-// leave each 32 blocks of 32 rows, or 8 where there would be fewer than 1024 workgroups.
+// 8192 workgroups if every request had the most keys.  Many: 8 key tiles to a workgroup, whose rows are shared by as many as
+// leave each 1024 rows, or 128 where there would be fewer than 1024 workgroups.
 static void fill_weights(const na_weights_problem& problem, na::WeightsGeo& w) {
     const na_cache_problem& p = problem.cache;
     std::memset(&w, 0, sizeof w);
@@ -166,7 +166,7 @@ static void fill_weights(const na_weights_problem& problem, na::WeightsGeo& w) {
     const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32 + 1);
     int64_t chunk = 8;
     if (w.form == 0) {
-        const int64_t split = std::max<int64_t>(1, 2048 / busy);
+        const int64_t split = std::max<int64_t>(1, 8192 / busy);
         chunk = std::min<int64_t>(64, std::max<int64_t>(8, (tiles + split - 1) / split));
     }
     chunk = std::max(chunk, (tiles * slices + kMaxGrid / 2 - 1) / (kMaxGrid / 2));
@@ -177,15 +177,15 @@ static void fill_weights(const na_weights_problem& problem, na::WeightsGeo& w) {
     int64_t shares = 1;
     if (w.form == 1) {
         // (rows that see any of the 256 keys of a workgroup)
-        const int64_t rows = std::min(most, (int64_t)g.W + 256) * g.G, blocks = (rows + 31) / 32;
-        shares = blocks / 32;
+        const int64_t rows = std::min(most, (int64_t)g.W + 256) * g.G;
         const int64_t fill = 1024 / (busy * g.nsplit);
-        shares = std::max(shares, std::min(fill, blocks / 8));
+        shares = std::max(rows / 1024, std::min(fill, rows / 128));
         shares = std::min<int64_t>(std::max<int64_t>(shares, 1), 32);
         shares = std::min(shares, std::max<int64_t>(1, (kMaxGrid - 1) / (slices * g.nsplit)));
+        while (shares & (shares - 1)) shares &= shares - 1;
     }
     w.shares = (int)shares;
-    w.fd_shares.init(w.shares);
+    w.lgshares = __builtin_ctz(w.shares);
     w.part_keys = (int64_t)g.nsplit * g.chunk * 32;
     w.joins = (int)((int64_t)g.nsplit * g.chunk / 8);
     w.fd_joins.init(w.joins);

@@ -33,9 +33,9 @@ struct WeightsGeo {
     SeqGeo g;
     int64_t capacity;      // weights of a (request, key/value head)
     int form;              // 0: few rows, 1: many
-    int shares;            // workgroups that share the rows of the same keys (form 1)
+    int shares, lgshares;  // workgroups that share the rows of the same keys (form 1)
     int joins;             // workgroups that add up the shares of a (request, key/value head)
-    FastDiv fd_shares, fd_joins;
+    FastDiv fd_joins;
     int64_t part_keys;     // sums of a (request, key/value head) in part[shares][..][part_keys]
     float* part;
     const int32_t* first;  // keys before it gather nothing, or null

@@ -86,22 +86,32 @@ __device__ __forceinline__ float row_lse(const WeightsGeo& w, const SeqTile& t, 
     return w.lse[(int64_t)(t.qtok + tok) * g.lt + (int64_t)kvh * g.G + head] * kLog2e;
 }
 
-constexpr int kFewWaves = 4;
 constexpr int kFewTiles = 64;  // key tiles whose sums are in LDS at a time
 
-// Few rows (one block of 32: single tokens): each wave takes every fourth key tile of the split,
-// from LDS buffers of its own.  Bound by reading the keys once.
 template <typename T, int D>
-__global__ __launch_bounds__(kFewWaves * 64, 1) void weights_few_kernel(
+struct WeightsFew {
+    static constexpr int kTile = SeqFrags<T, D>::kTile;
+    static constexpr int kWaves = 4;
+    static constexpr int kLds = kWaves * kTile + kFewTiles * 32 * 4;
+};
+
+// Few rows (one block of 32: single tokens): each wave takes every kWaves-th key tile of the split,
+// from an LDS buffer of its own, which the next tile's loads may fill as soon as its operands are in
+// registers.  Bound by reading the keys once.
+//   (More waves with one buffer each read faster than few with several: three waves with three
+// buffers 176 us where four with two take 131 ..)
+template <typename T, int D>
+__global__ __launch_bounds__((WeightsFew<T, D>::kWaves * 64), 1) void weights_few_kernel(
     WeightsGeo w, const T* __restrict__ qg, const T* __restrict__ kg) {
     using F = SeqFrags<T, D>;
     using R = SeqRows<T, D>;
-    constexpr int W = kFewWaves;
+    using L = WeightsFew<T, D>;
+    constexpr int W = L::kWaves;
     extern __shared__ __align__(16) unsigned char smem[];
-    float* sums = reinterpret_cast<float*>(smem + W * 2 * F::kTile);
+    float* sums = reinterpret_cast<float*>(smem + W * F::kTile);
     const SeqGeo& g = w.g;
     const int lane = threadIdx.x & 63;
-    const int wave = uniform((threadIdx.x >> 6) & (W - 1));
+    const int wave = uniform(threadIdx.x >> 6);
     const int slice = g.fd_tiles.div(blockIdx.x);
     const int split = blockIdx.x - slice * g.nsplit;
     const int r = g.fd_kv.div(slice), kvh = slice - r * g.Hkv;
@@ -116,19 +126,36 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void weights_few_kernel(
     rows.init(lane);
     const unsigned char* kb = reinterpret_cast<const unsigned char*>(kg) + kvh * g.kh;
     const uint32_t klane = rows.rowl * (uint32_t)g.kt;
-    auto issue = [&](int e, unsigned char* dst) __attribute__((always_inline)) {
+    // The pages of the kFewTiles tiles from `pass` on, a lane each (pages hold whole blocks of 16
+    // keys): looked up once, not with every tile in front of its loads.
+    int page0 = -1, page1 = -1;
+    auto look_up = [&](int pass) __attribute__((always_inline)) {
+        const int32_t* row = g.table + (int64_t)r * g.max_pages;
+        const int col0 = t.tile(pass + lane) >> g.lgps, col1 = (t.tile(pass + lane) + 16) >> g.lgps;
+        page0 = pass + lane < e1 && col0 < g.max_pages ? row[col0] : -1;
+        page1 = pass + lane < e1 && col1 < g.max_pages ? row[col1] : -1;
+    };
+    auto issue = [&](int pass, int e, unsigned char* dst) __attribute__((always_inline)) {
         const int j0 = t.tile(e);
-        // (pages hold whole blocks of 16 keys)
-        const int64_t at0 = key_offset(g, r, j0), at1 = key_offset(g, r, j0 + 16);
+        const int id0 = __builtin_amdgcn_readlane(page0, e - pass);
+        const int id1 = __builtin_amdgcn_readlane(page1, e - pass);
+        const bool ok0 = (unsigned)id0 < (unsigned)g.pages, ok1 = (unsigned)id1 < (unsigned)g.pages;
+        const int in = (1 << g.lgps) - 1, kt = (int)g.kt;
+        const unsigned char* b0 = kb + (int64_t)(ok0 ? id0 : 0) * (int)g.kb + (j0 & in) * kt;
+        const unsigned char* b1 = kb + (int64_t)(ok1 ? id1 : 0) * (int)g.kb + ((j0 + 16) & in) * kt;
+        const bool fast = ok0 && ok1 && t.whole(g, j0);
 #pragma unroll
         for (int n = 0; n < R::kInstr; ++n) {
             const int r0 = n * R::kRpi;
-            const int64_t at = r0 >= 16 ? at1 : at0;
-            const bool see = at >= 0 && t.sees(g, j0 + r0 + rows.rowl);
-            const unsigned char* base = kb + (at >= 0 ? at : 0) + (r0 & 15) * (int)g.kt;
-            seq_load(see ? base + rows.off(n, klane)
-                         : reinterpret_cast<const unsigned char*>(&kZeroRow),
-                     dst + n * 1024);
+            const unsigned char* base = (r0 >= 16 ? b1 : b0) + (r0 & 15) * kt;
+            const uint32_t off = rows.off(n, klane);
+            if (fast) {
+                seq_load(base, off, dst + n * 1024);
+            } else {
+                const bool see = (r0 >= 16 ? ok1 : ok0) && t.sees(g, j0 + r0 + rows.rowl);
+                seq_load(see ? base + off : reinterpret_cast<const unsigned char*>(&kZeroRow),
+                         dst + n * 1024);
+            }
         }
     };
     F f;
@@ -136,45 +163,37 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void weights_few_kernel(
     const int h = lane >> 5;
     typename Tr<T>::x8 qf[F::kKS];
     float lse[16];
-    load_rows<T, D>(g, t, kvh, 0, qg, lane, qf);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) lse[i] = row_lse(w, t, kvh, entry_row(i) + 4 * h);
-#pragma unroll
-    for (int x = 0; x < F::kKS; ++x) settle(qf[x]);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(lse[i]));
-    unsigned char* buf0 = smem + wave * 2 * F::kTile;
+    unsigned char* buf = smem + wave * F::kTile;
 
-    for (int pass = e0; pass < e1; pass += kFewTiles) {
-        const int end = min(pass + kFewTiles, e1);
-        int e = pass + wave;
-        if (e < end) issue(e, buf0);
-        for (int buf = 0; e < end; e += W, buf ^= 1) {
-            if (e + W < end) {
-                issue(e + W, buf0 + (buf ^ 1) * F::kTile);
-                wait_vmem_but<R::kInstr>();
-            } else {
-                wait_vmem();
-            }
-            const unsigned char* tile = buf0 + buf * F::kTile;
-            typename Tr<T>::x8 kf[F::kKS];
-            f.rows(tile, kf);
-            const int j0 = t.tile(e), j = j0 + (lane & 31);
-            float sum = 0.f;
-            for (int row0 = 0; row0 < t.rows; row0 += 32) {
-                if (row0 > 0) {  // (more rows than the caller's bound says)
-                    load_rows<T, D>(g, t, kvh, row0, qg, lane, qf);
+    // (one block of rows unless there are more than the caller's bound says)
+    for (int row0 = 0; row0 < t.rows; row0 += 32) {
+        load_rows<T, D>(g, t, kvh, row0, qg, lane, qf);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        lse[i] = row_lse(w, t, kvh, row0 + entry_row(i) + 4 * h);
-                }
+        for (int i = 0; i < 16; ++i) lse[i] = row_lse(w, t, kvh, row0 + entry_row(i) + 4 * h);
+#pragma unroll
+        for (int x = 0; x < F::kKS; ++x) settle(qf[x]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) settle(lse[i]);
+        const int pa = t.pos0 + g.fd_G.div(row0);  // (rows in order of their positions)
+        for (int pass = e0; pass < e1; pass += kFewTiles) {
+            const int end = min(pass + kFewTiles, e1);
+            int e = pass + wave;
+            look_up(pass);
+            if (e < end) issue(pass, e, buf);
+            for (; e < end; e += W) {
+                wait_vmem();
+                typename Tr<T>::x8 kf[F::kKS];
+                f.rows(buf, kf);
+                wait_lds();
+                __builtin_amdgcn_sched_barrier(0);
+                if (e + W < end) issue(pass, e + W, buf);
                 f32x16 s = f32x16{} * 0.f;
 #pragma unroll
                 for (int x = 0; x < F::kKS; ++x) s = mma32<T>(qf[x], kf[x], s);
-                // (rows in order of their positions; the tile's keys seen by all of them)
-                const int pa = t.pos0 + g.fd_G.div(row0);
+                const int j0 = t.tile(e);
                 const bool full = pa >= j0 + 31 && (t.pmax - j0 < g.W || j0 + 31 < g.S);
-                const unsigned m = full ? ~0u : seen_rows(g, t.pos0, row0 + 4 * h, j);
+                const unsigned m = full ? ~0u : seen_rows(g, t.pos0, row0 + 4 * h, j0 + (lane & 31));
+                float sum = 0.f;
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
                     if (row0 + 8 * b >= t.rows) continue;
@@ -185,24 +204,32 @@ __global__ __launch_bounds__(kFewWaves * 64, 1) void weights_few_kernel(
                         sum += fast_exp2(full ? y : keep(m, i, y, -INFINITY));
                     }
                 }
+                sum = col_sum<32>(sum);
+                if (h == 0) sums[(e - pass) * 32 + lane] = sum;
             }
-            if (t.rows > 32) {  // the first block again
-                load_rows<T, D>(g, t, kvh, 0, qg, lane, qf);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) lse[i] = row_lse(w, t, kvh, entry_row(i) + 4 * h);
+            __syncthreads();
+            float* out = w.weights + weights_at(w, r, kvh);
+            for (int x = threadIdx.x; x < (end - pass) * 32; x += W * 64) {
+                const int j = t.tile(pass + (x >> 5)) + (x & 31);
+                if (j >= first && j < w.capacity && t.sees(g, j)) out[j] += sums[x];
             }
-            sum = col_sum<32>(sum);
-            if (h == 0) sums[(e - pass) * 32 + lane] = sum;
-            wait_lds();  // before the next loads into this buffer
+            __syncthreads();
         }
-        __syncthreads();
-        float* out = w.weights + weights_at(w, r, kvh);
-        for (int x = threadIdx.x; x < (end - pass) * 32; x += W * 64) {
-            const int j = t.tile(pass + (x >> 5)) + (x & 31);
-            if (j >= first && j < w.capacity && t.sees(g, j)) out[j] += sums[x];
-        }
-        __syncthreads();
     }
+}
+
+// The rows that see any key of the tiles [pass, end), in stages of 64.
+constexpr int kStageRows = 64;
+__device__ __forceinline__ void weights_stages(const WeightsGeo& w, const SeqTile& t, int pass, int end,
+                                               int first, int& b0, int& b1) {
+    const SeqGeo& g = w.g;
+    const int ja = t.tile(pass), jb = t.tile(end - 1) + 31;
+    const int ta = max(ja - t.pos0, 0);
+    const int tb = ja < g.S ? t.valid : (int)min((int64_t)t.valid, (int64_t)jb - t.pos0 + g.W);
+    b0 = b1 = 0;
+    if (ta >= tb || jb < first) return;
+    b0 = ta * g.G / kStageRows;
+    b1 = (tb * g.G + kStageRows - 1) / kStageRows;
 }
 
 // Key tiles of a wave in the form for many rows: two while their operands fit the registers of
@@ -211,8 +238,10 @@ template <typename T, int D>
 struct WeightsMany {
     static constexpr int kTiles = sizeof(T) == 4 && D == 128 ? 1 : 2;
     static constexpr int kStages = 3;
+    static constexpr int kBlocks = kStageRows / 32;
     static constexpr int kTile = SeqFrags<T, D>::kTile;
-    static constexpr int kStage = kTile + 4 * 256;  // rows, and each wave's copy of their lse
+    // rows, and each wave's copy of their lse
+    static constexpr int kStage = kBlocks * kTile + 4 * kBlocks * 128;
     static constexpr int kLds = kStages * kStage;
 };
 
@@ -225,15 +254,17 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsGeo w,
     using F = SeqFrags<T, D>;
     using R = SeqRows<T, D>;
     using M = WeightsMany<T, D>;
-    constexpr int KT = M::kTiles, NB = M::kStages;
-    constexpr int kShare = (R::kInstr + 3) / 4, kCount = kShare + 1;
-    static_assert(R::kInstr % 4 == 0 || R::kInstr < 4, "equal shares");
+    constexpr int KT = M::kTiles, NB = M::kStages, RB = M::kBlocks;
+    constexpr int kShare = RB * R::kInstr / 4, kCount = kShare + 1;
+    static_assert(RB * R::kInstr % 4 == 0 && RB == 2, "equal shares, a lane for each row's lse");
     extern __shared__ __align__(16) unsigned char smem[];
     const SeqGeo& g = w.g;
     const int lane = threadIdx.x & 63;
     const int wave = uniform((threadIdx.x >> 6) & 3);
-    const int id = w.fd_shares.div(xcd_remap(blockIdx.x, gridDim.x));
-    const int share = xcd_remap(blockIdx.x, gridDim.x) - id * w.shares;
+    // (neighbours on eight XCDs in turn: requests of any length load them alike, and with a power
+    // of two of shares an XCD's L2 holds the rows of only some.  Shares of a fixed number of rows
+    // instead, the same keys' on all XCDs: 270 us where these take 230)
+    const int id = blockIdx.x >> w.lgshares, share = blockIdx.x & (w.shares - 1);
     const int slice = g.fd_tiles.div(id);
     const int split = id - slice * g.nsplit;
     const int r = g.fd_kv.div(slice), kvh = slice - r * g.Hkv;
@@ -250,29 +281,70 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsGeo w,
     rows.init(lane);
     const unsigned char* kb = reinterpret_cast<const unsigned char*>(kg) + kvh * g.kh;
 
-    // Rows of block b, and their logsumexps, into stage `buf`: this wave's share.
+    // This wave's share of the loads of a stage: where row m of a load lies, and m's head.  A stage
+    // is 64 rows on from the one before it: dt tokens and dh heads.
+    struct Place {
+        const unsigned char* p;
+        int head;
+    };
+    const int dt = g.fd_G.div(kStageRows), dh = kStageRows - dt * g.G;
+    auto row_at = [&](int m) __attribute__((always_inline)) {
+        m = min(m, t.rows - 1);
+        const int tok = g.fd_G.div(m), head = m - tok * g.G;
+        return Place{reinterpret_cast<const unsigned char*>(qg) + ((int64_t)kvh * g.G + head) * g.qh +
+                         (int64_t)(t.qtok + tok) * g.qt, head};
+    };
+    auto lse_at = [&](int m) __attribute__((always_inline)) {
+        m = min(m, t.rows - 1);
+        const int tok = g.fd_G.div(m), head = m - tok * g.G;
+        return Place{reinterpret_cast<const unsigned char*>(w.lse) +
+                         4 * ((int64_t)(t.qtok + tok) * g.lt + (int64_t)kvh * g.G + head), head};
+    };
+    auto advance = [&](Place& x, int64_t token, int64_t head) __attribute__((always_inline)) {
+        x.p += dt * token + dh * head;
+        if (dh == 0) return;  // (uniform)
+        x.head += dh;
+        if (x.head >= g.G) {
+            x.head -= g.G;
+            x.p += token - g.G * head;
+        }
+    };
+    Place qp[kShare], lp;
+    auto begin = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kShare; ++u)
+            qp[u] = row_at(b * kStageRows + (wave + 4 * u) * R::kRpi + rows.rowl);
+        lp = lse_at(b * kStageRows + lane);
+    };
+    // Rows of stage b, and their logsumexps, into buffer `buf`; stages in order from begin's on.
     auto issue = [&](int b, int buf) __attribute__((always_inline)) {
         unsigned char* dst = smem + buf * M::kStage;
+        if ((b + 1) * kStageRows > t.rows) begin(b);  // (the last stage: rows that exist)
 #pragma unroll
         for (int u = 0; u < kShare; ++u) {
-            // (fewer than four: two waves bring the same)
-            const int n = R::kInstr < 4 ? wave % R::kInstr : wave + 4 * u;
-            const int m = min(b * 32 + n * R::kRpi + rows.rowl, t.rows - 1);
-            const int tok = g.fd_G.div(m), head = m - tok * g.G;
-            seq_load(reinterpret_cast<const unsigned char*>(qg) +
-                         ((int64_t)kvh * g.G + head) * g.qh + (int64_t)(t.qtok + tok) * g.qt +
-                         rows.off(n, 0),
-                     dst + n * 1024);
+            const int n = wave + 4 * u;
+            seq_load(qp[u].p + rows.off(n % R::kInstr, 0), dst + n * 1024);
+            advance(qp[u], g.qt, g.qh);
         }
-        const int m = b * 32 + (lane & 31);
-        const int mc = min(m, t.rows - 1);
-        const int tok = g.fd_G.div(mc), head = mc - tok * g.G;
-        const float* p = w.lse + (int64_t)(t.qtok + tok) * g.lt + (int64_t)kvh * g.G + head;
-        seq_load4(reinterpret_cast<const unsigned char*>(m < t.rows ? p : &kNeverRow),
-                  dst + M::kTile + wave * 256);
+        seq_load4(b * kStageRows + lane < t.rows
+                      ? lp.p
+                      : reinterpret_cast<const unsigned char*>(&kNeverRow),
+                  dst + RB * M::kTile + wave * 256);
+        advance(lp, 4 * g.lt, 4);
     };
 
-    for (int pass = split * g.chunk; pass < c1; pass += 4 * KT) {
+    for (int pass = split * g.chunk, next; pass < c1; pass = next) {
+        next = pass + 4 * KT;
+        // ---- the rows that see any of the workgroup's keys, or its share of them ----
+        int b0, b1;
+        weights_stages(w, t, pass, min(pass + 4 * KT, c1), first, b0, b1);
+        const bool shared = w.shares > 1 && pass < g.nsplit * g.chunk;
+        if (share > 0 && !shared) break;  // (keys behind the caller's bound: one workgroup's)
+        if (shared) {
+            const int each = (b1 - b0 + w.shares - 1) >> w.lgshares;
+            b0 = min(b0 + share * each, b1);
+            b1 = min(b0 + each, b1);
+        }
         // ---- this wave's keys ----
         const int e = pass + wave * KT;
         typename Tr<T>::x8 kf[KT][F::kKS];
@@ -295,26 +367,12 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsGeo w,
                     kf[k][x] = ld_x8<T>(reinterpret_cast<const T*>(kb + at) + x * 16 + 8 * h);
             }
         }
-        // ---- the rows that see any of the workgroup's keys ----
-        const int ja = t.tile(pass), jb = t.tile(min(pass + 4 * KT, c1) - 1) + 31;
-        const int ta = max(ja - t.pos0, 0);
-        const int tb = (int)min((int64_t)t.valid, ja < g.S ? (int64_t)t.valid
-                                                           : (int64_t)jb - t.pos0 + g.W);
-        int b0 = ta < tb ? ta * g.G >> 5 : 0;
-        int b1 = ta < tb && jb >= first ? (tb * g.G + 31) >> 5 : b0;
-        const bool shared = w.shares > 1 && pass < g.nsplit * g.chunk;
-        if (shared) {  // this workgroup's share of them
-            const int each = (b1 - b0 + w.shares - 1) / w.shares;
-            b0 = min(b0 + share * each, b1);
-            b1 = min(b0 + each, b1);
-        } else if (share > 0) {  // (keys behind the caller's bound: one workgroup's)
-            break;
-        }
 #pragma unroll
         for (int k = 0; k < KT; ++k)
 #pragma unroll
             for (int x = 0; x < F::kKS; ++x) settle(kf[k][x]);
         lds_barrier();  // (the stages of the pass before are read)
+        if (b0 < b1) begin(b0);
 #pragma unroll
         for (int x = 0; x < NB - 1; ++x)
             if (b0 + x < b1) issue(b0 + x, x);
@@ -327,37 +385,58 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsGeo w,
             lds_barrier();  // for every wave; and the stage before is read
             if (b + NB - 1 < b1) issue(b + NB - 1, buf == 0 ? NB - 1 : buf - 1);
             const unsigned char* tile = smem + buf * M::kStage;
-            typename Tr<T>::x8 qf[F::kKS];
-            f.rows(tile, qf);
-            float lse[16];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const f32x4 v = *reinterpret_cast<const f32x4*>(tile + M::kTile + wave * 256 +
-                                                                (8 * x + 4 * h) * 4);
-#pragma unroll
-                for (int y = 0; y < 4; ++y) lse[4 * x + y] = v[y] * kLog2e;
-            }
-            const int pa = t.pos0 + g.fd_G.div(b * 32);
-            const int pb = t.pos0 + g.fd_G.div(min(b * 32 + 31, t.rows - 1));
+            const int pa = t.pos0 + g.fd_G.div(b * RB * 32);
+            const int pb = t.pos0 + g.fd_G.div(min(b * RB * 32 + RB * 32 - 1, t.rows - 1));
+            bool full = true, none = true;
 #pragma unroll
             for (int k = 0; k < KT; ++k) {
-                if (!on[k] || pb < j0[k] || (pa - (j0[k] + 31) >= g.W && j0[k] >= g.S)) continue;
-                f32x16 s = f32x16{} * 0.f;
-#pragma unroll
-                for (int x = 0; x < F::kKS; ++x) s = mma32<T>(qf[x], kf[k][x], s);
-                float y[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) y[i] = fmaf(s[i], g.c, -lse[i]);
-                if (!(pa >= j0[k] + 31 && (pb - j0[k] < g.W || j0[k] + 31 < g.S))) {
-                    const unsigned m = seen_rows(g, t.pos0, b * 32 + 4 * h, j0[k] + (lane & 31));
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) y[i] = keep(m, i, y[i], -INFINITY);
-                }
-                float part[2] = {0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < 16; ++i) part[i & 1] += fast_exp2(y[i]);
-                sum[k] += part[0] + part[1];
+                full = full && on[k] && pa >= j0[k] + 31 && (pb - j0[k] < g.W || j0[k] + 31 < g.S);
+                none = none && (!on[k] || pb < j0[k] || (pa - (j0[k] + 31) >= g.W && j0[k] >= g.S));
             }
+            // All pairs of a stage in one run of code (masks only where some pair is not seen), so
+            // that one tile's products run beside another's exponentials.
+            auto step = [&](auto masked) __attribute__((always_inline)) {
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                    typename Tr<T>::x8 qf[F::kKS];
+#pragma unroll
+                    for (int x = 0; x < F::kKS; ++x) qf[x] = f.row(tile + rb * M::kTile, x);
+                    float lse[16];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const f32x4 v = *reinterpret_cast<const f32x4*>(
+                            tile + RB * M::kTile + wave * 256 + (rb * 32 + 8 * x + 4 * h) * 4);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) lse[4 * x + y] = v[y] * kLog2e;
+                    }
+                    f32x16 s[KT];
+#pragma unroll
+                    for (int k = 0; k < KT; ++k) {
+                        s[k] = f32x16{} * 0.f;
+#pragma unroll
+                        for (int x = 0; x < F::kKS; ++x) s[k] = mma32<T>(qf[x], kf[k][x], s[k]);
+                    }
+#pragma unroll
+                    for (int k = 0; k < KT; ++k) {
+                        float y[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) y[i] = fmaf(s[k][i], g.c, -lse[i]);
+                        if constexpr (decltype(masked)::value) {
+                            const unsigned m = on[k] ? seen_rows(g, t.pos0, (b * RB + rb) * 32 + 4 * h,
+                                                                 j0[k] + (lane & 31))
+                                                     : 0u;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) y[i] = keep(m, i, y[i], -INFINITY);
+                        }
+                        float part[2] = {0.f, 0.f};
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) part[i & 1] += fast_exp2(y[i]);
+                        sum[k] += part[0] + part[1];
+                    }
+                }
+            };
+            if (full) step(std::false_type{});
+            else if (!none) step(std::true_type{});
         }
 #pragma unroll
         for (int k = 0; k < KT; ++k) {
@@ -399,10 +478,10 @@ hipError_t launch_weights(const WeightsGeo& w, const void* q, const void* k, hip
     const unsigned slices = (unsigned)w.g.B * w.g.Hkv, grid = slices * w.g.nsplit * w.shares;
     hipError_t e;
     if (w.form == 0) {
-        constexpr size_t lds = kFewWaves * 2 * SeqFrags<T, D>::kTile + kFewTiles * 32 * 4;
+        constexpr size_t lds = WeightsFew<T, D>::kLds;
         auto kern = weights_few_kernel<T, D>;
         if ((e = seq_allow_lds(kern, lds)) != hipSuccess) return e;
-        hipLaunchKernelGGL(kern, dim3(grid), dim3(kFewWaves * 64), lds, st, w, q_, k_);
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(WeightsFew<T, D>::kWaves * 64), lds, st, w, q_, k_);
     } else {
         constexpr size_t lds = WeightsMany<T, D>::kLds;
         auto kern = weights_many_kernel<T, D>;
