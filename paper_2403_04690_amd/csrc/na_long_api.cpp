@@ -78,6 +78,12 @@ void fill_shared(const na_shared_problem& s, na::SharedGeo& x) {
     keys = s.max_shared > 0 ? std::min(s.max_shared, room) : room;
     cut_side(shared, keys, std::max((rows + Ms - 1) / Ms, std::min(s.groups, p.tokens)), g.Hkv,
              half);
+    // (one grid for both sides)
+    const int64_t own_jobs = (int64_t)own.ntiles * g.Hkv * own.nsplit;
+    const int64_t tiles = (int64_t)shared.ntiles * g.Hkv;
+    const int64_t most = std::max<int64_t>(1, (kMaxGrid - 1 - own_jobs) / tiles);
+    if (shared.nsplit > most) shared.nsplit = (int)most;
+    x.shared_jobs = (int)(tiles * shared.nsplit);
 }
 
 size_t shared_bytes(const na_shared_problem& s, const na::SharedGeo& x) {

@@ -45,10 +45,17 @@ struct SeqState {
     // scheduling groups, was 1 to 8 % slower than leaving it to the compiler.)
     //   (One body with a branch around the mask alone: two bodies that meet again in the
     // accumulators cost registers.)
-    template <int N, typename Seen>
+    //   after_k and after_v run when this wave has read the tiles' keys and their values, before_v
+    // in front of the values' reads.
+    struct Nothing {
+        __device__ __forceinline__ void operator()() const {}
+    };
+    template <int N, typename Seen, typename AfterK = Nothing, typename BeforeV = Nothing,
+              typename AfterV = Nothing>
     __device__ __forceinline__ void fold(const F& f, const unsigned char* (&tile)[N],
                                          int lane, float c, bool full, const int (&j0)[N],
-                                         const bool (&on)[N], Seen seen) {
+                                         const bool (&on)[N], Seen seen, AfterK after_k = {},
+                                         BeforeV before_v = {}, AfterV after_v = {}) {
         f32x16 s[N];
         x8 kf[N][F::kKS];
 #pragma unroll
@@ -56,6 +63,7 @@ struct SeqState {
 #pragma unroll
             for (int st = 0; st < F::kKS; ++st) kf[n][st] = f.row(tile[n], st);
         }
+        after_k();
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             s[n] = f32x16{} * 0.f;
@@ -96,6 +104,7 @@ struct SeqState {
         }
         x8 vf[N][2][F::kDB], pf[N][2];
         float sum[2];
+        before_v();
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -103,6 +112,7 @@ struct SeqState {
 #pragma unroll
                 for (int db = 0; db < F::kDB; ++db)
                     vf[n][bi][db] = f.col(tile[n] + F::kTile, db, bi, lane);
+        after_v();
 #pragma unroll
         for (int n = 0; n < N; ++n) {
 #pragma unroll

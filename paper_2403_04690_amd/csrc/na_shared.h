@@ -20,6 +20,7 @@ struct SharedGeo {
     SeqGeo g;  // the requests (paged form); ntiles as own_side's
     int groups;
     SharedSide shared_side, own_side;
+    int shared_jobs;  // workgroups of shared_side
     const int32_t *cu_groups, *shared;
     float *part, *part_lse;  // [parts][tokens][heads] of D values, and of logsumexps
 };

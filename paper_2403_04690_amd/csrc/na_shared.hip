@@ -91,22 +91,48 @@ __device__ __forceinline__ int last_at(int lo, int span, int v, int lane, At at)
 __device__ __forceinline__ int context_of(const SeqGeo& g, int c) {
     return min(max(c, 0), g.max_pages << g.lgps);
 }
-__device__ __forceinline__ int shared_of(const SharedGeo& s, int x) {
-    return context_of(s.g, s.shared[x]);
-}
+// What every lane reads first, for all that follows: group `lane` (where there are at most 64).
+struct Groups {
+    int begin, end, shared;
+    __device__ __forceinline__ void load(const SharedGeo& s, int lane) {
+        begin = end = INT32_MAX;
+        shared = 0;
+        if (s.groups > 64 || lane >= s.groups) return;
+        begin = s.cu_groups[lane];
+        end = s.cu_groups[lane + 1];
+        shared = s.shared[lane];
+    }
+};
 
 // Row tile `tile` of M = 2^lgM rows of the groups -> its rows.  False: no such tile.  Group x has
 // tiles from floor(first row / M) + x on, at least as many as it needs.
-__device__ __forceinline__ bool locate_group(const SharedGeo& s, int tile, int lgM, int lane,
-                                             SharedTile& t, int& to) {
+__device__ __forceinline__ bool locate_group(const SharedGeo& s, const Groups& all, int tile, int lgM,
+                                             int lane, SharedTile& t, int& to) {
     const SeqGeo& g = s.g;
-    auto request = [&](int x) { return min(max(s.cu_groups[x], 0), g.B); };
-    auto token = [&](int x) { return min(max(g.cu[request(x)], 0), g.n); };
-    const int x = last_at(0, s.groups, tile, lane,
-                          [&](int i) { return (token(i) * g.G >> lgM) + i; });
-    t.r0 = uniform(request(x));
-    t.r1 = uniform(request(x + 1));
-    const int start = uniform(token(x)), n = uniform(token(x + 1)) - start;
+    auto request = [&](int r) { return min(max(r, 0), g.B); };
+    auto token = [&](int r) { return min(max(g.cu[request(r)], 0), g.n); };
+    int x, start, n, shared;
+    if (s.groups <= 64) {  // (two loads after each other)
+        const bool in = lane < s.groups;
+        const int a = in ? token(all.begin) : 0, b = in ? token(all.end) : 0;
+        const uint64_t m = __builtin_amdgcn_ballot_w64(in && (a * g.G >> lgM) + lane <= tile);
+        x = max(__builtin_popcountll(m) - 1, 0);
+        t.r0 = __builtin_amdgcn_readlane(all.begin, x);
+        t.r1 = __builtin_amdgcn_readlane(all.end, x);
+        start = __builtin_amdgcn_readlane(a, x);
+        n = __builtin_amdgcn_readlane(b, x) - start;
+        shared = __builtin_amdgcn_readlane(all.shared, x);
+    } else {
+        x = last_at(0, s.groups, tile, lane,
+                    [&](int i) { return (token(s.cu_groups[i]) * g.G >> lgM) + i; });
+        t.r0 = uniform(s.cu_groups[x]);
+        t.r1 = uniform(s.cu_groups[x + 1]);
+        start = uniform(token(t.r0));
+        n = uniform(token(t.r1)) - start;
+        shared = uniform(s.shared[x]);
+    }
+    t.r0 = request(t.r0);
+    t.r1 = request(t.r1);
     if (t.r0 >= t.r1 || n <= 0) return false;
     const int at = tile - (start * g.G >> lgM) - x;
     if (at < 0 || at >= kSeqMaxTiles) return false;
@@ -118,15 +144,32 @@ __device__ __forceinline__ bool locate_group(const SharedGeo& s, int tile, int l
     t.pos0 = 0;
     t.valid = n;
     t.from = 0;
-    to = uniform(shared_of(s, x));
+    to = context_of(g, shared);
     return true;
 }
 
-// Group of request r, or -1.
-__device__ __forceinline__ int group_of(const SharedGeo& s, int r, int lane) {
+// Group of request r (-1: none) and the tokens that it shares.
+__device__ __forceinline__ int group_of(const SharedGeo& s, const Groups& all, int r, int lane,
+                                        int& shared) {
+    shared = 0;
     if (s.groups == 0) return -1;
-    const int x = last_at(0, s.groups, r, lane, [&](int i) { return s.cu_groups[i]; });
-    return uniform(s.cu_groups[x] <= r && r < s.cu_groups[x + 1] ? x : -1);
+    int x, begin, end;
+    if (s.groups <= 64) {
+        const uint64_t m = __builtin_amdgcn_ballot_w64(all.begin <= r);  // (none behind the last)
+        x = max(__builtin_popcountll(m) - 1, 0);
+        begin = __builtin_amdgcn_readlane(all.begin, x);
+        end = __builtin_amdgcn_readlane(all.end, x);
+        shared = __builtin_amdgcn_readlane(all.shared, x);
+    } else {
+        x = last_at(0, s.groups, r, lane, [&](int i) { return s.cu_groups[i]; });
+        begin = uniform(s.cu_groups[x]);
+        end = uniform(s.cu_groups[x + 1]);
+        shared = uniform(s.shared[x]);
+    }
+    shared = context_of(s.g, shared);
+    if (begin <= r && r < end) return x;
+    shared = 0;
+    return -1;
 }
 
 // Position of row `tok` of q (each lane its own; `least` the wave's least) among the requests
@@ -182,12 +225,13 @@ struct SharedJob {
         tile = g.fd_kv.div(id);
         kvh = id - tile * g.Hkv;
         part = split + (GROUP ? 0 : s.shared_side.nsplit);
+        Groups all;
+        all.load(s, lane);
         if constexpr (GROUP) {
-            return locate_group(s, tile, LGM, lane, t, to);
+            return locate_group(s, all, tile, LGM, lane, t, to);
         } else {
             if (!seq_locate(g, tile, LGM, lane, t)) return false;
-            group = group_of(s, t.b, lane);
-            t.from = group < 0 ? 0 : uniform(shared_of(s, group));
+            group = group_of(s, all, t.b, lane, t.from);
             t.span(g, t.pmin, t.pmax, INT32_MAX);
             return true;
         }
@@ -216,17 +260,17 @@ __device__ __forceinline__ void no_shared_part(const SharedGeo& s, const Job& jo
 // Many rows: four waves of 32 rows each share the staged key tiles (as the wide form of
 // na_seq_fwd.hip).
 template <typename T, int D, bool GROUP>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 4) : 1)) void shared_wide_kernel(
-    SharedGeo s, const T* __restrict__ qg, const T* __restrict__ kg, const T* __restrict__ vg) {
+__device__ __forceinline__ void shared_wide(const SharedGeo& s, int bid, const T* __restrict__ qg,
+                                            const T* __restrict__ kg, const T* __restrict__ vg,
+                                            unsigned char* smem) {
     using F = SeqFrags<T, D>;
     using Ring = SeqRing<T, D>;
     constexpr int SK = Ring::kTiles, NB = Ring::kStages;
-    extern __shared__ __align__(16) unsigned char smem[];
     const SeqGeo& g = s.g;
     const int lane = threadIdx.x & 63;
     const int wave = uniform((threadIdx.x >> 6) & 3);
     SharedJob<GROUP, 7> job;
-    if (!job.locate(s, blockIdx.x, lane)) return;
+    if (!job.locate(s, bid, lane)) return;
     SharedTile& t = job.t;
 
     // ---- this lane's row, and the positions of the wave's rows ----
@@ -346,20 +390,37 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 4) : 1)) voi
                               st.o[db][4 * i + 3]} * inv);
 }
 
-// Few rows (one block of 32): the waves take every fourth key tile each and join (as the narrow
-// form of na_seq_fwd.hip).
+// LDS of the narrow form: a key and a value tile for each of four waves; then the join, as many
+// columns at a time as fit there.
+template <typename T, int D>
+struct SharedNarrow {
+    static constexpr int W = 4;
+    static constexpr int kTile = SeqFrags<T, D>::kTile;
+    static constexpr int kStages = W * 2 * kTile;
+    static constexpr int kCols = D == 32 ? 32 : D / 2;      // columns joined at a time
+    static constexpr int kRow = (kCols + 4) * 4;            // (padded: LDS banks)
+    static constexpr int kJoin = W * 32 * kRow;
+    static constexpr int kStat = kStages > kJoin ? kStages : kJoin;  // offset of the statistics
+    static constexpr int kLds = kStat + W * 32 * 8;
+};
+
+// Few rows (one block of 32): the waves take every fourth key tile each and join.  A wave has one
+// buffer for keys and one for values: the next tile's keys load as soon as this one's are in
+// registers, its values likewise, so more waves fit a CU than with two buffers each; and the
+// pages of 64 tiles are looked up at a time.
 template <typename T, int D, bool GROUP>
-__global__ __launch_bounds__((seq_narrow_waves<T, D>() * 64), 1) void shared_narrow_kernel(
-    SharedGeo s, const T* __restrict__ qg, const T* __restrict__ kg, const T* __restrict__ vg) {
+__device__ __forceinline__ void shared_narrow(const SharedGeo& s, int bid, const T* __restrict__ qg,
+                                              const T* __restrict__ kg, const T* __restrict__ vg,
+                                              unsigned char* smem) {
     using F = SeqFrags<T, D>;
-    using N = SeqNarrow<T, D>;
+    using R = SeqRows<T, D>;
+    using N = SharedNarrow<T, D>;
     constexpr int W = N::W;
-    extern __shared__ __align__(16) unsigned char smem[];
     const SeqGeo& g = s.g;
     const int lane = threadIdx.x & 63;
     const int wave = uniform((threadIdx.x >> 6) & (W - 1));
     SharedJob<GROUP, 5> job;
-    if (!job.locate(s, blockIdx.x, lane)) return;
+    if (!job.locate(s, bid, lane)) return;
     SharedTile& t = job.t;
     int tok, head, pos;
     seq_row(g, t, lane & 31, tok, head);
@@ -375,16 +436,48 @@ __global__ __launch_bounds__((seq_narrow_waves<T, D>() * 64), 1) void shared_nar
     int e0, e1;
     job.keys(s, e0, e1);
 
-    SeqStage<T, D, true, 1> ld;
-    ld.init(g, t, job.kvh, lane, kg, vg);
-    unsigned char* buf0 = smem + wave * 4 * F::kTile;
+    // ---- loads of a tile's keys or values ----
+    R rows;
+    rows.init(lane);
+    const int kt = (int)g.kt;
+    const uint32_t lane_rows = rows.rowl * (uint32_t)kt;
+    const unsigned char* kb = reinterpret_cast<const unsigned char*>(kg) + job.kvh * g.kh;
+    const unsigned char* vb = reinterpret_cast<const unsigned char*>(vg) + job.kvh * g.vh;
     const int all[1] = {pos};
-    auto issue = [&](int e, unsigned char* dst) __attribute__((always_inline)) {
-        if (GROUP && t.gaps) t.look(g, t.tile(e), all);
-        ld.issue(g, t, e, 0, dst);
+    int pass = e0, page0, page1;
+    auto look_up = [&]() __attribute__((always_inline)) {  // pages hold whole blocks of 16 keys
+        const int32_t* row = g.table + (int64_t)t.b * g.max_pages;
+        const int col0 = t.tile(pass + lane) >> g.lgps, col1 = (t.tile(pass + lane) + 16) >> g.lgps;
+        page0 = pass + lane < e1 && col0 < g.max_pages ? row[col0] : -1;
+        page1 = pass + lane < e1 && col1 < g.max_pages ? row[col1] : -1;
     };
-    int e = e0 + wave;
-    if (e < e1) issue(e, buf0);
+    auto issue = [&](int e, const unsigned char* head_rows, unsigned char* dst)
+                     __attribute__((always_inline)) {
+        const int j0 = t.tile(e);
+        if (GROUP && t.gaps) t.look(g, j0, all);
+        const int id0 = __builtin_amdgcn_readlane(page0, e - pass);
+        const int id1 = __builtin_amdgcn_readlane(page1, e - pass);
+        const bool ok0 = (unsigned)id0 < (unsigned)g.pages, ok1 = (unsigned)id1 < (unsigned)g.pages;
+        const int in = (1 << g.lgps) - 1;
+        const unsigned char* b0 = head_rows + (int64_t)(ok0 ? id0 : 0) * (int)g.kb + (j0 & in) * kt;
+        const unsigned char* b1 =
+            head_rows + (int64_t)(ok1 ? id1 : 0) * (int)g.kb + ((j0 + 16) & in) * kt;
+        const bool fast = ok0 && ok1 && t.whole(g, j0);
+#pragma unroll
+        for (int n = 0; n < R::kInstr; ++n) {
+            const int r0 = n * R::kRpi;
+            const unsigned char* base = (r0 >= 16 ? b1 : b0) + (r0 & 15) * kt;
+            const uint32_t off = rows.off(n, lane_rows);
+            if (fast) {
+                seq_load(base, off, dst + n * 1024);
+            } else {
+                const bool see = (r0 >= 16 ? ok1 : ok0) && t.sees(g, j0 + r0 + rows.rowl);
+                seq_load(see ? base + off : reinterpret_cast<const unsigned char*>(&kZeroRow),
+                         dst + n * 1024);
+            }
+        }
+    };
+
     const int64_t hq = (int64_t)job.kvh * g.G + head;
     SeqState<T, D> st;
     st.init();
@@ -397,27 +490,48 @@ __global__ __launch_bounds__((seq_narrow_waves<T, D>() * 64), 1) void shared_nar
     }
     F f;
     f.init(lane);
-#pragma unroll
-    for (int x = 0; x < F::kKS; ++x) settle(st.qf[x]);
-    wait_vmem();  // (the first tile too: from here on only stage loads are outstanding)
     auto seen = [&](int base) __attribute__((always_inline)) {
         return seen_keys(pos - base, g.W, g.S - base) & below(t.end - base) & ~below(t.from - base);
     };
-    for (int buf = 0; e < e1; e += W, buf ^= 1) {
-        if (e + W < e1) {
-            issue(e + W, buf0 + (buf ^ 1) * 2 * F::kTile);
-            wait_vmem_but<2 * SeqRows<T, D>::kInstr>();
-        } else {
-            wait_vmem();
+    unsigned char* buf = smem + wave * 2 * F::kTile;
+    for (; pass < e1; pass += kWave) {
+        const int end = min(pass + kWave, e1);
+        int e = pass + wave;
+        look_up();
+        settle(page0);
+        settle(page1);
+#pragma unroll
+        for (int x = 0; x < F::kKS; ++x) settle(st.qf[x]);
+        if (e < end) {
+            issue(e, kb, buf);
+            issue(e, vb, buf + F::kTile);
         }
-        const unsigned char* ks[1] = {buf0 + buf * 2 * F::kTile};
-        const int j0 = t.tile(e);
-        const bool full = j0 + 31 <= wmin && (wmax - j0 < g.W || j0 + 31 < g.S) && j0 >= t.from &&
-                          j0 + 31 < t.end;
-        const int js[1] = {j0};
-        const bool on[1] = {true};
-        st.template fold<1>(f, ks, lane, g.c, full, js, on, seen);
-        wait_lds();  // before the next loads into this buffer
+        for (; e < end; e += W) {
+            const bool more = e + W < end;
+            wait_vmem_but<R::kInstr>();  // (all but the values')
+            const unsigned char* ks[1] = {buf};
+            const int j0 = t.tile(e);
+            const bool full = j0 + 31 <= wmin && (wmax - j0 < g.W || j0 + 31 < g.S) &&
+                              j0 >= t.from && j0 + 31 < t.end;
+            const int js[1] = {j0};
+            const bool on[1] = {true};
+            st.template fold<1>(
+                f, ks, lane, g.c, full, js, on, seen,
+                [&]() __attribute__((always_inline)) {
+                    wait_lds();
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (more) issue(e + W, kb, buf);
+                },
+                [&]() __attribute__((always_inline)) {
+                    if (more) wait_vmem_but<R::kInstr>();  // (all but the next keys')
+                    else wait_vmem();
+                },
+                [&]() __attribute__((always_inline)) {
+                    wait_lds();
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (more) issue(e + W, vb, buf + F::kTile);
+                });
+        }
     }
 
     // ---- join the waves: every sum relative to the largest reference ----
@@ -436,44 +550,64 @@ __global__ __launch_bounds__((seq_narrow_waves<T, D>() * 64), 1) void shared_nar
 #pragma unroll
     for (int w = 0; w < W; ++w) top = fmaxf(top, stat[(w * 32 + col) * 2]);
     const float scale = st.mref == -INFINITY ? 0.f : fast_exp2(st.mref - top);
-    {
+    constexpr int kBlocks = N::kCols / 32;  // column blocks joined at a time
+#pragma unroll
+    for (int c0 = 0; c0 < F::kDB; c0 += kBlocks) {
         float* mine = reinterpret_cast<float*>(smem + (wave * 32 + col) * N::kRow);
 #pragma unroll
-        for (int db = 0; db < F::kDB; ++db)
+        for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i) {
+                const f32x16& o = st.o[c0 + db];
                 st16<f32x4>(mine + db * 32 + i * 8 + h * 4,
-                            f32x4{st.o[db][4 * i], st.o[db][4 * i + 1], st.o[db][4 * i + 2],
-                                  st.o[db][4 * i + 3]} * scale);
-    }
-    __syncthreads();
-    // each thread: four columns of a row
-    for (int x = threadIdx.x; x < t.rows * (D / 4); x += W * 64) {
-        const int row = x / (D / 4), d = x % (D / 4) * 4;
-        float mx = -INFINITY, sum = 0.f;
-        f32x4 acc{0.f, 0.f, 0.f, 0.f};
+                            f32x4{o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]} * scale);
+            }
+        __syncthreads();
+        // each thread: four columns of a row
+        for (int x = threadIdx.x; x < t.rows * (N::kCols / 4); x += W * 64) {
+            const int row = x / (N::kCols / 4), d = x % (N::kCols / 4) * 4;
+            float mx = -INFINITY, sum = 0.f;
+            f32x4 acc{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < W; ++w) mx = fmaxf(mx, stat[(w * 32 + row) * 2]);
+            for (int w = 0; w < W; ++w) mx = fmaxf(mx, stat[(w * 32 + row) * 2]);
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-            const float m = stat[(w * 32 + row) * 2];
-            sum += m == -INFINITY ? 0.f : fast_exp2(m - mx) * stat[(w * 32 + row) * 2 + 1];
-            acc += *reinterpret_cast<const f32x4*>(smem + (w * 32 + row) * N::kRow + d * 4);
+            for (int w = 0; w < W; ++w) {
+                const float m = stat[(w * 32 + row) * 2];
+                sum += m == -INFINITY ? 0.f : fast_exp2(m - mx) * stat[(w * 32 + row) * 2 + 1];
+                acc += *reinterpret_cast<const f32x4*>(smem + (w * 32 + row) * N::kRow + d * 4);
+            }
+            const bool some = sum > 0.f;
+            int tk, hd;
+            seq_row(g, t, row, tk, hd);
+            const int64_t pr = part_row(s, job.part, t.qtok + tk, (int64_t)job.kvh * g.G + hd);
+            if (some) st16(s.part + pr * D + c0 * 32 + d, acc * (1.f / sum));
+            if (c0 == 0 && d == 0) s.part_lse[pr] = some ? mx + __log2f(sum) : -INFINITY;
         }
-        const bool some = sum > 0.f;
-        int tk, hd;
-        seq_row(g, t, row, tk, hd);
-        const int64_t pr = part_row(s, job.part, t.qtok + tk, (int64_t)job.kvh * g.G + hd);
-        if (some) st16(s.part + pr * D + d, acc * (1.f / sum));
-        if (d == 0) s.part_lse[pr] = some ? mx + __log2f(sum) : -INFINITY;
+        if (c0 + kBlocks < F::kDB) __syncthreads();
+    }
+}
+
+// Both problems in one launch: the workgroups of the shared keys, then those of the requests' own.
+template <typename T, int D, bool NARROW_SHARED, bool NARROW_OWN>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 ? (D == 128 ? 2 : 4) : 1)) void shared_kernel(
+    SharedGeo s, const T* __restrict__ qg, const T* __restrict__ kg, const T* __restrict__ vg) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int bid = (int)blockIdx.x - s.shared_jobs;
+    if (bid < 0) {
+        if constexpr (NARROW_SHARED) shared_narrow<T, D, true>(s, blockIdx.x, qg, kg, vg, smem);
+        else shared_wide<T, D, true>(s, blockIdx.x, qg, kg, vg, smem);
+    } else {
+        if constexpr (NARROW_OWN) shared_narrow<T, D, false>(s, bid, qg, kg, vg, smem);
+        else shared_wide<T, D, false>(s, bid, qg, kg, vg, smem);
     }
 }
 
 // Joins the parts of each row in a fixed order.  One workgroup per 32 rows of a (row tile of the
-// requests, key/value head); D / 4 threads a row.
+// requests, key/value head); D / 4 threads a row, which read a part's logsumexp each.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedGeo s, int lgM, T* __restrict__ og,
                                                           float* __restrict__ lseg) {
+    constexpr int kThreads = D / 4;  // of a row: 8, 16 or 32 neighbouring lanes
     const SeqGeo& g = s.g;
     const int id = blockIdx.x >> (lgM - 5), r0 = (blockIdx.x & ((1 << (lgM - 5)) - 1)) * 32;
     const int tile = g.fd_kv.div(id);
@@ -482,52 +616,60 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedGeo s, int lgM, 
     if (!seq_locate(g, tile, lgM, threadIdx.x & 63, t)) return;
     const int parts = s.shared_side.nsplit + s.own_side.nsplit;
     const int64_t apart = (int64_t)g.n * g.Hkv * g.G;
-    const int end = min(32, t.rows - r0) * (D / 4);
-    for (int x = threadIdx.x; x < end; x += 256) {
-        const int row = r0 + x / (D / 4), d = x % (D / 4) * 4;
+    const int mine = threadIdx.x % kThreads;
+    for (int row = r0 + threadIdx.x / kThreads; row < min(r0 + 32, t.rows); row += 256 / kThreads) {
         int tok, head;
         seq_row(g, t, row, tok, head);
         const int64_t hr = (int64_t)kvh * g.G + head;
         const int64_t at = part_row(s, 0, t.qtok + tok, hr);
-        float mx = -INFINITY, sum = 0.f;
-        for (int p = 0; p < parts; ++p) mx = fmaxf(mx, s.part_lse[at + p * apart]);
+        const float* lse = s.part_lse + at;
+        const float* y = s.part + at * D + mine * 4;
+        float mx = -INFINITY;
+        for (int p = mine; p < parts; p += kThreads) mx = fmaxf(mx, lse[p * apart]);
+#pragma unroll
+        for (int d = kThreads / 2; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d, kWave));
+        float sum = 0.f;
         f32x4 acc{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int p = 0; p < parts; ++p) {
-            const float e = s.part_lse[at + p * apart];
-            if (e == -INFINITY) continue;
-            const float w = fast_exp2(e - mx);
-            sum += w;
-            acc += ld16<f32x4>(s.part + (at + p * apart) * D + d) * w;
+        for (int p0 = 0; p0 < parts; p0 += kThreads) {
+            // (a part that sees nothing has no mean: it may hold anything)
+            const float e = p0 + mine < parts ? lse[(p0 + mine) * apart] : -INFINITY;
+            const float w = e == -INFINITY ? 0.f : fast_exp2(e - mx);
+            const int n = min(kThreads, parts - p0);
+            for (int x0 = 0; x0 < n; x0 += 8) {
+                f32x4 v[8];
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                    v[x] = ld16<f32x4>(y + (int64_t)(p0 + min(x0 + x, n - 1)) * apart * D);
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    const float wx = x0 + x < n ? __shfl(w, (x0 + x) % kThreads, kThreads) : 0.f;
+                    sum += wx;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) acc[c] = wx > 0.f ? fmaf(v[x][c], wx, acc[c]) : acc[c];
+                }
+            }
         }
         const bool some = sum > 0.f;
         T* op = reinterpret_cast<T*>(reinterpret_cast<unsigned char*>(og) + hr * g.oh +
                                      (int64_t)(t.qtok + tok) * g.ot);
-        st_x4<T>(op + d, acc * (some ? 1.f / sum : 0.f));
-        if (d == 0)
+        st_x4<T>(op + mine * 4, acc * (some ? 1.f / sum : 0.f));
+        if (mine == 0)
             lseg[hr * g.lh + (int64_t)(t.qtok + tok) * g.lt] =
                 some ? (mx + __log2f(sum)) * kLn2 : -INFINITY;
     }
 }
 
 // ---- host ----
-template <typename T, int D, bool GROUP>
-hipError_t launch_side(const SharedGeo& s, bool narrow, const T* q, const T* k, const T* v,
-                       hipStream_t st) {
-    const SharedSide& side = GROUP ? s.shared_side : s.own_side;
-    const unsigned grid = (unsigned)side.ntiles * s.g.Hkv * side.nsplit;
-    hipError_t e;
-    if (narrow) {
-        using N = SeqNarrow<T, D>;
-        auto kern = shared_narrow_kernel<T, D, GROUP>;
-        if ((e = seq_allow_lds(kern, N::kLds)) != hipSuccess) return e;
-        hipLaunchKernelGGL(kern, dim3(grid), dim3(N::W * 64), N::kLds, st, s, q, k, v);
-    } else {
-        constexpr size_t lds = SeqRing<T, D>::kLds;
-        auto kern = shared_wide_kernel<T, D, GROUP>;
-        if ((e = seq_allow_lds(kern, lds)) != hipSuccess) return e;
-        hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, st, s, q, k, v);
-    }
+template <typename T, int D, bool NARROW_SHARED, bool NARROW_OWN>
+hipError_t launch_both(const SharedGeo& s, const T* q, const T* k, const T* v, hipStream_t st) {
+    constexpr size_t wide = SeqRing<T, D>::kLds, narrow = SharedNarrow<T, D>::kLds;
+    constexpr size_t lds = NARROW_SHARED && NARROW_OWN ? narrow
+                           : NARROW_SHARED || NARROW_OWN ? std::max(wide, narrow) : wide;
+    auto kern = shared_kernel<T, D, NARROW_SHARED, NARROW_OWN>;
+    const hipError_t e = seq_allow_lds(kern, lds);
+    if (e != hipSuccess) return e;
+    const unsigned own = (unsigned)s.own_side.ntiles * s.g.Hkv * s.own_side.nsplit;
+    hipLaunchKernelGGL(kern, dim3(s.shared_jobs + own), dim3(256), lds, st, s, q, k, v);
     return hipGetLastError();
 }
 
@@ -537,12 +679,12 @@ hipError_t launch_shared(const SharedGeo& s, const void* q, const void* k, const
     auto q_ = static_cast<const T*>(q);
     auto k_ = static_cast<const T*>(k);
     auto v_ = static_cast<const T*>(v);
-    hipError_t e;
-    if (s.shared_side.nsplit > 0 &&
-        (e = launch_side<T, D, true>(s, s.shared_side.narrow, q_, k_, v_, st)) != hipSuccess)
-        return e;
-    if ((e = launch_side<T, D, false>(s, s.own_side.narrow, q_, k_, v_, st)) != hipSuccess) return e;
     const bool narrow = s.own_side.narrow;
+    const hipError_t e = narrow && s.shared_side.narrow ? launch_both<T, D, true, true>(s, q_, k_, v_, st)
+                         : narrow                       ? launch_both<T, D, false, true>(s, q_, k_, v_, st)
+                         : s.shared_side.narrow         ? launch_both<T, D, true, false>(s, q_, k_, v_, st)
+                                                        : launch_both<T, D, false, false>(s, q_, k_, v_, st);
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL((shared_join_kernel<T, D>),
                        dim3((unsigned)s.g.ntiles * s.g.Hkv * (narrow ? 1 : 4)), dim3(256), 0, st, s,
                        narrow ? 5 : 7, static_cast<T*>(out), lse);
