@@ -38,7 +38,7 @@ na_status check_shared(const na_shared_problem& s) {
 void cut_side(na::SharedSide& side, int64_t keys, int64_t busy, int64_t Hkv, bool half) {
     const bool narrow = side.narrow;
     const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32 + 1);
-    int64_t split = std::max<int64_t>(1, (narrow ? 1024 : 512) / std::max<int64_t>(1, busy * Hkv));
+    int64_t split = std::max<int64_t>(1, (narrow ? 512 : 256) / std::max<int64_t>(1, busy * Hkv));
     split = std::min<int64_t>(split, na::kSeqMaxSplit);
     split = std::min(split, std::max<int64_t>(1, (kMaxGrid - 1) / ((int64_t)side.ntiles * Hkv)));
     const int64_t least = half ? (narrow ? 12 : 8) : (narrow ? 8 : 2);

@@ -257,6 +257,86 @@ __device__ __forceinline__ void no_shared_part(const SharedGeo& s, const Job& jo
         s.part_lse[part_row(s, x, job.t.qtok + tok, (int64_t)job.kvh * s.g.G + head)] = -INFINITY;
 }
 
+// Stages key or value rows.  The pages of 64 tiles are looked up at a time, a lane each, not with
+// every tile in front of its loads (which cost the wide form 1 us of every 2.4 us stage).
+template <typename T, int D, bool GROUP>
+struct SharedStage {
+    using R = SeqRows<T, D>;
+    R rows;
+    const unsigned char *kb, *vb;  // the head's rows of page 0
+    uint32_t lane_rows;
+    int pass, page0, page1;  // pages of tiles pass + lane (pages hold whole blocks of 16 rows)
+
+    __device__ __forceinline__ void init(const SeqGeo& g, int kvh, int lane, const void* k,
+                                         const void* v) {
+        rows.init(lane);
+        kb = static_cast<const unsigned char*>(k) + kvh * g.kh;
+        vb = static_cast<const unsigned char*>(v) + kvh * g.vh;
+        lane_rows = rows.rowl * (uint32_t)g.kt;
+    }
+    __device__ __forceinline__ void look_up(const SeqGeo& g, const SharedTile& t, int first, int e1,
+                                            int lane) {
+        pass = first;
+        const int32_t* row = g.table + (int64_t)t.b * g.max_pages;
+        const int j = t.tile(pass + lane), col0 = j >> g.lgps, col1 = (j + 16) >> g.lgps;
+        page0 = pass + lane < e1 && col0 < g.max_pages ? row[col0] : -1;
+        page1 = pass + lane < e1 && col1 < g.max_pages ? row[col1] : -1;
+    }
+    // Instructions first, first + STEP, .. of tile e's keys to kdst and of its values to vdst (those
+    // of the two that are asked for); pos: see look().
+    template <int STEP, bool K, bool V, int N>
+    __device__ __forceinline__ void issue(const SeqGeo& g, SharedTile& t, int e, int first,
+                                          const int (&pos)[N], unsigned char* kdst,
+                                          unsigned char* vdst) const {
+        const int j0 = t.tile(e);
+        if (GROUP && t.gaps) t.look(g, j0, pos);
+        const int id0 = __builtin_amdgcn_readlane(page0, e - pass);
+        const int id1 = __builtin_amdgcn_readlane(page1, e - pass);
+        const bool ok0 = (unsigned)id0 < (unsigned)g.pages, ok1 = (unsigned)id1 < (unsigned)g.pages;
+        const int in = (1 << g.lgps) - 1, kt = (int)g.kt;
+        const int64_t at0 = (int64_t)(ok0 ? id0 : 0) * (int)g.kb + (j0 & in) * kt;
+        const int64_t at1 = (int64_t)(ok1 ? id1 : 0) * (int)g.kb + ((j0 + 16) & in) * kt;
+        // (one branch for all loads: a choice for each of them took a third of a stage)
+        if (ok0 && ok1 && t.whole(g, j0)) {
+            if constexpr (K) load<STEP, true>(g, t, j0, first, kb + at0, kb + at1, true, true, kdst);
+            if constexpr (V) load<STEP, true>(g, t, j0, first, vb + at0, vb + at1, true, true, vdst);
+        } else {
+            if constexpr (K) load<STEP, false>(g, t, j0, first, kb + at0, kb + at1, ok0, ok1, kdst);
+            if constexpr (V) load<STEP, false>(g, t, j0, first, vb + at0, vb + at1, ok0, ok1, vdst);
+        }
+    }
+    template <int STEP, bool FAST>
+    __device__ __forceinline__ void load(const SeqGeo& g, const SharedTile& t, int j0, int first,
+                                         const unsigned char* b0, const unsigned char* b1, bool ok0,
+                                         bool ok1, unsigned char* dst) const {
+#pragma unroll
+        for (int u = 0; u < (R::kInstr + STEP - 1) / STEP; ++u) {
+            const int n = first + u * STEP, r0 = n * R::kRpi;
+            const unsigned char* base = (r0 >= 16 ? b1 : b0) + (r0 & 15) * (int)g.kt;
+            const uint32_t off = rows.off(n, lane_rows);
+            if constexpr (FAST) {
+                seq_load(base, off, dst + n * 1024);
+            } else {
+                const bool see = (r0 >= 16 ? ok1 : ok0) && t.sees(g, j0 + r0 + rows.rowl);
+                seq_load(see ? base + off : reinterpret_cast<const unsigned char*>(&kZeroRow),
+                         dst + n * 1024);
+            }
+        }
+    }
+};
+
+// The operand of this lane's row of q.
+template <typename T, int D>
+__device__ __forceinline__ void load_query(const SeqGeo& g, const SharedTile& t, int kvh, int tok,
+                                           int head, const T* qg, int lane,
+                                           typename Tr<T>::x8 (&qf)[D / 16]) {
+    const unsigned char* qp = reinterpret_cast<const unsigned char*>(qg) +
+                              ((int64_t)kvh * g.G + head) * g.qh + (int64_t)(t.qtok + tok) * g.qt;
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x)
+        qf[x] = ld_x8<T>(reinterpret_cast<const T*>(qp) + x * 16 + 8 * (lane >> 5));
+}
+
 // Many rows: four waves of 32 rows each share the staged key tiles (as the wide form of
 // na_seq_fwd.hip).
 template <typename T, int D, bool GROUP>
@@ -277,6 +357,9 @@ __device__ __forceinline__ void shared_wide(const SharedGeo& s, int bid, const T
     const int m = wave * 32 + (lane & 31);
     int tok, head, pos;
     seq_row(g, t, m, tok, head);
+    SeqState<T, D> st;
+    st.init();
+    load_query<T, D>(g, t, job.kvh, tok, head, qg, lane, st.qf);  // (arrives while the rest is found)
     int tf, hh;
     seq_row(g, t, wave * 32, tf, hh);
     int wmin, wmax;
@@ -301,14 +384,34 @@ __device__ __forceinline__ void shared_wide(const SharedGeo& s, int bid, const T
     int e0, e1;
     job.keys(s, e0, e1);
 
-    SeqStage<T, D, true, 4> ld;
-    ld.init(g, t, job.kvh, lane, kg, vg);
+    // Instructions of K and V by wave: those from kInstr on are V's, where the waves divide K's
+    // evenly in equal shares of both, otherwise (D = 32 in 16 bits) two waves' of each.
+    using R = SeqRows<T, D>;
+    constexpr bool kEven = R::kInstr % 4 == 0;
+    constexpr int kCount = 2 * R::kInstr / 4;
+    static_assert(kEven || R::kInstr == 2, "equal shares");
+    SharedStage<T, D, GROUP> ld;
+    ld.init(g, job.kvh, lane, kg, vg);
+    ld.look_up(g, t, e0, e1, lane);
+    settle(ld.page0);
+    settle(ld.page1);
     auto issue_stage = [&](int e, int buf) __attribute__((always_inline)) {
         if (e >= e1) return;
+        if (e - ld.pass >= kWave - SK + 1) {  // (uniform)
+            ld.look_up(g, t, e, e1, lane);
+            settle(ld.page0);
+            settle(ld.page1);
+        }
 #pragma unroll
         for (int i = 0; i < SK; ++i) {  // (a tile behind the last one: zeros)
-            if (GROUP && t.gaps) t.look(g, t.tile(e + i), all);
-            ld.issue(g, t, e + i, wave, smem + buf * Ring::kStage + i * 2 * F::kTile);
+            unsigned char* dst = smem + buf * Ring::kStage + i * 2 * F::kTile;
+            if constexpr (kEven) {
+                ld.template issue<4, true, true>(g, t, e + i, wave, all, dst, dst + F::kTile);
+            } else if (wave < 2) {
+                ld.template issue<2, true, false>(g, t, e + i, wave, all, dst, dst);
+            } else {
+                ld.template issue<2, false, true>(g, t, e + i, wave - 2, all, dst, dst + F::kTile);
+            }
         }
     };
 #pragma unroll
@@ -316,15 +419,6 @@ __device__ __forceinline__ void shared_wide(const SharedGeo& s, int bid, const T
 
     const bool live = wave * 32 < t.rows;
     const int64_t hq = (int64_t)job.kvh * g.G + head;
-    SeqState<T, D> st;
-    st.init();
-    {
-        const unsigned char* qp = reinterpret_cast<const unsigned char*>(qg) + hq * g.qh +
-                                  (int64_t)(t.qtok + tok) * g.qt;
-#pragma unroll
-        for (int x = 0; x < F::kKS; ++x)
-            st.qf[x] = ld_x8<T>(reinterpret_cast<const T*>(qp) + x * 16 + 8 * (lane >> 5));
-    }
     F f;
     f.init(lane);
 #pragma unroll
@@ -337,7 +431,7 @@ __device__ __forceinline__ void shared_wide(const SharedGeo& s, int bid, const T
     auto stage = [&](int e, auto BUF) __attribute__((always_inline)) {
         constexpr int kBuf = decltype(BUF)::value;
         if (NB > 2 && e + (NB - 2) * SK < e1)
-            wait_vmem_but<(NB - 2) * SK * decltype(ld)::kCount>();
+            wait_vmem_but<(NB - 2) * SK * kCount>();
         else
             wait_vmem();
         lds_barrier();
@@ -406,8 +500,7 @@ struct SharedNarrow {
 
 // Few rows (one block of 32): the waves take every fourth key tile each and join.  A wave has one
 // buffer for keys and one for values: the next tile's keys load as soon as this one's are in
-// registers, its values likewise, so more waves fit a CU than with two buffers each; and the
-// pages of 64 tiles are looked up at a time.
+// registers, its values likewise, so more waves fit a CU than with two buffers each.
 template <typename T, int D, bool GROUP>
 __device__ __forceinline__ void shared_narrow(const SharedGeo& s, int bid, const T* __restrict__ qg,
                                               const T* __restrict__ kg, const T* __restrict__ vg,
@@ -424,6 +517,9 @@ __device__ __forceinline__ void shared_narrow(const SharedGeo& s, int bid, const
     SharedTile& t = job.t;
     int tok, head, pos;
     seq_row(g, t, lane & 31, tok, head);
+    SeqState<T, D> st;
+    st.init();
+    load_query<T, D>(g, t, job.kvh, tok, head, qg, lane, st.qf);  // (arrives while the rest is found)
     if constexpr (GROUP) {
         int tf, hh;
         seq_row(g, t, 0, tf, hh);
@@ -436,75 +532,25 @@ __device__ __forceinline__ void shared_narrow(const SharedGeo& s, int bid, const
     int e0, e1;
     job.keys(s, e0, e1);
 
-    // ---- loads of a tile's keys or values ----
-    R rows;
-    rows.init(lane);
-    const int kt = (int)g.kt;
-    const uint32_t lane_rows = rows.rowl * (uint32_t)kt;
-    const unsigned char* kb = reinterpret_cast<const unsigned char*>(kg) + job.kvh * g.kh;
-    const unsigned char* vb = reinterpret_cast<const unsigned char*>(vg) + job.kvh * g.vh;
+    SharedStage<T, D, GROUP> ld;
+    ld.init(g, job.kvh, lane, kg, vg);
     const int all[1] = {pos};
-    int pass = e0, page0, page1;
-    auto look_up = [&]() __attribute__((always_inline)) {  // pages hold whole blocks of 16 keys
-        const int32_t* row = g.table + (int64_t)t.b * g.max_pages;
-        const int col0 = t.tile(pass + lane) >> g.lgps, col1 = (t.tile(pass + lane) + 16) >> g.lgps;
-        page0 = pass + lane < e1 && col0 < g.max_pages ? row[col0] : -1;
-        page1 = pass + lane < e1 && col1 < g.max_pages ? row[col1] : -1;
-    };
-    auto issue = [&](int e, const unsigned char* head_rows, unsigned char* dst)
-                     __attribute__((always_inline)) {
-        const int j0 = t.tile(e);
-        if (GROUP && t.gaps) t.look(g, j0, all);
-        const int id0 = __builtin_amdgcn_readlane(page0, e - pass);
-        const int id1 = __builtin_amdgcn_readlane(page1, e - pass);
-        const bool ok0 = (unsigned)id0 < (unsigned)g.pages, ok1 = (unsigned)id1 < (unsigned)g.pages;
-        const int in = (1 << g.lgps) - 1;
-        const unsigned char* b0 = head_rows + (int64_t)(ok0 ? id0 : 0) * (int)g.kb + (j0 & in) * kt;
-        const unsigned char* b1 =
-            head_rows + (int64_t)(ok1 ? id1 : 0) * (int)g.kb + ((j0 + 16) & in) * kt;
-        const bool fast = ok0 && ok1 && t.whole(g, j0);
-#pragma unroll
-        for (int n = 0; n < R::kInstr; ++n) {
-            const int r0 = n * R::kRpi;
-            const unsigned char* base = (r0 >= 16 ? b1 : b0) + (r0 & 15) * kt;
-            const uint32_t off = rows.off(n, lane_rows);
-            if (fast) {
-                seq_load(base, off, dst + n * 1024);
-            } else {
-                const bool see = (r0 >= 16 ? ok1 : ok0) && t.sees(g, j0 + r0 + rows.rowl);
-                seq_load(see ? base + off : reinterpret_cast<const unsigned char*>(&kZeroRow),
-                         dst + n * 1024);
-            }
-        }
-    };
-
-    const int64_t hq = (int64_t)job.kvh * g.G + head;
-    SeqState<T, D> st;
-    st.init();
-    {
-        const unsigned char* qp = reinterpret_cast<const unsigned char*>(qg) + hq * g.qh +
-                                  (int64_t)(t.qtok + tok) * g.qt;
-#pragma unroll
-        for (int x = 0; x < F::kKS; ++x)
-            st.qf[x] = ld_x8<T>(reinterpret_cast<const T*>(qp) + x * 16 + 8 * (lane >> 5));
-    }
     F f;
     f.init(lane);
     auto seen = [&](int base) __attribute__((always_inline)) {
         return seen_keys(pos - base, g.W, g.S - base) & below(t.end - base) & ~below(t.from - base);
     };
     unsigned char* buf = smem + wave * 2 * F::kTile;
-    for (; pass < e1; pass += kWave) {
+    for (int pass = e0; pass < e1; pass += kWave) {
         const int end = min(pass + kWave, e1);
         int e = pass + wave;
-        look_up();
-        settle(page0);
-        settle(page1);
+        ld.look_up(g, t, pass, e1, lane);
+        settle(ld.page0);
+        settle(ld.page1);
 #pragma unroll
         for (int x = 0; x < F::kKS; ++x) settle(st.qf[x]);
         if (e < end) {
-            issue(e, kb, buf);
-            issue(e, vb, buf + F::kTile);
+            ld.template issue<1, true, true>(g, t, e, 0, all, buf, buf + F::kTile);
         }
         for (; e < end; e += W) {
             const bool more = e + W < end;
@@ -520,7 +566,7 @@ __device__ __forceinline__ void shared_narrow(const SharedGeo& s, int bid, const
                 [&]() __attribute__((always_inline)) {
                     wait_lds();
                     __builtin_amdgcn_sched_barrier(0);
-                    if (more) issue(e + W, kb, buf);
+                    if (more) ld.template issue<1, true, false>(g, t, e + W, 0, all, buf, buf);
                 },
                 [&]() __attribute__((always_inline)) {
                     if (more) wait_vmem_but<R::kInstr>();  // (all but the next keys')
@@ -529,7 +575,7 @@ __device__ __forceinline__ void shared_narrow(const SharedGeo& s, int bid, const
                 [&]() __attribute__((always_inline)) {
                     wait_lds();
                     __builtin_amdgcn_sched_barrier(0);
-                    if (more) issue(e + W, vb, buf + F::kTile);
+                    if (more) ld.template issue<1, false, true>(g, t, e + W, 0, all, buf, buf + F::kTile);
                 });
         }
     }
