@@ -257,15 +257,19 @@ __device__ __forceinline__ void no_shared_part(const SharedGeo& s, const Job& jo
         s.part_lse[part_row(s, x, job.t.qtok + tok, (int64_t)job.kvh * s.g.G + head)] = -INFINITY;
 }
 
-// Stages key or value rows.  The pages of 64 tiles are looked up at a time, a lane each, not with
-// every tile in front of its loads (which cost the wide form 1 us of every 2.4 us stage).
+// Stages key or value rows.  Where the rows of 64 tiles are, and which of them every row or no row of
+// the wave sees, is found at a time, a lane each: found tile by tile it took the wide form 1 us of
+// every 2.4 us stage.
 template <typename T, int D, bool GROUP>
 struct SharedStage {
     using R = SeqRows<T, D>;
     R rows;
     const unsigned char *kb, *vb;  // the head's rows of page 0
     uint32_t lane_rows;
-    int pass, page0, page1;  // pages of tiles pass + lane (pages hold whole blocks of 16 rows)
+    int pass;                 // tiles pass + lane:
+    int64_t at0, at1;         // bytes of their two blocks of 16 rows from the head's rows of page 0
+    uint64_t fast, ok0, ok1;  // (uniform) both blocks exist and every row is seen; a block exists
+    uint64_t out, full;       // (uniform) no row of the wave sees any key, every row sees all
 
     __device__ __forceinline__ void init(const SeqGeo& g, int kvh, int lane, const void* k,
                                          const void* v) {
@@ -274,13 +278,31 @@ struct SharedStage {
         vb = static_cast<const unsigned char*>(v) + kvh * g.vh;
         lane_rows = rows.rowl * (uint32_t)g.kt;
     }
+    // wmin, wmax: positions of the wave's rows.
     __device__ __forceinline__ void look_up(const SeqGeo& g, const SharedTile& t, int first, int e1,
-                                            int lane) {
+                                            int lane, int wmin, int wmax) {
         pass = first;
         const int32_t* row = g.table + (int64_t)t.b * g.max_pages;
         const int j = t.tile(pass + lane), col0 = j >> g.lgps, col1 = (j + 16) >> g.lgps;
-        page0 = pass + lane < e1 && col0 < g.max_pages ? row[col0] : -1;
-        page1 = pass + lane < e1 && col1 < g.max_pages ? row[col1] : -1;
+        const int in = (1 << g.lgps) - 1;
+        const bool on = pass + lane < e1;
+        const int id0 = on && col0 < g.max_pages ? row[col0] : -1;
+        const int id1 = on && col1 < g.max_pages ? row[col1] : -1;
+        const bool is0 = (unsigned)id0 < (unsigned)g.pages, is1 = (unsigned)id1 < (unsigned)g.pages;
+        at0 = (int64_t)(is0 ? id0 : 0) * g.kb + (j & in) * g.kt;
+        at1 = (int64_t)(is1 ? id1 : 0) * g.kb + ((j + 16) & in) * g.kt;
+        ok0 = __builtin_amdgcn_ballot_w64(is0);
+        ok1 = __builtin_amdgcn_ballot_w64(is1);
+        fast = __builtin_amdgcn_ballot_w64(is0 && is1 && !(GROUP && t.gaps) && t.whole(g, j));
+        out = __builtin_amdgcn_ballot_w64(!on || j > wmax ||
+                                          (wmin - (j + 31) >= g.W && j >= g.S));
+        full = __builtin_amdgcn_ballot_w64(on && j + 31 <= wmin &&
+                                           (wmax - j < g.W || j + 31 < g.S) && j >= t.from &&
+                                           j + 31 < t.end);
+    }
+    __device__ __forceinline__ static int64_t of_lane(int64_t x, int lane) {
+        const uint32_t lo = __builtin_amdgcn_readlane((int)x, lane);
+        return (int64_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | lo;
     }
     // Instructions first, first + STEP, .. of tile e's keys to kdst and of its values to vdst (those
     // of the two that are asked for); pos: see look().
@@ -288,21 +310,18 @@ struct SharedStage {
     __device__ __forceinline__ void issue(const SeqGeo& g, SharedTile& t, int e, int first,
                                           const int (&pos)[N], unsigned char* kdst,
                                           unsigned char* vdst) const {
-        const int j0 = t.tile(e);
-        if (GROUP && t.gaps) t.look(g, j0, pos);
-        const int id0 = __builtin_amdgcn_readlane(page0, e - pass);
-        const int id1 = __builtin_amdgcn_readlane(page1, e - pass);
-        const bool ok0 = (unsigned)id0 < (unsigned)g.pages, ok1 = (unsigned)id1 < (unsigned)g.pages;
-        const int in = (1 << g.lgps) - 1, kt = (int)g.kt;
-        const int64_t at0 = (int64_t)(ok0 ? id0 : 0) * (int)g.kb + (j0 & in) * kt;
-        const int64_t at1 = (int64_t)(ok1 ? id1 : 0) * (int)g.kb + ((j0 + 16) & in) * kt;
-        // (one branch for all loads: a choice for each of them took a third of a stage)
-        if (ok0 && ok1 && t.whole(g, j0)) {
-            if constexpr (K) load<STEP, true>(g, t, j0, first, kb + at0, kb + at1, true, true, kdst);
-            if constexpr (V) load<STEP, true>(g, t, j0, first, vb + at0, vb + at1, true, true, vdst);
+        const int x = e - pass;
+        const int64_t a0 = of_lane(at0, x), a1 = of_lane(at1, x);
+        // (one branch for all loads: a choice for each of them took as long again)
+        if (fast >> x & 1) {
+            if constexpr (K) load<STEP, true>(g, t, 0, first, kb + a0, kb + a1, true, true, kdst);
+            if constexpr (V) load<STEP, true>(g, t, 0, first, vb + a0, vb + a1, true, true, vdst);
         } else {
-            if constexpr (K) load<STEP, false>(g, t, j0, first, kb + at0, kb + at1, ok0, ok1, kdst);
-            if constexpr (V) load<STEP, false>(g, t, j0, first, vb + at0, vb + at1, ok0, ok1, vdst);
+            const int j0 = t.tile(e);
+            const bool b0 = ok0 >> x & 1, b1 = ok1 >> x & 1;
+            if (GROUP && t.gaps) t.look(g, j0, pos);
+            if constexpr (K) load<STEP, false>(g, t, j0, first, kb + a0, kb + a1, b0, b1, kdst);
+            if constexpr (V) load<STEP, false>(g, t, j0, first, vb + a0, vb + a1, b0, b1, vdst);
         }
     }
     template <int STEP, bool FAST>
@@ -392,16 +411,11 @@ __device__ __forceinline__ void shared_wide(const SharedGeo& s, int bid, const T
     static_assert(kEven || R::kInstr == 2, "equal shares");
     SharedStage<T, D, GROUP> ld;
     ld.init(g, job.kvh, lane, kg, vg);
-    ld.look_up(g, t, e0, e1, lane);
-    settle(ld.page0);
-    settle(ld.page1);
+    ld.look_up(g, t, e0, e1, lane, wmin, wmax);
     auto issue_stage = [&](int e, int buf) __attribute__((always_inline)) {
         if (e >= e1) return;
-        if (e - ld.pass >= kWave - SK + 1) {  // (uniform)
-            ld.look_up(g, t, e, e1, lane);
-            settle(ld.page0);
-            settle(ld.page1);
-        }
+        if (e - ld.pass > kWave - SK)  // (uniform; from the stage on that is worked on)
+            ld.look_up(g, t, e - (NB - 1) * SK, e1, lane, wmin, wmax);
 #pragma unroll
         for (int i = 0; i < SK; ++i) {  // (a tile behind the last one: zeros)
             unsigned char* dst = smem + buf * Ring::kStage + i * 2 * F::kTile;
@@ -439,15 +453,15 @@ __device__ __forceinline__ void shared_wide(const SharedGeo& s, int bid, const T
         const unsigned char* base = smem + kBuf * Ring::kStage;
         const unsigned char* tile[SK];
         int j0[SK];
-        bool on[SK], out = true, full = true;
+        bool on[SK];
+        constexpr uint64_t kAll = (1ull << SK) - 1;
+        const bool out = (~ld.out >> (e - ld.pass) & kAll) == 0;
+        const bool full = (~ld.full >> (e - ld.pass) & kAll) == 0;
 #pragma unroll
         for (int i = 0; i < SK; ++i) {
             tile[i] = base + i * 2 * F::kTile;
             j0[i] = t.tile(e + i);
             on[i] = i == 0 || e + i < e1;
-            out = out && (!on[i] || j0[i] > wmax || (wmin - (j0[i] + 31) >= g.W && j0[i] >= g.S));
-            full = full && on[i] && j0[i] + 31 <= wmin && (wmax - j0[i] < g.W || j0[i] + 31 < g.S) &&
-                   j0[i] >= t.from && j0[i] + 31 < t.end;
         }
         if (live && !out) st.template fold<SK>(f, tile, lane, g.c, full, j0, on, seen);
     };
@@ -544,9 +558,7 @@ __device__ __forceinline__ void shared_narrow(const SharedGeo& s, int bid, const
     for (int pass = e0; pass < e1; pass += kWave) {
         const int end = min(pass + kWave, e1);
         int e = pass + wave;
-        ld.look_up(g, t, pass, e1, lane);
-        settle(ld.page0);
-        settle(ld.page1);
+        ld.look_up(g, t, pass, e1, lane, wmin, wmax);
 #pragma unroll
         for (int x = 0; x < F::kKS; ++x) settle(st.qf[x]);
         if (e < end) {
@@ -557,8 +569,7 @@ __device__ __forceinline__ void shared_narrow(const SharedGeo& s, int bid, const
             wait_vmem_but<R::kInstr>();  // (all but the values')
             const unsigned char* ks[1] = {buf};
             const int j0 = t.tile(e);
-            const bool full = j0 + 31 <= wmin && (wmax - j0 < g.W || j0 + 31 < g.S) &&
-                              j0 >= t.from && j0 + 31 < t.end;
+            const bool full = ld.full >> (e - pass) & 1;
             const int js[1] = {j0};
             const bool on[1] = {true};
             st.template fold<1>(
