@@ -181,20 +181,23 @@ static void fill_weights(const na_weights_problem& problem, na::WeightsGeo& w) {
     g.nsplit = (int)((tiles + chunk - 1) / chunk);
     g.fd_tiles.init(g.nsplit);
     int64_t shares = 1;
-    if (w.form == 1) {
+    w.part_keys = (int64_t)g.nsplit * g.chunk * 32;
+    w.joins = (int)((int64_t)g.nsplit * g.chunk / 8);
+    w.fd_joins.init(w.joins);
+    if (w.form == 1 && slices * w.joins < kMaxGrid) {
         // (rows that see any of the 256 keys of a workgroup)
         const int64_t rows = std::min(most, (int64_t)g.W + 256) * g.G;
         const int64_t fill = 1024 / (busy * g.nsplit);
         shares = std::max(rows / 1024, std::min(fill, rows / 128));
         shares = std::min<int64_t>(std::max<int64_t>(shares, 1), 32);
         shares = std::min(shares, std::max<int64_t>(1, (kMaxGrid - 1) / (slices * g.nsplit)));
+        // (the shares' sums take no more than 256 MiB; with no bound of the context they are as long
+        // as the table)
+        shares = std::min(shares, std::max<int64_t>(1, (int64_t(1) << 26) / (slices * w.part_keys)));
         while (shares & (shares - 1)) shares &= shares - 1;
     }
     w.shares = (int)shares;
     w.lgshares = __builtin_ctz(w.shares);
-    w.part_keys = (int64_t)g.nsplit * g.chunk * 32;
-    w.joins = (int)((int64_t)g.nsplit * g.chunk / 8);
-    w.fd_joins.init(w.joins);
 }
 
 static size_t weights_bytes(const na::WeightsGeo& w) {

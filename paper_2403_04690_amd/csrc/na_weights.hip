@@ -143,20 +143,24 @@ __global__ __launch_bounds__((WeightsFew<T, D>::kWaves * 64), 1) void weights_fe
         const int in = (1 << g.lgps) - 1, kt = (int)g.kt;
         const unsigned char* b0 = kb + (int64_t)(ok0 ? id0 : 0) * (int)g.kb + (j0 & in) * kt;
         const unsigned char* b1 = kb + (int64_t)(ok1 ? id1 : 0) * (int)g.kb + ((j0 + 16) & in) * kt;
-        const bool fast = ok0 && ok1 && t.whole(g, j0);
+        auto load = [&](auto fast) __attribute__((always_inline)) {
 #pragma unroll
-        for (int n = 0; n < R::kInstr; ++n) {
-            const int r0 = n * R::kRpi;
-            const unsigned char* base = (r0 >= 16 ? b1 : b0) + (r0 & 15) * kt;
-            const uint32_t off = rows.off(n, klane);
-            if (fast) {
-                seq_load(base, off, dst + n * 1024);
-            } else {
-                const bool see = (r0 >= 16 ? ok1 : ok0) && t.sees(g, j0 + r0 + rows.rowl);
-                seq_load(see ? base + off : reinterpret_cast<const unsigned char*>(&kZeroRow),
-                         dst + n * 1024);
+            for (int n = 0; n < R::kInstr; ++n) {
+                const int r0 = n * R::kRpi;
+                const unsigned char* base = (r0 >= 16 ? b1 : b0) + (r0 & 15) * kt;
+                const uint32_t off = rows.off(n, klane);
+                if constexpr (decltype(fast)::value) {
+                    seq_load(base, off, dst + n * 1024);
+                } else {
+                    const bool see = (r0 >= 16 ? ok1 : ok0) && t.sees(g, j0 + r0 + rows.rowl);
+                    seq_load(see ? base + off : reinterpret_cast<const unsigned char*>(&kZeroRow),
+                             dst + n * 1024);
+                }
             }
-        }
+        };
+        // (one branch for all loads, not a choice for each)
+        if (ok0 && ok1 && t.whole(g, j0)) load(std::true_type{});
+        else load(std::false_type{});
     };
     F f;
     f.init(lane);
