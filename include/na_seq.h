@@ -259,7 +259,8 @@ typedef struct {
  * NA_ERR_SHAPE: page_size and the table's size as in na_cache_attention; kv_heads is below 1 or
  * requests * kv_heads reaches 2^20; budget is below 1, recent or capacity negative, one of
  * budget and num_free reaches 2^30, requests * kv_heads * capacity reaches 2^40; a page's bytes
- * reach 2^31; or new_head is head, or new_context is context_lens.
+ * reach 2^31; or new_head is head, new_context context_lens, new_weights weights, or v_pages
+ * k_pages.
  */
 size_t na_cache_evict_workspace(const na_evict_problem* problem);
 na_status na_cache_evict(const na_evict_problem* problem, const float* weights,

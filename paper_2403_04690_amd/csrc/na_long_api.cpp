@@ -34,7 +34,11 @@ na_status check_shared(const na_shared_problem& s) {
 }
 
 // The cut of the keys of one side over workgroups.  keys: the most that a row tile has;
-// busy: row tiles that are expected to have rows.
+// busy: row tiles that are expected to have rows.  The least lengths are those of cache_attention's
+// splits; a join there is in any case.  256 workgroups of the wide form are aimed at and 512 of the
+// narrow one (64 requests behind 8192 shared tokens, both launches: 30 us; with 512 and 1024 36, with
+// 128 wide 31; proposed tokens behind three prompts 23, with 128 wide 27; chunks of prompts no
+// difference from 128 to 1536).
 void cut_side(na::SharedSide& side, int64_t keys, int64_t busy, int64_t Hkv, bool half) {
     const bool narrow = side.narrow;
     const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32 + 1);
@@ -154,8 +158,10 @@ static na_status check_weights(const na_weights_problem& w) {
 }
 
 // The cut of the work.  Few rows: chunks of 8 to 64 key tiles (what a workgroup sums up at a time),
-// 8192 workgroups if every request had the most keys.  Many: 8 key tiles to a workgroup, whose rows are shared by as many as
-// leave each 1024 rows, or 128 where there would be fewer than 1024 workgroups.
+// 8192 workgroups if every request had the most keys (32 requests of 8k to 32k tokens 112 us, with 4096
+// 118).  Many: 8 key tiles to a workgroup, whose rows are shared by as many as leave each 1024 rows, or
+// 128 where there would be fewer than 1024 workgroups (chunks of 1500 tokens over 2k to 7k: 226 us,
+// with 512 rows the same, with 2048 242; unshared 262).
 static void fill_weights(const na_weights_problem& problem, na::WeightsGeo& w) {
     const na_cache_problem& p = problem.cache;
     std::memset(&w, 0, sizeof w);
@@ -295,7 +301,9 @@ na_status na_cache_evict(const na_evict_problem* problem, const float* weights,
         if (!aligned(x, 4)) return NA_ERR_ALIGNMENT;
     if (!aligned(k_pages, 16) || !aligned(v_pages, 16) || !aligned(workspace, 4))
         return NA_ERR_ALIGNMENT;
-    if (head == new_head || (some && new_context == context_lens)) return NA_ERR_SHAPE;
+    if (head == new_head || (some && new_context == context_lens) ||
+        (some && p.capacity && new_weights == weights) || (some && p.pages && k_pages == v_pages))
+        return NA_ERR_SHAPE;
     const size_t need = na_cache_evict_workspace(problem);
     if (workspace_bytes < need) return NA_ERR_WORKSPACE;
     if (need && !workspace) return NA_ERR_NULL;

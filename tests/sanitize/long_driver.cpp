@@ -212,8 +212,8 @@ int main() {
         e.recent = wild ? any() : pick({0, 1, 100, INT64_MAX});
         e.dtype = c.dtype;
         work_bytes = na_cache_evict_workspace(&e);
-        const na_status es = na_cache_evict(&e, f, dummy, dummy, dummy, dummy, dummy, p, p, dummy + 1, f,
-                                            dummy, dummy + 2, work_base, work_bytes, s);
+        const na_status es = na_cache_evict(&e, f, dummy, dummy, dummy, dummy, dummy, p, dummy + 4,
+                                            dummy + 1, f + 1, dummy, dummy + 2, work_base, work_bytes, s);
         if (!wild && it % 10 && fits) CHECK(es == NA_OK);
     }
     std::printf("ok long %ld %ld\n", checks, launches);

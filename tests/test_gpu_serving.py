@@ -115,6 +115,7 @@ SHARED_CASES = [
     ([50, 90], [1, 3], [0, 2], [200], 4, 1, 64, 16, "fp16", 100, 4),
     ([5, 40, 200], [2, 1, 30], [0, 3], [70], 4, 4, 32, 16, "fp32", 33, 90),
     ([5, 40, 200], [2, 1, 30], [0, 3], [70], 4, 2, 128, 16, "bf16", 1, 1),
+    ([20, 9], [3, 1], [0, 2], [70], 200, 2, 32, 16, "fp16", 60, 2),
     # a whole block of heads of one token, and more
     ([3, 3], [1, 1], [0, 2], [100], 64, 1, 64, 16, "bf16", None, 0),
     # chunks of prompts
@@ -140,6 +141,10 @@ def test_long_shared_tokens_are_split_and_joined(na, dtype, D, new):
     own, hint = [900, 0, 31], {"max_new": max(new), "max_shared": 4000, "max_own": 1000}
     _shared_check(na, own, new, [0, 3], [4000], 4, 2, D, 16, dtype, **hint)
     _shared_check(na, own, new, [0, 1, 3], [700, 3333], 4, 2, D, 64, dtype, 3000, 5, **hint)
+    # one workgroup for all shared keys of its rows, and for all own ones
+    few = {"max_new": max(new), "max_shared": 1, "max_own": 1}
+    _shared_check(na, own, new, [0, 3], [4000], 4, 2, D, 16, dtype, **few)
+    _shared_check(na, [3000, 2500, 5], new, [0, 2, 3], [700, 90], 4, 2, D, 32, dtype, 2300, 70, **few)
 
 
 def test_shared_tokens_reach_past_a_context(na):
@@ -350,6 +355,8 @@ WEIGHT_CASES = [
     ([600], [300], 3, 3, 64, 16, "fp32", 7, 0, None),
     ([2000], [40], 2, 2, 32, 16, "fp16", 300, 16, [5]),
     ([900, 0], [33, 257], 14, 2, 128, 16, "bf16", 700, 1, None),
+    ([200, 3], [9, 3], 200, 2, 32, 16, "fp16", 60, 2, None),  # heads of a token over several stages
+    ([200, 3], [9, 30], 48, 1, 64, 16, "bf16", None, 0, None),
 ]
 
 
@@ -371,6 +378,9 @@ def test_weights_behind_the_capacity_are_not_kept(na, capacity):
 def test_weights_of_long_contexts(na, dtype, D):
     _weights_check(na, [9000, 1290], [1, 1], 4, 2, D, 16, dtype, max_new=1, max_context=9001)
     _weights_check(na, [5000, 1290], [1, 90], 4, 2, D, 64, dtype, 4000, 4, max_new=90)
+    # one workgroup for all keys of a request
+    _weights_check(na, [5000, 1290], [1, 1], 4, 2, D, 16, dtype, max_new=1, max_context=1)
+    _weights_check(na, [2500, 700], [1, 90], 4, 2, D, 16, dtype, max_new=90, max_context=1)
 
 
 def test_weights_of_many_requests(na):
@@ -543,6 +553,19 @@ def test_evict_of_many_requests(na):
     context = [rng.choice((0, -4, rng.randint(1, 90))) for _ in range(R)]
     first = [rng.randint(-1, 40) for _ in range(R)]
     _evict_check(na, _weights(R, 2, 90), context, 32, 16, "fp16", 30, 6, first)
+
+
+def test_evict_returns_pages_of_very_many_requests(na):
+    """More requests, and more freed pages, than are looked at in one go."""
+    rng = random.Random(7)
+    R = 2100
+    context = [rng.choice((0, 5, rng.randint(1, 80))) for _ in range(R)]
+    _evict_check(na, _weights(R, 1, 80), context, 32, 16, "fp16", 17, 3)
+    _evict_check(na, _weights(2, 1, 40000), [40000, 39000], 32, 16, "fp16", 5000, 3)
+    table, P, _ = _tables([40000, 39000], [0, 0], 16, [0], [])
+    for r, x in ((0, 400), (0, 1999), (1, 2000), (1, 313)):
+        table[r][x] = -1
+    _evict_check(na, _weights(2, 1, 40000), [40000, 39000], 32, 16, "fp16", 5000, 3, table=table)
 
 
 def test_evict_pages_that_do_not_exist(na):

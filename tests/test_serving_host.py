@@ -113,7 +113,8 @@ EVICT = ("weights", "ctx", "first", "table", "head", "free", "kp", "vp", "new_ct
 
 
 def _cut(lib, p, work=FAKE, size=1 << 50, **ptr):
-    ps = [ptr.get(n, FAKE + (64 if n in ("new_head", "new_ctx") else 0)) for n in EVICT]
+    other = ("new_head", "new_ctx", "new_weights", "vp")
+    ps = [ptr.get(n, FAKE + (64 if n in other else 0)) for n in EVICT]
     return lib.na_cache_evict(p, *ps, work, size, None)
 
 
@@ -141,6 +142,8 @@ def test_evict_pointers_and_workspace(lib):
         assert _cut(lib, _evict(), **{name: FAKE + 8}) == ALIGN
     assert _cut(lib, _evict(), new_head=FAKE) == SHAPE
     assert _cut(lib, _evict(), new_ctx=FAKE) == SHAPE
+    assert _cut(lib, _evict(), new_weights=FAKE) == SHAPE
+    assert _cut(lib, _evict(), vp=FAKE) == SHAPE
     need = lib.na_cache_evict_workspace(_evict())
     assert need == 3 * 2 * (2 * 20 + 2) * 4
     assert _cut(lib, _evict(), size=need - 1) == WORKSPACE
