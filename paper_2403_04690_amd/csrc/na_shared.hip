@@ -347,6 +347,14 @@ struct SharedStage {
     }
 };
 
+// Bits e of the keys base + e that a row at position pos sees.  (Rows of a group stand far apart: a
+// distance is cut off where no key is seen any more, so that the window's end stays in 32 bits.)
+__device__ __forceinline__ unsigned visible_keys(const SeqGeo& g, const SharedTile& t, int pos,
+                                                 int base) {
+    return seen_keys(max(pos - base, -64), g.W, g.S - base) & below(t.end - base) &
+           ~below(t.from - base);
+}
+
 // The operand of this lane's row of q.
 template <typename T, int D>
 __device__ __forceinline__ void load_query(const SeqGeo& g, const SharedTile& t, int kvh, int tok,
@@ -444,7 +452,7 @@ __device__ __forceinline__ void shared_wide(const SharedGeo& s, int bid, const T
 #pragma unroll
     for (int x = 0; x < F::kKS; ++x) settle(st.qf[x]);
     auto seen = [&](int base) __attribute__((always_inline)) {
-        return seen_keys(pos - base, g.W, g.S - base) & below(t.end - base) & ~below(t.from - base);
+        return visible_keys(g, t, pos, base);
     };
 
     // One stage, in buffer BUF (see na_seq_fwd.hip).
@@ -558,7 +566,7 @@ __device__ __forceinline__ void shared_narrow(const SharedGeo& s, int bid, const
     F f;
     f.init(lane);
     auto seen = [&](int base) __attribute__((always_inline)) {
-        return seen_keys(pos - base, g.W, g.S - base) & below(t.end - base) & ~below(t.from - base);
+        return visible_keys(g, t, pos, base);
     };
     unsigned char* buf = smem + wave * 2 * F::kTile;
     for (int pass = e0; pass < e1; pass += kWave) {
