@@ -167,7 +167,8 @@ def cache_evict(weights, k_pages, v_pages, page_table, context_lens, free_pages,
     and of the others those that lie behind their part of the positions fill the places of those
     that go, in order; keys and values move with them, on the request's own pages.  Pages that
     are no longer needed return to free_pages below index head (int32 [1]).  Requests may share
-    the pages of their first first[r] tokens, no others.
+    pages that hold nothing but tokens before min(first[r], budget); a page with any token behind
+    them belongs to one request.
     Returns (context_lens, weights, kept, head): the lengths after it, the weights that moved along
     (0 behind the tokens), for every position the one that its token had (int32 [requests,
     kv_heads, budget], -1 behind the tokens) and the free list's new head.  page_table is left as
