@@ -323,7 +323,8 @@ na_status na_cache_evict(const na_evict_problem* problem, const float* weights,
     while (v.lgslice > 6 && (slices * 2 << (v.lgrow - v.lgslice)) < 1024) --v.lgslice;
     // (8192 workgroups, most of which may find nothing to move: 8 long prompts 80 us, with 2048 90)
     const int64_t most = std::max<int64_t>(1, std::min(p.budget, p.max_pages * p.page_size));
-    const int64_t chunks = std::min((most + 127) / 128, std::max<int64_t>(1, 4096 / std::max<int64_t>(1, slices)));
+    const int64_t chunks = std::min(
+        (most + 127) / 128, std::max<int64_t>(1, 4096 / std::max<int64_t>(1, slices)));
     v.chunk = (int)((most + chunks - 1) / chunks);
     v.chunks = (int)((most + v.chunk - 1) / v.chunk);
     v.fd_chunks.init(v.chunks);

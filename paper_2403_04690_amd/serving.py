@@ -101,7 +101,8 @@ def _check_first(first, requests, device):
 @functools.lru_cache(maxsize=256)
 def _weights_plan(kernel_size, sinks, scale, max_new, max_context, metas):
     """The problem of na_cache_weights (kept alive by the cache's entry), its address and its
-    workspace's size.  metas: of q, lse, k_pages, page_table, context_lens, cu_new, weights and first."""
+    workspace's size.  metas: of q, lse, k_pages, page_table, context_lens, cu_new, weights and
+    first."""
     q, lse, k_pages, table, context, cu_new, weights, first = metas
     if lse is None:
         raise ValueError("lse is needed")
@@ -124,8 +125,8 @@ def cache_weights(q, lse, k_pages, page_table, context_lens, cu_new, weights, ke
     were.  Start a request's entries at 0."""
     _library()
     p, at, need = _weights_plan(*_window(kernel_size, sinks, scale), *_bounds(max_new, max_context),
-                          _metas(q, lse, k_pages, page_table, context_lens, cu_new, weights,
-                                 first))
+                                _metas(q, lse, k_pages, page_table, context_lens, cu_new, weights,
+                                       first))
     work = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     _call("na_cache_weights", q.device, at, q.data_ptr(), lse.data_ptr(), k_pages.data_ptr(),
           page_table.data_ptr(), context_lens.data_ptr(), cu_new.data_ptr(),
