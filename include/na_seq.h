@@ -175,7 +175,9 @@ typedef struct {
  * Both are int32 device arrays (they may be NULL where groups is 0).  max_new bounds the new tokens
  * of a request, max_shared the shared ones of a group, max_own those of a request behind the
  * shared ones, the new ones among them (0: unknown): they choose how the work is split, and are
- * not relied on for the result.
+ * not relied on for the result.  A row that sees a key whose score is NaN or +inf (a key that is
+ * not finite, or a product beyond fp32) gets NaN in out and logsumexp; a value that is not finite
+ * makes its column so, as in na_cache_attention.
  * workspace: na_cache_shared_attention_workspace(problem) bytes; NA_ERR_WORKSPACE if
  * workspace_bytes is less.  (0 for a problem that is empty or not valid.)
  * NA_ERR_SHAPE: what na_cache_attention refuses; groups is negative or reaches 2^24; a bound is

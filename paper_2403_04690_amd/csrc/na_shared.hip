@@ -6,8 +6,8 @@
 // so the shared keys are one problem of all the rows of a group (every request's new tokens times
 // the heads of a key/value head), the keys behind them one problem a request, and a second
 // launch joins the parts.  Each of the problems is cut into splits of its keys; every
-// split of every row leaves a logsumexp (-inf where the row sees nothing of it) and, unless it
-// is -inf, its mean of the values, both in fp32.
+// split of every row leaves a logsumexp (-inf where the row sees nothing of it, NaN where a score
+// is none or infinite) and, unless it is -inf, its mean of the values, both in fp32.
 //   64 requests of one token behind 8192 shared ones and 16 to 1024 of their own, 16 heads on 4, bf16
 // D = 128: 28 us a call; request by request the shared keys and values alone would be 1.1 GB.  Chunks
 // of 64 to 300 tokens of 16 requests behind 4k and 6k shared ones: 208 us (0.71 PFLOP/s).
@@ -245,6 +245,28 @@ struct SharedJob {
         e1 = split == side.nsplit - 1 ? t.nT : min(e0 + side.chunk, t.nT);
     }
 };
+
+// The build takes floats for numbers, so whether one is NaN is asked of its bits, behind a point
+// at which the compiler knows nothing of it.
+constexpr uint32_t kNaN = 0x7fc00000u;
+__device__ __forceinline__ uint32_t bits_of(float x) {
+    settle(x);
+    return __float_as_uint(x);
+}
+__device__ __forceinline__ bool is_nan(uint32_t bits) { return (bits & 0x7fffffffu) > 0x7f800000u; }
+
+// x, or NaN where `nan`, for stores and conversions.
+__device__ __forceinline__ float or_nan(float x, bool nan) {
+    float y = __uint_as_float(nan ? kNaN : bits_of(x));
+    settle(y);
+    return y;
+}
+
+// Logsumexp in base 2 from its reference and its sum: -inf where the sum is 0.  (A score that is
+// NaN or +inf leaves a sum of NaN; the row has no result then.)
+__device__ __forceinline__ float logsumexp2(float mref, float sum) {
+    return sum > 0.f ? mref + __log2f(sum) : -INFINITY;
+}
 
 // Place of a row's part: its logsumexp (base 2); D times that its mean of the values.
 __device__ __forceinline__ int64_t part_row(const SharedGeo& s, int part, int tok, int64_t head) {
@@ -500,7 +522,7 @@ __device__ __forceinline__ void shared_wide(const SharedGeo& s, int bid, const T
     const float inv = some ? 1.f / l : 0.f;
     const int h = lane >> 5;
     const int64_t row = part_row(s, job.part, t.qtok + tok, hq);
-    if (h == 0) s.part_lse[row] = some ? st.mref + __log2f(l) : -INFINITY;
+    if (h == 0) s.part_lse[row] = or_nan(logsumexp2(st.mref, l), is_nan(bits_of(l)));
     if (!some) return;
     float* po = s.part + row * D;
 #pragma unroll
@@ -638,13 +660,15 @@ __device__ __forceinline__ void shared_narrow(const SharedGeo& s, int bid, const
         for (int x = threadIdx.x; x < t.rows * (N::kCols / 4); x += W * 64) {
             const int row = x / (N::kCols / 4), d = x % (N::kCols / 4) * 4;
             float mx = -INFINITY, sum = 0.f;
+            bool nan = false;
             f32x4 acc{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < W; ++w) mx = fmaxf(mx, stat[(w * 32 + row) * 2]);
 #pragma unroll
             for (int w = 0; w < W; ++w) {
-                const float m = stat[(w * 32 + row) * 2];
-                sum += m == -INFINITY ? 0.f : fast_exp2(m - mx) * stat[(w * 32 + row) * 2 + 1];
+                const float m = stat[(w * 32 + row) * 2], lw = stat[(w * 32 + row) * 2 + 1];
+                nan = nan || is_nan(bits_of(lw));
+                sum += m == -INFINITY ? 0.f : fast_exp2(m - mx) * lw;
                 acc += *reinterpret_cast<const f32x4*>(smem + (w * 32 + row) * N::kRow + d * 4);
             }
             const bool some = sum > 0.f;
@@ -652,7 +676,7 @@ __device__ __forceinline__ void shared_narrow(const SharedGeo& s, int bid, const
             seq_row(g, t, row, tk, hd);
             const int64_t pr = part_row(s, job.part, t.qtok + tk, (int64_t)job.kvh * g.G + hd);
             if (some) st16(s.part + pr * D + c0 * 32 + d, acc * (1.f / sum));
-            if (c0 == 0 && d == 0) s.part_lse[pr] = some ? mx + __log2f(sum) : -INFINITY;
+            if (c0 == 0 && d == 0) s.part_lse[pr] = or_nan(logsumexp2(mx, sum), nan);
         }
         if (c0 + kBlocks < F::kDB) __syncthreads();
     }
@@ -698,15 +722,24 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedGeo s, int lgM, 
         const float* lse = s.part_lse + at;
         const float* y = s.part + at * D + mine * 4;
         float mx = -INFINITY;
-        for (int p = mine; p < parts; p += kThreads) mx = fmaxf(mx, lse[p * apart]);
+        int nan = 0;
+        for (int p = mine; p < parts; p += kThreads) {
+            const float e = lse[p * apart];
+            nan |= is_nan(bits_of(e));
+            mx = fmaxf(mx, e);
+        }
 #pragma unroll
-        for (int d = kThreads / 2; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d, kWave));
+        for (int d = kThreads / 2; d > 0; d >>= 1) {
+            mx = fmaxf(mx, __shfl_xor(mx, d, kWave));
+            nan |= __shfl_xor(nan, d, kWave);
+        }
         float sum = 0.f;
         f32x4 acc{0.f, 0.f, 0.f, 0.f};
         for (int p0 = 0; p0 < parts; p0 += kThreads) {
-            // (a part that sees nothing has no mean: it may hold anything)
+            // (a part that sees nothing has no mean: it may hold anything, and weighs -1.  One whose
+            // weight vanishes has a mean, which may be infinite or NaN)
             const float e = p0 + mine < parts ? lse[(p0 + mine) * apart] : -INFINITY;
-            const float w = e == -INFINITY ? 0.f : fast_exp2(e - mx);
+            const float w = e == -INFINITY ? -1.f : fast_exp2(e - mx);
             const int n = min(kThreads, parts - p0);
             for (int x0 = 0; x0 < n; x0 += 8) {
                 f32x4 v[8];
@@ -715,20 +748,23 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedGeo s, int lgM, 
                     v[x] = ld16<f32x4>(y + (int64_t)(p0 + min(x0 + x, n - 1)) * apart * D);
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {
-                    const float wx = x0 + x < n ? __shfl(w, (x0 + x) % kThreads, kThreads) : 0.f;
-                    sum += wx;
+                    const float wx = x0 + x < n ? __shfl(w, (x0 + x) % kThreads, kThreads) : -1.f;
+                    sum += fmaxf(wx, 0.f);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) acc[c] = wx > 0.f ? fmaf(v[x][c], wx, acc[c]) : acc[c];
+                    for (int c = 0; c < 4; ++c) acc[c] = wx >= 0.f ? fmaf(v[x][c], wx, acc[c]) : acc[c];
                 }
             }
         }
         const bool some = sum > 0.f;
         T* op = reinterpret_cast<T*>(reinterpret_cast<unsigned char*>(og) + hr * g.oh +
                                      (int64_t)(t.qtok + tok) * g.ot);
-        st_x4<T>(op + mine * 4, acc * (some ? 1.f / sum : 0.f));
+        acc *= some ? 1.f / sum : 0.f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[c] = or_nan(acc[c], nan);
+        st_x4<T>(op + mine * 4, acc);
         if (mine == 0)
             lseg[hr * g.lh + (int64_t)(t.qtok + tok) * g.lt] =
-                some ? (mx + __log2f(sum)) * kLn2 : -INFINITY;
+                or_nan(logsumexp2(mx, sum) * kLn2, nan);
     }
 }
 

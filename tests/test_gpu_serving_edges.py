@@ -1,0 +1,126 @@
+"""The cache operators for long contexts at the edges of their inputs: values that are not finite,
+positions that are far apart."""
+import math
+
+import pytest
+import torch
+
+from tests import sequence_plain as plain
+from tests import serving_plain as ref
+from tests.test_gpu_serving import (DT, WHOLE, _int, _offsets, _randn, _tables,  # noqa: F401
+                                    na)
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------- values that are not finite
+
+class _Served:
+    """Requests 0 and 1 share 100 tokens, request 2 is in no group; every request lists the shared
+    pages, so that cache_attention reads the same keys."""
+
+    def __init__(self, na, dtype, D, new, own=(40, 470, 20), H=4, Hkv=2, page=16, scale=None):
+        self.na, self.scale, self.new = na, scale, new
+        self.context = [own[0] + 100, own[1] + 100, own[2]]
+        table, P, _ = _tables(self.context, new, page, [0, 2], [96])
+        self.table = table
+        self.kp, self.vp = (_randn((P, Hkv, page, D), dtype, 1 + i) for i in range(2))
+        # (the page in which the shared tokens end is request 0's and, copied, request 1's)
+        for t in (self.kp, self.vp):
+            t[table[1][6], :, :4] = t[table[0][6], :, :4]
+        self.q = _randn((sum(new), H, D), dtype, 3)
+        self.page, self.G = page, H // Hkv
+
+    def put(self, pages, r, j, head, value):
+        """The row of position j of request r; shared ones of both that have them."""
+        for x in ((0, 1) if r < 2 and j < 100 else (r,)):
+            pages[self.table[x][j // self.page], head, j % self.page] = value
+
+    def shared(self, **hints):
+        return self.na.cache_shared_attention(
+            self.q, self.kp, self.vp, torch.tensor(self.table).int().cuda(), _int(self.context),
+            _offsets(self.new), _int([0, 2]), _int([100]), None, 0, self.scale, **hints)
+
+    def attend(self):
+        return self.na.cache_attention(
+            self.q, self.kp, self.vp, torch.tensor(self.table).int().cuda(), _int(self.context),
+            _offsets(self.new), None, 0, self.scale)[0]
+
+
+FORMS = [([1, 1, 1], {"max_new": 1, "max_shared": 100, "max_own": 500}), ([40, 3, 2], {}),
+         ([1, 1, 1], {"max_new": 1, "max_shared": 1, "max_own": 1}),
+         ([90, 130, 1], {"max_new": 130, "max_shared": 100, "max_own": 1})]
+
+
+@pytest.mark.parametrize("dtype,D", [("fp32", 32), ("fp16", 64), ("bf16", 128), ("fp32", 128)])
+@pytest.mark.parametrize("new,hints", FORMS)
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+@pytest.mark.parametrize("request_,j", [(0, 33), (0, 120), (1, 400), (1, 98), (2, 7)])
+def test_a_key_that_is_not_finite_shows_in_the_rows_that_see_it(na, dtype, D, new, hints, value,
+                                                               request_, j):
+    x = _Served(na, dtype, D, new)
+    out, lse = x.shared(**hints)
+    assert bool(out.isfinite().all()) and bool(lse.isfinite().all())
+    x.put(x.kp, request_, j, 1, value)  # (of head 1: heads 2 and 3 of the queries)
+    bad, bad_lse = x.shared(**hints)
+    hit = torch.zeros(sum(new), 4, dtype=torch.bool)
+    at = [sum(new[:r]) for r in range(4)]
+    for r in ((0, 1) if request_ < 2 and j < 100 else (request_,)):
+        hit[at[r]:at[r + 1], 2:] = True
+    hit = hit.cuda()
+    assert not bool(bad.isfinite()[hit].any()) and not bool(bad_lse.isfinite()[hit].any())
+    assert torch.equal(bad[~hit], out[~hit]) and torch.equal(bad_lse[~hit], lse[~hit])
+    assert torch.equal(x.attend().isfinite(), bad.isfinite())
+
+
+@pytest.mark.parametrize("dtype,D", [("fp32", 32), ("fp16", 64), ("bf16", 128)])
+@pytest.mark.parametrize("new,hints", FORMS)
+def test_a_query_that_is_not_finite_shows_in_its_row(na, dtype, D, new, hints):
+    x = _Served(na, dtype, D, new)
+    out, lse = x.shared(**hints)
+    hit = torch.zeros(sum(new), 4, dtype=torch.bool, device="cuda")
+    for t, h, value in ((0, 1, math.nan), (sum(new) - 1, 3, math.inf), (new[0], 2, math.nan)):
+        x.q[t, h, 5:7] = value
+        hit[t, h] = True
+    x.q[sum(new) - 1, 3, 6] = -math.inf
+    bad, bad_lse = x.shared(**hints)
+    nan = torch.zeros_like(hit)
+    nan[0, 1] = nan[new[0], 2] = True
+    assert not bool(bad.isfinite()[nan].any()) and not bool(bad_lse.isfinite()[nan].any())
+    # (infinite scores of both signs are among the keys of the third one)
+    assert not bool(bad.isfinite()[hit].any()) and not bool(bad_lse.isfinite()[hit].any())
+    assert torch.equal(bad[~hit], out[~hit]) and torch.equal(bad_lse[~hit], lse[~hit])
+
+
+@pytest.mark.parametrize("new,hints", FORMS)
+def test_scores_that_overflow_show(na, new, hints):
+    """Finite queries and keys whose products are beyond fp32."""
+    for j in (33, 120):
+        x = _Served(na, "bf16", 64, new)
+        x.put(x.kp, 0, j, 0, 1e30)
+        x.q[0, 0] = 1e30
+        out, lse = x.shared(**hints)
+        assert not bool(out[0, 0].isfinite().any()) and not bool(lse[0, 0].isfinite())
+        assert not bool(x.attend()[0, 0].isfinite().any())
+
+
+@pytest.mark.parametrize("dtype,D", [("fp32", 64), ("fp16", 128), ("bf16", 32)])
+@pytest.mark.parametrize("new,hints", FORMS)
+@pytest.mark.parametrize("scale", [None, 400.0])
+def test_values_that_are_not_finite_show_where_cache_attention_has_them(na, dtype, D, new, hints, scale):
+    """In their column, with a weight that vanishes against the other keys' too."""
+    x = _Served(na, dtype, D, new, scale=scale)
+    out, lse = x.shared(**hints)
+    places = [(0, 33, 5, math.nan), (1, 400, 9, math.nan), (2, 7, 3, math.nan), (0, 120, 1, math.nan)]
+    for r, j, d, value in places:
+        for y in ((0, 1) if r < 2 and j < 100 else (r,)):
+            x.vp[x.table[y][j // 16], 1, j % 16, d] = value
+    bad, bad_lse = x.shared(**hints)
+    assert torch.equal(bad_lse, lse)
+    hit = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+    at = [sum(new[:r]) for r in range(4)]
+    for r, j, d, _ in places:
+        for y in ((0, 1) if r < 2 and j < 100 else (r,)):
+            hit[at[y]:at[y + 1], 2:, d] = True
+    assert not bool(bad.isfinite()[hit].any()) and torch.equal(bad[~hit], out[~hit])
+    assert torch.equal(x.attend().isfinite(), bad.isfinite())
