@@ -34,17 +34,18 @@ na_status check_shared(const na_shared_problem& s) {
 }
 
 // The cut of the keys of one side over workgroups.  keys: the most that a row tile has;
-// busy: row tiles that are expected to have rows.  The least lengths are those of cache_attention's
-// splits; a join there is in any case.  256 workgroups of the wide form are aimed at and 512 of the
-// narrow one (64 requests behind 8192 shared tokens, both launches: 30 us; with 512 and 1024 36, with
+// busy: row tiles that are expected to have rows; room: the most workgroups.  The least lengths
+// are those of cache_attention's splits; a join there is in any case.  256 workgroups of the wide
+// form are aimed at and 512 of the narrow one (64 requests behind 8192 shared tokens, both launches: 30 us; with 512 and 1024 36, with
 // 128 wide 31; proposed tokens behind three prompts 23, with 128 wide 27; chunks of prompts no
 // difference from 128 to 1536).
-void cut_side(na::SharedSide& side, int64_t keys, int64_t busy, int64_t Hkv, bool half) {
+void cut_side(na::SharedSide& side, int64_t keys, int64_t busy, int64_t Hkv, bool half,
+              int64_t room) {
     const bool narrow = side.narrow;
     const int64_t tiles = std::max<int64_t>(1, (keys + 31) / 32 + 1);
     int64_t split = std::max<int64_t>(1, (narrow ? 512 : 256) / std::max<int64_t>(1, busy * Hkv));
     split = std::min<int64_t>(split, na::kSeqMaxSplit);
-    split = std::min(split, std::max<int64_t>(1, (kMaxGrid - 1) / ((int64_t)side.ntiles * Hkv)));
+    split = std::min(split, std::max<int64_t>(1, room / ((int64_t)side.ntiles * Hkv)));
     const int64_t least = half ? (narrow ? 12 : 8) : (narrow ? 8 : 2);
     const int64_t step = narrow ? 4 : 2;
     int64_t chunk = split == 1 ? tiles : std::max<int64_t>(least, (tiles + split - 1) / split);
@@ -64,30 +65,31 @@ void fill_shared(const na_shared_problem& s, na::SharedGeo& x) {
     const bool half = p.dtype != NA_FP32;
     x.groups = (int)s.groups;
 
-    na::SharedSide& own = x.own_side;
+    na::SharedSide &own = x.own_side, &shared = x.shared_side;
     own.narrow = cache_narrow(p);
-    const int64_t M = own.narrow ? 32 : 128;
-    own.ntiles = g.ntiles = (int)(rows / M + p.requests);
-    int64_t keys = s.max_own > 0 ? std::min(s.max_own, room) : room;
-    keys = std::min(keys, (int64_t)g.W + g.S + M + 64);
-    cut_side(own, keys, std::max((rows + M - 1) / M, std::min(p.requests, p.tokens)), g.Hkv, half);
-
-    na::SharedSide& shared = x.shared_side;
-    shared.fd_tiles.init(1);
-    if (s.groups == 0) return;
     // (the narrow form where a group's rows are expected to fill one block of 32)
     shared.narrow = rows <= 32 * s.groups;
+    auto tiles = [&](bool narrow, int64_t n) { return n ? rows / (narrow ? 32 : 128) + n : 0; };
+    // One grid for both sides.  Where narrow tiles of both would not fit it: wide ones, for which
+    // check_shared has left room.
+    if ((tiles(own.narrow, p.requests) + tiles(shared.narrow, s.groups)) * g.Hkv >= kMaxGrid)
+        own.narrow = shared.narrow = false;
+    own.ntiles = g.ntiles = (int)tiles(own.narrow, p.requests);
+    shared.ntiles = (int)tiles(shared.narrow, s.groups);
+
+    const int64_t M = own.narrow ? 32 : 128;
+    int64_t keys = s.max_own > 0 ? std::min(s.max_own, room) : room;
+    keys = std::min(keys, (int64_t)g.W + g.S + M + 64);
+    cut_side(own, keys, std::max((rows + M - 1) / M, std::min(p.requests, p.tokens)), g.Hkv, half,
+             kMaxGrid - 1 - (int64_t)shared.ntiles * g.Hkv);
+
+    shared.fd_tiles.init(1);
+    if (s.groups == 0) return;
     const int64_t Ms = shared.narrow ? 32 : 128;
-    shared.ntiles = (int)(rows / Ms + s.groups);
     keys = s.max_shared > 0 ? std::min(s.max_shared, room) : room;
     cut_side(shared, keys, std::max((rows + Ms - 1) / Ms, std::min(s.groups, p.tokens)), g.Hkv,
-             half);
-    // (one grid for both sides)
-    const int64_t own_jobs = (int64_t)own.ntiles * g.Hkv * own.nsplit;
-    const int64_t tiles = (int64_t)shared.ntiles * g.Hkv;
-    const int64_t most = std::max<int64_t>(1, (kMaxGrid - 1 - own_jobs) / tiles);
-    if (shared.nsplit > most) shared.nsplit = (int)most;
-    x.shared_jobs = (int)(tiles * shared.nsplit);
+             half, kMaxGrid - 1 - (int64_t)own.ntiles * g.Hkv * own.nsplit);
+    x.shared_jobs = shared.ntiles * g.Hkv * shared.nsplit;
 }
 
 size_t shared_bytes(const na_shared_problem& s, const na::SharedGeo& x) {
