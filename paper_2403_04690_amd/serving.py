@@ -24,12 +24,14 @@ from operator import index
 
 import torch
 
-from . import DTYPES
+from . import DTYPES, _check
 from .sequence import (_attention_problem, _bounds, _call, _check_pages, _contiguous, _count,
                        _EvictProblem, _ints, _layout, _library, _lse_shape, _metas, _rows,
                        _SharedProblem, _WeightsProblem, _window)
 
 __all__ = ["cache_shared_attention", "cache_weights", "cache_evict"]
+
+_ERR_NULL = 1  # NA_ERR_NULL
 
 
 @functools.lru_cache(maxsize=256)
@@ -156,6 +158,11 @@ def _evict_plan(budget, recent, metas):
     p = _EvictProblem(context[0][0], kv_heads, D, P, page_size, table[0][1], free[0][0],
                       weights[0][2], _count(budget, "budget", 1), _count(recent, "recent", 0),
                       DTYPES[k_pages[2]])
+    # (without pointers: what the library refuses of the problem itself it refuses before those, and
+    # here before the call's outputs, which have its sizes, are allocated)
+    status = _library().na_cache_evict(p, *[None] * 13, 0, None)
+    if status != _ERR_NULL:
+        _check(status)
     return p, ctypes.addressof(p), _library().na_cache_evict_workspace(p)
 
 

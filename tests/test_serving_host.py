@@ -248,6 +248,26 @@ def test_plans_check_what_belongs_together(lib):
             cut(**bad)
 
 
+def test_evict_plans_refuse_what_the_library_refuses(lib):
+    """Before the call allocates outputs of such sizes."""
+    gpu = "cuda:0"
+    kp, w = _meta(torch.zeros(5, 2, 16, 32), gpu), _meta(torch.zeros(2, 2, 64), gpu)
+    table, ctx = _meta(torch.zeros(2, 4, dtype=torch.int32), gpu), _meta(_ints(3, 4), gpu)
+    free, head = _meta(_ints(1, 2, 3), gpu), _meta(_ints(0), gpu)
+
+    def cut(budget, kp=kp, w=w):
+        return serving._evict_plan.__wrapped__(budget, 0, (w, kp, kp, table, ctx, free, head, None))
+
+    assert cut(2 ** 30 - 1)[0].budget == 2 ** 30 - 1
+    odd = torch.Size((5, 2, 24, 32)), (2 * 24 * 32, 24 * 32, 32, 1), torch.float32, kp[3]
+    for bad, status in (({"budget": 2 ** 30}, SHAPE), ({"budget": 2 ** 40}, SHAPE),
+                        ({"budget": 9, "kp": odd}, SHAPE),
+                        ({"budget": 9, "kp": _meta(torch.zeros(5, 2, 16, 48), gpu)}, HEAD_DIM)):
+        with pytest.raises(na.NAError) as e:
+            cut(**bad)
+        assert e.value.status == status
+
+
 # ---------------------------------------------------------------- the plain forms
 
 def test_plain_shared_is_plain_attention_where_nothing_is_shared():
