@@ -399,7 +399,7 @@ __device__ __forceinline__ void seq_contiguous(const SeqGeo& g, int tile, int sl
 }
 
 // Stages key tile `e` of the workgroup's tile: instructions first, first + STEP, ... of the
-// 2 kInstr of K and V (first < STEP).  Tile: a SeqTile, or one with the same members.
+// 2 kInstr of K and V (first < STEP).
 template <typename T, int D, bool PAGED, int STEP>
 struct SeqStage {
     using R = SeqRows<T, D>;
@@ -413,8 +413,7 @@ struct SeqStage {
     uint32_t klane, vlane;  // rowl * token stride
     int kt, vt;             // token strides (below 2^26 bytes)
 
-    template <typename Tile>
-    __device__ __forceinline__ void init(const SeqGeo& g, const Tile& t, int kvh, int lane,
+    __device__ __forceinline__ void init(const SeqGeo& g, const SeqTile& t, int kvh, int lane,
                                          const void* k, const void* v) {
         rows.init(lane);
         kb = static_cast<const unsigned char*>(k) + kvh * g.kh;
@@ -429,8 +428,7 @@ struct SeqStage {
         vlane = rows.rowl * (uint32_t)vt;
     }
 
-    template <typename Tile>
-    __device__ __forceinline__ void issue(const SeqGeo& g, const Tile& t, int e, int first,
+    __device__ __forceinline__ void issue(const SeqGeo& g, const SeqTile& t, int e, int first,
                                           unsigned char* dst) const {
         const int j0 = t.tile(e);
         bool fast = t.whole(g, j0);
@@ -471,11 +469,11 @@ struct SeqStage {
     // The loads themselves, from the first rows of the blocks; FAST: every row exists and is
     // seen by some row.  (Everything by value: selects between captured references end up in
     // scratch memory.)
-    template <bool FAST, typename Tile>
+    template <bool FAST>
     __device__ __forceinline__ void load(const unsigned char* k0, const unsigned char* k1,
                                          const unsigned char* v0, const unsigned char* v1,
                                          int first, unsigned char* dst, bool ok0, bool ok1,
-                                         const Tile& t, const SeqGeo& g, int j0) const {
+                                         const SeqTile& t, const SeqGeo& g, int j0) const {
 #pragma unroll
         for (int u = 0; u < kCount; ++u) {
             const int x = first + u * STEP;

@@ -23,7 +23,7 @@ namespace na {
 namespace {
 
 // A tile of rows against the keys [from, end) of a request, or of those that a group shares.
-// (The members that SeqStage reads are SeqTile's.)
+// (Where its rows are is SeqTile's, as seq_locate and seq_row take it.)
 struct SharedTile : SeqTile {
     int r0, r1;       // requests that its rows belong to
     int from, end;    // keys of this side
