@@ -163,7 +163,7 @@ __device__ __forceinline__ void evict_choose(const EvictGeo& v, const EvictSplit
     const int m = (last + kThreads - 1) / kThreads;
     const int base = uniform(((int)threadIdx.x >> 6) * m * 64);
     const int cap = (int)min(v.capacity, (int64_t)last);  // (weights behind it are 0)
-    int32_t* __restrict__ to = v.to + (int64_t)slice * v.budget;
+    int32_t* to = v.to + (int64_t)slice * v.budget;  // (holes are written, then read)
     int32_t* __restrict__ from = v.from + (int64_t)slice * v.budget;
     uint32_t held[SLOTS > 0 ? SLOTS : 1];
     auto read = [&](int u) __attribute__((always_inline)) {
@@ -287,7 +287,6 @@ __device__ __forceinline__ void evict_choose(const EvictGeo& v, const EvictSplit
         holes += __builtin_popcountll(hole);
     });
     __syncthreads();  // (every hole is written)
-    const int32_t* place = v.to + (int64_t)slice * v.budget;
     // (ties: of the blocks before `back` too)
     const int back = some ? 0 : min(max((p.end - base) >> 6, 0), m);
     ties = ties0;
@@ -298,7 +297,7 @@ __device__ __forceinline__ void evict_choose(const EvictGeo& v, const EvictSplit
         if (mover >> lane & 1) {
             const int at = movers + rank_in(mover);
             from[at] = i;
-            put(place[at], i, w);
+            put(to[at], i, w);
             if (i < v.budget) atomicMax(&found[0], (uint32_t)at + 1);
         }
         movers += __builtin_popcountll(mover);
