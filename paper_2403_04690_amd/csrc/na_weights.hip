@@ -237,8 +237,10 @@ __device__ __forceinline__ void weights_stages(const WeightsGeo& w, const SeqTil
     b1 = (tb * g.G + kStageRows - 1) / kStageRows;
 }
 
-// Key tiles of a wave in the form for many rows: two while their operands fit the registers of
-// two waves a SIMD.
+// Key tiles of a wave in the form for many rows: two while their operands leave the loop over the
+// rows enough of the 256 registers of two waves a SIMD.  (16 bits at D = 128 and fp32 at D = 64 take
+// all of them, and 4 and 6 more values are spilled: stored once in front of the first pass over
+// the rows and read again once a pass, none within it.)
 template <typename T, int D>
 struct WeightsMany {
     static constexpr int kTiles = sizeof(T) == 4 && D == 128 ? 1 : 2;

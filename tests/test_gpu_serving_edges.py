@@ -7,7 +7,7 @@ import torch
 
 from tests import sequence_plain as plain
 from tests import serving_plain as ref
-from tests.test_gpu_serving import (DT, WHOLE, _int, _offsets, _randn, _tables,  # noqa: F401
+from tests.test_gpu_serving import (WHOLE, _int, _offsets, _randn, _tables,  # noqa: F401
                                     na)
 
 pytestmark = pytest.mark.gpu
@@ -124,3 +124,25 @@ def test_values_that_are_not_finite_show_where_cache_attention_has_them(na, dtyp
             hit[at[y]:at[y + 1], 2:, d] = True
     assert not bool(bad.isfinite()[hit].any()) and torch.equal(bad[~hit], out[~hit])
     assert torch.equal(x.attend().isfinite(), bad.isfinite())
+
+
+# ---------------------------------------------------------------- positions far apart
+
+@pytest.mark.parametrize("dtype,D", [("fp32", 32), ("bf16", 128)])
+@pytest.mark.parametrize("new,hints", [([1, 1, 2], {"max_new": 2}), ([60, 3, 80], {})])
+@pytest.mark.parametrize("W", [None, 2 ** 31 - 1, 2 ** 31 - 129, 2 ** 30, 4000, 130])
+def test_rows_of_a_group_that_stand_far_apart(na, dtype, D, new, hints, W):
+    """A row before most of the keys that its group shares, beside rows behind all of them: its
+    distances from those keys, less the widest window, are beyond 32 bits."""
+    context, shared, page = [0, 5000, 300], 4900, 64
+    most = [max(c + n, shared) for c, n in zip(context, new)]
+    made, P, _ = _tables(most, [0, 0, 0], page, [0, 3], [shared])
+    kp, vp = (_randn((P, 2, page, D), dtype, 1 + i) for i in range(2))
+    q = _randn((sum(new), 4, D), dtype, 3)
+    w = WHOLE if W is None else W
+    want = ref.shared(q, kp, vp, made, context, new, [0, 3], [shared], w, 3, D ** -0.5)
+    out, lse = na.cache_shared_attention(
+        q, kp, vp, torch.tensor(made).int().cuda(), _int(context), _offsets(new), _int([0, 3]),
+        _int([shared]), W, 3, **hints)
+    plain.close(out, want[0], want[2], "out")
+    plain.close(lse, want[1], want[3], "lse")

@@ -60,3 +60,21 @@ def test_forward_kernels_keep_their_operands_in_registers(tmp_path):
     # up to six values that only the epilogue reads (offsets, row sums); operands take more
     assert {s: n for s, n in fwd.items() if n > 6} == {}
     assert {s: n for s, n in narrow.items() if "DF16b" in s and n} == {}
+
+
+def test_long_context_kernels_keep_their_operands_in_registers(tmp_path):
+    if not os.path.exists(READELF):
+        pytest.skip("no llvm-readelf")
+    kernels = _spills(tmp_path)
+    if not kernels:
+        pytest.skip("a library without device code")
+    long = {s: n for s, n in kernels
+            if re.search(r"13shared_kernel|18shared_join_kernel|18weights_few_kernel|"
+                         r"19weights_many_kernel|19weights_join_kernel|19evict_select_kernel|"
+                         r"17evict_move_kernel", s)}
+    # 3 types, 3 head sizes: 4 pairs of forms, the join, two forms of the weights; the others
+    assert len(long) == 9 * 4 + 9 + 2 * 9 + 3, len(long)
+    # values that a pass over the rows needs at its ends; operands take more
+    many = {s: n for s, n in long.items() if re.search(r"many_kernelI(DF16b?_?Li128|fLi64)", s)}
+    assert len(many) == 3 and max(many.values()) <= 6, many
+    assert {s: n for s, n in long.items() if n and s not in many} == {}
