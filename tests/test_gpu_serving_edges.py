@@ -146,3 +146,52 @@ def test_rows_of_a_group_that_stand_far_apart(na, dtype, D, new, hints, W):
         _int([shared]), W, 3, **hints)
     plain.close(out, want[0], want[2], "out")
     plain.close(lse, want[1], want[3], "lse")
+
+
+# ---------------------------------------------------------------- memory that held something else
+
+def _used_before(value, dtype):
+    """What the allocator hands out next held this."""
+    free = [torch.full((n,), value, dtype=dtype, device="cuda")
+            for n in (2 ** 20, 2 ** 24) + (2 ** 14,) * 8 + (2 ** 17,) * 4]
+    del free
+
+
+@pytest.mark.parametrize("dtype,D", [("fp32", 64), ("bf16", 128)])
+@pytest.mark.parametrize("new", [[1] * 40, [70, 3] + [1] * 38])
+def test_results_do_not_depend_on_what_workspaces_held(na, dtype, D, new):
+    """Requests with and without a group, many splits of their keys; other calls in between."""
+    R, H, Hkv, page = 40, 8, 2, 64
+    cu, shared = [0, 30, 36], [3000, 90]
+    own = [(97 * r) % 600 for r in range(R)]
+    of = ref.groups_of(R, cu, shared)
+    context = [c + s for c, (_, s) in zip(own, of)]
+    table, P, _ = _tables(context, new, page, cu, shared)
+    kp, vp = (_randn((P, Hkv, page, D), dtype, 1 + i) for i in range(2))
+    q = _randn((sum(new), H, D), dtype, 3)
+    t, ctx, off = torch.tensor(table).int().cuda(), _int(context), _offsets(new)
+    hints = {"max_new": max(new)}
+    first = _int([s // 2 for _, s in of])
+    # (eviction: of requests that share no pages)
+    lens = [1 + (211 * r) % 1900 for r in range(R)]
+    apart, P2, _ = _tables(lens, [0] * R, page, [0], [], seed=1)
+    t2, pool = torch.tensor(apart).int().cuda(), _randn((P2, Hkv, page, D), dtype, 7)
+    weights = torch.rand((R, Hkv, t2.shape[1] * page), device="cuda").mul(40).round()
+
+    def run():
+        out, lse = na.cache_shared_attention(q, kp, vp, t, ctx, off, _int(cu), _int(shared),
+                                             max_shared=3000, max_own=700, **hints)
+        w = torch.zeros(R, Hkv, t.shape[1] * page, device="cuda")
+        na.cache_weights(q, lse, kp, t, ctx, off, w, first=first, max_context=3700, **hints)
+        free, head = torch.full((P2,), -1, dtype=torch.int32, device="cuda"), _int([P2])
+        k, v = pool.clone(), -pool
+        cut = na.cache_evict(weights, k, v, t2, _int(lens), free, head, 500, 50, first // 4)
+        return (out, lse, w, k, v, free) + cut
+
+    want = run()
+    for value, kind in ((math.nan, torch.float32), (-1, torch.int32), (2 ** 30, torch.int32),
+                        (math.inf, torch.float32)):
+        _used_before(value, kind)
+        na.cache_shared_attention(-q, vp, kp, t, ctx, off, _int(cu), _int(shared))
+        for a, b in zip(run(), want):
+            assert torch.equal(a, b)
