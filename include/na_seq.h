@@ -177,7 +177,7 @@ typedef struct {
  * shared ones, the new ones among them (0: unknown): they choose how the work is split, and are
  * not relied on for the result.  A row that sees a key whose score is NaN or +inf (a key that is
  * not finite, or a product beyond fp32) gets NaN in out and logsumexp; a value that is not finite
- * makes its column so, as in na_cache_attention.
+ * makes its column so in the rows that see it, and may in rows beside them, as in na_cache_attention.
  * workspace: na_cache_shared_attention_workspace(problem) bytes; NA_ERR_WORKSPACE if
  * workspace_bytes is less.  (0 for a problem that is empty or not valid.)
  * NA_ERR_SHAPE: what na_cache_attention refuses; groups is negative or reaches 2^24; a bound is
@@ -206,7 +206,8 @@ typedef struct {
  * with the logsumexp ([tokens, heads], 4-byte aligned) that na_cache_attention (or the form above)
  * returned for the same tokens.  The keys of the new tokens are in the cache.  Entries before
  * first[r] (int32 [requests] or NULL: none), of keys that no new token sees, and of requests
- * without new tokens are left as they were.  A page outside the pool reads as zero keys.
+ * without new tokens are left as they were.  (Keys before first[r] are read all the same.)  All keys are
+ * read on each request's own pages.  A page outside the pool reads as zero keys.
  * Deterministic: the same inputs give the same bits.  Weights must overlap no input.
  * max_new and max_context as in na_cache_attention.
  * workspace: na_cache_weights_workspace(problem) bytes (it may be 0: then NULL is fine);
@@ -248,13 +249,17 @@ typedef struct {
  *   kept[requests, kv_heads, budget]         position at which what is there now was; -1 behind
  *                                            the tokens of a request below the budget
  *   new_weights[requests, kv_heads, capacity] the weights of what is there now, 0 behind it
- *   new_context[requests]                    min(context_lens[r], budget)
+ *   new_context[requests]                    min(context_lens[r], budget), context_lens[r] clamped
+ *                                            to [0, max_pages * page_size]
  *   new_head[1], free_pages[num_free]        pages of the positions from budget on return to the
  *                                            list that na_cache_tables takes from: new_head is
  *                                            *head minus their number (not below 0), and they are
  *                                            entered from there on, request by request; entries
  *                                            outside [0, num_free) are dropped.  The page table is
  *                                            left as it is.
+ * From then on a position is a place in the cache: na_cache_tables counts the new tokens' positions on
+ * from new_context, and kernel_size counts places.  Where a token stands in its text, for keys that
+ * were rotated by it, is for the caller to keep (kept says where a place's token was).
  * Outputs overlap neither the inputs nor each other.  All of it is exact, and the same inputs give
  * the same bits.
  * workspace: na_cache_evict_workspace(problem) bytes; NA_ERR_WORKSPACE if workspace_bytes is less.

@@ -469,7 +469,7 @@ struct EvictMover {
 // order (a place lies before its source, so what a pass writes is read already).  Slices
 // let few requests fill the GPU; whole rows are read faster where many move (8 prompts of 8k to 32k tokens
 // cut to 4096, 8 heads, bf16 D = 128: 113 us with slices alone, 80 with both, 2.6 TB/s; trimming
-// 64 requests of 2049 to 2304 tokens to 2048, 4 heads: 23 us, 4.2 TB/s).
+// 64 requests of 2049 to 2304 tokens to 2048, 4 heads: 26 us, 3.6 TB/s).
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictGeo v, unsigned char* k_pages,
                                                                   unsigned char* v_pages) {
     const int lgs = v.lgrow - v.lgslice;  // log2 of the slices of a row

@@ -36,9 +36,9 @@ na_status check_shared(const na_shared_problem& s) {
 // The cut of the keys of one side over workgroups.  keys: the most that a row tile has;
 // busy: row tiles that are expected to have rows; room: the most workgroups.  The least lengths
 // are those of cache_attention's splits; a join there is in any case.  256 workgroups of the wide
-// form are aimed at and 512 of the narrow one (64 requests behind 8192 shared tokens, both launches: 30 us; with 512 and 1024 36, with
-// 128 wide 31; proposed tokens behind three prompts 23, with 128 wide 27; chunks of prompts no
-// difference from 128 to 1536).
+// form are aimed at and 512 of the narrow one.  us a call, of 64 requests behind 8192 shared tokens,
+// proposed tokens behind three prompts, and chunks of prompts: 28.0, 20.0 and 215; with 512 and 1024
+// 31.7, 20.7 and 215, with 128 wide 28.4, 23.5 and 215, with 1536 wide 30.6, 20.8 and 225.
 void cut_side(na::SharedSide& side, int64_t keys, int64_t busy, int64_t Hkv, bool half,
               int64_t room) {
     const bool narrow = side.narrow;
@@ -160,10 +160,11 @@ static na_status check_weights(const na_weights_problem& w) {
 }
 
 // The cut of the work.  Few rows: chunks of 8 to 64 key tiles (what a workgroup sums up at a time),
-// 8192 workgroups if every request had the most keys (32 requests of 8k to 32k tokens 112 us, with 4096
-// 118).  Many: 8 key tiles to a workgroup, whose rows are shared by as many as leave each 1024 rows, or
-// 128 where there would be fewer than 1024 workgroups (chunks of 1500 tokens over 2k to 7k: 226 us,
-// with 512 rows the same, with 2048 242; unshared 262).
+// 8192 workgroups if every request had the most keys (32 requests of 8k to 32k tokens 109 us a call,
+// with 4096 115).  Many: 8 key tiles to a workgroup, whose rows are shared by as many as leave each
+// 1024 rows, or 128 where there would be fewer than 1024 workgroups (chunks of 1500 tokens over 2k to
+// 7k: 195 us; with 512 rows 189, at twice the workspace; with 2048 221, unshared 225.  Windowed chunks of up
+// to 400 tokens 15.3, unshared 27).
 static void fill_weights(const na_weights_problem& problem, na::WeightsGeo& w) {
     const na_cache_problem& p = problem.cache;
     std::memset(&w, 0, sizeof w);
@@ -323,7 +324,8 @@ na_status na_cache_evict(const na_evict_problem* problem, const float* weights,
     v.lgrow = v.lgslice = __builtin_ctzll(row);
     const int64_t slices = p.requests * p.kv_heads;
     while (v.lgslice > 6 && (slices * 2 << (v.lgrow - v.lgslice)) < 1024) --v.lgslice;
-    // (8192 workgroups, most of which may find nothing to move: 8 long prompts 80 us, with 2048 90)
+    // (8192 workgroups, most of which may find nothing to move: 8 long prompts 147 us a call, with
+    // 2048 157)
     const int64_t most = std::max<int64_t>(1, std::min(p.budget, p.max_pages * p.page_size));
     const int64_t chunks = std::min(
         (most + 127) / 128, std::max<int64_t>(1, 4096 / std::max<int64_t>(1, slices)));

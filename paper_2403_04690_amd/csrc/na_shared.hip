@@ -7,10 +7,12 @@
 // the heads of a key/value head), the keys behind them one problem a request, and a second
 // launch joins the parts.  Each of the problems is cut into splits of its keys; every
 // split of every row leaves a logsumexp (-inf where the row sees nothing of it, NaN where a score
-// is none or infinite) and, unless it is -inf, its mean of the values, both in fp32.
+// is NaN or +inf) and, unless it is -inf, its mean of the values, both in fp32.
 //   64 requests of one token behind 8192 shared ones and 16 to 1024 of their own, 16 heads on 4, bf16
-// D = 128: 28 us a call; request by request the shared keys and values alone would be 1.1 GB.  Chunks
-// of 64 to 300 tokens of 16 requests behind 4k and 6k shared ones: 208 us (0.71 PFLOP/s).
+// D = 128: 28 us a call; read request by request (cache_attention over tables that list the shared
+// pages) 97.  Chunks of 64 to 300 tokens of 16 requests behind 4k and 6k shared ones: 208 to 215 us
+// (0.68 to 0.71 PFLOP/s), kernels 191 and 24; there the products bound both, the parts and their join come
+// on top, and cache_attention takes 202.
 #include <cmath>
 #include <type_traits>
 
@@ -284,7 +286,7 @@ __device__ __forceinline__ void no_shared_part(const SharedGeo& s, const Job& jo
 
 // Stages key or value rows.  Where the rows of 64 tiles are, and which of them every row or no row of
 // the wave sees, is found at a time, a lane each: found tile by tile it took the wide form 1 us of
-// every 2.4 us stage.
+// every 2.4 us stage (the first passes of a process, before the clocks are up).
 template <typename T, int D, bool GROUP>
 struct SharedStage {
     using R = SeqRows<T, D>;
@@ -392,8 +394,8 @@ __device__ __forceinline__ void load_query(const SeqGeo& g, const SharedTile& t,
 // Many rows: four waves of 32 rows each share the staged key tiles (as the wide form of
 // na_seq_fwd.hip).  Bound by a wave's chain through a stage: at D = 128 two waves a SIMD have 1.5 us
 // of products, exponentials and LDS reads for two key tiles and 0.4 to 0.6 us of issuing the next
-// ones' loads; the matrix cores are busy 33 % of the cycles.  (Issuing them inside the fold, behind
-// its key reads, spills: chunks behind a prompt 317 us instead of 237.)
+// ones' loads; the matrix cores are busy 32 % of the cycles.  (Issuing them inside the fold, behind
+// its key reads, spills: chunks behind a prompt 317 us instead of 237, kernel times of first passes.)
 template <typename T, int D, bool GROUP>
 __device__ __forceinline__ void shared_wide(const SharedGeo& s, int bid, const T* __restrict__ qg,
                                             const T* __restrict__ kg, const T* __restrict__ vg,

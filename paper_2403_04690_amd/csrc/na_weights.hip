@@ -100,7 +100,8 @@ struct WeightsFew {
 // registers.  Bound by reading the keys once.
 //   One new token for each of 32 requests over 8k to 32k cached ones, 16 heads on 4, bf16 D = 128: 553 MB
 // in 109 us (5.1 TB/s).  With two buffers a wave, and so half the waves, 131; with the pages looked up
-// tile by tile 150; three waves of three buffers 176 so.
+// tile by tile 150; three waves of three buffers 176 so.  Keys before `first` are read and multiplied
+// like the others, and left out when the sums are stored.
 template <typename T, int D>
 __global__ __launch_bounds__((WeightsFew<T, D>::kWaves * 64), 1) void weights_few_kernel(
     WeightsGeo w, const T* __restrict__ qg, const T* __restrict__ kg) {
@@ -253,10 +254,10 @@ struct WeightsMany {
 };
 
 // Many rows (chunks of prompts): four waves of kTiles x 32 keys each, whose operands stay in registers,
-// share stages of 64 rows.  Bound by the vector unit (44 % of the cycles: an exponential, its
+// share stages of 64 rows.  Bound by the vector unit (42 % of the cycles: an exponential, its
 // argument and the sum for each pair) and the matrix cores (27 %) in turn, with two waves a SIMD:
-// chunks of 1432 to 1846 tokens over 2k to 7k cached ones, 4 requests, 16 heads on 4, bf16 D = 128 193 us a
-// call (0.69 PFLOP/s).
+// chunks of 1432 to 1846 tokens over 2k to 7k cached ones, 4 requests, 16 heads on 4, bf16 D = 128 193
+// to 196 us a call (0.68 PFLOP/s), kernels 191 and 5.
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsGeo w,
                                                              const T* __restrict__ qg,
@@ -273,7 +274,7 @@ __global__ __launch_bounds__(256, 2) void weights_many_kernel(WeightsGeo w,
     const int wave = uniform((threadIdx.x >> 6) & 3);
     // (neighbours on eight XCDs in turn: requests of any length load them alike, and with a power
     // of two of shares an XCD's L2 holds the rows of only some.  Shares of a fixed number of rows
-    // instead, the same keys' on all XCDs: 270 us where these take 230)
+    // instead, the same keys' on all XCDs: 270 us where these took 230, kernel times of first passes)
     const int id = blockIdx.x >> w.lgshares, share = blockIdx.x & (w.shares - 1);
     const int slice = g.fd_tiles.div(id);
     const int split = id - slice * g.nsplit;

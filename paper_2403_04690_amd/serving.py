@@ -16,7 +16,9 @@ A serving loop over a cache whose requests share a system prompt:
                                                     context_lens, free_pages, head, budget,
                                                     recent, first=prompt_lens)
 
-Nothing here synchronises; all work is on the current stream of the tensors' device.
+Pass max_new (and max_shared and max_own, max_context) where they are known: without them a
+batch of single tokens takes the forms for chunks, 1.5 to 1.7 times as long.  Nothing here
+synchronises; all work is on the current stream of the tensors' device.
 """
 import ctypes
 import functools
@@ -63,6 +65,9 @@ def cache_shared_attention(q, k_pages, v_pages, page_table, context_lens, cu_new
     request's own pages.  Requests outside of all groups share nothing.  max_new, max_shared and
     max_own, bounds of the new tokens of a request, of the shared ones of a group and of a
     request's tokens behind those (the new ones among them), only choose how the work is split.
+    It pays where many rows meet the shared keys: single or a few new tokens of many requests.  For
+    chunks of prompts cache_attention, over tables that list the shared pages, takes as long.  A row
+    that sees a key with a score of NaN or +inf gets NaN.
     Returns (out, logsumexp [tokens, heads] fp32); rows from cu_new[requests] on are left as they
     were."""
     _library()
@@ -124,7 +129,8 @@ def cache_weights(q, lse, k_pages, page_table, context_lens, cu_new, weights, ke
     that see position j and the query heads of key/value head c.  lse [tokens, heads]: what
     cache_attention or cache_shared_attention returned for them, with the same kernel_size,
     sinks and scale.  Entries before first[r] (int32 [requests]; None: 0) are left as they
-    were.  Start a request's entries at 0."""
+    were, though their keys are read.  All keys are read on each request's own pages.  Start a
+    request's entries at 0."""
     _library()
     p, at, need = _weights_plan(*_window(kernel_size, sinks, scale), *_bounds(max_new, max_context),
                                 _metas(q, lse, k_pages, page_table, context_lens, cu_new, weights,
@@ -180,7 +186,11 @@ def cache_evict(weights, k_pages, v_pages, page_table, context_lens, free_pages,
     Returns (context_lens, weights, kept, head): the lengths after it, the weights that moved along
     (0 behind the tokens), for every position the one that its token had (int32 [requests,
     kv_heads, budget], -1 behind the tokens) and the free list's new head.  page_table is left as
-    it is; its entries behind a request's tokens mean nothing any more."""
+    it is; its entries behind a request's tokens mean nothing any more.  Positions are places in
+    the cache from then on: cache_tables counts a request's new tokens on from its shortened
+    length, and kernel_size counts places.  Where keys are rotated by their tokens' places in the
+    text, keep those beside the cache (kept says where a place's token was), and rotate new
+    tokens by them, not by the positions of cache_tables."""
     _library()
     p, at, need = _evict_plan(index(budget), index(recent),
                               _metas(weights, k_pages, v_pages, page_table, context_lens,
