@@ -73,6 +73,34 @@ def test_a_key_that_is_not_finite_shows_in_the_rows_that_see_it(na, dtype, D, ne
     assert torch.equal(x.attend().isfinite(), bad.isfinite())
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("new,hints", FORMS)
+def test_every_form_shows_keys_queries_and_values_that_are_not_finite(na, dtype, D, new, hints):
+    x = _Served(na, dtype, D, new)
+    want, want_lse = x.shared(**hints)
+    keys, values, query = x.kp.clone(), x.vp.clone(), x.q.clone()
+    for j in (33, 120):
+        x.put(x.kp, 0, j, 0, math.nan)
+        out, lse = x.shared(**hints)
+        assert not bool(out[0, :2].isfinite().any()) and not bool(lse[0, :2].isfinite().any())
+        assert torch.equal(out[0, 2:], want[0, 2:]) and torch.equal(lse[0, 2:], want_lse[0, 2:])
+        x.kp.copy_(keys)
+        x.put(x.vp, 0, j, 0, math.inf)
+        out, lse = x.shared(**hints)
+        assert not bool(out[0, :2].isfinite().any()) and torch.equal(lse, want_lse)
+        assert torch.equal(out[0, 2:], want[0, 2:])
+        x.vp.copy_(values)
+    x.q[0, 0, 3] = math.nan
+    out, lse = x.shared(**hints)
+    assert not bool(out[0, 0].isfinite().any()) and not bool(lse[0, 0].isfinite())
+    out[0, 0], lse[0, 0] = want[0, 0], want_lse[0, 0]
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    x.q.copy_(query)
+    out, lse = x.shared(**hints)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
 @pytest.mark.parametrize("dtype,D", [("fp32", 32), ("fp16", 64), ("bf16", 128)])
 @pytest.mark.parametrize("new,hints", FORMS)
 def test_a_query_that_is_not_finite_shows_in_its_row(na, dtype, D, new, hints):
